@@ -427,6 +427,110 @@ int adagc_muon_gemm_nt_batched(const void* P, int64_t ldp, const void* Q, int64_
                                float alpha, float beta, const void* Dt, int64_t lddt, void* C, int64_t ldc, void* Ct,
                                int64_t ldct, int32_t symmetric, int64_t batch, const int64_t* strides, void* stream);
 
+/*
+ * Operators around the step: what makes the gradients that the step takes.  They need no context and allocate nothing; each call only
+ * launches kernels on `stream` and may be recorded into a HIP graph.  Matrices are row-major DEVICE arrays with consecutive elements in a
+ * row and a leading dimension (elements from row to row) >= the row's length; rows may start at any element (the pointer's alignment is
+ * the element's).  Values are fp32 or bf16, arithmetic is fp32, results are rounded to nearest even.  Zero rows are a valid
+ * call.  Outputs must not overlap inputs or each other unless said otherwise.  Lengths and leading dimensions up to 2^31 - 1024.
+ * Calls on different streams are independent if their outputs and workspaces are.
+ */
+#define ADAGC_F32  0   /* = ADAGC_GRAD_F32 */
+#define ADAGC_BF16 1   /* = ADAGC_GRAD_BF16 */
+#define ADAGC_MAX_TOP 64
+
+/*
+ * Log-probabilities of given tokens: for each row z of logits, with M = max_j z_j and L = ln sum_j exp(scale (z_j - M)),
+ *     logp_j = scale (z_j - M) - L
+ * (scale: the inverse temperature), the log-probability of its target, the distribution's entropy -sum_j exp(logp_j) logp_j and the
+ * top_k most likely tokens.  One pass over the logits.
+ *   logits       DEVICE dtype[rows][ld], vocab values a row; -inf masks a token
+ *   targets      DEVICE int64[rows] (NULL if logprob is); outside 0 .. vocab-1 (-1, -100): the row has no target
+ *   scale        > 0, finite
+ *   top_k        0 .. min(ADAGC_MAX_TOP, vocab)
+ *   logprob      DEVICE fp32[rows], 0 for rows without a target; or NULL
+ *   entropy      DEVICE fp32[rows]; or NULL
+ *   stats        DEVICE fp32[rows][2]: M and L, which the backward pass takes (scale M + L is the row's log-sum-exp); or NULL
+ *   top_logprob  DEVICE fp32[rows][top_k], largest first                     (NULL if top_k = 0)
+ *   top_index    DEVICE int32[rows][top_k]; of equal logits the lowest index comes first, NaN before everything else
+ *   workspace    DEVICE, adagc_token_logprobs_workspace_bytes of it (0: may be NULL), 16-byte aligned, contents before and after without meaning
+ * At least one output is wanted.  A row whose logits are all -inf has log-probabilities -inf, entropy 0, M = -inf, L = 0.  A row
+ * with a NaN or +inf has NaN log-probabilities and entropy.
+ * Errors: INVALID_ARG, TOO_LARGE (also more than 2^24 - 1 rows), HIP.
+ */
+int64_t adagc_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int32_t top_k);
+int adagc_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, const int64_t* targets,
+                         float scale, int32_t top_k, float* logprob, float* entropy, float* stats, float* top_logprob,
+                         int32_t* top_index, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Gradient of the logits of adagc_token_logprobs for the gradients of its log-probabilities and entropies:
+ *     d_z_j = scale ( d_logprob (1[j = target] - p_j) - d_entropy p_j (logp_j + entropy) ),   p_j = exp(logp_j),
+ * without the d_logprob part for rows without a target, and 0 where p_j = 0 (masked tokens; all of a row of -inf).
+ *   logits, targets, scale   as the forward call had them
+ *   stats, entropy           DEVICE, the forward call's (entropy NULL if d_entropy is)
+ *   d_logprob                DEVICE fp32[rows], or NULL for none (then targets may be NULL)
+ *   d_entropy                DEVICE fp32[rows], or NULL for none
+ *   d_logits                 DEVICE dtype[rows][ld_d]; may be the logits themselves (with the same leading dimension)
+ * Errors: INVALID_ARG, TOO_LARGE, HIP.
+ */
+int adagc_token_logprobs_backward(const void* logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, const int64_t* targets,
+                                  float scale, const float* stats, const float* entropy, const float* d_logprob,
+                                  const float* d_entropy, void* d_logits, int64_t ld_d, void* stream);
+
+/*
+ * Activation checkpoints: a rows x cols matrix in 8 bits a value and 8 bits for every 32 of them.  Blocks of 32 consecutive values of
+ * a row share a power of two 2^e, e the smallest exponent >= -100 for which the block's largest finite value is at most 448 * 2^e; a code
+ * is the e4m3 number (OCP) nearest to x / 2^e, ties to even: a value is off by at most 2^-4 of itself (below 2^-6 * 2^e by at
+ * most 2^-10 * 2^e).  From 1.9375 * 2^127 on a value is held as 1.875 * 2^127; infinities and NaN become NaN, code 0x7F.
+ *   ckpt  DEVICE, adagc_act8_bytes(rows, cols) bytes, 16-byte aligned: with ld8 = cols rounded up to a multiple of 32,
+ *         codes u8[rows][ld8] (codes of columns beyond cols are 0), then e + 127 as u8[rows][ld8 / 32]
+ * adagc_act8_bytes returns a negative error code for sizes that are refused.
+ * Errors: INVALID_ARG, TOO_LARGE, HIP.
+ */
+int64_t adagc_act8_bytes(int64_t rows, int64_t cols);
+int adagc_act8_pack(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t ld, void* ckpt, void* stream);
+int adagc_act8_unpack(const void* ckpt, int64_t rows, int64_t cols, void* x, int32_t dtype, int64_t ld, void* stream);
+
+/*
+ * Gated activation out = silu(gate) * up, silu(g) = g / (1 + exp(-g)), with gate and up left in checkpoints for the backward pass in
+ * the same pass over them.
+ *   gate, up             DEVICE dtype[rows][ld_gate], [rows][ld_up] (halves of one matrix, for instance)
+ *   out                  DEVICE dtype[rows][ld_out]; may be gate or up itself (with the same leading dimension)
+ *   gate_ckpt, up_ckpt   DEVICE checkpoints of rows x cols, or both NULL
+ * Errors: INVALID_ARG, TOO_LARGE, HIP.
+ */
+int adagc_swiglu(const void* gate, int64_t ld_gate, const void* up, int64_t ld_up, int32_t dtype, int64_t rows, int64_t cols,
+                 void* out, int64_t ld_out, void* gate_ckpt, void* up_ckpt, void* stream);
+
+/*
+ * Its gradient at the values g, u that the checkpoints hold, with t = 1 / (1 + exp(-g)):
+ *     d_up = d_out g t,   d_gate = d_out u t (1 + g (1 - t)),
+ * and, for the next layer's weight gradient, out = g t u again.
+ *   d_out         DEVICE dtype[rows][ld_d_out]
+ *   d_gate, d_up  DEVICE dtype[rows][...]; one of them may be d_out itself (with the same leading dimension)
+ *   out           DEVICE dtype[rows][ld_out], or NULL
+ * Errors: INVALID_ARG, TOO_LARGE, HIP.
+ */
+int adagc_swiglu_backward(const void* d_out, int64_t ld_d_out, int32_t dtype, const void* gate_ckpt, const void* up_ckpt,
+                          int64_t rows, int64_t cols, void* d_gate, int64_t ld_d_gate, void* d_up, int64_t ld_d_up, void* out,
+                          int64_t ld_out, void* stream);
+
+/*
+ * Weight gradient of a linear layer y = W x from the gradient of its output and a checkpoint of its input, for rows tokens:
+ *     d_weight[o][i] = sum_t d_out[t][o] x[t][i]   (+ d_weight[o][i] with accumulate = 1), products exact, sums in fp32.
+ *   d_out      DEVICE dtype[rows][ld_d_out], n_out values a row
+ *   ckpt       DEVICE checkpoint of rows x n_in
+ *   d_weight   DEVICE weight_dtype[n_out][ld_weight], n_in values a row; zero rows of d_out make it 0 (or leave it)
+ *   workspace  DEVICE, adagc_act8_wgrad_workspace_bytes of it (0: may be NULL), 16-byte aligned, contents without meaning
+ * The result does not depend on what else runs: sums are taken in a fixed order.
+ * Errors: INVALID_ARG, TOO_LARGE, HIP.
+ */
+int64_t adagc_act8_wgrad_workspace_bytes(int64_t rows, int64_t n_out, int64_t n_in, int32_t dtype);
+int adagc_act8_wgrad(const void* d_out, int32_t dtype, int64_t ld_d_out, const void* ckpt, int64_t rows, int64_t n_out, int64_t n_in,
+                     void* d_weight, int32_t weight_dtype, int64_t ld_weight, int32_t accumulate, void* workspace,
+                     int64_t workspace_bytes, void* stream);
+
 /* Static description of an error code. */
 const char* adagc_strerror(int code);
 

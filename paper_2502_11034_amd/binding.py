@@ -21,6 +21,8 @@ ADAGC_ERR_STATE = -5
 
 ADAGC_OPT_ADAMW, ADAGC_OPT_LION, ADAGC_OPT_MUON = 0, 1, 2
 ADAGC_GRAD_F32, ADAGC_GRAD_BF16 = 0, 1
+ADAGC_F32, ADAGC_BF16 = 0, 1
+ADAGC_MAX_TOP = 64
 ADAGC_MODE_ADAGC, ADAGC_MODE_GLOBALGC, ADAGC_MODE_GLOBAL_ADAGC, ADAGC_MODE_ZCLIP = 0, 1, 2, 3
 ADAGC_MODE_AGC, ADAGC_MODE_CLIPPY = 4, 5
 
@@ -29,6 +31,8 @@ EXPORTS = [
     "adagc_set_param_copies", "adagc_step", "adagc_step_graph", "adagc_step_static", "adagc_get_norms", "adagc_get_state_norms", "adagc_num_tensors",
     "adagc_num_chunks", "adagc_get_segment_table", "adagc_profile_begin", "adagc_profile_end", "adagc_muon_gemm_nt", "adagc_muon_gemm_nt_batched", "adagc_muon_attach",
     "adagc_muon_workspace_bytes", "adagc_muon_step",
+    "adagc_token_logprobs_workspace_bytes", "adagc_token_logprobs", "adagc_token_logprobs_backward", "adagc_act8_bytes", "adagc_act8_pack",
+    "adagc_act8_unpack", "adagc_swiglu", "adagc_swiglu_backward", "adagc_act8_wgrad_workspace_bytes", "adagc_act8_wgrad",
     "adagc_strerror",
 ]
 
@@ -132,6 +136,27 @@ def lib():
                                              vp, i64, i32, i64, vp, vp]
     L.adagc_muon_workspace_bytes.restype = ctypes.c_int64
     L.adagc_muon_workspace_bytes.argtypes = [vp]
+    f32 = ctypes.c_float
+    L.adagc_token_logprobs_workspace_bytes.restype = i64
+    L.adagc_token_logprobs_workspace_bytes.argtypes = [i64, i64, i32]
+    L.adagc_token_logprobs.restype = ctypes.c_int
+    L.adagc_token_logprobs.argtypes = [vp, i32, i64, i64, i64, vp, f32, i32, vp, vp, vp, vp, vp, vp, i64, vp]
+    L.adagc_token_logprobs_backward.restype = ctypes.c_int
+    L.adagc_token_logprobs_backward.argtypes = [vp, i32, i64, i64, i64, vp, f32, vp, vp, vp, vp, vp, i64, vp]
+    L.adagc_act8_bytes.restype = i64
+    L.adagc_act8_bytes.argtypes = [i64, i64]
+    L.adagc_act8_pack.restype = ctypes.c_int
+    L.adagc_act8_pack.argtypes = [vp, i32, i64, i64, i64, vp, vp]
+    L.adagc_act8_unpack.restype = ctypes.c_int
+    L.adagc_act8_unpack.argtypes = [vp, i64, i64, vp, i32, i64, vp]
+    L.adagc_swiglu.restype = ctypes.c_int
+    L.adagc_swiglu.argtypes = [vp, i64, vp, i64, i32, i64, i64, vp, i64, vp, vp, vp]
+    L.adagc_swiglu_backward.restype = ctypes.c_int
+    L.adagc_swiglu_backward.argtypes = [vp, i64, i32, vp, vp, i64, i64, vp, i64, vp, i64, vp, i64, vp]
+    L.adagc_act8_wgrad_workspace_bytes.restype = i64
+    L.adagc_act8_wgrad_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    L.adagc_act8_wgrad.restype = ctypes.c_int
+    L.adagc_act8_wgrad.argtypes = [vp, i32, i64, vp, i64, i64, i64, vp, i32, i64, i32, vp, i64, vp]
     L.adagc_strerror.restype = ctypes.c_char_p
     L.adagc_strerror.argtypes = [ctypes.c_int]
     _lib = L
@@ -227,6 +252,154 @@ def adagc_muon_gemm_nt_batched(P, Q, alpha=1.0, beta=0.0, Dt=None, C=None, Ct=No
                                             ld(Dt), dp(C), ld(C), dp(Ct), ld(Ct), int(bool(symmetric)), int(batch), strides,
                                             ctypes.c_void_p(stream) if stream else None),
            "adagc_muon_gemm_nt_batched")
+
+
+# ---- operators around the step: 2-D device tensors, fp32 or bf16, consecutive elements in a row
+
+def _matrix(t, shape, name, dtype=None):
+    """(pointer, dtype code, leading dimension) of a 2-D tensor."""
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError("%s: shape %s, expected %s" % (name, tuple(t.shape), "2-D" if shape is None else tuple(shape)))
+    code = {"torch.float32": ADAGC_F32, "torch.bfloat16": ADAGC_BF16}.get(str(t.dtype))
+    if code is None or (dtype is not None and code != dtype):
+        raise TypeError("%s: dtype %s" % (name, t.dtype))
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError("%s: elements of a row are not consecutive" % name)
+    return t.data_ptr(), code, t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _dense(t, shape, dtype, name):
+    """Pointer of a contiguous tensor (None for None)."""
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s: shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+    if str(t.dtype) != dtype:
+        raise TypeError("%s: dtype %s, expected %s" % (name, t.dtype, dtype))
+    if not t.is_contiguous():
+        raise ValueError("%s is not contiguous" % name)
+    return t.data_ptr()
+
+
+def _bytes(t, least, name):
+    """(pointer, bytes) of a contiguous device buffer (None: (None, 0)) of at least so many bytes."""
+    if t is None:
+        n = 0
+    elif not t.is_contiguous():
+        raise ValueError("%s is not contiguous" % name)
+    else:
+        n = t.numel() * t.element_size()
+    if n < least:
+        raise ValueError("%s: %d bytes, %d needed" % (name, n, least))
+    return (t.data_ptr() if t is not None else None), n
+
+
+def _size(rc, where):
+    if rc < 0:
+        raise AdagcError(rc, where)
+    return int(rc)
+
+
+def _stream(stream):
+    return ctypes.c_void_p(stream) if stream else None
+
+
+def adagc_token_logprobs_workspace_bytes(rows, vocab, top_k=0):
+    return _size(lib().adagc_token_logprobs_workspace_bytes(int(rows), int(vocab), int(top_k)), "adagc_token_logprobs_workspace_bytes")
+
+
+def adagc_token_logprobs(logits, targets=None, logprob=None, entropy=None, stats=None, top_logprob=None, top_index=None, scale=1.0,
+                         workspace=None, stream=None):
+    """adagc_token_logprobs on logits [rows, vocab]; the outputs that are given are written.  targets: int64 [rows]; stats: fp32 [rows, 2];
+    top_logprob fp32, top_index int32 [rows, k]; workspace: adagc_token_logprobs_workspace_bytes(rows, vocab, k) bytes."""
+    p, dtype, ld = _matrix(logits, None, "logits")
+    rows, vocab = logits.shape
+    k = 0 if top_index is None else (top_index.shape[1] if top_index.dim() == 2 else -1)
+    ws, ws_bytes = _bytes(workspace, adagc_token_logprobs_workspace_bytes(rows, vocab, k) if rows and vocab else 0, "workspace")
+    _check(lib().adagc_token_logprobs(p, dtype, rows, vocab, ld, _dense(targets, (rows,), "torch.int64", "targets"), float(scale), k,
+                                      _dense(logprob, (rows,), "torch.float32", "logprob"),
+                                      _dense(entropy, (rows,), "torch.float32", "entropy"),
+                                      _dense(stats, (rows, 2), "torch.float32", "stats"),
+                                      _dense(top_logprob, (rows, k), "torch.float32", "top_logprob"),
+                                      _dense(top_index, (rows, k), "torch.int32", "top_index"), ws, ws_bytes, _stream(stream)),
+           "adagc_token_logprobs")
+
+
+def adagc_token_logprobs_backward(logits, targets, stats, entropy, d_logprob, d_entropy, d_logits, scale=1.0, stream=None):
+    """adagc_token_logprobs_backward: writes d_logits (which may be logits).  d_logprob, d_entropy: fp32 [rows] or None."""
+    p, dtype, ld = _matrix(logits, None, "logits")
+    rows, vocab = logits.shape
+    d, _, ld_d = _matrix(d_logits, logits.shape, "d_logits", dtype)
+    _check(lib().adagc_token_logprobs_backward(p, dtype, rows, vocab, ld, _dense(targets, (rows,), "torch.int64", "targets"),
+                                               float(scale), _dense(stats, (rows, 2), "torch.float32", "stats"),
+                                               _dense(entropy, (rows,), "torch.float32", "entropy"),
+                                               _dense(d_logprob, (rows,), "torch.float32", "d_logprob"),
+                                               _dense(d_entropy, (rows,), "torch.float32", "d_entropy"), d, ld_d, _stream(stream)),
+           "adagc_token_logprobs_backward")
+
+
+def adagc_act8_bytes(rows, cols):
+    """Bytes of a checkpoint of a rows x cols matrix."""
+    return _size(lib().adagc_act8_bytes(int(rows), int(cols)), "adagc_act8_bytes")
+
+
+def adagc_act8_pack(x, ckpt, stream=None):
+    """Writes the checkpoint of x [rows, cols] to the buffer ckpt."""
+    p, dtype, ld = _matrix(x, None, "x")
+    rows, cols = x.shape
+    c, _ = _bytes(ckpt, adagc_act8_bytes(rows, cols), "ckpt")
+    _check(lib().adagc_act8_pack(p, dtype, rows, cols, ld, c, _stream(stream)), "adagc_act8_pack")
+
+
+def adagc_act8_unpack(ckpt, x, stream=None):
+    """Writes what the checkpoint holds to x [rows, cols]."""
+    p, dtype, ld = _matrix(x, None, "x")
+    rows, cols = x.shape
+    c, _ = _bytes(ckpt, adagc_act8_bytes(rows, cols), "ckpt")
+    _check(lib().adagc_act8_unpack(c, rows, cols, p, dtype, ld, _stream(stream)), "adagc_act8_unpack")
+
+
+def adagc_swiglu(gate, up, out, gate_ckpt=None, up_ckpt=None, stream=None):
+    """out = silu(gate) up, all [rows, cols] of one type; gate and up are left in the checkpoints, if given."""
+    g, dtype, ld_g = _matrix(gate, None, "gate")
+    rows, cols = gate.shape
+    u, _, ld_u = _matrix(up, gate.shape, "up", dtype)
+    o, _, ld_o = _matrix(out, gate.shape, "out", dtype)
+    least = adagc_act8_bytes(rows, cols) if gate_ckpt is not None or up_ckpt is not None else 0
+    gc, _ = _bytes(gate_ckpt, least, "gate_ckpt")
+    uc, _ = _bytes(up_ckpt, least, "up_ckpt")
+    _check(lib().adagc_swiglu(g, ld_g, u, ld_u, dtype, rows, cols, o, ld_o, gc, uc, _stream(stream)), "adagc_swiglu")
+
+
+def adagc_swiglu_backward(d_out, gate_ckpt, up_ckpt, d_gate, d_up, out=None, stream=None):
+    """Writes d_gate, d_up and, if given, out again, from d_out [rows, cols] and the checkpoints of gate and up."""
+    d, dtype, ld_d = _matrix(d_out, None, "d_out")
+    rows, cols = d_out.shape
+    g, _, ld_g = _matrix(d_gate, d_out.shape, "d_gate", dtype)
+    u, _, ld_u = _matrix(d_up, d_out.shape, "d_up", dtype)
+    o, _, ld_o = _matrix(out, d_out.shape, "out", dtype) if out is not None else (None, 0, 0)
+    least = adagc_act8_bytes(rows, cols)
+    _check(lib().adagc_swiglu_backward(d, ld_d, dtype, _bytes(gate_ckpt, least, "gate_ckpt")[0], _bytes(up_ckpt, least, "up_ckpt")[0],
+                                       rows, cols, g, ld_g, u, ld_u, o, ld_o, _stream(stream)), "adagc_swiglu_backward")
+
+
+def adagc_act8_wgrad_workspace_bytes(rows, n_out, n_in, dtype):
+    return _size(lib().adagc_act8_wgrad_workspace_bytes(int(rows), int(n_out), int(n_in), int(dtype)), "adagc_act8_wgrad_workspace_bytes")
+
+
+def adagc_act8_wgrad(d_out, ckpt, d_weight, accumulate=False, workspace=None, stream=None):
+    """d_weight [n_out, n_in] = (d_weight +) d_out^T x for d_out [rows, n_out] and the checkpoint of x [rows, n_in]; workspace:
+    adagc_act8_wgrad_workspace_bytes(rows, n_out, n_in, dtype of d_out) bytes."""
+    d, dtype, ld_d = _matrix(d_out, None, "d_out")
+    rows, n_out = d_out.shape
+    w, weight_dtype, ld_w = _matrix(d_weight, None, "d_weight")
+    if d_weight.shape[0] != n_out:
+        raise ValueError("d_weight: %d rows, expected %d" % (d_weight.shape[0], n_out))
+    n_in = d_weight.shape[1]
+    c, _ = _bytes(ckpt, adagc_act8_bytes(rows, n_in), "ckpt")
+    ws, ws_bytes = _bytes(workspace, adagc_act8_wgrad_workspace_bytes(rows, n_out, n_in, dtype), "workspace")
+    _check(lib().adagc_act8_wgrad(d, dtype, ld_d, c, rows, n_out, n_in, w, weight_dtype, ld_w, int(bool(accumulate)), ws, ws_bytes,
+                                  _stream(stream)), "adagc_act8_wgrad")
 
 
 ADAGC_STATIC_MAX_TENSORS = 32768

@@ -1,0 +1,444 @@
+// Log-probabilities of target tokens, with entropy, the most likely alternatives and the gradient of the logits, for gfx950.
+//
+// With M = max_j z_j and L = ln sum_j exp(s (z_j - M)) of a row of logits z and a scale s (the inverse temperature),
+//   logp_j = s (z_j - M) - L,   p_j = exp(logp_j),   entropy H = -sum_j p_j logp_j = L - s sum_j p_j (z_j - M),
+//   d z_j = s ( d_logprob (1[j = target] - p_j) - d_entropy p_j (logp_j + H) ).
+// M and L are kept apart: s M + L in one fp32 number would lose L's digits where logits are large (a row of the type's lowest
+// value, which masks are often made of, is uniform here).
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "adagc.h"
+#include "operators_internal.h"
+
+namespace adagc {
+namespace {
+
+constexpr float kLowest = -3.402823466e38f;
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr int64_t kMaxRows = (1 << 24) - 1;      // a launch has at most 2^32 - 1 lanes
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+
+// Partial result of a part of a row: sums relative to the part's largest value.
+struct RowPart {
+    float most;      // max z; -inf: nothing but masked values
+    float sum;       // sum exp(s (z - most))
+    float weighted;  // sum (z - most) exp(s (z - most))
+    float pad;
+};
+
+struct ForwardArgs {
+    const void*    logits;
+    const int64_t* targets;
+    int64_t        ld;
+    int64_t        rows;
+    int32_t        vocab;
+    int32_t        parts;         // of a row
+    int32_t        part_vectors;  // 16-byte vectors of a part
+    int32_t        top_k;
+    float          scale;
+    float*         logprob;
+    float*         entropy;
+    float*         stats;
+    float*         top_logprob;
+    int32_t*       top_index;
+    RowPart*       part;          // [rows][parts]
+    uint64_t*      part_keys;     // [rows][parts][top_k]
+};
+
+// exp(x) of a difference already times log2 e
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// A running sum of exponentials relative to `ref`, which trails the largest value by kSlack at most: moving it along with
+// every new maximum would cost an exponential and a few products each time, and any reference within a few powers of e is as exact.
+constexpr float kSlack = 4.0f;   // in units of s z
+template <bool ENTROPY>
+struct Running {
+    float ref = kLowest, most = -INFINITY, sum = 0.f, weighted = 0.f;
+
+    __device__ __forceinline__ void move_to(float m, float c)
+    {
+        if (sum != 0.f) {                        // also with NaN
+            const float f = exp2_fast((ref - m) * c);
+            // a distance that exp takes to 0 may be infinite in fp32
+            if (ENTROPY) weighted = f == 0.f ? 0.f : (weighted + (ref - m) * sum) * f;
+            sum *= f;
+        }
+        ref = m;
+    }
+    template <int N>
+    __device__ __forceinline__ void add(const float (&z)[N], float vmax, float c, float slack)
+    {
+        most = maximum(most, vmax);
+        if (vmax > ref + slack) move_to(vmax, c);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float d = z[i] - ref;
+            const float e = exp2_fast(d * c);    // NaN stays NaN; -inf gives 0
+            sum += e;
+            if (ENTROPY) weighted += fmaxf(d, kLowest) * e;
+        }
+    }
+    // both relative to the larger of the two maxima
+    __device__ __forceinline__ void join(float m2, float s2, float w2, float c)
+    {
+        const float m = maximum(most, m2);
+        const float to = m == -INFINITY ? kLowest : m;
+        Running other;
+        other.ref = m2;
+        other.sum = s2;
+        other.weighted = w2;
+        move_to(to, c);
+        other.move_to(to, c);
+        most = m;
+        sum += other.sum;
+        weighted += other.weighted;
+    }
+};
+
+// The top_k largest values of a wave as keys in its lanes, largest first: the value's bits in an order-keeping form, then the index's
+// complement, so that keys are unique and equal values go to the lower index.  0: none.
+struct TopList {
+    uint64_t mine = 0, least = 0;                // this lane's; the last one kept, the same in all lanes
+    float    bar = NAN;                          // its value; NaN: the list is not full
+
+    static __device__ __forceinline__ uint64_t key(float z, uint32_t index)
+    {
+        uint32_t b = __float_as_uint(z + 0.0f);  // -0 is 0
+        if (z != z) b = 0x7FFFFFFFu;
+        b = (b & 0x80000000u) ? ~b : b | 0x80000000u;
+        return (uint64_t)b << 32 | (0xFFFFFFFFu - index);
+    }
+    static __device__ __forceinline__ float value(uint64_t key)
+    {
+        const uint32_t b = (uint32_t)(key >> 32);
+        return __uint_as_float((b & 0x80000000u) ? b & 0x7FFFFFFFu : ~b);
+    }
+    static __device__ __forceinline__ uint32_t index(uint64_t key) { return 0xFFFFFFFFu - (uint32_t)key; }
+
+    // Takes every lane's candidate that belongs into the list; called by whole waves.
+    __device__ __forceinline__ void take(uint64_t candidate, int k)
+    {
+        uint64_t mask = __ballot(candidate > least);
+        if (!mask) return;
+        const int lane = threadIdx.x & 63;
+        do {
+            const int from = __builtin_ctzll(mask);
+            const uint64_t key = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(candidate >> 32), from) << 32 |
+                                 (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)candidate, from);
+            const int at = __builtin_popcountll(__ballot(mine > key));
+            const uint64_t above = __shfl_up(mine, 1);
+            mine = lane < at ? mine : lane == at ? key : above;
+            if (lane >= k) mine = 0;
+            least = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), k - 1) << 32 |
+                    (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, k - 1);
+            mask &= mask - 1;
+            mask &= __ballot(candidate > least);
+        } while (mask);
+        bar = least ? value(least) : NAN;
+    }
+};
+
+// Results of a row from its sums, by one wave.
+template <bool ENTROPY, bool TOP, class T>
+__device__ __forceinline__ void write_row(const ForwardArgs& a, int64_t row, const Running<ENTROPY>& r, const TopList& top)
+{
+    const int lane = threadIdx.x & 63;
+    const bool none = r.most == -INFINITY && r.sum == 0.f;
+    // relative to ref, which is the maximum here
+    const float log_sum = none ? 0.f : logf(r.sum);
+    if (lane == 0) {
+        if (a.logprob) {
+            const int64_t t = a.targets[row];
+            float v = 0.f;
+            if (t >= 0 && t < a.vocab) {
+                const float z = to_float(static_cast<const T*>(a.logits)[row * a.ld + t]);
+                v = none ? -INFINITY : a.scale * (z - r.most) - log_sum;
+            }
+            a.logprob[row] = v;
+        }
+        if (ENTROPY && a.entropy) a.entropy[row] = none ? 0.f : log_sum - a.scale * (r.weighted / r.sum);
+        if (a.stats) {
+            a.stats[2 * row] = r.most;
+            a.stats[2 * row + 1] = log_sum;
+        }
+    }
+    if (TOP && lane < a.top_k) {
+        const float z = TopList::value(top.mine);
+        a.top_logprob[row * a.top_k + lane] = none ? -INFINITY : a.scale * (z - r.most) - log_sum;
+        a.top_index[row * a.top_k + lane] = (int32_t)TopList::index(top.mine);
+    }
+}
+
+// One workgroup per part of a row.
+template <class T, bool ENTROPY, bool TOP, bool SPLIT>
+__global__ __launch_bounds__(kThreads) void logprobs_kernel(const ForwardArgs a)
+{
+    constexpr int N = 16 / sizeof(T);
+    const int64_t row = SPLIT ? blockIdx.x / (uint32_t)a.parts : blockIdx.x;
+    const int part = SPLIT ? (int)(blockIdx.x - (uint32_t)row * (uint32_t)a.parts) : 0;
+    const T* z = static_cast<const T*>(a.logits) + row * a.ld;
+    const int first = SPLIT ? part * a.part_vectors : 0;
+    const int all = (int)(((int64_t)a.vocab + N - 1) / N);
+    const int last = SPLIT ? min(first + a.part_vectors, all) : all;
+    const float c = a.scale * kLog2e, slack = kSlack / a.scale;
+    Running<ENTROPY> r;
+    TopList top;
+    auto one = [&](const Vector<T>& v, int vector) __attribute__((always_inline)) {
+        float x[N];
+        widen(v, x);
+        float vmax = x[0];
+#pragma unroll
+        for (int i = 1; i < N; ++i) vmax = maximum(vmax, x[i]);
+        r.add(x, vmax, c, slack);
+        if constexpr (TOP) {
+            // later values have higher indices than all in the list, so only a larger one comes in; a list that is not full takes any
+            if (__ballot(!(vmax <= top.bar))) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const int64_t at = (int64_t)vector * N + i;
+                    top.take(vector < last && at < a.vocab ? TopList::key(x[i], (uint32_t)at) : 0, a.top_k);
+                }
+            }
+        }
+    };
+    // whole waves go round together: lanes past the end get masked values
+    for (int v0 = first; v0 < last; v0 += 4 * kThreads) {
+        Vector<T> v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int i = v0 + u * kThreads + (int)threadIdx.x;
+            v[u] = load_vector(z, (int64_t)i * N, i < last ? a.vocab : 0, masked<T>());
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (v0 + u * kThreads < last) one(v[u], v0 + u * kThreads + (int)threadIdx.x);
+    }
+
+    // lanes, then waves
+    float most = r.most;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) most = maximum(most, __shfl_xor(most, d));
+    r.most = most;
+    r.move_to(most == -INFINITY ? kLowest : most, c);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        r.sum += __shfl_xor(r.sum, d);
+        if (ENTROPY) r.weighted += __shfl_xor(r.weighted, d);
+    }
+    __shared__ RowPart wave_part[kWaves];
+    __shared__ uint64_t wave_keys[TOP ? kWaves * ADAGC_MAX_TOP : 1];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    if (lane == 0) wave_part[wave] = {r.most, r.sum, r.weighted, 0.f};
+    if (TOP && lane < a.top_k) wave_keys[wave * a.top_k + lane] = top.mine;
+    __syncthreads();
+    if (wave != 0) return;
+    for (int w = 1; w < kWaves; ++w) {
+        r.join(wave_part[w].most, wave_part[w].sum, wave_part[w].weighted, c);
+        if (TOP) top.take(lane < a.top_k ? wave_keys[w * a.top_k + lane] : 0, a.top_k);
+    }
+    if constexpr (SPLIT) {
+        if (lane == 0) a.part[row * a.parts + part] = {r.most, r.sum, r.weighted, 0.f};
+        if (TOP && lane < a.top_k) a.part_keys[(row * a.parts + part) * a.top_k + lane] = top.mine;
+    } else {
+        write_row<ENTROPY, TOP, T>(a, row, r, top);
+    }
+}
+
+// One wave per row joins the row's parts.
+template <class T, bool ENTROPY, bool TOP>
+__global__ __launch_bounds__(64) void join_parts_kernel(const ForwardArgs a)
+{
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x;
+    const float c = a.scale * kLog2e;
+    Running<ENTROPY> r;
+    TopList top;
+    for (int p = 0; p < a.parts; ++p) {
+        const RowPart x = a.part[row * a.parts + p];
+        r.join(x.most, x.sum, x.weighted, c);
+        if (TOP) top.take(lane < a.top_k ? a.part_keys[(row * a.parts + p) * a.top_k + lane] : 0, a.top_k);
+    }
+    write_row<ENTROPY, TOP, T>(a, row, r, top);
+}
+
+struct BackwardArgs {
+    const void*    logits;
+    void*          d_logits;
+    const int64_t* targets;
+    const float*   stats;
+    const float*   entropy;
+    const float*   d_logprob;
+    const float*   d_entropy;
+    int64_t        ld, ld_d;
+    int64_t        rows;
+    int32_t        vocab;
+    float          scale;
+    uint32_t       row_blocks;    // workgroup items per row
+    uint64_t       items;
+};
+
+constexpr int kBackwardVectors = 4;  // per lane and item
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(const BackwardArgs a)
+{
+    constexpr int N = 16 / sizeof(T);
+    for (uint64_t item = blockIdx.x; item < a.items; item += gridDim.x) {
+        const int64_t row = (int64_t)(item / a.row_blocks);
+        const uint32_t block = (uint32_t)(item - (uint64_t)row * a.row_blocks);
+        const T* z = static_cast<const T*>(a.logits) + row * a.ld;
+        T* d_z = static_cast<T*>(a.d_logits) + row * a.ld_d;
+        const float most = a.stats[2 * row], log_sum = a.stats[2 * row + 1];
+        const int64_t target = a.targets ? a.targets[row] : -1;
+        const bool has = target >= 0 && target < a.vocab;
+        const float d_lp = has && a.d_logprob ? a.d_logprob[row] : 0.f;
+        const float d_h = a.d_entropy ? a.d_entropy[row] : 0.f;
+        const float h = a.d_entropy ? a.entropy[row] : 0.f;
+        const bool none = most == -INFINITY;
+        const float k0 = -a.scale * (d_lp + d_h * h), k1 = -a.scale * d_h;
+        const int64_t col0 = ((int64_t)block * kBackwardVectors * kThreads + threadIdx.x) * N;
+        Vector<T> v[kBackwardVectors];
+#pragma unroll
+        for (int u = 0; u < kBackwardVectors; ++u) v[u] = load_vector(z, col0 + (int64_t)u * kThreads * N, a.vocab, masked<T>());
+#pragma unroll
+        for (int u = 0; u < kBackwardVectors; ++u) {
+            const int64_t col = col0 + (int64_t)u * kThreads * N;
+            float x[N];
+            widen(v[u], x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float logp = a.scale * (x[i] - most) - log_sum;
+                const float p = none ? 0.f : __builtin_exp2f(logp * kLog2e);      // down to subnormal numbers, which factors may raise
+                x[i] = p == 0.f ? 0.f : p * fmaf(k1, logp, k0);
+                if (has && !none && target == col + i) x[i] += a.scale * d_lp;
+            }
+            store_vector(d_z, col, a.vocab, narrow<T>(x));
+        }
+    }
+}
+
+// Parts of a row: one, unless there are too few rows to fill the chip.
+int parts_of(int64_t rows, int64_t vocab)
+{
+    const int64_t wanted = 1024 / std::max<int64_t>(rows, 1), most = vocab / 4096;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({wanted, most, 64}));
+}
+
+template <class T, bool ENTROPY, bool TOP>
+void launch_forward(const ForwardArgs& a, hipStream_t stream)
+{
+    if (a.parts == 1) {
+        logprobs_kernel<T, ENTROPY, TOP, false><<<dim3((uint32_t)a.rows), dim3(kThreads), 0, stream>>>(a);
+    } else {
+        logprobs_kernel<T, ENTROPY, TOP, true><<<dim3((uint32_t)(a.rows * a.parts)), dim3(kThreads), 0, stream>>>(a);
+        join_parts_kernel<T, ENTROPY, TOP><<<dim3((uint32_t)a.rows), dim3(64), 0, stream>>>(a);
+    }
+}
+
+template <class T>
+void launch_forward(const ForwardArgs& a, hipStream_t stream)
+{
+    if (a.entropy && a.top_k) launch_forward<T, true, true>(a, stream);
+    else if (a.entropy) launch_forward<T, true, false>(a, stream);
+    else if (a.top_k) launch_forward<T, false, true>(a, stream);
+    else launch_forward<T, false, false>(a, stream);
+}
+
+int check_rows(int64_t rows, int64_t vocab, int32_t dtype, float scale)
+{
+    if (rows < 0 || vocab < 1 || (dtype != ADAGC_F32 && dtype != ADAGC_BF16) || !(scale > 0.f) || !(scale < INFINITY)) return ADAGC_ERR_INVALID_ARG;
+    if (rows > kMaxRows || vocab > kMaxCols) return ADAGC_ERR_TOO_LARGE;
+    return ADAGC_OK;
+}
+
+}  // namespace
+}  // namespace adagc
+
+using namespace adagc;
+
+extern "C" int64_t adagc_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int32_t top_k)
+{
+    if (rows < 0 || vocab < 1 || top_k < 0 || top_k > ADAGC_MAX_TOP || top_k > vocab) return ADAGC_ERR_INVALID_ARG;
+    if (rows > kMaxRows || vocab > kMaxCols) return ADAGC_ERR_TOO_LARGE;
+    const int64_t parts = parts_of(rows, vocab);
+    return parts == 1 ? 0 : rows * parts * (int64_t)(sizeof(RowPart) + 8 * top_k);
+}
+
+extern "C" int adagc_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, const int64_t* targets,
+                                    float scale, int32_t top_k, float* logprob, float* entropy, float* stats, float* top_logprob,
+                                    int32_t* top_index, void* workspace, int64_t workspace_bytes, void* stream)
+{
+    if (const int rc = check_rows(rows, vocab, dtype, scale)) return rc;
+    if (top_k < 0 || top_k > ADAGC_MAX_TOP || top_k > vocab || ld < vocab || workspace_bytes < 0) return ADAGC_ERR_INVALID_ARG;
+    if (ld > kMaxLd) return ADAGC_ERR_TOO_LARGE;
+    if (rows == 0) return ADAGC_OK;
+    if (!logits || (logprob && !targets) || (top_k > 0) != (top_logprob != nullptr) || (top_k > 0) != (top_index != nullptr) ||
+        (!logprob && !entropy && !stats && top_k == 0))
+        return ADAGC_ERR_INVALID_ARG;
+    const int64_t need = adagc_token_logprobs_workspace_bytes(rows, vocab, top_k);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return ADAGC_ERR_INVALID_ARG;
+    if (misaligned(logits, dtype_size(dtype)) || misaligned(targets, 8) || misaligned(logprob, 4) || misaligned(entropy, 4) ||
+        misaligned(stats, 4) || misaligned(top_logprob, 4) || misaligned(top_index, 4) || (need > 0 && misaligned(workspace, 16)))
+        return ADAGC_ERR_INVALID_ARG;
+    ForwardArgs a{};
+    a.logits = logits;
+    a.targets = targets;
+    a.ld = ld;
+    a.rows = rows;
+    a.vocab = (int32_t)vocab;
+    a.parts = parts_of(rows, vocab);
+    const int64_t n = 16 / dtype_size(dtype), vectors = (vocab + n - 1) / n;
+    a.part_vectors = (int32_t)((vectors + a.parts - 1) / a.parts);
+    a.top_k = top_k;
+    a.scale = scale;
+    a.logprob = logprob;
+    a.entropy = entropy;
+    a.stats = stats;
+    a.top_logprob = top_logprob;
+    a.top_index = top_index;
+    a.part = static_cast<RowPart*>(workspace);
+    a.part_keys = reinterpret_cast<uint64_t*>(a.part + rows * a.parts);
+    if (dtype == ADAGC_F32) launch_forward<float>(a, static_cast<hipStream_t>(stream));
+    else launch_forward<uint16_t>(a, static_cast<hipStream_t>(stream));
+    return hipGetLastError() == hipSuccess ? ADAGC_OK : ADAGC_ERR_HIP;
+}
+
+extern "C" int adagc_token_logprobs_backward(const void* logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t ld,
+                                             const int64_t* targets, float scale, const float* stats, const float* entropy,
+                                             const float* d_logprob, const float* d_entropy, void* d_logits, int64_t ld_d, void* stream)
+{
+    if (const int rc = check_rows(rows, vocab, dtype, scale)) return rc;
+    if (ld < vocab || ld_d < vocab) return ADAGC_ERR_INVALID_ARG;
+    if (ld > kMaxLd || ld_d > kMaxLd) return ADAGC_ERR_TOO_LARGE;
+    if (rows == 0) return ADAGC_OK;
+    if (!logits || !stats || !d_logits || (d_logprob && !targets) || (d_entropy && !entropy) || (d_logits == logits && ld_d != ld))
+        return ADAGC_ERR_INVALID_ARG;
+    if (misaligned(logits, dtype_size(dtype)) || misaligned(d_logits, dtype_size(dtype)) || misaligned(targets, 8) || misaligned(stats, 4) ||
+        misaligned(entropy, 4) || misaligned(d_logprob, 4) || misaligned(d_entropy, 4))
+        return ADAGC_ERR_INVALID_ARG;
+    BackwardArgs a{};
+    a.logits = logits;
+    a.d_logits = d_logits;
+    a.targets = d_logprob ? targets : nullptr;
+    a.stats = stats;
+    a.entropy = entropy;
+    a.d_logprob = d_logprob;
+    a.d_entropy = d_entropy;
+    a.ld = ld;
+    a.ld_d = ld_d;
+    a.rows = rows;
+    a.vocab = (int32_t)vocab;
+    a.scale = scale;
+    const int64_t per_block = (int64_t)kThreads * kBackwardVectors * (16 / dtype_size(dtype));
+    a.row_blocks = (uint32_t)((vocab + per_block - 1) / per_block);
+    a.items = (uint64_t)rows * a.row_blocks;
+    const uint32_t grid = (uint32_t)std::min<uint64_t>(a.items, 1u << 23);
+    if (dtype == ADAGC_F32) logprobs_backward_kernel<float><<<dim3(grid), dim3(kThreads), 0, static_cast<hipStream_t>(stream)>>>(a);
+    else logprobs_backward_kernel<uint16_t><<<dim3(grid), dim3(kThreads), 0, static_cast<hipStream_t>(stream)>>>(a);
+    return hipGetLastError() == hipSuccess ? ADAGC_OK : ADAGC_ERR_HIP;
+}

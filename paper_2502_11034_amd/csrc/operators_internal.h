@@ -1,0 +1,119 @@
+// Shared by the kernels of the operators around the step: token log-probabilities (logprobs.hip), 8-bit checkpoints and the gated
+// activation (act8.hip), the weight gradient from a checkpoint (act8_wgrad.hip).
+#ifndef ADAGC_OPERATORS_INTERNAL_H
+#define ADAGC_OPERATORS_INTERNAL_H
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <string.h>
+
+#include "adagc.h"
+
+namespace adagc {
+
+constexpr int64_t kMaxCols = INT32_MAX - 1023;   // columns and leading dimensions: index arithmetic within a row fits 32 bits
+constexpr int64_t kMaxLd = kMaxCols;
+
+inline int dtype_size(int32_t dtype) { return dtype == ADAGC_F32 ? 4 : 2; }
+inline bool misaligned(const void* p, int to) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(to - 1)) != 0; }
+inline bool known_dtype(int32_t dtype) { return dtype == ADAGC_F32 || dtype == ADAGC_BF16; }
+
+// Bytes of a checkpoint's row of codes; a row's scales are a 32nd of that.
+inline __host__ __device__ int64_t act8_ld(int64_t cols) { return (cols + 31) / 32 * 32; }
+
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+
+// 16 bytes of fp32 or bf16 (uint16_t) values
+template <class T>
+struct Vector {
+    uint32_t w[4];
+};
+
+// Larger of two, NaN if one is.
+__device__ __forceinline__ float maximum(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+
+__device__ __forceinline__ void widen(const Vector<float>& v, float (&x)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(v.w[i]);
+}
+__device__ __forceinline__ void widen(const Vector<uint16_t>& v, float (&x)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(v.w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(v.w[i] & 0xFFFF0000u);
+    }
+}
+
+// Rounded to nearest even where the type is bf16.
+template <class T>
+__device__ __forceinline__ Vector<T> narrow(const float (&x)[16 / sizeof(T)])
+{
+    Vector<T> v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            v.w[i] = __float_as_uint(x[i]);
+        } else {
+            const f32x2_t two = {x[2 * i], x[2 * i + 1]};
+            v.w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, bf16x2_t));
+        }
+    }
+    return v;
+}
+
+// The 16 bytes at column `col` of a row of n columns, `fill` (16 / sizeof(T) values' bits in a word) from its end on.  Rows start
+// at any element: the hardware takes 16-byte accesses at any address, and a wave's together touch one cache line more.
+template <class T>
+__device__ __forceinline__ Vector<T> load_vector(const T* row, int64_t col, int64_t n, uint32_t fill)
+{
+    constexpr int N = 16 / sizeof(T);
+    Vector<T> v;
+    if (col + N <= n) {
+        memcpy(v.w, row + col, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                v.w[i] = col + i < n ? __float_as_uint(row[col + i]) : fill;
+            } else {
+                const uint32_t lo = col + 2 * i < n ? row[col + 2 * i] : fill & 0xFFFFu;
+                const uint32_t hi = col + 2 * i + 1 < n ? row[col + 2 * i + 1] : fill >> 16;
+                v.w[i] = lo | hi << 16;
+            }
+        }
+    }
+    return v;
+}
+
+template <class T>
+__device__ __forceinline__ void store_vector(T* row, int64_t col, int64_t n, const Vector<T>& v)
+{
+    constexpr int N = 16 / sizeof(T);
+    if (col + N <= n) {
+        memcpy(row + col, v.w, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (col + i < n) {
+                if constexpr (sizeof(T) == 4) row[col + i] = __uint_as_float(v.w[i]);
+                else row[col + i] = (uint16_t)(v.w[i / 2] >> (16 * (i & 1)));
+            }
+        }
+    }
+}
+
+// -inf as `fill`
+template <class T>
+__device__ __forceinline__ constexpr uint32_t masked()
+{
+    return sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;
+}
+
+}  // namespace adagc
+#endif
