@@ -12,6 +12,8 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
+#include <utility>
 
 #include "act8_device.h"
 #include "operators_internal.h"
@@ -37,6 +39,7 @@ struct WgradArgs {
     int32_t        whole;         // tiles computed by one workgroup each; the others by `split`
     int32_t        split;
     int32_t        accumulate;
+    int32_t        weight_bf16;
 };
 
 // Compute units: a round of the launch is as many workgroups of the large tile.
@@ -56,13 +59,13 @@ __device__ __forceinline__ void place_of_tile(const WgradArgs& a, int n, int* to
     *to = 8 * band + in_band - *ti * high;
 }
 
-// A lane's four consecutive values of a row of the result.
+// A lane's four consecutive values of row o of the result, from column i on; rows below o_least and columns below i_least belong to
+// another tile.
 template <class W>
-__device__ __forceinline__ void store_results(const WgradArgs& a, int64_t o, int64_t i, f32x4 v)
+__device__ __forceinline__ void store_typed(const WgradArgs& a, int64_t o, int64_t i, int64_t i_least, f32x4 v)
 {
-    if (o >= a.n_out || i >= a.n_in) return;
     W* w = static_cast<W*>(a.d_weight) + o * a.ld_w + i;
-    if (i + 4 <= a.n_in) {
+    if (i >= i_least && i + 4 <= a.n_in) {
         if constexpr (sizeof(W) == 4) {
             if (a.accumulate) {
                 f32x4 old;
@@ -87,23 +90,44 @@ __device__ __forceinline__ void store_results(const WgradArgs& a, int64_t o, int
     } else {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-            if (i + r < a.n_in) {
+            if (i + r >= i_least && i + r < a.n_in) {
                 const float x = v[r] + (a.accumulate ? to_float(w[r]) : 0.f);
                 if constexpr (sizeof(W) == 4) w[r] = x;
                 else w[r] = __builtin_bit_cast(uint16_t, (__bf16)x);
             }
     }
 }
+__device__ __forceinline__ void store_results(const WgradArgs& a, int64_t o, int64_t o_least, int64_t i, int64_t i_least, f32x4 v)
+{
+    if (o < o_least || o >= a.n_out || i >= a.n_in) return;
+    if (a.weight_bf16) store_typed<uint16_t>(a, o, i, i_least, v);
+    else store_typed<float>(a, o, i, i_least, v);
+}
 
-// BM x BN tile of dW (BM along n_out), kWM x kWN waves, kDeep tokens at a time.
-template <class T, int BM, int BN, int kWM, int kWN, int kDeep>
+// f(integral_constant 0), ..., f(integral_constant N-1)
+template <class F, int... I>
+__device__ __forceinline__ void static_for_impl(F&& f, std::integer_sequence<int, I...>)
+{
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void static_for(F&& f)
+{
+    static_for_impl(f, std::make_integer_sequence<int, N>{});
+}
+
+// Tokens of a step, one matrix-core instruction deep, and the places of LDS that steps go round in.
+constexpr int kDeep = 32, kPlaces = 3;
+
+// BM x BN tile of dW (BM along n_out), kWM x kWN waves.
+template <class T, int BM_, int BN_, int kWM_, int kWN_>
 struct Tile {
+    static constexpr int BM = BM_, BN = BN_, kWM = kWM_, kWN = kWN_;
     static constexpr int kThreads = 64 * kWM * kWN;
     static constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
     static constexpr int kTM = BM / kWM / 16, kTN = BN / kWN / 16;         // 16 x 16 blocks of a wave
     static constexpr int kY = kDeep * BM, kX = kDeep * BN;                 // elements of a staged operand tile
-    static constexpr int kBuffer = (kParts * kY + kX) * 2;                 // bytes
-    static constexpr int kLds = 2 * kBuffer;
+    static constexpr int kPlace = (kParts * kY + kX) * 2;                  // bytes
     static constexpr int kYUnits = kY / 8 / kThreads, kXUnits = kX / 16 / kThreads;     // of a lane: 8 values of dY, 16 codes
     static_assert(kY % (8 * kThreads) == 0 && kX % (16 * kThreads) == 0, "operand tiles are dealt evenly");
 
@@ -114,51 +138,84 @@ struct Tile {
     static __device__ __forceinline__ int at(int r, int v) { return r * C * 2 + ((v >> 1) ^ swizzle(r)) * 32 + (v & 1) * 16; }
 };
 
-template <class T, class W, int BM, int BN, int kWM, int kWN, int kDeep>
-__global__ __launch_bounds__(64 * kWM * kWN, 2) void wgrad_kernel(const WgradArgs a)
+// s_waitcnt for "at most n LDS accesses of this wave still outstanding", nothing else waited for
+#define ADAGC_WAIT_LDS(n) __builtin_amdgcn_s_waitcnt(0xF | (3 << 14) | (7 << 4) | ((n) << 8))
+// nothing is moved across this point by the compiler's instruction scheduler
+#define ADAGC_SCHED_FENCE() __builtin_amdgcn_sched_barrier(0)
+
+// EDGE: dW is smaller than a tile in one direction, or rows of dY are too far apart for 32-bit offsets.  Otherwise the last tile of a
+// direction begins a tile before the end, so that every tile is whole, and stores only what no other tile does.
+//
+// Main loop.  A step's operands are staged in a place of LDS; while step k is multiplied from registers, step k + 1 is read to
+// registers from its place (of dY, each fragment as soon as its multiplications are issued; of X, to a second set), step k + 2 goes from
+// the registers it was loaded to into its place, and those take step k + 4.  One barrier a step: what it orders is the writes of k + 2
+// before their reads in the next step; the reads of a place are done a step before it is written again.  Loads past the last step take
+// the last one again: a loop without conditions lets the compiler count what is outstanding.
+template <class S, class T, bool EDGE>
+__global__ __launch_bounds__(S::kThreads, 2) void wgrad_kernel(const WgradArgs a)
 {
-    typedef Tile<T, BM, BN, kWM, kWN, kDeep> Shape;
-    constexpr int kThreads = Shape::kThreads, kTM = Shape::kTM, kTN = Shape::kTN, kParts = Shape::kParts;
-    constexpr int kYUnits = Shape::kYUnits, kXUnits = Shape::kXUnits;
-    __shared__ __attribute__((aligned(512))) uint8_t lds[Shape::kLds];
+    constexpr int BM = S::BM, BN = S::BN, kThreads = S::kThreads, kTM = S::kTM, kTN = S::kTN, kParts = S::kParts;
+    constexpr int kYUnits = S::kYUnits, kXUnits = S::kXUnits, kH = (int)sizeof(T) / 2;
+    __shared__ __attribute__((aligned(512))) uint8_t lds[kPlaces * S::kPlace];
     const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>(&lds[0]);      // low half of the flat address = LDS offset
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave / kWN, wn = wave % kWN;
+    const int wm = wave / S::kWN, wn = wave % S::kWN;
 
     // the tile and the tokens of this workgroup
     const int item = (int)blockIdx.x;
     int tile = item, part = 0;
-    if (item >= a.whole) {
+    const bool alone = item < a.whole;
+    if (!alone) {
         tile = a.whole + (item - a.whole) / a.split;
         part = (item - a.whole) % a.split;
     }
     int to, ti;
     place_of_tile(a, tile, &to, &ti);
-    const int64_t o0 = (int64_t)to * BM, i0 = (int64_t)ti * BN;
-    const int64_t steps = (a.rows + kDeep - 1) / kDeep;
-    const bool alone = item < a.whole;
-    const int64_t step0 = alone ? 0 : steps * part / a.split, step1 = alone ? steps : steps * (part + 1) / a.split;
+    const int64_t o_least = (int64_t)to * BM, i_least = (int64_t)ti * BN;
+    const int64_t o0 = EDGE ? o_least : min(o_least, (int64_t)a.n_out - BM), i0 = EDGE ? i_least : min(i_least, (int64_t)a.ld - BN);
+    const int64_t full = a.rows / kDeep;
+    const int64_t step0 = alone ? 0 : full * part / a.split, step1 = alone ? full : full * (part + 1) / a.split;
+    const bool last = alone || part == a.split - 1;
 
-    // staging: a lane's units, in registers between the load and the write to LDS
+    // Staging: a lane's units, in registers between the load and the write to LDS.  A lane's units are whole rows apart.
     struct Staged {
-        Vector<T> y[kYUnits][sizeof(T) / 2];
+        Vector<T> y[kYUnits][kH];
         u32x4     x[kXUnits];
         uint32_t  scale[kXUnits];
     };
+    const int yr = tid / (BM / 8), yv = tid % (BM / 8), xr = tid / (BN / 16), xv = tid % (BN / 16) * 2;
+    constexpr int kYRows = kThreads / (BM / 8), kXRows = kThreads / (BN / 16);
+    const uint32_t lane_y = (uint32_t)(yr * (uint32_t)a.ld_d + (uint32_t)yv * 8) * sizeof(T);
+    const uint32_t lane_x = (uint32_t)xr * (uint32_t)a.ld + (uint32_t)xv * 8;
+    const uint32_t lane_scale = (uint32_t)xr * (uint32_t)(a.ld / 32) + (uint32_t)xv / 4;
+    // inside the matrices nothing is checked, and a lane's address is a wave-wide base and 32 bits
+    auto load_y = [&](int64_t step, int n, Staged& s) __attribute__((always_inline)) {
+        const uint8_t* row = static_cast<const uint8_t*>(a.d_out) + ((step * kDeep + n * kYRows) * a.ld_d + o0) * sizeof(T);
+#pragma unroll
+        for (int h = 0; h < kH; ++h) memcpy(s.y[n][h].w, row + lane_y + h * 16, 16);
+    };
+    auto load_x = [&](int64_t step, int n, Staged& s) __attribute__((always_inline)) {
+        const int64_t at = (step * kDeep + n * kXRows) * a.ld + i0;
+        s.x[n] = *reinterpret_cast<const u32x4*>(a.codes + at + lane_x);
+        s.scale[n] = (a.scales + at / 32)[lane_scale];
+    };
     auto load = [&](int64_t step, Staged& s) __attribute__((always_inline)) {
 #pragma unroll
-        for (int n = 0; n < kYUnits; ++n) {
-            const int u = n * kThreads + tid, r = u / (BM / 8);
-            const int64_t t = step * kDeep + r, o = o0 + u % (BM / 8) * 8;
-            const T* row = static_cast<const T*>(a.d_out) + t * a.ld_d;
-            const int64_t end = t < a.rows ? a.n_out : 0;
+        for (int n = 0; n < kYUnits; ++n) load_y(step, n, s);
 #pragma unroll
-            for (int h = 0; h < (int)sizeof(T) / 2; ++h) s.y[n][h] = load_vector(row, o + h * 4, end, 0);
+        for (int n = 0; n < kXUnits; ++n) load_x(step, n, s);
+    };
+    auto load_checked = [&](int64_t step, Staged& s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < kYUnits; ++n) {
+            const int64_t t = step * kDeep + yr + n * kYRows;
+            const T* row = static_cast<const T*>(a.d_out) + t * a.ld_d;
+#pragma unroll
+            for (int h = 0; h < kH; ++h) s.y[n][h] = load_vector(row, o0 + yv * 8 + h * 4, t < a.rows ? a.n_out : 0, 0);
         }
 #pragma unroll
         for (int n = 0; n < kXUnits; ++n) {
-            const int u = n * kThreads + tid, r = u / (BN / 16);
-            const int64_t t = step * kDeep + r, i = i0 + u % (BN / 16) * 16;
+            const int64_t t = step * kDeep + xr + n * kXRows, i = i0 + xv * 8;
             s.x[n] = u32x4{0, 0, 0, 0};
             s.scale[n] = 127;
             if (t < a.rows && i < a.ld) {
@@ -167,97 +224,149 @@ __global__ __launch_bounds__(64 * kWM * kWN, 2) void wgrad_kernel(const WgradArg
             }
         }
     };
-    auto write = [&](const Staged& s, uint8_t* to_lds) __attribute__((always_inline)) {
+    const uint32_t write_y_at = (uint32_t)S::template at<BM>(yr, yv), write_x_at = (uint32_t)(kParts * S::kY * 2 + S::template at<BN>(xr, xv));
+    static_assert(kYRows % 16 == 0 && kXRows % 16 == 0, "a lane's units are at the same place of the swizzle");
+    auto write_y = [&](const Staged& s, int n, uint32_t place) __attribute__((always_inline)) {
+        const uint32_t at = place + write_y_at + (uint32_t)(n * kYRows * BM * 2);
+        if constexpr (kParts == 1) {
+            *reinterpret_cast<ADAGC_LDS u32x4*>(at) = u32x4{s.y[n][0].w[0], s.y[n][0].w[1], s.y[n][0].w[2], s.y[n][0].w[3]};
+        } else {
+            // x = hi + mid + lo, each the upper half of what is left: exact.  (Of an infinity nothing is left.)
+            u32x4 p[3];
 #pragma unroll
-        for (int n = 0; n < kYUnits; ++n) {
-            const int u = n * kThreads + tid, r = u / (BM / 8), v = u % (BM / 8);
-            uint8_t* at = to_lds + Shape::template at<BM>(r, v);
-            if constexpr (kParts == 1) {
-                *reinterpret_cast<u32x4*>(at) = u32x4{s.y[n][0].w[0], s.y[n][0].w[1], s.y[n][0].w[2], s.y[n][0].w[3]};
-            } else {
-                // x = hi + mid + lo, each the upper half of what is left: exact.  (An infinity stays one: nothing is left of it.)
-                u32x4 p[3];
+            for (int k = 0; k < 4; ++k) {
+                uint32_t two[3] = {0, 0, 0};
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    uint32_t two[3] = {0, 0, 0};
+                for (int e = 0; e < 2; ++e) {
+                    float x = __uint_as_float(s.y[n][k / 2].w[k % 2 * 2 + e]);
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float x = __uint_as_float(s.y[n][k / 2].w[k % 2 * 2 + e]);
-#pragma unroll
-                        for (int q = 0; q < 3; ++q) {
-                            const uint32_t top = __float_as_uint(x) & 0xFFFF0000u;
-                            two[q] |= e ? top : top >> 16;
-                            x = x == __uint_as_float(top) ? 0.f : x - __uint_as_float(top);
-                        }
+                    for (int q = 0; q < 3; ++q) {
+                        const uint32_t top = __float_as_uint(x) & 0xFFFF0000u;
+                        two[q] |= e ? top : top >> 16;
+                        x = x == __uint_as_float(top) ? 0.f : x - __uint_as_float(top);
                     }
-#pragma unroll
-                    for (int q = 0; q < 3; ++q) p[q][k] = two[q];
                 }
 #pragma unroll
-                for (int q = 0; q < 3; ++q) *reinterpret_cast<u32x4*>(at + q * Shape::kY * 2) = p[q];
+                for (int q = 0; q < 3; ++q) p[q][k] = two[q];
             }
-        }
-        uint8_t* xs = to_lds + kParts * Shape::kY * 2;
 #pragma unroll
-        for (int n = 0; n < kXUnits; ++n) {
-            const int u = n * kThreads + tid, r = u / (BN / 16), v = u % (BN / 16) * 2;
-            const float scale = __uint_as_float(s.scale[n] << 23);
-            u32x4 w[2];
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                w[k / 4][k % 4] = __builtin_bit_cast(uint32_t, k % 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(s.x[n][k / 2], scale, true)
-                                                                     : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(s.x[n][k / 2], scale, false));
-            u32x4* at = reinterpret_cast<u32x4*>(xs + Shape::template at<BN>(r, v));
-            at[0] = w[0];
-            at[1] = w[1];
+            for (int q = 0; q < 3; ++q) *reinterpret_cast<ADAGC_LDS u32x4*>(at + q * S::kY * 2) = p[q];
         }
+    };
+    auto write_x = [&](const Staged& s, int n, uint32_t place) __attribute__((always_inline)) {
+        const float scale = __uint_as_float(s.scale[n] << 23);
+        u32x4 w[2];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            w[k / 4][k % 4] = __builtin_bit_cast(uint32_t, k % 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(s.x[n][k / 2], scale, true)
+                                                                 : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(s.x[n][k / 2], scale, false));
+        const uint32_t at = place + write_x_at + (uint32_t)(n * kXRows * BN * 2);
+        *reinterpret_cast<ADAGC_LDS u32x4*>(at) = w[0];
+        *reinterpret_cast<ADAGC_LDS u32x4*>(at + 16) = w[1];
+    };
+    auto write = [&](const Staged& s, uint32_t place) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < kYUnits; ++n) write_y(s, n, place);
+#pragma unroll
+        for (int n = 0; n < kXUnits; ++n) write_x(s, n, place);
     };
 
     // Fragments.  16 lanes read 4 rows of 16 columns and get a column each; lane l's are rows 8 (l / 16) .. + 7 of column l mod 16.
     const int fr = 8 * (lane >> 4) + ((lane >> 2) & 3);
-    const uint32_t fy = fr * BM * 2 + (((wm * kTM) ^ Shape::swizzle(fr)) * 32) + (lane & 3) * 8;
-    const uint32_t fx = kParts * Shape::kY * 2 + fr * BN * 2 + (((wn * kTN) ^ Shape::swizzle(fr)) * 32) + (lane & 3) * 8;
-    auto fragment = [&](uint32_t from, uint32_t pitch) __attribute__((always_inline)) {
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ADAGC_LDS s16x4*>(from));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ADAGC_LDS s16x4*>(from + 4 * pitch));
-        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    const uint32_t fy = fr * BM * 2 + (((wm * kTM) ^ S::swizzle(fr)) * 32) + (lane & 3) * 8;
+    const uint32_t fx = kParts * S::kY * 2 + fr * BN * 2 + (((wn * kTN) ^ S::swizzle(fr)) * 32) + (lane & 3) * 8;
+    auto read4 = [](uint32_t at) __attribute__((always_inline)) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ADAGC_LDS s16x4*>(at)); };
+    auto fragment = [&](uint32_t at, uint32_t pitch) __attribute__((always_inline)) {
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(read4(at), read4(at + 4 * pitch), 0, 1, 2, 3, 4, 5, 6, 7));
     };
+    auto read_y = [&](int g, uint32_t place) __attribute__((always_inline)) {
+        return fragment(place + (fy ^ (uint32_t)(g % kTM * 32)) + (uint32_t)(g / kTM * S::kY * 2), BM * 2);
+    };
+    auto read_x = [&](int n, uint32_t place) __attribute__((always_inline)) { return fragment(place + (fx ^ (uint32_t)(n * 32)), BN * 2); };
 
     f32x4 acc[kTM][kTN];
 #pragma unroll
     for (int m = 0; m < kTM; ++m)
 #pragma unroll
         for (int n = 0; n < kTN; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    constexpr int kG = kParts * kTM;               // fragments of dY
+    bf16x8 y[kG], x[2][kTN];
 
-    Staged staged;
-    if (step0 < step1) {
-        load(step0, staged);
-        write(staged, lds);
-        if (step0 + 1 < step1) load(step0 + 1, staged);
-    }
-    __syncthreads();
-    int buffer = 0;
-    for (int64_t step = step0; step < step1; ++step) {
-        const uint32_t from = lds0 + (uint32_t)(buffer * Shape::kBuffer);
-        if (step + 1 < step1) write(staged, lds + (buffer ^ 1) * Shape::kBuffer);
-        if (step + 2 < step1) load(step + 2, staged);
-#pragma unroll
-        for (int kk = 0; kk < kDeep / 32; ++kk) {
-            bf16x8 x[kTN];
-#pragma unroll
-            for (int n = 0; n < kTN; ++n) x[n] = fragment(from + (fx ^ (n * 32)) + kk * 32 * BN * 2, BN * 2);
-#pragma unroll
-            for (int q = 0; q < kParts; ++q)
-#pragma unroll
-                for (int m = 0; m < kTM; ++m) {
-                    const bf16x8 y = fragment(from + (fy ^ (m * 32)) + q * Shape::kY * 2 + kk * 32 * BM * 2, BM * 2);
-#pragma unroll
-                    for (int n = 0; n < kTN; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[n], y, acc[m][n], 0, 0, 0);
-                }
-        }
+    auto plain_step = [&](int64_t step) __attribute__((always_inline)) {
+        Staged s;
         __syncthreads();
-        buffer ^= 1;
+        load_checked(step, s);
+        write(s, lds0);
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < kTN; ++n) x[0][n] = read_x(n, lds0);
+#pragma unroll
+        for (int g = 0; g < kG; ++g) {
+            y[0] = read_y(g, lds0);
+#pragma unroll
+            for (int n = 0; n < kTN; ++n) acc[g % kTM][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[0][n], y[0], acc[g % kTM][n], 0, 0, 0);
+        }
+    };
+
+    if constexpr (EDGE) {
+        for (int64_t step = step0; step < step1; ++step) plain_step(step);
+    } else if (step0 < step1) {
+        Staged staged[2];
+        auto clamp = [&](int64_t step) { return min(step, step1 - 1); };
+        load(step0, staged[0]);
+        load(clamp(step0 + 1), staged[1]);
+        write(staged[0], lds0);
+        load(clamp(step0 + 2), staged[0]);
+        write(staged[1], lds0 + S::kPlace);
+        load(clamp(step0 + 3), staged[1]);
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < kTN; ++n) x[0][n] = read_x(n, lds0);
+#pragma unroll
+        for (int g = 0; g < kG; ++g) y[g] = read_y(g, lds0);
+        uint32_t next = lds0 + S::kPlace;          // the place of step k + 1
+        auto after = [&](uint32_t place) { return place == lds0 + (kPlaces - 1) * S::kPlace ? lds0 : place + S::kPlace; };
+        auto one_step = [&](auto PARITY, int64_t step) __attribute__((always_inline)) {
+            constexpr int p = decltype(PARITY)::value;
+            constexpr int kSlots = kG * kTN;
+            constexpr int kWrites = kYUnits + kXUnits;
+            const uint32_t to_place = after(next);
+            const int64_t ahead = clamp(step + 4);
+            static_for<kSlots>([&](auto SLOT) __attribute__((always_inline)) {
+                constexpr int slot = decltype(SLOT)::value, g = slot / kTN, n = slot % kTN;
+                acc[g % kTM][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[p][n], y[g], acc[g % kTM][n], 0, 0, 0);
+                ADAGC_SCHED_FENCE();
+                if constexpr (slot % 2 == 0 && slot / 2 < kTN) x[p ^ 1][slot / 2] = read_x(slot / 2, next);
+                if constexpr (n == kTN - 1) y[g] = read_y(g, next);
+                static_for<kWrites>([&](auto N) __attribute__((always_inline)) {
+                    constexpr int w = decltype(N)::value;
+                    if constexpr (kSlots / 4 + w * (kSlots / 4) / kWrites + 1 == slot) {
+                        if constexpr (w < kYUnits) write_y(staged[p], w, to_place);
+                        else write_x(staged[p], w - kYUnits, to_place);
+                    }
+                    if constexpr (kSlots / 2 + 2 + w * (kSlots / 4) / kWrites == slot) {
+                        if constexpr (w < kYUnits) load_y(ahead, w, staged[p]);
+                        else load_x(ahead, w - kYUnits, staged[p]);
+                    }
+                });
+                ADAGC_SCHED_FENCE();
+            });
+            // the writes, in the first half of the step, are done; the fragments read since may still be on their way
+            constexpr int kSince = 2 * (kG / 2 - 1);
+            ADAGC_WAIT_LDS(kSince < 15 ? kSince : 15);
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            ADAGC_SCHED_FENCE();
+            next = to_place;
+        };
+        int64_t step = step0;
+        for (; step + 1 < step1; step += 2) {
+            one_step(std::integral_constant<int, 0>{}, step);
+            one_step(std::integral_constant<int, 1>{}, step + 1);
+        }
+        if (step < step1) one_step(std::integral_constant<int, 0>{}, step);
     }
+    if (last && a.rows % kDeep) plain_step(full);
 
     // lane l holds rows (l / 16) * 4 .. + 3 (of X's block) of column l mod 16 (of dY's)
     if (alone) {
@@ -265,7 +374,7 @@ __global__ __launch_bounds__(64 * kWM * kWN, 2) void wgrad_kernel(const WgradArg
         for (int m = 0; m < kTM; ++m)
 #pragma unroll
             for (int n = 0; n < kTN; ++n)
-                store_results<W>(a, o0 + (wm * kTM + m) * 16 + (lane & 15), i0 + (wn * kTN + n) * 16 + (lane >> 4) * 4, acc[m][n]);
+                store_results(a, o0 + (wm * kTM + m) * 16 + (lane & 15), o_least, i0 + (wn * kTN + n) * 16 + (lane >> 4) * 4, i_least, acc[m][n]);
     } else {
         f32x4* to_ws = reinterpret_cast<f32x4*>(a.workspace) + (size_t)(item - a.whole) * (BM * BN / 4) + tid;
 #pragma unroll
@@ -276,19 +385,20 @@ __global__ __launch_bounds__(64 * kWM * kWN, 2) void wgrad_kernel(const WgradArg
 }
 
 // Adds the parts of the split tiles, in order: a workgroup takes one 16 x 16 block of every wave.
-template <class T, class W, int BM, int BN, int kWM, int kWN, int kDeep>
-__global__ __launch_bounds__(64 * kWM * kWN) void join_kernel(const WgradArgs a)
+template <class S, bool EDGE>
+__global__ __launch_bounds__(S::kThreads) void join_kernel(const WgradArgs a)
 {
-    typedef Tile<T, BM, BN, kWM, kWN, kDeep> Shape;
-    constexpr int kTM = Shape::kTM, kTN = Shape::kTN;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / kWN, wn = wave % kWN;
+    constexpr int kTM = S::kTM, kTN = S::kTN, BM = S::BM, BN = S::BN;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / S::kWN, wn = wave % S::kWN;
     const int n_tile = (int)blockIdx.x / (kTM * kTN), block = (int)blockIdx.x % (kTM * kTN), m = block / kTN, n = block % kTN;
     int to, ti;
     place_of_tile(a, a.whole + n_tile, &to, &ti);
-    const f32x4* from = reinterpret_cast<const f32x4*>(a.workspace) + (size_t)n_tile * a.split * (BM * BN / 4) + (size_t)block * Shape::kThreads + tid;
+    const int64_t o_least = (int64_t)to * BM, i_least = (int64_t)ti * BN;
+    const int64_t o0 = EDGE ? o_least : min(o_least, (int64_t)a.n_out - BM), i0 = EDGE ? i_least : min(i_least, (int64_t)a.ld - BN);
+    const f32x4* from = reinterpret_cast<const f32x4*>(a.workspace) + (size_t)n_tile * a.split * (BM * BN / 4) + (size_t)block * S::kThreads + tid;
     f32x4 sum = from[0];
     for (int p = 1; p < a.split; ++p) sum += from[(size_t)p * (BM * BN / 4)];
-    store_results<W>(a, (int64_t)to * BM + (wm * kTM + m) * 16 + (lane & 15), (int64_t)ti * BN + (wn * kTN + n) * 16 + (lane >> 4) * 4, sum);
+    store_results(a, o0 + (wm * kTM + m) * 16 + (lane & 15), o_least, i0 + (wn * kTN + n) * 16 + (lane >> 4) * 4, i_least, sum);
 }
 
 int check(int64_t rows, int64_t n_out, int64_t n_in, int32_t dtype)
@@ -300,7 +410,6 @@ int check(int64_t rows, int64_t n_out, int64_t n_in, int32_t dtype)
 
 // How a call is cut: square tiles of dW, and those of the last, partial round of workgroups also along the tokens, so that they
 // fill the chip too.
-constexpr int kDeep16 = 64, kDeep32 = 32;        // tokens at a time with bf16 and fp32 dY
 struct Plan {
     int     side;
     int64_t tiles_out, tiles_in, whole, rest, split;
@@ -310,35 +419,36 @@ Plan plan_of(int64_t rows, int64_t n_out, int64_t n_in, int32_t dtype)
 {
     Plan p{};
     auto tiles = [&](int64_t side) { return ((n_out + side - 1) / side) * ((n_in + side - 1) / side); };
-    p.side = dtype == ADAGC_BF16 && tiles(256) >= kUnits / 2 ? 256 : 128;
+    p.side = dtype == ADAGC_BF16 && n_out >= 256 && act8_ld(n_in) >= 256 && tiles(256) >= kUnits / 2 ? 256 : 128;
     p.tiles_out = (n_out + p.side - 1) / p.side;
     p.tiles_in = (n_in + p.side - 1) / p.side;
-    const int64_t all = p.tiles_out * p.tiles_in, round = p.side == 256 ? kUnits : 2 * kUnits;
-    const int64_t deep = dtype == ADAGC_BF16 ? kDeep16 : kDeep32, steps = (rows + deep - 1) / deep;
+    const int64_t all = p.tiles_out * p.tiles_in, round = p.side == 256 ? kUnits : 2 * kUnits, steps = rows / kDeep;
     p.rest = all % round;
-    p.split = p.rest ? std::max<int64_t>(1, std::min(round / p.rest, steps / 4)) : 1;
+    p.split = p.rest ? std::max<int64_t>(1, std::min(round / p.rest, steps / 8)) : 1;
     if (p.split == 1) p.rest = 0;
     p.whole = all - p.rest;
     return p;
 }
 
-template <class T, class W, int SIDE, int kWM, int kWN, int kDeep>
+template <class S, class T, bool EDGE>
 int launch(const WgradArgs& a, const Plan& p, hipStream_t s)
 {
-    typedef Tile<T, SIDE, SIDE, kWM, kWN, kDeep> Shape;
-    wgrad_kernel<T, W, SIDE, SIDE, kWM, kWN, kDeep>
-        <<<dim3((uint32_t)(p.whole + p.rest * p.split)), dim3(Shape::kThreads), 0, s>>>(a);
-    if (p.rest)
-        join_kernel<T, W, SIDE, SIDE, kWM, kWN, kDeep>
-            <<<dim3((uint32_t)(p.rest * Shape::kTM * Shape::kTN)), dim3(Shape::kThreads), 0, s>>>(a);
+    wgrad_kernel<S, T, EDGE><<<dim3((uint32_t)(p.whole + p.rest * p.split)), dim3(S::kThreads), 0, s>>>(a);
+    if (p.rest) join_kernel<S, EDGE><<<dim3((uint32_t)(p.rest * S::kTM * S::kTN)), dim3(S::kThreads), 0, s>>>(a);
     return hipGetLastError() == hipSuccess ? ADAGC_OK : ADAGC_ERR_HIP;
 }
-template <class W>
-int launch(const WgradArgs& a, const Plan& p, int32_t dtype, hipStream_t s)
+template <class T>
+int launch(const WgradArgs& a, const Plan& p, hipStream_t s)
 {
-    if (dtype == ADAGC_F32) return launch<float, W, 128, 2, 2, kDeep32>(a, p, s);
-    if (p.side == 256) return launch<uint16_t, W, 256, 2, 4, kDeep16>(a, p, s);
-    return launch<uint16_t, W, 128, 2, 2, kDeep16>(a, p, s);
+    const bool narrow_rows = a.ld_d < (int64_t)1 << 24;            // 32 of them are within 32 bits
+    if constexpr (sizeof(T) == 2) {
+        if (p.side == 256) {
+            if (narrow_rows) return launch<Tile<T, 256, 256, 2, 4>, T, false>(a, p, s);
+            return launch<Tile<T, 256, 256, 2, 4>, T, true>(a, p, s);
+        }
+    }
+    if (narrow_rows && a.n_out >= 128 && a.ld >= 128) return launch<Tile<T, 128, 128, 2, 2>, T, false>(a, p, s);
+    return launch<Tile<T, 128, 128, 2, 2>, T, true>(a, p, s);
 }
 
 }  // namespace
@@ -384,6 +494,7 @@ extern "C" int adagc_act8_wgrad(const void* d_out, int32_t dtype, int64_t ld_d_o
     a.whole = (int32_t)p.whole;
     a.split = (int32_t)p.split;
     a.accumulate = accumulate;
+    a.weight_bf16 = weight_dtype == ADAGC_BF16;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    return weight_dtype == ADAGC_F32 ? launch<float>(a, p, dtype, s) : launch<uint16_t>(a, p, dtype, s);
+    return dtype == ADAGC_F32 ? launch<float>(a, p, s) : launch<uint16_t>(a, p, s);
 }

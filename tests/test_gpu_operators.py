@@ -448,6 +448,39 @@ def test_wgrad(dtype, dw, rows, n_out, n_in, ld_d, offset, ld_w, accumulate):
     near(got, want, off, TYPES[dw])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows, n_out, n_in, ld_d, offset, accumulate", [
+    (700, 2048, 4096, None, 0, False),                 # tiles that are all split along the tokens
+    (1027, 2901, 2999, 2903, 1, True),                 # odd everything: the last tiles begin inside others
+    (97, 5003, 4100, None, 0, True),
+    (31, 4096, 4096, None, 0, False),                  # less than a step
+    (2500, 12345, 1500, None, 0, False),               # whole tiles and split ones
+    (40, 3000, 3000, 2 ** 24, 0, False),               # rows far apart
+])
+def test_wgrad_large_tiles(dtype, rows, n_out, n_in, ld_d, offset, accumulate):
+    """The oracle's formulas with the product on the GPU, in 64 bits."""
+    g = torch.Generator(device=DEV).manual_seed(rows)
+    rand = lambda *s: torch.randn(*s, generator=g, device=DEV)
+    flat = torch.full((offset + (rows - 1) * (ld_d or n_out) + n_out,), math.nan, dtype=TYPES[dtype], device=DEV)
+    d_out = flat[offset:].as_strided((rows, n_out), (ld_d or n_out, 1), offset)
+    d_out.copy_(rand(rows, n_out))
+    x = (rand(rows, n_in) * torch.exp(rand(1, n_in))).bfloat16()
+    ckpt = torch.empty(B.adagc_act8_bytes(rows, n_in), dtype=torch.uint8, device=DEV)
+    B.adagc_act8_pack(x, ckpt)
+    held = torch.empty(rows, n_in, device=DEV)
+    B.adagc_act8_unpack(ckpt, held)
+    w = Framed(n_out, n_in, torch.float32, n_in + 1, 1)
+    start = rand(n_out, n_in) if accumulate else torch.zeros(n_out, n_in, device=DEV)
+    w.t.copy_(start)
+    code = B.ADAGC_F32 if dtype == "f32" else B.ADAGC_BF16
+    B.adagc_act8_wgrad(d_out, ckpt, w.t, accumulate=accumulate, workspace=workspace(B.adagc_act8_wgrad_workspace_bytes(rows, n_out, n_in, code)))
+    y, held = d_out.double(), held.double()
+    want = y.t().contiguous() @ held + start
+    off = (rows + 8) * 2 * O.U32 * (y.abs().t().contiguous() @ held.abs()) + 2 * O.U32 * want.abs()
+    assert ((w.t.double() - want).abs() <= off).all()
+    assert (w.flat[~w.inside] == FILL).all()
+
+
 @pytest.mark.parametrize("dw", ["f32", "bf16"])
 def test_wgrad_no_rows(dw):
     d_out, x = torch.zeros(0, 70), torch.zeros(0, 45, dtype=torch.bfloat16)
