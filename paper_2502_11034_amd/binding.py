@@ -256,25 +256,38 @@ def adagc_muon_gemm_nt_batched(P, Q, alpha=1.0, beta=0.0, Dt=None, C=None, Ct=No
 
 # ---- operators around the step: 2-D device tensors, fp32 or bf16, consecutive elements in a row
 
+_TYPES = {}                    # torch dtypes seen so far: (code or None, name)
+
+
+def _type(dtype):
+    known = _TYPES.get(dtype)
+    if known is None:
+        name = str(dtype)
+        known = _TYPES[dtype] = ({"torch.float32": ADAGC_F32, "torch.bfloat16": ADAGC_BF16}.get(name), name)
+    return known
+
+
 def _matrix(t, shape, name, dtype=None):
     """(pointer, dtype code, leading dimension) of a 2-D tensor."""
-    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
-        raise ValueError("%s: shape %s, expected %s" % (name, tuple(t.shape), "2-D" if shape is None else tuple(shape)))
-    code = {"torch.float32": ADAGC_F32, "torch.bfloat16": ADAGC_BF16}.get(str(t.dtype))
+    own = t.shape
+    if len(own) != 2 or (shape is not None and own != shape):
+        raise ValueError("%s: shape %s, expected %s" % (name, tuple(own), "2-D" if shape is None else tuple(shape)))
+    code = _type(t.dtype)[0]
     if code is None or (dtype is not None and code != dtype):
         raise TypeError("%s: dtype %s" % (name, t.dtype))
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if step != 1 and own[1] > 1:
         raise ValueError("%s: elements of a row are not consecutive" % name)
-    return t.data_ptr(), code, t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return t.data_ptr(), code, ld if own[0] > 1 else own[1]
 
 
 def _dense(t, shape, dtype, name):
     """Pointer of a contiguous tensor (None for None)."""
     if t is None:
         return None
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError("%s: shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
-    if str(t.dtype) != dtype:
+    if _type(t.dtype)[1] != dtype:
         raise TypeError("%s: dtype %s, expected %s" % (name, t.dtype, dtype))
     if not t.is_contiguous():
         raise ValueError("%s is not contiguous" % name)
@@ -284,14 +297,15 @@ def _dense(t, shape, dtype, name):
 def _bytes(t, least, name):
     """(pointer, bytes) of a contiguous device buffer (None: (None, 0)) of at least so many bytes."""
     if t is None:
-        n = 0
-    elif not t.is_contiguous():
+        if least > 0:
+            raise ValueError("%s: %d bytes needed" % (name, least))
+        return None, 0
+    if not t.is_contiguous():
         raise ValueError("%s is not contiguous" % name)
-    else:
-        n = t.numel() * t.element_size()
+    n = t.nbytes
     if n < least:
         raise ValueError("%s: %d bytes, %d needed" % (name, n, least))
-    return (t.data_ptr() if t is not None else None), n
+    return t.data_ptr(), n
 
 
 def _size(rc, where):

@@ -10,6 +10,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "act8_device.h"
 #include "operators_internal.h"
@@ -34,19 +35,25 @@ struct Args {
     int64_t    rows;
     int32_t    cols, ld;         // of the checkpoints
     uint32_t   row_vectors;      // vectors of a row of ld elements
+    uint32_t   reciprocal;       // 2^32 / row_vectors, rounded down
     uint64_t   vectors;
 };
 
-// Vector number v of the matrix: its row and first column.
 struct Place {
     int64_t row;
     int32_t col;
 };
-template <int N>
-__device__ __forceinline__ Place place_of(const Args& a, uint64_t v)
+
+template <bool WHOLE, class T>
+__device__ __forceinline__ Vector<T> fetch(const T* row, const Args& a, int32_t col)
 {
-    const uint64_t row = v / a.row_vectors;
-    return {(int64_t)row, (int32_t)(v - row * a.row_vectors) * N};
+    return WHOLE ? load_whole(row + col) : load_vector(row, col, a.cols, 0);
+}
+template <bool WHOLE, class T>
+__device__ __forceinline__ void put(T* row, const Args& a, int32_t col, const Vector<T>& v)
+{
+    if constexpr (WHOLE) store_whole(row + col, v);
+    else store_vector(row, col, a.cols, v);
 }
 
 template <class T>
@@ -135,31 +142,44 @@ __device__ __forceinline__ float sigmoid(float g)
 // finish(place, load(place)) for every vector; a lane's loads come before its first store, of which the compiler could not tell that
 // they touch nothing of what is still to be loaded.  Lanes of a block go together: vectors are dealt to lanes in order, and a row has
 // whole blocks.
+// WHOLE: rows end with a block of 32, so no vector is cut.
 template <int N, class Load, class Finish>
 __device__ __forceinline__ void each_vector(const Args& a, Load&& load, Finish&& finish)
 {
-    const uint64_t per_item = (uint64_t)kThreads * kPerLane;
-    for (uint64_t first = blockIdx.x * per_item; first < a.vectors; first += gridDim.x * per_item) {
+    constexpr uint32_t kItem = kThreads * kPerLane;
+    for (uint64_t first = (uint64_t)blockIdx.x * kItem; first < a.vectors; first += (uint64_t)gridDim.x * kItem) {
+        // the first vector's row by a division, the same in all lanes; the others' from there, by a product that is one short at most
+        const uint64_t row0 = a.vectors >> 32 ? first / a.row_vectors : (uint32_t)first / a.row_vectors;
+        const uint32_t col0 = (uint32_t)(first - row0 * a.row_vectors), left = (uint32_t)min(a.vectors - first, (uint64_t)kItem);
+        auto place = [&](uint32_t n) __attribute__((always_inline)) {
+            const uint32_t from = col0 + n;
+            uint32_t rows = __umulhi(from, a.reciprocal), col = from - rows * a.row_vectors;
+            if (col >= a.row_vectors) {
+                ++rows;
+                col -= a.row_vectors;
+            }
+            return Place{(int64_t)(row0 + rows), (int32_t)(col * N)};
+        };
         Place at[kPerLane];
         decltype(load(at[0])) in[kPerLane];
 #pragma unroll
         for (int u = 0; u < kPerLane; ++u) {
-            const uint64_t v = first + (uint64_t)(u * kThreads) + threadIdx.x;
-            at[u] = place_of<N>(a, v < a.vectors ? v : 0);
+            const uint32_t n = (uint32_t)(u * kThreads) + threadIdx.x;
+            at[u] = place(n < left ? n : 0);
             in[u] = load(at[u]);
         }
 #pragma unroll
         for (int u = 0; u < kPerLane; ++u)
-            if (first + (uint64_t)(u * kThreads) + threadIdx.x < a.vectors) finish(at[u], in[u]);
+            if ((uint32_t)(u * kThreads) + threadIdx.x < left) finish(at[u], in[u]);
     }
 }
 
-template <class T>
+template <class T, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void pack_kernel(const Args a)
 {
     constexpr int N = 16 / sizeof(T);
     each_vector<N>(
-        a, [&](const Place& at) { return load_vector(row_of<T>(a.x, at.row), at.col, a.cols, 0); },
+        a, [&](const Place& at) { return fetch<WHOLE>(row_of<T>(a.x, at.row), a, at.col); },
         [&](const Place& at, const Vector<T>& in) {
             float x[N];
             widen(in, x);
@@ -167,7 +187,7 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const Args a)
         });
 }
 
-template <class T>
+template <class T, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void unpack_kernel(const Args a)
 {
     constexpr int N = 16 / sizeof(T);
@@ -176,12 +196,12 @@ __global__ __launch_bounds__(kThreads) void unpack_kernel(const Args a)
         [&](const Place& at, const Packed& in) {
             float x[N];
             unpack_vector(in, x);
-            store_vector(out_row<T>(a.x, at.row), at.col, a.cols, narrow<T>(x));
+            put<WHOLE>(out_row<T>(a.x, at.row), a, at.col, narrow<T>(x));
         });
 }
 
 // x: gate, y: up, z: out
-template <class T, bool PACK>
+template <class T, bool WHOLE, bool PACK>
 __global__ __launch_bounds__(kThreads) void swiglu_kernel(const Args a)
 {
     constexpr int N = 16 / sizeof(T);
@@ -191,7 +211,7 @@ __global__ __launch_bounds__(kThreads) void swiglu_kernel(const Args a)
     each_vector<N>(
         a,
         [&](const Place& at) {
-            return In{load_vector(row_of<T>(a.x, at.row), at.col, a.cols, 0), load_vector(row_of<T>(a.y, at.row), at.col, a.cols, 0)};
+            return In{fetch<WHOLE>(row_of<T>(a.x, at.row), a, at.col), fetch<WHOLE>(row_of<T>(a.y, at.row), a, at.col)};
         },
         [&](const Place& at, const In& in) {
             float g[N], u[N], h[N];
@@ -199,7 +219,7 @@ __global__ __launch_bounds__(kThreads) void swiglu_kernel(const Args a)
             widen(in.up, u);
 #pragma unroll
             for (int i = 0; i < N; ++i) h[i] = g[i] * sigmoid(g[i]) * u[i];
-            store_vector(out_row<T>(a.z, at.row), at.col, a.cols, narrow<T>(h));
+            put<WHOLE>(out_row<T>(a.z, at.row), a, at.col, narrow<T>(h));
             if constexpr (PACK) {
                 pack_vector(a, a.a, at, g);
                 pack_vector(a, a.b, at, u);
@@ -208,7 +228,7 @@ __global__ __launch_bounds__(kThreads) void swiglu_kernel(const Args a)
 }
 
 // x: d_out, y: d_gate, z: d_up, w: out (or null)
-template <class T>
+template <class T, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void swiglu_backward_kernel(const Args a)
 {
     constexpr int N = 16 / sizeof(T);
@@ -219,7 +239,7 @@ __global__ __launch_bounds__(kThreads) void swiglu_backward_kernel(const Args a)
     each_vector<N>(
         a,
         [&](const Place& at) {
-            return In{load_vector(row_of<T>(a.x, at.row), at.col, a.cols, 0), load_packed<N>(a, a.a, at), load_packed<N>(a, a.b, at)};
+            return In{fetch<WHOLE>(row_of<T>(a.x, at.row), a, at.col), load_packed<N>(a, a.a, at), load_packed<N>(a, a.b, at)};
         },
         [&](const Place& at, const In& in) {
             float g[N], u[N], d[N], dg[N], h[N];
@@ -233,9 +253,9 @@ __global__ __launch_bounds__(kThreads) void swiglu_backward_kernel(const Args a)
                 h[i] = silu * u[i];
                 d[i] *= silu;
             }
-            store_vector(out_row<T>(a.y, at.row), at.col, a.cols, narrow<T>(dg));
-            store_vector(out_row<T>(a.z, at.row), at.col, a.cols, narrow<T>(d));
-            if (a.w.p) store_vector(out_row<T>(a.w, at.row), at.col, a.cols, narrow<T>(h));
+            put<WHOLE>(out_row<T>(a.y, at.row), a, at.col, narrow<T>(dg));
+            put<WHOLE>(out_row<T>(a.z, at.row), a, at.col, narrow<T>(d));
+            if (a.w.p) put<WHOLE>(out_row<T>(a.w, at.row), a, at.col, narrow<T>(h));
         });
 }
 
@@ -252,6 +272,7 @@ Args arguments(int64_t rows, int64_t cols, int32_t dtype)
     a.cols = (int32_t)cols;
     a.ld = (int32_t)act8_ld(cols);
     a.row_vectors = (uint32_t)(a.ld * dtype_size(dtype) / 16);
+    a.reciprocal = a.row_vectors == 1 ? UINT32_MAX : (uint32_t)((1ull << 32) / a.row_vectors);
     a.vectors = (uint64_t)rows * a.row_vectors;
     return a;
 }
@@ -276,7 +297,15 @@ int check_matrix(const void* p, int64_t ld, int64_t cols, int32_t dtype)
 }
 int check_checkpoint(const void* p) { return !p || misaligned(p, 16) ? ADAGC_ERR_INVALID_ARG : ADAGC_OK; }
 
-int done() { return hipGetLastError() == hipSuccess ? ADAGC_OK : ADAGC_ERR_HIP; }
+// f(T{}, bool constant whether rows end with a block) for the call's type and columns
+template <class F>
+int dispatch(int32_t dtype, const Args& a, F&& f)
+{
+    const bool whole = a.cols == a.ld;
+    if (dtype == ADAGC_F32) whole ? f(0.0f, std::true_type{}) : f(0.0f, std::false_type{});
+    else whole ? f(uint16_t{}, std::true_type{}) : f(uint16_t{}, std::false_type{});
+    return hipGetLastError() == hipSuccess ? ADAGC_OK : ADAGC_ERR_HIP;
+}
 
 }  // namespace
 }  // namespace adagc
@@ -299,9 +328,9 @@ extern "C" int adagc_act8_pack(const void* x, int32_t dtype, int64_t rows, int64
     a.x = {const_cast<void*>(x), ld};
     a.a = checkpoint(ckpt, rows, cols);
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    if (dtype == ADAGC_F32) pack_kernel<float><<<grid_of(a), dim3(kThreads), 0, s>>>(a);
-    else pack_kernel<uint16_t><<<grid_of(a), dim3(kThreads), 0, s>>>(a);
-    return done();
+    return dispatch(dtype, a, [&](auto t, auto whole) {
+        pack_kernel<decltype(t), decltype(whole)::value><<<grid_of(a), dim3(kThreads), 0, s>>>(a);
+    });
 }
 
 extern "C" int adagc_act8_unpack(const void* ckpt, int64_t rows, int64_t cols, void* x, int32_t dtype, int64_t ld, void* stream)
@@ -314,9 +343,9 @@ extern "C" int adagc_act8_unpack(const void* ckpt, int64_t rows, int64_t cols, v
     a.x = {x, ld};
     a.a = checkpoint(ckpt, rows, cols);
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    if (dtype == ADAGC_F32) unpack_kernel<float><<<grid_of(a), dim3(kThreads), 0, s>>>(a);
-    else unpack_kernel<uint16_t><<<grid_of(a), dim3(kThreads), 0, s>>>(a);
-    return done();
+    return dispatch(dtype, a, [&](auto t, auto whole) {
+        unpack_kernel<decltype(t), decltype(whole)::value><<<grid_of(a), dim3(kThreads), 0, s>>>(a);
+    });
 }
 
 extern "C" int adagc_swiglu(const void* gate, int64_t ld_gate, const void* up, int64_t ld_up, int32_t dtype, int64_t rows, int64_t cols,
@@ -338,13 +367,11 @@ extern "C" int adagc_swiglu(const void* gate, int64_t ld_gate, const void* up, i
     if (gate_ckpt) {
         a.a = checkpoint(gate_ckpt, rows, cols);
         a.b = checkpoint(up_ckpt, rows, cols);
-        if (dtype == ADAGC_F32) swiglu_kernel<float, true><<<grid_of(a), dim3(kThreads), 0, s>>>(a);
-        else swiglu_kernel<uint16_t, true><<<grid_of(a), dim3(kThreads), 0, s>>>(a);
-    } else {
-        if (dtype == ADAGC_F32) swiglu_kernel<float, false><<<grid_of(a), dim3(kThreads), 0, s>>>(a);
-        else swiglu_kernel<uint16_t, false><<<grid_of(a), dim3(kThreads), 0, s>>>(a);
     }
-    return done();
+    return dispatch(dtype, a, [&](auto t, auto whole) {
+        if (gate_ckpt) swiglu_kernel<decltype(t), decltype(whole)::value, true><<<grid_of(a), dim3(kThreads), 0, s>>>(a);
+        else swiglu_kernel<decltype(t), decltype(whole)::value, false><<<grid_of(a), dim3(kThreads), 0, s>>>(a);
+    });
 }
 
 extern "C" int adagc_swiglu_backward(const void* d_out, int64_t ld_d_out, int32_t dtype, const void* gate_ckpt, const void* up_ckpt,
@@ -369,7 +396,7 @@ extern "C" int adagc_swiglu_backward(const void* d_out, int64_t ld_d_out, int32_
     a.a = checkpoint(gate_ckpt, rows, cols);
     a.b = checkpoint(up_ckpt, rows, cols);
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    if (dtype == ADAGC_F32) swiglu_backward_kernel<float><<<grid_of(a), dim3(kThreads), 0, s>>>(a);
-    else swiglu_backward_kernel<uint16_t><<<grid_of(a), dim3(kThreads), 0, s>>>(a);
-    return done();
+    return dispatch(dtype, a, [&](auto t, auto whole) {
+        swiglu_backward_kernel<decltype(t), decltype(whole)::value><<<grid_of(a), dim3(kThreads), 0, s>>>(a);
+    });
 }

@@ -23,7 +23,6 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 #define ADAGC_LDS __attribute__((address_space(3)))
 
@@ -68,15 +67,17 @@ __device__ __forceinline__ void store_typed(const WgradArgs& a, int64_t o, int64
     if (i >= i_least && i + 4 <= a.n_in) {
         if constexpr (sizeof(W) == 4) {
             if (a.accumulate) {
-                f32x4 old;
-                memcpy(&old, w, 16);
-                v += old;
+                float old[4];
+                widen(load_whole(w), old);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[r] += old[r];
             }
-            memcpy(w, &v, 16);
+            store_whole(w, {__builtin_bit_cast(u32x4, v)});
         } else {
-            uint32_t two[2];
+            typedef uint32_t u32x2_of_bf16 __attribute__((ext_vector_type(2), aligned(2)));
+            u32x2_of_bf16 two;
             if (a.accumulate) {
-                memcpy(two, w, 8);
+                two = *reinterpret_cast<const u32x2_of_bf16*>(w);
                 v[0] += __uint_as_float(two[0] << 16);
                 v[1] += __uint_as_float(two[0] & 0xFFFF0000u);
                 v[2] += __uint_as_float(two[1] << 16);
@@ -85,7 +86,7 @@ __device__ __forceinline__ void store_typed(const WgradArgs& a, int64_t o, int64
             const f32x2_t lo = {v[0], v[1]}, hi = {v[2], v[3]};
             two[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2_t));
             two[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2_t));
-            memcpy(w, two, 8);
+            *reinterpret_cast<u32x2_of_bf16*>(w) = two;
         }
     } else {
 #pragma unroll
@@ -152,7 +153,7 @@ struct Tile {
 // before their reads in the next step; the reads of a place are done a step before it is written again.  Loads past the last step take
 // the last one again: a loop without conditions lets the compiler count what is outstanding.
 template <class S, class T, bool EDGE>
-__global__ __launch_bounds__(S::kThreads, 2) void wgrad_kernel(const WgradArgs a)
+__global__ __launch_bounds__(S::kThreads, S::kThreads == 256 && S::kParts == 3 ? 1 : 2) void wgrad_kernel(const WgradArgs a)
 {
     constexpr int BM = S::BM, BN = S::BN, kThreads = S::kThreads, kTM = S::kTM, kTN = S::kTN, kParts = S::kParts;
     constexpr int kYUnits = S::kYUnits, kXUnits = S::kXUnits, kH = (int)sizeof(T) / 2;
@@ -192,7 +193,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void wgrad_kernel(const WgradArgs a
     auto load_y = [&](int64_t step, int n, Staged& s) __attribute__((always_inline)) {
         const uint8_t* row = static_cast<const uint8_t*>(a.d_out) + ((step * kDeep + n * kYRows) * a.ld_d + o0) * sizeof(T);
 #pragma unroll
-        for (int h = 0; h < kH; ++h) memcpy(s.y[n][h].w, row + lane_y + h * 16, 16);
+        for (int h = 0; h < kH; ++h) s.y[n][h] = load_whole(reinterpret_cast<const T*>(row + lane_y) + h * 4);
     };
     auto load_x = [&](int64_t step, int n, Staged& s) __attribute__((always_inline)) {
         const int64_t at = (step * kDeep + n * kXRows) * a.ld + i0;
@@ -229,7 +230,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void wgrad_kernel(const WgradArgs a
     auto write_y = [&](const Staged& s, int n, uint32_t place) __attribute__((always_inline)) {
         const uint32_t at = place + write_y_at + (uint32_t)(n * kYRows * BM * 2);
         if constexpr (kParts == 1) {
-            *reinterpret_cast<ADAGC_LDS u32x4*>(at) = u32x4{s.y[n][0].w[0], s.y[n][0].w[1], s.y[n][0].w[2], s.y[n][0].w[3]};
+            *reinterpret_cast<ADAGC_LDS u32x4*>(at) = s.y[n][0].w;
         } else {
             // x = hi + mid + lo, each the upper half of what is left: exact.  (Of an infinity nothing is left.)
             u32x4 p[3];
@@ -408,21 +409,24 @@ int check(int64_t rows, int64_t n_out, int64_t n_in, int32_t dtype)
     return ADAGC_OK;
 }
 
-// How a call is cut: square tiles of dW, and those of the last, partial round of workgroups also along the tokens, so that they
+// How a call is cut: tiles of dW, and those of the last, partial round of workgroups also along the tokens, so that they
 // fill the chip too.
 struct Plan {
-    int     side;
+    int     bm, bn;
     int64_t tiles_out, tiles_in, whole, rest, split;
-    int64_t workspace() const { return split > 1 ? rest * split * side * side * 4 : 0; }
+    int64_t workspace() const { return split > 1 ? rest * split * bm * bn * 4 : 0; }
 };
 Plan plan_of(int64_t rows, int64_t n_out, int64_t n_in, int32_t dtype)
 {
     Plan p{};
-    auto tiles = [&](int64_t side) { return ((n_out + side - 1) / side) * ((n_in + side - 1) / side); };
-    p.side = dtype == ADAGC_BF16 && n_out >= 256 && act8_ld(n_in) >= 256 && tiles(256) >= kUnits / 2 ? 256 : 128;
-    p.tiles_out = (n_out + p.side - 1) / p.side;
-    p.tiles_in = (n_in + p.side - 1) / p.side;
-    const int64_t all = p.tiles_out * p.tiles_in, round = p.side == 256 ? kUnits : 2 * kUnits, steps = rows / kDeep;
+    auto tiles = [&](int64_t bm, int64_t bn) { return ((n_out + bm - 1) / bm) * ((n_in + bn - 1) / bn); };
+    const bool large = dtype == ADAGC_BF16 && n_out >= 256 && act8_ld(n_in) >= 256 && tiles(256, 256) >= kUnits / 2;
+    const bool wide = dtype == ADAGC_F32 && n_out >= 128 && act8_ld(n_in) >= 256;
+    p.bm = large ? 256 : 128;
+    p.bn = large || wide ? 256 : 128;
+    p.tiles_out = (n_out + p.bm - 1) / p.bm;
+    p.tiles_in = (n_in + p.bn - 1) / p.bn;
+    const int64_t all = p.tiles_out * p.tiles_in, round = p.bn == 256 ? kUnits : 2 * kUnits, steps = rows / kDeep;
     p.rest = all % round;
     p.split = p.rest ? std::max<int64_t>(1, std::min(round / p.rest, steps / 8)) : 1;
     if (p.split == 1) p.rest = 0;
@@ -440,15 +444,13 @@ int launch(const WgradArgs& a, const Plan& p, hipStream_t s)
 template <class T>
 int launch(const WgradArgs& a, const Plan& p, hipStream_t s)
 {
-    const bool narrow_rows = a.ld_d < (int64_t)1 << 24;            // 32 of them are within 32 bits
+    const bool edge = a.ld_d >= (int64_t)1 << 24 || a.n_out < p.bm || a.ld < p.bn;     // 32 rows are not within 32 bits, or less than a tile
     if constexpr (sizeof(T) == 2) {
-        if (p.side == 256) {
-            if (narrow_rows) return launch<Tile<T, 256, 256, 2, 4>, T, false>(a, p, s);
-            return launch<Tile<T, 256, 256, 2, 4>, T, true>(a, p, s);
-        }
+        if (p.bm == 256) return edge ? launch<Tile<T, 256, 256, 2, 4>, T, true>(a, p, s) : launch<Tile<T, 256, 256, 2, 4>, T, false>(a, p, s);
+    } else {
+        if (p.bn == 256) return edge ? launch<Tile<T, 128, 256, 2, 4>, T, true>(a, p, s) : launch<Tile<T, 128, 256, 2, 4>, T, false>(a, p, s);
     }
-    if (narrow_rows && a.n_out >= 128 && a.ld >= 128) return launch<Tile<T, 128, 128, 2, 2>, T, false>(a, p, s);
-    return launch<Tile<T, 128, 128, 2, 2>, T, true>(a, p, s);
+    return edge ? launch<Tile<T, 128, 128, 2, 2>, T, true>(a, p, s) : launch<Tile<T, 128, 128, 2, 2>, T, false>(a, p, s);
 }
 
 }  // namespace

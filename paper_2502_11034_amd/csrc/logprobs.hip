@@ -104,7 +104,7 @@ struct Running {
 // complement, so that keys are unique and equal values go to the lower index.  0: none.
 struct TopList {
     uint64_t mine = 0, least = 0;                // this lane's; the last one kept, the same in all lanes
-    float    bar = NAN;                          // its value; NaN: the list is not full
+    float    bar = NAN;                          // only larger values come in (its value, once the list is full); NaN: any value
 
     static __device__ __forceinline__ uint64_t key(float z, uint32_t index)
     {
@@ -139,9 +139,39 @@ struct TopList {
             mask &= mask - 1;
             mask &= __ballot(candidate > least);
         } while (mask);
-        bar = least ? value(least) : NAN;
+        if (least) bar = value(least);
+    }
+
+    // Sets the bar for an empty list from the first values: one of each lane, its largest.  The k-th largest of those is no larger
+    // than the k-th largest of all, so what is below it does not belong into the list: a wave's first 2048 values then cost about
+    // k insertions instead of k ln(2048 / k).  Found bit by bit.
+    __device__ __forceinline__ void begin(float lane_most, int k)
+    {
+        const uint32_t mine_bits = (uint32_t)(key(lane_most, 0) >> 32);
+        uint32_t at = 0;
+        for (uint32_t bit = 0x80000000u; bit; bit >>= 1)
+            if (__builtin_popcountll(__ballot(mine_bits >= (at | bit))) >= k) at |= bit;
+        // just below it (0 and -0 count as one value); with -inf or NaN there the list takes any value
+        const float kth = value((uint64_t)at << 32);
+        bar = kth > -INFINITY ? value((uint64_t)(at - (kth == 0.f ? 2 : 1)) << 32) : NAN;
     }
 };
+
+// Every lane's sums become the wave's, relative to its largest value.
+template <bool ENTROPY>
+__device__ __forceinline__ void reduce_lanes(Running<ENTROPY>& r, float c)
+{
+    float most = r.most;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) most = maximum(most, __shfl_xor(most, d));
+    r.most = most;
+    r.move_to(most == -INFINITY ? kLowest : most, c);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        r.sum += __shfl_xor(r.sum, d);
+        if (ENTROPY) r.weighted += __shfl_xor(r.weighted, d);
+    }
+}
 
 // Results of a row from its sums, by one wave.
 template <bool ENTROPY, bool TOP, class T>
@@ -182,57 +212,67 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const ForwardArgs a)
     const int64_t row = SPLIT ? blockIdx.x / (uint32_t)a.parts : blockIdx.x;
     const int part = SPLIT ? (int)(blockIdx.x - (uint32_t)row * (uint32_t)a.parts) : 0;
     const T* z = static_cast<const T*>(a.logits) + row * a.ld;
+    const int all = (a.vocab + N - 1) / N;
     const int first = SPLIT ? part * a.part_vectors : 0;
-    const int all = (int)(((int64_t)a.vocab + N - 1) / N);
     const int last = SPLIT ? min(first + a.part_vectors, all) : all;
+    const int last_whole = min(last, a.vocab / N);         // all but one at most
     const float c = a.scale * kLog2e, slack = kSlack / a.scale;
+    const int tid = (int)threadIdx.x;
     Running<ENTROPY> r;
     TopList top;
-    auto one = [&](const Vector<T>& v, int vector) __attribute__((always_inline)) {
+    auto largest = [](const float (&x)[N]) __attribute__((always_inline)) {
+        float m = x[0];
+#pragma unroll
+        for (int i = 1; i < N; ++i) m = maximum(m, x[i]);
+        return m;
+    };
+    // count: values of the vector that there are
+    auto one = [&](const Vector<T>& v, int vector, int count) __attribute__((always_inline)) {
         float x[N];
         widen(v, x);
-        float vmax = x[0];
-#pragma unroll
-        for (int i = 1; i < N; ++i) vmax = maximum(vmax, x[i]);
+        const float vmax = largest(x);
         r.add(x, vmax, c, slack);
         if constexpr (TOP) {
-            // later values have higher indices than all in the list, so only a larger one comes in; a list that is not full takes any
+            // These values have higher indices than all in the list, so only a larger one comes in; among themselves, which are taken
+            // value by value of all lanes, equal ones may come in any order.
             if (__ballot(!(vmax <= top.bar))) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const int64_t at = (int64_t)vector * N + i;
-                    top.take(vector < last && at < a.vocab ? TopList::key(x[i], (uint32_t)at) : 0, a.top_k);
-                }
+                for (int i = 0; i < N; ++i)
+                    if (__ballot(!(x[i] < top.bar))) top.take(i < count ? TopList::key(x[i], (uint32_t)(vector * N + i)) : 0, a.top_k);
             }
         }
     };
-    // whole waves go round together: lanes past the end get masked values
-    for (int v0 = first; v0 < last; v0 += 4 * kThreads) {
-        Vector<T> v[4];
+    // whole waves go round together
+    constexpr int kAhead = 4;
+    int v0 = first;
+    for (; v0 + kAhead * kThreads <= last_whole; v0 += kAhead * kThreads) {
+        Vector<T> v[kAhead];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int i = v0 + u * kThreads + (int)threadIdx.x;
-            v[u] = load_vector(z, (int64_t)i * N, i < last ? a.vocab : 0, masked<T>());
+        for (int u = 0; u < kAhead; ++u) v[u] = load_whole(z + (size_t)(v0 + u * kThreads) * N + (uint32_t)(tid * N));
+        if constexpr (TOP) {
+            if (v0 == first) {
+                float m = -INFINITY;
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) {
+                    float x[N];
+                    widen(v[u], x);
+                    m = maximum(m, largest(x));
+                }
+                top.begin(m, a.top_k);
+            }
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (v0 + u * kThreads < last) one(v[u], v0 + u * kThreads + (int)threadIdx.x);
+        for (int u = 0; u < kAhead; ++u) one(v[u], v0 + u * kThreads + tid, N);
+    }
+    for (; v0 < last; v0 += kThreads) {
+        const int i = v0 + tid, count = i < last ? min(N, a.vocab - i * N) : 0;
+        one(load_vector(z, (int64_t)i * N, count > 0 ? a.vocab : 0, masked<T>()), i, count);
     }
 
-    // lanes, then waves
-    float most = r.most;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) most = maximum(most, __shfl_xor(most, d));
-    r.most = most;
-    r.move_to(most == -INFINITY ? kLowest : most, c);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        r.sum += __shfl_xor(r.sum, d);
-        if (ENTROPY) r.weighted += __shfl_xor(r.weighted, d);
-    }
+    reduce_lanes(r, c);
     __shared__ RowPart wave_part[kWaves];
     __shared__ uint64_t wave_keys[TOP ? kWaves * ADAGC_MAX_TOP : 1];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int wave = tid >> 6, lane = tid & 63;
     if (lane == 0) wave_part[wave] = {r.most, r.sum, r.weighted, 0.f};
     if (TOP && lane < a.top_k) wave_keys[wave * a.top_k + lane] = top.mine;
     __syncthreads();
@@ -249,7 +289,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const ForwardArgs a)
     }
 }
 
-// One wave per row joins the row's parts.
+// One wave per row joins the row's parts, at most 64, one in each lane.
 template <class T, bool ENTROPY, bool TOP>
 __global__ __launch_bounds__(64) void join_parts_kernel(const ForwardArgs a)
 {
@@ -258,10 +298,19 @@ __global__ __launch_bounds__(64) void join_parts_kernel(const ForwardArgs a)
     const float c = a.scale * kLog2e;
     Running<ENTROPY> r;
     TopList top;
-    for (int p = 0; p < a.parts; ++p) {
-        const RowPart x = a.part[row * a.parts + p];
+    const bool has = lane < a.parts;
+    if (has) {
+        const RowPart x = a.part[row * a.parts + lane];
         r.join(x.most, x.sum, x.weighted, c);
-        if (TOP) top.take(lane < a.top_k ? a.part_keys[(row * a.parts + p) * a.top_k + lane] : 0, a.top_k);
+    }
+    reduce_lanes(r, c);
+    if constexpr (TOP) {
+        const uint64_t* keys = a.part_keys + (row * a.parts + lane) * a.top_k;
+        for (int j = 0; j < a.top_k; ++j) {
+            const uint64_t key = has ? keys[j] : 0;
+            if (!__ballot(key > top.least)) break;         // each part's keys fall
+            top.take(key, a.top_k);
+        }
     }
     write_row<ENTROPY, TOP, T>(a, row, r, top);
 }
@@ -282,6 +331,7 @@ struct BackwardArgs {
     uint64_t       items;
 };
 
+constexpr float kMaskedLogp = -1e4f;
 constexpr int kBackwardVectors = 4;  // per lane and item
 
 template <class T>
@@ -293,31 +343,43 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(const Backw
         const uint32_t block = (uint32_t)(item - (uint64_t)row * a.row_blocks);
         const T* z = static_cast<const T*>(a.logits) + row * a.ld;
         T* d_z = static_cast<T*>(a.d_logits) + row * a.ld_d;
-        const float most = a.stats[2 * row], log_sum = a.stats[2 * row + 1];
-        const int64_t target = a.targets ? a.targets[row] : -1;
-        const bool has = target >= 0 && target < a.vocab;
-        const float d_lp = has && a.d_logprob ? a.d_logprob[row] : 0.f;
+        const float stat = a.stats[2 * row];
+        // nothing but masked values: every p is 0
+        const float most = stat == -INFINITY ? 0.f : stat, log_sum = stat == -INFINITY ? INFINITY : a.stats[2 * row + 1];
+        const int64_t t = a.targets ? a.targets[row] : -1;
+        const int target = t >= 0 && t < a.vocab && stat != -INFINITY ? (int)t : -1;
+        const float d_lp = t >= 0 && t < a.vocab ? a.d_logprob[row] : 0.f;
         const float d_h = a.d_entropy ? a.d_entropy[row] : 0.f;
         const float h = a.d_entropy ? a.entropy[row] : 0.f;
-        const bool none = most == -INFINITY;
         const float k0 = -a.scale * (d_lp + d_h * h), k1 = -a.scale * d_h;
-        const int64_t col0 = ((int64_t)block * kBackwardVectors * kThreads + threadIdx.x) * N;
-        Vector<T> v[kBackwardVectors];
-#pragma unroll
-        for (int u = 0; u < kBackwardVectors; ++u) v[u] = load_vector(z, col0 + (int64_t)u * kThreads * N, a.vocab, masked<T>());
-#pragma unroll
-        for (int u = 0; u < kBackwardVectors; ++u) {
-            const int64_t col = col0 + (int64_t)u * kThreads * N;
+        auto one = [&](const Vector<T>& v, int col) __attribute__((always_inline)) {
             float x[N];
-            widen(v[u], x);
+            widen(v, x);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const float logp = a.scale * (x[i] - most) - log_sum;
-                const float p = none ? 0.f : __builtin_exp2f(logp * kLog2e);      // down to subnormal numbers, which factors may raise
-                x[i] = p == 0.f ? 0.f : p * fmaf(k1, logp, k0);
-                if (has && !none && target == col + i) x[i] += a.scale * d_lp;
+                const float p = __builtin_exp2f(logp * kLog2e);        // down to subnormal numbers, which factors may raise
+                x[i] = p * fmaf(k1, fmaxf(logp, kMaskedLogp), k0);     // p is 0 from far above kMaskedLogp on
             }
-            store_vector(d_z, col, a.vocab, narrow<T>(x));
+            if ((uint32_t)(target - col) < (uint32_t)N) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] += target == col + i ? a.scale * d_lp : 0.f;
+            }
+            return narrow<T>(x);
+        };
+        const int col0 = (int)block * kBackwardVectors * kThreads * N, col = col0 + (int)threadIdx.x * N;
+        Vector<T> v[kBackwardVectors];
+        if (col0 + kBackwardVectors * kThreads * N <= a.vocab) {
+#pragma unroll
+            for (int u = 0; u < kBackwardVectors; ++u) v[u] = load_whole(z + col + u * kThreads * N);
+#pragma unroll
+            for (int u = 0; u < kBackwardVectors; ++u) store_whole(d_z + col + u * kThreads * N, one(v[u], col + u * kThreads * N));
+        } else {
+#pragma unroll
+            for (int u = 0; u < kBackwardVectors; ++u) v[u] = load_vector(z, (int64_t)col + u * kThreads * N, a.vocab, masked<T>());
+#pragma unroll
+            for (int u = 0; u < kBackwardVectors; ++u)
+                store_vector(d_z, (int64_t)col + u * kThreads * N, a.vocab, one(v[u], col + u * kThreads * N));
         }
     }
 }

@@ -5,7 +5,6 @@
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
-#include <string.h>
 
 #include "adagc.h"
 
@@ -24,11 +23,22 @@ inline __host__ __device__ int64_t act8_ld(int64_t cols) { return (cols + 31) / 
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 // 16 bytes of fp32 or bf16 (uint16_t) values
 template <class T>
 struct Vector {
-    uint32_t w[4];
+    u32x4 w;
 };
+
+// 16-byte accesses of arrays whose elements, but nothing more, are aligned: the hardware takes them at any address, and a wave's
+// together touch one cache line more.  (Through memcpy the compiler moves the same bytes, but takes them apart one by one.)
+typedef u32x4 u32x4_of_f32 __attribute__((aligned(4)));
+typedef u32x4 u32x4_of_bf16 __attribute__((aligned(2)));
+__device__ __forceinline__ Vector<float> load_whole(const float* p) { return {*reinterpret_cast<const u32x4_of_f32*>(p)}; }
+__device__ __forceinline__ Vector<uint16_t> load_whole(const uint16_t* p) { return {*reinterpret_cast<const u32x4_of_bf16*>(p)}; }
+__device__ __forceinline__ void store_whole(float* p, const Vector<float>& v) { *reinterpret_cast<u32x4_of_f32*>(p) = v.w; }
+__device__ __forceinline__ void store_whole(uint16_t* p, const Vector<uint16_t>& v) { *reinterpret_cast<u32x4_of_bf16*>(p) = v.w; }
 
 // Larger of two, NaN if one is.
 __device__ __forceinline__ float maximum(float a, float b) { return __builtin_elementwise_maximum(a, b); }
@@ -67,15 +77,14 @@ __device__ __forceinline__ Vector<T> narrow(const float (&x)[16 / sizeof(T)])
     return v;
 }
 
-// The 16 bytes at column `col` of a row of n columns, `fill` (16 / sizeof(T) values' bits in a word) from its end on.  Rows start
-// at any element: the hardware takes 16-byte accesses at any address, and a wave's together touch one cache line more.
+// The 16 bytes at column `col` of a row of n columns, `fill` (a word's bits) from its end on.
 template <class T>
 __device__ __forceinline__ Vector<T> load_vector(const T* row, int64_t col, int64_t n, uint32_t fill)
 {
     constexpr int N = 16 / sizeof(T);
     Vector<T> v;
     if (col + N <= n) {
-        memcpy(v.w, row + col, 16);
+        v = load_whole(row + col);
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -96,7 +105,7 @@ __device__ __forceinline__ void store_vector(T* row, int64_t col, int64_t n, con
 {
     constexpr int N = 16 / sizeof(T);
     if (col + N <= n) {
-        memcpy(row + col, v.w, 16);
+        store_whole(row + col, v);
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
