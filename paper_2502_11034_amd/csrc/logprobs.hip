@@ -10,6 +10,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "adagc.h"
 #include "operators_internal.h"
@@ -100,11 +101,20 @@ struct Running {
     }
 };
 
-// The top_k largest values of a wave as keys in its lanes, largest first: the value's bits in an order-keeping form, then the index's
-// complement, so that keys are unique and equal values go to the lower index.  0: none.
+// The top_k largest values that a wave has seen, as keys in its lanes, largest first: the value's bits in an order-keeping form, then
+// the index's complement, so that keys are unique and equal values go to the lower index.  0: none.
+//
+// Candidates, values above the bar, wait in LDS and are sorted into the list many at a time: one alone costs the latencies of some
+// thirty dependent instructions (about 600 clocks, seven microseconds for the 30 of a row's wave with top_k = 8), while the ranks
+// of n of them are n independent comparisons.  Called by whole waves.
 struct TopList {
-    uint64_t mine = 0, least = 0;                // this lane's; the last one kept, the same in all lanes
-    float    bar = NAN;                          // only larger values come in (its value, once the list is full); NaN: any value
+    uint64_t  mine = 0;                          // this lane's
+    int       count = 0, waiting = 0;            // in the list, in LDS
+    float     bar = NAN;                         // only larger values come in (the last one's, once the list is full); NaN: any value
+    uint64_t* lds;                               // 64 of the wave's own
+    int       k;
+
+    __device__ __forceinline__ TopList(uint64_t* lds_, int k_) : lds(lds_), k(k_) {}
 
     static __device__ __forceinline__ uint64_t key(float z, uint32_t index)
     {
@@ -119,58 +129,112 @@ struct TopList {
         return __uint_as_float((b & 0x80000000u) ? b & 0x7FFFFFFFu : ~b);
     }
     static __device__ __forceinline__ uint32_t index(uint64_t key) { return 0xFFFFFFFFu - (uint32_t)key; }
-
-    // Takes every lane's candidate that belongs into the list; called by whole waves.
-    __device__ __forceinline__ void take(uint64_t candidate, int k)
+    static __device__ __forceinline__ uint64_t of_lane(uint64_t x, int lane)
     {
-        uint64_t mask = __ballot(candidate > least);
-        if (!mask) return;
-        const int lane = threadIdx.x & 63;
-        do {
-            const int from = __builtin_ctzll(mask);
-            const uint64_t key = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(candidate >> 32), from) << 32 |
-                                 (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)candidate, from);
-            const int at = __builtin_popcountll(__ballot(mine > key));
-            const uint64_t above = __shfl_up(mine, 1);
-            mine = lane < at ? mine : lane == at ? key : above;
-            if (lane >= k) mine = 0;
-            least = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), k - 1) << 32 |
-                    (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, k - 1);
-            mask &= mask - 1;
-            mask &= __ballot(candidate > least);
-        } while (mask);
-        if (least) bar = value(least);
+        return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane);
+    }
+    // LDS accesses of a wave are carried out in order; the compiler is told that other lanes' are meant
+    static __device__ __forceinline__ void in_order()
+    {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     }
 
-    // Sets the bar for an empty list from the first values: one of each lane, its largest.  The k-th largest of those is no larger
-    // than the k-th largest of all, so what is below it does not belong into the list: a wave's first 2048 values then cost about
-    // k insertions instead of k ln(2048 / k).  Found bit by bit.
-    __device__ __forceinline__ void begin(float lane_most, int k)
+    // Sorts the keys in the first n lanes' `fresh` (0: none) into the list.
+    __device__ __forceinline__ void merge(uint64_t fresh, int n)
     {
-        const uint32_t mine_bits = (uint32_t)(key(lane_most, 0) >> 32);
-        uint32_t at = 0;
-        for (uint32_t bit = 0x80000000u; bit; bit >>= 1)
-            if (__builtin_popcountll(__ballot(mine_bits >= (at | bit))) >= k) at |= bit;
-        // just below it (0 and -0 count as one value); with -inf or NaN there the list takes any value
+        const int lane = threadIdx.x & 63;
+        int rank = lane, fresh_rank = 0;
+        for (int j = 0; j < n; ++j) {
+            const uint64_t other = of_lane(fresh, j);
+            rank += other > mine;
+            fresh_rank += other > fresh;
+        }
+        for (int j = 0; j < count; ++j) fresh_rank += of_lane(mine, j) > fresh;
+        in_order();
+        if (lane < count && rank < k) lds[rank] = mine;
+        const bool there = lane < n && fresh != 0;
+        if (there && fresh_rank < k) lds[fresh_rank] = fresh;
+        in_order();
+        count = min(k, count + __builtin_popcountll(__ballot(there)));
+        mine = lane < count ? lds[lane] : 0;
+        in_order();
+        if (count == k) bar = value(of_lane(mine, k - 1));
+    }
+    __device__ __forceinline__ void flush()
+    {
+        const int lane = threadIdx.x & 63, n = waiting;
+        waiting = 0;
+        if (n) {
+            in_order();
+            merge(lane < n ? lds[lane] : 0, n);
+        }
+    }
+    // A value of each lane, or none.  Ones that equal the bar wait too: they may have come with the list's last, a lower index.
+    __device__ __forceinline__ void offer(float z, uint32_t index, bool there)
+    {
+        uint64_t mask = __ballot(there && !(z < bar));
+        if (!mask) return;
+        if (waiting + __builtin_popcountll(mask) > 64) {
+            flush();
+            mask = __ballot(there && !(z < bar));
+        }
+        const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+        if (mask >> (threadIdx.x & 63) & 1) lds[waiting + before] = key(z, index);
+        waiting += __builtin_popcountll(mask);
+    }
+
+    // The bar for a list that gets none of what lies below the k-th largest of 64 J values (J of each lane, 0 < k <= 64 J): just below
+    // that, found bit by bit, its upper half being enough; NaN if it is -inf or NaN, for then any value may come in.
+    template <int J>
+    static __device__ __forceinline__ float bar_of(const float (&values)[J], int k)
+    {
+        uint32_t bits[J], at = 0;
+#pragma unroll
+        for (int j = 0; j < J; ++j) bits[j] = (uint32_t)(key(values[j], 0) >> 32);
+        for (uint32_t bit = 0x80000000u; bit != 0x8000u; bit >>= 1) {
+            int above = 0;
+#pragma unroll
+            for (int j = 0; j < J; ++j) above += __builtin_popcountll(__ballot(bits[j] >= (at | bit)));
+            if (above >= k) at |= bit;
+        }
         const float kth = value((uint64_t)at << 32);
-        bar = kth > -INFINITY ? value((uint64_t)(at - (kth == 0.f ? 2 : 1)) << 32) : NAN;
+        return kth > -INFINITY ? value((uint64_t)(at - (kth == 0.f ? 2 : 1)) << 32) : NAN;      // 0 and -0 count as one value
     }
 };
+
+template <int N>
+__device__ __forceinline__ float largest_of(const float (&x)[N])
+{
+    float m = x[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) m = maximum(m, x[i]);
+    return m;
+}
+
+// op over the wave's lanes, in all of them; op(x, y) = op(y, x).
+template <class Op>
+__device__ __forceinline__ float all_lanes(float x, Op&& op)
+{
+    auto moved = [](float v, auto CTRL) { return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), decltype(CTRL)::value, 0xF, 0xF, true)); };
+    x = op(x, moved(x, std::integral_constant<int, 0xB1>{}));      // lane ^ 1
+    x = op(x, moved(x, std::integral_constant<int, 0x4E>{}));      // lane ^ 2
+    x = op(x, moved(x, std::integral_constant<int, 0x141>{}));     // the other four of eight
+    x = op(x, moved(x, std::integral_constant<int, 0x140>{}));     // the other eight of sixteen
+    const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = op(__uint_as_float(rows[0]), __uint_as_float(rows[1]));
+    const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return op(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
+}
 
 // Every lane's sums become the wave's, relative to its largest value.
 template <bool ENTROPY>
 __device__ __forceinline__ void reduce_lanes(Running<ENTROPY>& r, float c)
 {
-    float most = r.most;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) most = maximum(most, __shfl_xor(most, d));
-    r.most = most;
-    r.move_to(most == -INFINITY ? kLowest : most, c);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        r.sum += __shfl_xor(r.sum, d);
-        if (ENTROPY) r.weighted += __shfl_xor(r.weighted, d);
-    }
+    r.most = all_lanes(r.most, [](float x, float y) { return maximum(x, y); });
+    r.move_to(r.most == -INFINITY ? kLowest : r.most, c);
+    r.sum = all_lanes(r.sum, [](float x, float y) { return x + y; });
+    if (ENTROPY) r.weighted = all_lanes(r.weighted, [](float x, float y) { return x + y; });
 }
 
 // Results of a row from its sums, by one wave.
@@ -204,6 +268,8 @@ __device__ __forceinline__ void write_row(const ForwardArgs& a, int64_t row, con
     }
 }
 
+constexpr int kAhead = 4;        // 16-byte vectors of a lane in a group
+
 // One workgroup per part of a row.
 template <class T, bool ENTROPY, bool TOP, bool SPLIT>
 __global__ __launch_bounds__(kThreads) void logprobs_kernel(const ForwardArgs a)
@@ -218,68 +284,106 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const ForwardArgs a)
     const int last_whole = min(last, a.vocab / N);         // all but one at most
     const float c = a.scale * kLog2e, slack = kSlack / a.scale;
     const int tid = (int)threadIdx.x;
+    const int wave = tid >> 6, lane = tid & 63;
+    __shared__ RowPart wave_part[kWaves];
+    __shared__ uint64_t wave_keys[TOP ? kWaves * ADAGC_MAX_TOP : 1];
     Running<ENTROPY> r;
-    TopList top;
-    auto largest = [](const float (&x)[N]) __attribute__((always_inline)) {
-        float m = x[0];
-#pragma unroll
-        for (int i = 1; i < N; ++i) m = maximum(m, x[i]);
-        return m;
-    };
-    // count: values of the vector that there are
-    auto one = [&](const Vector<T>& v, int vector, int count) __attribute__((always_inline)) {
+    TopList top(wave_keys + (TOP ? wave * ADAGC_MAX_TOP : 0), a.top_k);
+    // returns the lane's largest value
+    auto add = [&](const Vector<T>& v) __attribute__((always_inline)) {
         float x[N];
         widen(v, x);
-        const float vmax = largest(x);
+        const float vmax = largest_of(x);
         r.add(x, vmax, c, slack);
-        if constexpr (TOP) {
-            // These values have higher indices than all in the list, so only a larger one comes in; among themselves, which are taken
-            // value by value of all lanes, equal ones may come in any order.
-            if (__ballot(!(vmax <= top.bar))) {
-#pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (__ballot(!(x[i] < top.bar))) top.take(i < count ? TopList::key(x[i], (uint32_t)(vector * N + i)) : 0, a.top_k);
-            }
-        }
+        return vmax;
     };
-    // whole waves go round together
-    constexpr int kAhead = 4;
-    int v0 = first;
-    for (; v0 + kAhead * kThreads <= last_whole; v0 += kAhead * kThreads) {
-        Vector<T> v[kAhead];
+    auto offer = [&](const Vector<T>& v, float vmax, int vector, int count) __attribute__((always_inline)) {
+        // these values have higher indices than all in the list, so one of them has to be larger
+        if (!__ballot(!(vmax <= top.bar))) return;
+        float x[N];
+        widen(v, x);
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) v[u] = load_whole(z + (size_t)(v0 + u * kThreads) * N + (uint32_t)(tid * N));
-        if constexpr (TOP) {
-            if (v0 == first) {
-                float m = -INFINITY;
+        for (int i = 0; i < N; ++i) top.offer(x[i], (uint32_t)(vector * N + i), i < count);
+    };
+    // The bar of the workgroup's lists from its first values, the largest of each lane: the k-th largest of those is no larger than
+    // the row's k-th.  Then all lists together get about top_k values of the first group, and as many of each later one.
+    __shared__ float lane_most[TOP ? kThreads + 1 : 1];
+    auto begin = [&](float m) __attribute__((always_inline)) {
+        lane_most[tid] = m;
+        __syncthreads();
+        if (wave == 0) {
+            float values[kWaves];
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u) {
-                    float x[N];
-                    widen(v[u], x);
-                    m = maximum(m, largest(x));
-                }
-                top.begin(m, a.top_k);
-            }
+            for (int w = 0; w < kWaves; ++w) values[w] = lane_most[w * 64 + lane];
+            const float bar = TopList::bar_of(values, a.top_k);
+            if (lane == 0) lane_most[kThreads] = bar;
         }
+        __syncthreads();
+        top.bar = lane_most[kThreads];
+    };
+    // Whole waves go round together.  A group's loads are on their way while the group before is worked on (the last group loads
+    // itself again: a loop without conditions).
+    constexpr int kGroup = kAhead * kThreads;
+    int v0 = first;
+    if (v0 + kGroup <= last_whole) {
+        Vector<T> v[kAhead], next[kAhead];
+        auto load = [&](int from, Vector<T> (&to)[kAhead]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) one(v[u], v0 + u * kThreads + tid, N);
+            for (int u = 0; u < kAhead; ++u) to[u] = load_whole(z + (size_t)(from + u * kThreads) * N + (uint32_t)(tid * N));
+        };
+        load(v0, v);
+        if constexpr (TOP) {
+            float m = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                float x[N];
+                widen(v[u], x);
+                m = maximum(m, largest_of(x));
+            }
+            begin(m);
+        }
+        for (; v0 + kGroup <= last_whole; v0 += kGroup) {
+            load(v0 + 2 * kGroup <= last_whole ? v0 + kGroup : v0, next);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const float vmax = add(v[u]);
+                if constexpr (TOP) offer(v[u], vmax, v0 + u * kThreads + tid, N);
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) v[u] = next[u];
+        }
     }
     for (; v0 < last; v0 += kThreads) {
         const int i = v0 + tid, count = i < last ? min(N, a.vocab - i * N) : 0;
-        one(load_vector(z, (int64_t)i * N, count > 0 ? a.vocab : 0, masked<T>()), i, count);
+        const Vector<T> v = load_vector(z, (int64_t)i * N, count > 0 ? a.vocab : 0, masked<T>());
+        if constexpr (TOP) {
+            if (v0 == first) {
+                float x[N];
+                widen(v, x);
+                begin(largest_of(x));
+            }
+        }
+        const float vmax = add(v);
+        if constexpr (TOP) offer(v, vmax, i, count);
     }
 
     reduce_lanes(r, c);
-    __shared__ RowPart wave_part[kWaves];
-    __shared__ uint64_t wave_keys[TOP ? kWaves * ADAGC_MAX_TOP : 1];
-    const int wave = tid >> 6, lane = tid & 63;
     if (lane == 0) wave_part[wave] = {r.most, r.sum, r.weighted, 0.f};
-    if (TOP && lane < a.top_k) wave_keys[wave * a.top_k + lane] = top.mine;
+    if constexpr (TOP) {
+        top.flush();
+        if (lane < a.top_k) wave_keys[wave * ADAGC_MAX_TOP + lane] = top.mine;
+    }
     __syncthreads();
     if (wave != 0) return;
-    for (int w = 1; w < kWaves; ++w) {
-        r.join(wave_part[w].most, wave_part[w].sum, wave_part[w].weighted, c);
-        if (TOP) top.take(lane < a.top_k ? wave_keys[w * a.top_k + lane] : 0, a.top_k);
+    for (int w = 1; w < kWaves; ++w) r.join(wave_part[w].most, wave_part[w].sum, wave_part[w].weighted, c);
+    if constexpr (TOP) {
+        // the other waves' keys, as many waves' at a time as the lanes hold
+        const int at_once = 64 / a.top_k;
+        for (int w = 1; w < kWaves; w += at_once) {
+            const int n = min(at_once, kWaves - w) * a.top_k, from = w + lane / a.top_k;
+            const uint64_t theirs = lane < n ? wave_keys[from * ADAGC_MAX_TOP + lane % a.top_k] : 0;
+            top.merge(theirs, n);
+        }
     }
     if constexpr (SPLIT) {
         if (lane == 0) a.part[row * a.parts + part] = {r.most, r.sum, r.weighted, 0.f};
@@ -296,8 +400,9 @@ __global__ __launch_bounds__(64) void join_parts_kernel(const ForwardArgs a)
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x;
     const float c = a.scale * kLog2e;
+    __shared__ uint64_t waiting[64];
     Running<ENTROPY> r;
-    TopList top;
+    TopList top(waiting, a.top_k);
     const bool has = lane < a.parts;
     if (has) {
         const RowPart x = a.part[row * a.parts + lane];
@@ -305,12 +410,15 @@ __global__ __launch_bounds__(64) void join_parts_kernel(const ForwardArgs a)
     }
     reduce_lanes(r, c);
     if constexpr (TOP) {
-        const uint64_t* keys = a.part_keys + (row * a.parts + lane) * a.top_k;
-        for (int j = 0; j < a.top_k; ++j) {
-            const uint64_t key = has ? keys[j] : 0;
-            if (!__ballot(key > top.least)) break;         // each part's keys fall
-            top.take(key, a.top_k);
+        const uint64_t* keys = a.part_keys + row * a.parts * a.top_k;
+        const uint64_t first = has ? keys[lane * a.top_k] : 0;
+        const float largest[1] = {first ? TopList::value(first) : -INFINITY};
+        top.bar = TopList::bar_of(largest, a.top_k);
+        for (int j = 0; j < a.parts * a.top_k; j += 64) {
+            const uint64_t key = j + lane < a.parts * a.top_k ? keys[j + lane] : 0;
+            top.offer(TopList::value(key), TopList::index(key), key != 0);
         }
+        top.flush();
     }
     write_row<ENTROPY, TOP, T>(a, row, r, top);
 }
