@@ -446,7 +446,7 @@ int adagc_muon_gemm_nt_batched(const void* P, int64_t ldp, const void* Q, int64_
  * top_k most likely tokens.  One pass over the logits.
  *   logits       DEVICE dtype[rows][ld], vocab values a row; -inf masks a token
  *   targets      DEVICE int64[rows] (NULL if logprob is); outside 0 .. vocab-1 (-1, -100): the row has no target
- *   scale        > 0, finite
+ *   scale        2^-100 .. 2^100
  *   top_k        0 .. min(ADAGC_MAX_TOP, vocab)
  *   logprob      DEVICE fp32[rows], 0 for rows without a target; or NULL
  *   entropy      DEVICE fp32[rows]; or NULL
@@ -466,7 +466,8 @@ int adagc_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int64_
 /*
  * Gradient of the logits of adagc_token_logprobs for the gradients of its log-probabilities and entropies:
  *     d_z_j = scale ( d_logprob (1[j = target] - p_j) - d_entropy p_j (logp_j + entropy) ),   p_j = exp(logp_j),
- * without the d_logprob part for rows without a target, and 0 where p_j = 0 (masked tokens; all of a row of -inf).
+ * without the d_logprob part for rows without a target, p_j (logp_j + entropy) being 0 where p_j = 0 (masked tokens), and 0 for all of a
+ * row of -inf.
  *   logits, targets, scale   as the forward call had them
  *   stats, entropy           DEVICE, the forward call's (entropy NULL if d_entropy is)
  *   d_logprob                DEVICE fp32[rows], or NULL for none (then targets may be NULL)

@@ -6,6 +6,7 @@ PyTorch is used by callers for device memory and streams; this module only reads
 ``tensor.data_ptr()``.
 """
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -256,19 +257,19 @@ def adagc_muon_gemm_nt_batched(P, Q, alpha=1.0, beta=0.0, Dt=None, C=None, Ct=No
 
 # ---- operators around the step: 2-D device tensors, fp32 or bf16, consecutive elements in a row
 
-_TYPES = {}                    # torch dtypes seen so far: (code or None, name)
+_KNOWN = {}                    # torch dtypes seen so far: (code or None, name)
 
 
 def _type(dtype):
-    known = _TYPES.get(dtype)
+    known = _KNOWN.get(dtype)
     if known is None:
         name = str(dtype)
-        known = _TYPES[dtype] = ({"torch.float32": ADAGC_F32, "torch.bfloat16": ADAGC_BF16}.get(name), name)
+        known = _KNOWN[dtype] = ({"torch.float32": ADAGC_F32, "torch.bfloat16": ADAGC_BF16}.get(name), name)
     return known
 
 
-def _matrix(t, shape, name, dtype=None):
-    """(pointer, dtype code, leading dimension) of a 2-D tensor."""
+def _matrix(t, name, shape=None, dtype=None):
+    """(pointer, dtype code, leading dimension, shape) of a 2-D tensor."""
     own = t.shape
     if len(own) != 2 or (shape is not None and own != shape):
         raise ValueError("%s: shape %s, expected %s" % (name, tuple(own), "2-D" if shape is None else tuple(shape)))
@@ -278,7 +279,7 @@ def _matrix(t, shape, name, dtype=None):
     ld, step = t.stride()
     if step != 1 and own[1] > 1:
         raise ValueError("%s: elements of a row are not consecutive" % name)
-    return t.data_ptr(), code, ld if own[0] > 1 else own[1]
+    return t.data_ptr(), code, ld if own[0] > 1 else own[1], own
 
 
 def _dense(t, shape, dtype, name):
@@ -308,112 +309,142 @@ def _bytes(t, least, name):
     return t.data_ptr(), n
 
 
+def _on_device(where, *tensors):
+    """A kernel that is given host memory would fault the GPU."""
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            raise AdagcError(ADAGC_ERR_INVALID_ARG, where + " (a tensor is not in device memory)")
+
+
 def _size(rc, where):
     if rc < 0:
         raise AdagcError(rc, where)
-    return int(rc)
+    return rc
 
 
-def _stream(stream):
-    return ctypes.c_void_p(stream) if stream else None
+# Sizes are functions of the arguments alone and are asked for at every call.
 
-
+@functools.lru_cache(maxsize=1024)
 def adagc_token_logprobs_workspace_bytes(rows, vocab, top_k=0):
-    return _size(lib().adagc_token_logprobs_workspace_bytes(int(rows), int(vocab), int(top_k)), "adagc_token_logprobs_workspace_bytes")
+    return _size(lib().adagc_token_logprobs_workspace_bytes(rows, vocab, top_k), "adagc_token_logprobs_workspace_bytes")
 
 
 def adagc_token_logprobs(logits, targets=None, logprob=None, entropy=None, stats=None, top_logprob=None, top_index=None, scale=1.0,
                          workspace=None, stream=None):
     """adagc_token_logprobs on logits [rows, vocab]; the outputs that are given are written.  targets: int64 [rows]; stats: fp32 [rows, 2];
     top_logprob fp32, top_index int32 [rows, k]; workspace: adagc_token_logprobs_workspace_bytes(rows, vocab, k) bytes."""
-    p, dtype, ld = _matrix(logits, None, "logits")
-    rows, vocab = logits.shape
-    k = 0 if top_index is None else (top_index.shape[1] if top_index.dim() == 2 else -1)
+    p, dtype, ld, (rows, vocab) = _matrix(logits, "logits")
+    k = 0
+    if top_index is not None:
+        k = top_index.shape[1] if top_index.dim() == 2 else -1
     ws, ws_bytes = _bytes(workspace, adagc_token_logprobs_workspace_bytes(rows, vocab, k) if rows and vocab else 0, "workspace")
-    _check(lib().adagc_token_logprobs(p, dtype, rows, vocab, ld, _dense(targets, (rows,), "torch.int64", "targets"), float(scale), k,
-                                      _dense(logprob, (rows,), "torch.float32", "logprob"),
-                                      _dense(entropy, (rows,), "torch.float32", "entropy"),
-                                      _dense(stats, (rows, 2), "torch.float32", "stats"),
-                                      _dense(top_logprob, (rows, k), "torch.float32", "top_logprob"),
-                                      _dense(top_index, (rows, k), "torch.int32", "top_index"), ws, ws_bytes, _stream(stream)),
-           "adagc_token_logprobs")
+    one = (rows,)
+    t = _dense(targets, one, "torch.int64", "targets")
+    lp = _dense(logprob, one, "torch.float32", "logprob")
+    h = _dense(entropy, one, "torch.float32", "entropy")
+    st = _dense(stats, (rows, 2), "torch.float32", "stats")
+    tl = _dense(top_logprob, (rows, k), "torch.float32", "top_logprob")
+    ti = _dense(top_index, (rows, k), "torch.int32", "top_index")
+    _on_device("adagc_token_logprobs", logits, targets, logprob, entropy, stats, top_logprob, top_index, workspace)
+    rc = lib().adagc_token_logprobs(p, dtype, rows, vocab, ld, t, scale, k, lp, h, st, tl, ti, ws, ws_bytes, stream)
+    if rc:
+        raise AdagcError(rc, "adagc_token_logprobs")
 
 
 def adagc_token_logprobs_backward(logits, targets, stats, entropy, d_logprob, d_entropy, d_logits, scale=1.0, stream=None):
     """adagc_token_logprobs_backward: writes d_logits (which may be logits).  d_logprob, d_entropy: fp32 [rows] or None."""
-    p, dtype, ld = _matrix(logits, None, "logits")
-    rows, vocab = logits.shape
-    d, _, ld_d = _matrix(d_logits, logits.shape, "d_logits", dtype)
-    _check(lib().adagc_token_logprobs_backward(p, dtype, rows, vocab, ld, _dense(targets, (rows,), "torch.int64", "targets"),
-                                               float(scale), _dense(stats, (rows, 2), "torch.float32", "stats"),
-                                               _dense(entropy, (rows,), "torch.float32", "entropy"),
-                                               _dense(d_logprob, (rows,), "torch.float32", "d_logprob"),
-                                               _dense(d_entropy, (rows,), "torch.float32", "d_entropy"), d, ld_d, _stream(stream)),
-           "adagc_token_logprobs_backward")
+    p, dtype, ld, shape = _matrix(logits, "logits")
+    rows, vocab = shape
+    d, _, ld_d, _ = _matrix(d_logits, "d_logits", shape, dtype)
+    one = (rows,)
+    t = _dense(targets, one, "torch.int64", "targets")
+    st = _dense(stats, (rows, 2), "torch.float32", "stats")
+    h = _dense(entropy, one, "torch.float32", "entropy")
+    dl = _dense(d_logprob, one, "torch.float32", "d_logprob")
+    dh = _dense(d_entropy, one, "torch.float32", "d_entropy")
+    _on_device("adagc_token_logprobs_backward", logits, targets, stats, entropy, d_logprob, d_entropy, d_logits)
+    rc = lib().adagc_token_logprobs_backward(p, dtype, rows, vocab, ld, t, scale, st, h, dl, dh, d, ld_d, stream)
+    if rc:
+        raise AdagcError(rc, "adagc_token_logprobs_backward")
 
 
+@functools.lru_cache(maxsize=1024)
 def adagc_act8_bytes(rows, cols):
     """Bytes of a checkpoint of a rows x cols matrix."""
-    return _size(lib().adagc_act8_bytes(int(rows), int(cols)), "adagc_act8_bytes")
+    return _size(lib().adagc_act8_bytes(rows, cols), "adagc_act8_bytes")
 
 
 def adagc_act8_pack(x, ckpt, stream=None):
     """Writes the checkpoint of x [rows, cols] to the buffer ckpt."""
-    p, dtype, ld = _matrix(x, None, "x")
-    rows, cols = x.shape
+    p, dtype, ld, (rows, cols) = _matrix(x, "x")
     c, _ = _bytes(ckpt, adagc_act8_bytes(rows, cols), "ckpt")
-    _check(lib().adagc_act8_pack(p, dtype, rows, cols, ld, c, _stream(stream)), "adagc_act8_pack")
+    _on_device("adagc_act8_pack", x, ckpt)
+    rc = lib().adagc_act8_pack(p, dtype, rows, cols, ld, c, stream)
+    if rc:
+        raise AdagcError(rc, "adagc_act8_pack")
 
 
 def adagc_act8_unpack(ckpt, x, stream=None):
     """Writes what the checkpoint holds to x [rows, cols]."""
-    p, dtype, ld = _matrix(x, None, "x")
-    rows, cols = x.shape
+    p, dtype, ld, (rows, cols) = _matrix(x, "x")
     c, _ = _bytes(ckpt, adagc_act8_bytes(rows, cols), "ckpt")
-    _check(lib().adagc_act8_unpack(c, rows, cols, p, dtype, ld, _stream(stream)), "adagc_act8_unpack")
+    _on_device("adagc_act8_unpack", x, ckpt)
+    rc = lib().adagc_act8_unpack(c, rows, cols, p, dtype, ld, stream)
+    if rc:
+        raise AdagcError(rc, "adagc_act8_unpack")
 
 
 def adagc_swiglu(gate, up, out, gate_ckpt=None, up_ckpt=None, stream=None):
     """out = silu(gate) up, all [rows, cols] of one type; gate and up are left in the checkpoints, if given."""
-    g, dtype, ld_g = _matrix(gate, None, "gate")
-    rows, cols = gate.shape
-    u, _, ld_u = _matrix(up, gate.shape, "up", dtype)
-    o, _, ld_o = _matrix(out, gate.shape, "out", dtype)
+    g, dtype, ld_g, shape = _matrix(gate, "gate")
+    rows, cols = shape
+    u, _, ld_u, _ = _matrix(up, "up", shape, dtype)
+    o, _, ld_o, _ = _matrix(out, "out", shape, dtype)
     least = adagc_act8_bytes(rows, cols) if gate_ckpt is not None or up_ckpt is not None else 0
     gc, _ = _bytes(gate_ckpt, least, "gate_ckpt")
     uc, _ = _bytes(up_ckpt, least, "up_ckpt")
-    _check(lib().adagc_swiglu(g, ld_g, u, ld_u, dtype, rows, cols, o, ld_o, gc, uc, _stream(stream)), "adagc_swiglu")
+    _on_device("adagc_swiglu", gate, up, out, gate_ckpt, up_ckpt)
+    rc = lib().adagc_swiglu(g, ld_g, u, ld_u, dtype, rows, cols, o, ld_o, gc, uc, stream)
+    if rc:
+        raise AdagcError(rc, "adagc_swiglu")
 
 
 def adagc_swiglu_backward(d_out, gate_ckpt, up_ckpt, d_gate, d_up, out=None, stream=None):
     """Writes d_gate, d_up and, if given, out again, from d_out [rows, cols] and the checkpoints of gate and up."""
-    d, dtype, ld_d = _matrix(d_out, None, "d_out")
-    rows, cols = d_out.shape
-    g, _, ld_g = _matrix(d_gate, d_out.shape, "d_gate", dtype)
-    u, _, ld_u = _matrix(d_up, d_out.shape, "d_up", dtype)
-    o, _, ld_o = _matrix(out, d_out.shape, "out", dtype) if out is not None else (None, 0, 0)
+    d, dtype, ld_d, shape = _matrix(d_out, "d_out")
+    rows, cols = shape
+    g, _, ld_g, _ = _matrix(d_gate, "d_gate", shape, dtype)
+    u, _, ld_u, _ = _matrix(d_up, "d_up", shape, dtype)
+    o, ld_o = None, 0
+    if out is not None:
+        o, _, ld_o, _ = _matrix(out, "out", shape, dtype)
     least = adagc_act8_bytes(rows, cols)
-    _check(lib().adagc_swiglu_backward(d, ld_d, dtype, _bytes(gate_ckpt, least, "gate_ckpt")[0], _bytes(up_ckpt, least, "up_ckpt")[0],
-                                       rows, cols, g, ld_g, u, ld_u, o, ld_o, _stream(stream)), "adagc_swiglu_backward")
+    gc, _ = _bytes(gate_ckpt, least, "gate_ckpt")
+    uc, _ = _bytes(up_ckpt, least, "up_ckpt")
+    _on_device("adagc_swiglu_backward", d_out, gate_ckpt, up_ckpt, d_gate, d_up, out)
+    rc = lib().adagc_swiglu_backward(d, ld_d, dtype, gc, uc, rows, cols, g, ld_g, u, ld_u, o, ld_o, stream)
+    if rc:
+        raise AdagcError(rc, "adagc_swiglu_backward")
 
 
+@functools.lru_cache(maxsize=1024)
 def adagc_act8_wgrad_workspace_bytes(rows, n_out, n_in, dtype):
-    return _size(lib().adagc_act8_wgrad_workspace_bytes(int(rows), int(n_out), int(n_in), int(dtype)), "adagc_act8_wgrad_workspace_bytes")
+    return _size(lib().adagc_act8_wgrad_workspace_bytes(rows, n_out, n_in, dtype), "adagc_act8_wgrad_workspace_bytes")
 
 
 def adagc_act8_wgrad(d_out, ckpt, d_weight, accumulate=False, workspace=None, stream=None):
     """d_weight [n_out, n_in] = (d_weight +) d_out^T x for d_out [rows, n_out] and the checkpoint of x [rows, n_in]; workspace:
     adagc_act8_wgrad_workspace_bytes(rows, n_out, n_in, dtype of d_out) bytes."""
-    d, dtype, ld_d = _matrix(d_out, None, "d_out")
-    rows, n_out = d_out.shape
-    w, weight_dtype, ld_w = _matrix(d_weight, None, "d_weight")
-    if d_weight.shape[0] != n_out:
-        raise ValueError("d_weight: %d rows, expected %d" % (d_weight.shape[0], n_out))
-    n_in = d_weight.shape[1]
+    d, dtype, ld_d, (rows, n_out) = _matrix(d_out, "d_out")
+    w, weight_dtype, ld_w, (w_rows, n_in) = _matrix(d_weight, "d_weight")
+    if w_rows != n_out:
+        raise ValueError("d_weight: %d rows, expected %d" % (w_rows, n_out))
     c, _ = _bytes(ckpt, adagc_act8_bytes(rows, n_in), "ckpt")
     ws, ws_bytes = _bytes(workspace, adagc_act8_wgrad_workspace_bytes(rows, n_out, n_in, dtype), "workspace")
-    _check(lib().adagc_act8_wgrad(d, dtype, ld_d, c, rows, n_out, n_in, w, weight_dtype, ld_w, int(bool(accumulate)), ws, ws_bytes,
-                                  _stream(stream)), "adagc_act8_wgrad")
+    _on_device("adagc_act8_wgrad", d_out, ckpt, d_weight, workspace)
+    rc = lib().adagc_act8_wgrad(d, dtype, ld_d, c, rows, n_out, n_in, w, weight_dtype, ld_w, 1 if accumulate else 0, ws, ws_bytes, stream)
+    if rc:
+        raise AdagcError(rc, "adagc_act8_wgrad")
 
 
 ADAGC_STATIC_MAX_TENSORS = 32768

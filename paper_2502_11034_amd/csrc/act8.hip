@@ -271,7 +271,7 @@ Args arguments(int64_t rows, int64_t cols, int32_t dtype)
     a.rows = rows;
     a.cols = (int32_t)cols;
     a.ld = (int32_t)act8_ld(cols);
-    a.row_vectors = (uint32_t)(a.ld * dtype_size(dtype) / 16);
+    a.row_vectors = (uint32_t)((int64_t)a.ld * dtype_size(dtype) / 16);
     a.reciprocal = a.row_vectors == 1 ? UINT32_MAX : (uint32_t)((1ull << 32) / a.row_vectors);
     a.vectors = (uint64_t)rows * a.row_vectors;
     return a;

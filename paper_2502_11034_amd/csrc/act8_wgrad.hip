@@ -144,7 +144,7 @@ struct Tile {
 // nothing is moved across this point by the compiler's instruction scheduler
 #define ADAGC_SCHED_FENCE() __builtin_amdgcn_sched_barrier(0)
 
-// EDGE: dW is smaller than a tile in one direction, or rows of dY are too far apart for 32-bit offsets.  Otherwise the last tile of a
+// EDGE: dW is smaller than a tile in one direction, or rows of an operand are too far apart for 32-bit offsets.  Otherwise the last tile of a
 // direction begins a tile before the end, so that every tile is whole, and stores only what no other tile does.
 //
 // Main loop.  A step's operands are staged in a place of LDS; while step k is multiplied from registers, step k + 1 is read to
@@ -444,7 +444,8 @@ int launch(const WgradArgs& a, const Plan& p, hipStream_t s)
 template <class T>
 int launch(const WgradArgs& a, const Plan& p, hipStream_t s)
 {
-    const bool edge = a.ld_d >= (int64_t)1 << 24 || a.n_out < p.bm || a.ld < p.bn;     // 32 rows are not within 32 bits, or less than a tile
+    // 32 rows are not within 32 bits, or less than a tile
+    const bool edge = a.ld_d >= (int64_t)1 << 24 || a.ld >= 1 << 26 || a.n_out < p.bm || a.ld < p.bn;
     if constexpr (sizeof(T) == 2) {
         if (p.bm == 256) return edge ? launch<Tile<T, 256, 256, 2, 4>, T, true>(a, p, s) : launch<Tile<T, 256, 256, 2, 4>, T, false>(a, p, s);
     } else {

@@ -21,6 +21,8 @@ namespace {
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int64_t kMaxRows = (1 << 24) - 1;      // a launch has at most 2^32 - 1 lanes
+// Scales with which s (z - M) log2 e neither overflows next to M nor needs the differences of z that do.
+constexpr float kLeastScale = 0x1p-100f, kMostScale = 0x1p100f;
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 
@@ -460,7 +462,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(const Backw
         const float d_h = a.d_entropy ? a.d_entropy[row] : 0.f;
         const float h = a.d_entropy ? a.entropy[row] : 0.f;
         const float k0 = -a.scale * (d_lp + d_h * h), k1 = -a.scale * d_h;
-        auto one = [&](const Vector<T>& v, int col) __attribute__((always_inline)) {
+        auto one = [&](const Vector<T>& v, uint32_t col) __attribute__((always_inline)) {
             float x[N];
             widen(v, x);
 #pragma unroll
@@ -469,25 +471,25 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(const Backw
                 const float p = __builtin_exp2f(logp * kLog2e);        // down to subnormal numbers, which factors may raise
                 x[i] = p * fmaf(k1, fmaxf(logp, kMaskedLogp), k0);     // p is 0 from far above kMaskedLogp on
             }
-            if ((uint32_t)(target - col) < (uint32_t)N) {
+            if ((uint32_t)target - col < (uint32_t)N) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) x[i] += target == col + i ? a.scale * d_lp : 0.f;
+                for (int i = 0; i < N; ++i) x[i] += (uint32_t)target == col + i ? a.scale * d_lp : 0.f;
             }
             return narrow<T>(x);
         };
         const int col0 = (int)block * kBackwardVectors * kThreads * N, col = col0 + (int)threadIdx.x * N;
         Vector<T> v[kBackwardVectors];
-        if (col0 + kBackwardVectors * kThreads * N <= a.vocab) {
+        if (kBackwardVectors * kThreads * N <= a.vocab - col0) {
 #pragma unroll
             for (int u = 0; u < kBackwardVectors; ++u) v[u] = load_whole(z + col + u * kThreads * N);
 #pragma unroll
-            for (int u = 0; u < kBackwardVectors; ++u) store_whole(d_z + col + u * kThreads * N, one(v[u], col + u * kThreads * N));
+            for (int u = 0; u < kBackwardVectors; ++u) store_whole(d_z + col + u * kThreads * N, one(v[u], (uint32_t)col + u * kThreads * N));
         } else {
 #pragma unroll
             for (int u = 0; u < kBackwardVectors; ++u) v[u] = load_vector(z, (int64_t)col + u * kThreads * N, a.vocab, masked<T>());
 #pragma unroll
             for (int u = 0; u < kBackwardVectors; ++u)
-                store_vector(d_z, (int64_t)col + u * kThreads * N, a.vocab, one(v[u], col + u * kThreads * N));
+                store_vector(d_z, (int64_t)col + u * kThreads * N, a.vocab, one(v[u], (uint32_t)col + u * kThreads * N));
         }
     }
 }
@@ -521,7 +523,7 @@ void launch_forward(const ForwardArgs& a, hipStream_t stream)
 
 int check_rows(int64_t rows, int64_t vocab, int32_t dtype, float scale)
 {
-    if (rows < 0 || vocab < 1 || (dtype != ADAGC_F32 && dtype != ADAGC_BF16) || !(scale > 0.f) || !(scale < INFINITY)) return ADAGC_ERR_INVALID_ARG;
+    if (rows < 0 || vocab < 1 || !known_dtype(dtype) || !(scale >= kLeastScale) || !(scale <= kMostScale)) return ADAGC_ERR_INVALID_ARG;
     if (rows > kMaxRows || vocab > kMaxCols) return ADAGC_ERR_TOO_LARGE;
     return ADAGC_OK;
 }
