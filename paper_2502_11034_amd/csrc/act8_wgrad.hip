@@ -23,6 +23,7 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 #define ADAGC_LDS __attribute__((address_space(3)))
 
@@ -117,24 +118,30 @@ __device__ __forceinline__ void static_for(F&& f)
     static_for_impl(f, std::make_integer_sequence<int, N>{});
 }
 
-// Tokens of a step, one matrix-core instruction deep, and the places of LDS that steps go round in.
+// Tokens of a step, and the places of LDS that steps go round in.
 constexpr int kDeep = 32, kPlaces = 3;
 
-// BM x BN tile of dW (BM along n_out), kWM x kWN waves.
-template <class T, int BM_, int BN_, int kWM_, int kWN_>
+// BM x BN tile of dW (BM along n_out), kWM x kWN waves, matrix-core instructions of kBlock x kBlock results.
+//
+// kBlock: with 32 the matrix cores read half the operand registers for the same products, in half the instructions: fp32 2048 tokens
+// 1024 x 2816 52.7 -> 49.5 us.  On the 256 x 256 tile, where the chip's power limit sets the clock, 16 is ahead: 8192 tokens
+// 14336 x 4096 816 against 853 us, and back to back 906 - 924 against 949 (on zeros, which take less power, 758 against 737).
+template <class T, int BM_, int BN_, int kWM_, int kWN_, int kBlock_>
 struct Tile {
-    static constexpr int BM = BM_, BN = BN_, kWM = kWM_, kWN = kWN_;
+    static constexpr int BM = BM_, BN = BN_, kWM = kWM_, kWN = kWN_, kBlock = kBlock_;
     static constexpr int kThreads = 64 * kWM * kWN;
     static constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
-    static constexpr int kTM = BM / kWM / 16, kTN = BN / kWN / 16;         // 16 x 16 blocks of a wave
+    static constexpr int kTM = BM / kWM / kBlock, kTN = BN / kWN / kBlock; // blocks of a wave
+    static constexpr int kHalves = kBlock / 16;                            // instructions of a step and block: one takes 512 / kBlock tokens
+    static constexpr int kPieces = kBlock * kBlock / 256;                  // of four results in a lane's part of a block
     static constexpr int kY = kDeep * BM, kX = kDeep * BN;                 // elements of a staged operand tile
     static constexpr int kPlace = (kParts * kY + kX) * 2;                  // bytes
     static constexpr int kYUnits = kY / 8 / kThreads, kXUnits = kX / 16 / kThreads;     // of a lane: 8 values of dY, 16 codes
     static_assert(kY % (8 * kThreads) == 0 && kX % (16 * kThreads) == 0, "operand tiles are dealt evenly");
 
-    // Byte offset of 16-byte vector v of row r of a staged tile of C columns: its 32-byte units are permuted so that the 8
-    // rows a transposed read takes 32 bytes each of (0 .. 3 and 8 .. 11) lie in different banks.
-    static __device__ __forceinline__ int swizzle(int r) { return (r & 3) | ((r >> 3) & 1) << 2; }
+    // Byte offset of 16-byte vector v of row r of a staged tile of C columns: its 32-byte units are permuted so that the eight that half
+    // a wave's transposed read takes (one of the rows 0 .. 3 and 8 .. 11 each, or two of 0 .. 3) lie in different banks.
+    static __device__ __forceinline__ int swizzle(int r) { return kBlock == 16 ? (r & 3) | ((r >> 3) & 1) << 2 : (r & 3) << 1; }
     template <int C>
     static __device__ __forceinline__ int at(int r, int v) { return r * C * 2 + ((v >> 1) ^ swizzle(r)) * 32 + (v & 1) * 16; }
 };
@@ -148,7 +155,7 @@ struct Tile {
 // direction begins a tile before the end, so that every tile is whole, and stores only what no other tile does.
 //
 // Main loop.  A step's operands are staged in a place of LDS; while step k is multiplied from registers, step k + 1 is read to
-// registers from its place (of dY, each fragment as soon as its multiplications are issued; of X, to a second set), step k + 2 goes from
+// registers from its place (each fragment as soon as its multiplications are issued, or to a second set), step k + 2 goes from
 // the registers it was loaded to into its place, and those take step k + 4.  One barrier a step: what it orders is the writes of k + 2
 // before their reads in the next step; the reads of a place are done a step before it is written again.  Loads past the last step take
 // the last one again: a loop without conditions lets the compiler count what is outstanding.
@@ -156,7 +163,7 @@ template <class S, class T, bool EDGE>
 __global__ __launch_bounds__(S::kThreads, S::kThreads == 256 && S::kParts == 3 ? 1 : 2) void wgrad_kernel(const WgradArgs a)
 {
     constexpr int BM = S::BM, BN = S::BN, kThreads = S::kThreads, kTM = S::kTM, kTN = S::kTN, kParts = S::kParts;
-    constexpr int kYUnits = S::kYUnits, kXUnits = S::kXUnits, kH = (int)sizeof(T) / 2;
+    constexpr int kHalves = S::kHalves, kYUnits = S::kYUnits, kXUnits = S::kXUnits, kH = (int)sizeof(T) / 2;
     __shared__ __attribute__((aligned(512))) uint8_t lds[kPlaces * S::kPlace];
     const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>(&lds[0]);      // low half of the flat address = LDS offset
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -272,26 +279,40 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads == 256 && S::kParts == 3 ?
         for (int n = 0; n < kXUnits; ++n) write_x(s, n, place);
     };
 
-    // Fragments.  16 lanes read 4 rows of 16 columns and get a column each; lane l's are rows 8 (l / 16) .. + 7 of column l mod 16.
-    const int fr = 8 * (lane >> 4) + ((lane >> 2) & 3);
-    const uint32_t fy = fr * BM * 2 + (((wm * kTM) ^ S::swizzle(fr)) * 32) + (lane & 3) * 8;
-    const uint32_t fx = kParts * S::kY * 2 + fr * BN * 2 + (((wn * kTN) ^ S::swizzle(fr)) * 32) + (lane & 3) * 8;
+    // Fragments.  16 lanes read 4 rows of 16 columns and get a column each; lane l's are rows 8 (l / kBlock) .. + 7 of column l mod kBlock.
+    constexpr int kBlock = S::kBlock, kUnits32 = kBlock / 16;       // 32-byte units of a block's row
+    const int fr = 8 * (lane / kBlock) + ((lane >> 2) & 3), fu = (lane >> 4) % kUnits32;
+    const uint32_t fy = fr * BM * 2 + (((wm * kTM * kUnits32 + fu) ^ S::swizzle(fr)) * 32) + (lane & 3) * 8;
+    const uint32_t fx = kParts * S::kY * 2 + fr * BN * 2 + (((wn * kTN * kUnits32 + fu) ^ S::swizzle(fr)) * 32) + (lane & 3) * 8;
     auto read4 = [](uint32_t at) __attribute__((always_inline)) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ADAGC_LDS s16x4*>(at)); };
     auto fragment = [&](uint32_t at, uint32_t pitch) __attribute__((always_inline)) {
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(read4(at), read4(at + 4 * pitch), 0, 1, 2, 3, 4, 5, 6, 7));
     };
+    // fragment g of dY: block g mod kTM, half, part; fragment f of X: block f mod kTN, half
     auto read_y = [&](int g, uint32_t place) __attribute__((always_inline)) {
-        return fragment(place + (fy ^ (uint32_t)(g % kTM * 32)) + (uint32_t)(g / kTM * S::kY * 2), BM * 2);
+        return fragment(place + (fy ^ (uint32_t)(g % kTM * kBlock * 2)) + (uint32_t)(g / kTM % kHalves * 16 * BM * 2 + g / kTM / kHalves * S::kY * 2), BM * 2);
     };
-    auto read_x = [&](int n, uint32_t place) __attribute__((always_inline)) { return fragment(place + (fx ^ (uint32_t)(n * 32)), BN * 2); };
+    auto read_x = [&](int f, uint32_t place) __attribute__((always_inline)) {
+        return fragment(place + (fx ^ (uint32_t)(f % kTN * kBlock * 2)) + (uint32_t)(f / kTN * 16 * BN * 2), BN * 2);
+    };
 
-    f32x4 acc[kTM][kTN];
+    typedef std::conditional_t<kBlock == 16, f32x4, f32x16> Results;
+    Results acc[kTM][kTN];
 #pragma unroll
     for (int m = 0; m < kTM; ++m)
 #pragma unroll
-        for (int n = 0; n < kTN; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    constexpr int kG = kParts * kTM;               // fragments of dY
-    bf16x8 y[kG], x[2][kTN];
+        for (int n = 0; n < kTN; ++n)
+#pragma unroll
+            for (int r = 0; r < 4 * S::kPieces; ++r) acc[m][n][r] = 0.f;
+    constexpr int kG = kParts * kHalves * kTM, kF = kHalves * kTN;         // fragments of dY, of X
+    constexpr int kSets = kHalves == 1 ? 2 : 1;      // of X's: with one half they are all in use to the step's end
+    bf16x8 y[kG], x[kSets][kF];
+
+    // acc[m][n] += x y^T
+    auto multiply = [](const bf16x8& x, const bf16x8& y, Results& sum) __attribute__((always_inline)) {
+        if constexpr (kBlock == 16) sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, sum, 0, 0, 0);
+        else sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, sum, 0, 0, 0);
+    };
 
     auto plain_step = [&](int64_t step) __attribute__((always_inline)) {
         Staged s;
@@ -300,12 +321,13 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads == 256 && S::kParts == 3 ?
         write(s, lds0);
         __syncthreads();
 #pragma unroll
-        for (int n = 0; n < kTN; ++n) x[0][n] = read_x(n, lds0);
+        for (int f = 0; f < kF; ++f) x[0][f] = read_x(f, lds0);
 #pragma unroll
         for (int g = 0; g < kG; ++g) {
             y[0] = read_y(g, lds0);
 #pragma unroll
-            for (int n = 0; n < kTN; ++n) acc[g % kTM][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[0][n], y[0], acc[g % kTM][n], 0, 0, 0);
+            for (int n = 0; n < kTN; ++n)
+                multiply(x[0][g / kTM % kHalves * kTN + n], y[0], acc[g % kTM][n]);
         }
     };
 
@@ -322,7 +344,7 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads == 256 && S::kParts == 3 ?
         load(clamp(step0 + 3), staged[1]);
         __syncthreads();
 #pragma unroll
-        for (int n = 0; n < kTN; ++n) x[0][n] = read_x(n, lds0);
+        for (int f = 0; f < kF; ++f) x[0][f] = read_x(f, lds0);
 #pragma unroll
         for (int g = 0; g < kG; ++g) y[g] = read_y(g, lds0);
         uint32_t next = lds0 + S::kPlace;          // the place of step k + 1
@@ -335,9 +357,14 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads == 256 && S::kParts == 3 ?
             const int64_t ahead = clamp(step + 4);
             static_for<kSlots>([&](auto SLOT) __attribute__((always_inline)) {
                 constexpr int slot = decltype(SLOT)::value, g = slot / kTN, n = slot % kTN;
-                acc[g % kTM][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[p][n], y[g], acc[g % kTM][n], 0, 0, 0);
+                multiply(x[p % kSets][g / kTM % kHalves * kTN + n], y[g], acc[g % kTM][n]);
                 ADAGC_SCHED_FENCE();
-                if constexpr (slot % 2 == 0 && slot / 2 < kTN) x[p ^ 1][slot / 2] = read_x(slot / 2, next);
+                // into the other set, or where a fragment's last multiplication is issued (a half step before its next)
+                if constexpr (kSets == 2) {
+                    if constexpr (slot % 2 == 0 && slot / 2 < kF) x[p ^ 1][slot / 2] = read_x(slot / 2, next);
+                } else if constexpr (g >= kG - kTM * kHalves && g % kTM == kTM - 1) {
+                    x[0][g / kTM % kHalves * kTN + n] = read_x(g / kTM % kHalves * kTN + n, next);
+                }
                 if constexpr (n == kTN - 1) y[g] = read_y(g, next);
                 static_for<kWrites>([&](auto N) __attribute__((always_inline)) {
                     constexpr int w = decltype(N)::value;
@@ -369,37 +396,42 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads == 256 && S::kParts == 3 ?
     }
     if (last && a.rows % kDeep) plain_step(full);
 
-    // lane l holds rows (l / 16) * 4 .. + 3 (of X's block) of column l mod 16 (of dY's)
-    if (alone) {
+    // lane l holds rows 8 q + 4 (l / kBlock) .. + 3 (of X's block), q = 0 .. kPieces - 1, of column l mod kBlock (of dY's)
+    auto each_piece = [&](auto&& f) __attribute__((always_inline)) {
 #pragma unroll
         for (int m = 0; m < kTM; ++m)
 #pragma unroll
             for (int n = 0; n < kTN; ++n)
-                store_results(a, o0 + (wm * kTM + m) * 16 + (lane & 15), o_least, i0 + (wn * kTN + n) * 16 + (lane >> 4) * 4, i_least, acc[m][n]);
+#pragma unroll
+                for (int q = 0; q < S::kPieces; ++q)
+                    f(m, n, q, f32x4{acc[m][n][4 * q], acc[m][n][4 * q + 1], acc[m][n][4 * q + 2], acc[m][n][4 * q + 3]});
+    };
+    if (alone) {
+        each_piece([&](int m, int n, int q, f32x4 v) __attribute__((always_inline)) {
+            store_results(a, o0 + (wm * kTM + m) * kBlock + lane % kBlock, o_least, i0 + (wn * kTN + n) * kBlock + q * 8 + lane / kBlock * 4, i_least, v);
+        });
     } else {
         f32x4* to_ws = reinterpret_cast<f32x4*>(a.workspace) + (size_t)(item - a.whole) * (BM * BN / 4) + tid;
-#pragma unroll
-        for (int m = 0; m < kTM; ++m)
-#pragma unroll
-            for (int n = 0; n < kTN; ++n) to_ws[(m * kTN + n) * kThreads] = acc[m][n];
+        each_piece([&](int m, int n, int q, f32x4 v) __attribute__((always_inline)) { to_ws[((m * kTN + n) * S::kPieces + q) * kThreads] = v; });
     }
 }
 
-// Adds the parts of the split tiles, in order: a workgroup takes one 16 x 16 block of every wave.
+// Adds the parts of the split tiles, in order: a workgroup takes one piece of four results of every lane.
 template <class S, bool EDGE>
 __global__ __launch_bounds__(S::kThreads) void join_kernel(const WgradArgs a)
 {
-    constexpr int kTM = S::kTM, kTN = S::kTN, BM = S::BM, BN = S::BN;
+    constexpr int kTN = S::kTN, kPieces = S::kTM * kTN * S::kPieces, BM = S::BM, BN = S::BN, kBlock = S::kBlock;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / S::kWN, wn = wave % S::kWN;
-    const int n_tile = (int)blockIdx.x / (kTM * kTN), block = (int)blockIdx.x % (kTM * kTN), m = block / kTN, n = block % kTN;
+    const int n_tile = (int)blockIdx.x / kPieces, piece = (int)blockIdx.x % kPieces, q = piece % S::kPieces;
+    const int m = piece / S::kPieces / kTN, n = piece / S::kPieces % kTN;
     int to, ti;
     place_of_tile(a, a.whole + n_tile, &to, &ti);
     const int64_t o_least = (int64_t)to * BM, i_least = (int64_t)ti * BN;
     const int64_t o0 = EDGE ? o_least : min(o_least, (int64_t)a.n_out - BM), i0 = EDGE ? i_least : min(i_least, (int64_t)a.ld - BN);
-    const f32x4* from = reinterpret_cast<const f32x4*>(a.workspace) + (size_t)n_tile * a.split * (BM * BN / 4) + (size_t)block * S::kThreads + tid;
+    const f32x4* from = reinterpret_cast<const f32x4*>(a.workspace) + (size_t)n_tile * a.split * (BM * BN / 4) + (size_t)piece * S::kThreads + tid;
     f32x4 sum = from[0];
     for (int p = 1; p < a.split; ++p) sum += from[(size_t)p * (BM * BN / 4)];
-    store_results(a, o0 + (wm * kTM + m) * 16 + (lane & 15), o_least, i0 + (wn * kTN + n) * 16 + (lane >> 4) * 4, i_least, sum);
+    store_results(a, o0 + (wm * S::kTM + m) * kBlock + lane % kBlock, o_least, i0 + (wn * kTN + n) * kBlock + q * 8 + lane / kBlock * 4, i_least, sum);
 }
 
 int check(int64_t rows, int64_t n_out, int64_t n_in, int32_t dtype)
@@ -438,7 +470,7 @@ template <class S, class T, bool EDGE>
 int launch(const WgradArgs& a, const Plan& p, hipStream_t s)
 {
     wgrad_kernel<S, T, EDGE><<<dim3((uint32_t)(p.whole + p.rest * p.split)), dim3(S::kThreads), 0, s>>>(a);
-    if (p.rest) join_kernel<S, EDGE><<<dim3((uint32_t)(p.rest * S::kTM * S::kTN)), dim3(S::kThreads), 0, s>>>(a);
+    if (p.rest) join_kernel<S, EDGE><<<dim3((uint32_t)(p.rest * S::kTM * S::kTN * S::kPieces)), dim3(S::kThreads), 0, s>>>(a);
     return hipGetLastError() == hipSuccess ? ADAGC_OK : ADAGC_ERR_HIP;
 }
 template <class T>
@@ -447,11 +479,11 @@ int launch(const WgradArgs& a, const Plan& p, hipStream_t s)
     // 32 rows are not within 32 bits, or less than a tile
     const bool edge = a.ld_d >= (int64_t)1 << 24 || a.ld >= 1 << 26 || a.n_out < p.bm || a.ld < p.bn;
     if constexpr (sizeof(T) == 2) {
-        if (p.bm == 256) return edge ? launch<Tile<T, 256, 256, 2, 4>, T, true>(a, p, s) : launch<Tile<T, 256, 256, 2, 4>, T, false>(a, p, s);
+        if (p.bm == 256) return edge ? launch<Tile<T, 256, 256, 2, 4, 16>, T, true>(a, p, s) : launch<Tile<T, 256, 256, 2, 4, 16>, T, false>(a, p, s);
     } else {
-        if (p.bn == 256) return edge ? launch<Tile<T, 128, 256, 2, 4>, T, true>(a, p, s) : launch<Tile<T, 128, 256, 2, 4>, T, false>(a, p, s);
+        if (p.bn == 256) return edge ? launch<Tile<T, 128, 256, 2, 4, 32>, T, true>(a, p, s) : launch<Tile<T, 128, 256, 2, 4, 32>, T, false>(a, p, s);
     }
-    return edge ? launch<Tile<T, 128, 128, 2, 2>, T, true>(a, p, s) : launch<Tile<T, 128, 128, 2, 2>, T, false>(a, p, s);
+    return edge ? launch<Tile<T, 128, 128, 2, 2, 32>, T, true>(a, p, s) : launch<Tile<T, 128, 128, 2, 2, 32>, T, false>(a, p, s);
 }
 
 }  // namespace
