@@ -219,6 +219,42 @@ def test_logprobs_offsets_beyond_32_bits():
     near(zd.cpu(), grad, off, torch.bfloat16)
 
 
+def test_logprobs_rows_of_the_largest_length():
+    """A row of 2^31 - 1024 tokens, all but some at its ends masked: the same as a row of those."""
+    vocab = 2 ** 31 - 1024
+    places = torch.tensor([0, 5, 2 ** 30 + 1, vocab - 7168, vocab - 7167, vocab - 2, vocab - 1])
+    z = torch.randn(1, len(places), generator=gen(14)).to(torch.bfloat16)
+    zd = torch.full((1, vocab), -math.inf, dtype=torch.bfloat16, device=DEV)
+    zd[0, places.to(DEV)] = z[0].to(DEV)
+    t = places[-2:-1].to(DEV)
+    logprob, entropy, stats = (torch.empty(s, device=DEV) for s in ((1,), (1,), (1, 2)))
+    top, index = torch.empty(1, 4, device=DEV), torch.empty(1, 4, dtype=torch.int32, device=DEV)
+    B.adagc_token_logprobs(zd, t, logprob, entropy, stats, top, index, workspace=workspace(B.adagc_token_logprobs_workspace_bytes(1, vocab, 4)))
+    small = torch.tensor([len(places) - 2])
+    want = O.logprobs(z, small, 1.0)
+    near(logprob, want["logprob"], want["logprob_off"])
+    near(entropy, want["entropy"], want["entropy_off"])
+    at = O.top(z, 4)
+    assert torch.equal(index.cpu().long(), places[at])
+    near(top, want["logp"].gather(1, at), want["logp_off"].gather(1, at))
+    one = torch.ones(1)
+    B.adagc_token_logprobs_backward(zd, t, stats, entropy, one.to(DEV), one.to(DEV), zd)
+    grad, off = O.logprobs_backward(z, small, 1.0, one, one)
+    near(zd[0, places.to(DEV)].cpu()[None], grad, off, torch.bfloat16)
+    assert sum(int(part.count_nonzero()) for part in zd[0].split(2 ** 28)) <= len(places)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -100, 2.0 ** 100])
+def test_logprobs_extreme_scales(scale):
+    """At the least every token is as likely but masked ones; at the most only the largest."""
+    z, t = make_logits(4, 5003, torch.float32, 15)
+    z[0, 7] = z[1, 9] = torch.finfo(torch.float32).min
+    z[1, ::2] = -math.inf
+    z[2, 8] = 1e8
+    zd, out = check_logprobs(z, t, scale, 3)
+    assert all(torch.isfinite(out["entropy"]))
+
+
 def test_logprobs_gradient_against_differences():
     """Central differences of the forward kernel's own sum in fp32: a step h gives h^2 |f'''| / 6 and rounding / h."""
     z, t = make_logits(4, 40, torch.float32, 11, size=1.0)
@@ -321,6 +357,21 @@ def test_checkpoint_offsets_beyond_32_bits():
     B.adagc_act8_unpack(ckpt, x)
     assert torch.equal(x[-100:].cpu().double(), O.values(want, 100, cols))
     assert not x[:-100].any()
+
+
+@pytest.mark.parametrize("dtype, cols", [("f32", 2 ** 29 + 40), ("bf16", 2 ** 30 + 40)])
+def test_checkpoint_of_a_long_row(dtype, cols):
+    x = torch.zeros(1, cols, dtype=TYPES[dtype], device=DEV)
+    end = make_activations(1, 104, TYPES[dtype], 16)
+    x[:, -104:] = end.to(DEV)                                        # from a block's first column on
+    ckpt = torch.empty(B.adagc_act8_bytes(1, cols), dtype=torch.uint8, device=DEV)
+    B.adagc_act8_pack(x, ckpt)
+    want = O.pack_bytes(end)
+    ld = O.ld8(cols)
+    assert torch.equal(ckpt[ld - 128:ld].cpu(), want[:128]) and torch.equal(ckpt[-4:].cpu(), want[128:])
+    x.fill_(5)
+    B.adagc_act8_unpack(ckpt, x)
+    assert torch.equal(x[:, -104:].cpu().double(), O.values(want, 1, 104)) and not x[:, :-104].any()
 
 
 # ------------------------------------------------------------------------------------------------ gated activation
@@ -555,6 +606,26 @@ def test_wgrad_offsets_beyond_32_bits():
     B.adagc_act8_wgrad(dd, ckpt, w.t, workspace=workspace(B.adagc_act8_wgrad_workspace_bytes(rows, n_out, n_in, B.ADAGC_BF16)))
     want, off = O.wgrad(d_out, O.values(ckpt.cpu(), rows, n_in))
     near(w.result(), want, off)
+
+
+def test_wgrad_offsets_within_a_step_beyond_32_bits():
+    """33 rows of 2^27 columns, zero but for the last row of the first step, the row after it and the last columns."""
+    rows, n_out, n_in = 33, 128, 2 ** 27
+    ckpt = torch.zeros(B.adagc_act8_bytes(rows, n_in), dtype=torch.uint8, device=DEV)
+    ckpt[rows * n_in:] = 127
+    x = torch.zeros(rows, 64, dtype=torch.bfloat16)
+    x[31], x[32] = 2.0, 0.5
+    x[:, 32:] = torch.randn(rows, 32, generator=gen(26)).sign()
+    codes = O.pack_bytes(x)
+    for columns, from_ in ((slice(0, 32), 0), (slice(n_in - 32, n_in), 32)):
+        ckpt[:rows * n_in].view(rows, n_in)[:, columns] = codes[:rows * 64].view(rows, 64)[:, from_:from_ + 32].to(DEV)
+        ckpt[rows * n_in:].view(rows, n_in // 32)[:, columns.start // 32] = codes[rows * 64:].view(rows, 2)[:, from_ // 32].to(DEV)
+    d_out = torch.randint(-8, 9, (rows, n_out), generator=gen(27)).to(torch.bfloat16)
+    w = torch.full((n_out, n_in), FILL, dtype=torch.bfloat16, device=DEV)
+    B.adagc_act8_wgrad(d_out.to(DEV), ckpt, w, workspace=workspace(max(1, B.adagc_act8_wgrad_workspace_bytes(rows, n_out, n_in, B.ADAGC_BF16))))
+    want = (d_out.double().t() @ x.double()).to(torch.bfloat16)      # sums of halves below 2^10: exact before the rounding
+    assert torch.equal(w[:, :32].cpu(), want[:, :32]) and torch.equal(w[:, -32:].cpu(), want[:, 32:])
+    assert not any(bool(part.any()) for part in w[:, 32:-32].split(2 ** 24, 1))
 
 
 # ------------------------------------------------------------------------------------------------ streams and graphs

@@ -86,6 +86,12 @@ def test_refused(call, code, arguments):
     assert call(**arguments) == code
 
 
+@pytest.mark.parametrize("call", [forward, backward])
+def test_scales_out_of_range_are_refused(call):
+    for scale in (2.0 ** -101, 2.0 ** 101, 1e-45, 3e38):
+        assert call(scale=scale) == BAD
+
+
 def test_no_rows_is_a_valid_call_with_nothing_to_do():
     assert forward(rows=0, logits=None, targets=None, logprob=None, entropy=None, stats=None) == OK
     assert backward(rows=0, logits=None, targets=None, stats=None, d_logits=None) == OK
@@ -140,6 +146,19 @@ def test_binding_refuses_tensors_that_do_not_fit():
         (ValueError, lambda: B.adagc_token_logprobs_backward(f(4, 10), None, f(4, 2), None, None, None, f(4, 11))),
     ]:
         with pytest.raises(error):
+            call()
+
+
+def test_binding_refuses_host_memory():
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)
+    f = lambda *s: torch.zeros(*s)
+    ckpt = torch.zeros(B.adagc_act8_bytes(4, 64), dtype=torch.uint8)
+    for call in (lambda: B.adagc_act8_pack(bf(4, 64), ckpt), lambda: B.adagc_act8_unpack(ckpt, bf(4, 64)),
+                 lambda: B.adagc_swiglu(bf(4, 64), bf(4, 64), bf(4, 64)),
+                 lambda: B.adagc_swiglu_backward(bf(4, 64), ckpt, ckpt.clone(), bf(4, 64), bf(4, 64)),
+                 lambda: B.adagc_act8_wgrad(bf(4, 10), ckpt, f(10, 64)), lambda: B.adagc_token_logprobs(f(4, 10), entropy=f(4)),
+                 lambda: B.adagc_token_logprobs_backward(f(4, 10), None, f(4, 2), f(4), None, f(4), f(4, 10))):
+        with pytest.raises(B.AdagcError, match="not in device memory"):
             call()
 
 
