@@ -81,8 +81,10 @@ __device__ __forceinline__ void pack_vector(const Args& a, const Checkpoint& to,
             }
         }
     }
-#pragma unroll
-    for (int d = 1; d < 32 / N; d *= 2) largest = max(largest, (uint32_t)__shfl_xor((int)largest, d));
+    // over the block's lanes, by moves between neighbours within the vector unit: lane ^ 1, lane ^ 2, the other four of eight
+    largest = max(largest, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)largest, 0xB1, 0xF, 0xF, true));
+    largest = max(largest, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)largest, 0x4E, 0xF, 0xF, true));
+    if constexpr (N == 4) largest = max(largest, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)largest, 0x141, 0xF, 0xF, true));
     const int e = act8_exponent(largest);
     const float inverse = power_of_two(-e);
     uint32_t code[N / 4];

@@ -314,30 +314,49 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads == 256 && S::kParts == 3 ?
         else sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, sum, 0, 0, 0);
     };
 
-    auto plain_step = [&](int64_t step) __attribute__((always_inline)) {
-        Staged s;
-        __syncthreads();
-        load_checked(step, s);
-        write(s, lds0);
+    // a step from the place at `place`, whose staged units are loaded
+    auto plain_step = [&](const Staged& s, uint32_t place) __attribute__((always_inline)) {
+        write(s, place);
         __syncthreads();
 #pragma unroll
-        for (int f = 0; f < kF; ++f) x[0][f] = read_x(f, lds0);
+        for (int f = 0; f < kF; ++f) x[0][f] = read_x(f, place);
 #pragma unroll
         for (int g = 0; g < kG; ++g) {
-            y[0] = read_y(g, lds0);
+            y[0] = read_y(g, place);
 #pragma unroll
-            for (int n = 0; n < kTN; ++n)
-                multiply(x[0][g / kTM % kHalves * kTN + n], y[0], acc[g % kTM][n]);
+            for (int n = 0; n < kTN; ++n) multiply(x[0][g / kTM % kHalves * kTN + n], y[0], acc[g % kTM][n]);
         }
     };
+    // Tokens after the last full step come first, so that their loads and the main loop's first are on their way together.
+    const bool rest = last && a.rows % kDeep;
+    constexpr uint32_t kRestPlace = (kPlaces - 1) * S::kPlace;
 
     if constexpr (EDGE) {
-        for (int64_t step = step0; step < step1; ++step) plain_step(step);
-    } else if (step0 < step1) {
+        for (int64_t step = step0; step < step1 + rest; ++step) {
+            Staged s;
+            __syncthreads();
+            load_checked(step, s);
+            plain_step(s, lds0);
+        }
+    } else if (step0 == step1) {
+        if (rest) {
+            Staged s;
+            load_checked(full, s);
+            plain_step(s, lds0 + kRestPlace);
+        }
+    } else {
         Staged staged[2];
         auto clamp = [&](int64_t step) { return min(step, step1 - 1); };
-        load(step0, staged[0]);
-        load(clamp(step0 + 1), staged[1]);
+        if (rest) {
+            Staged s;
+            load_checked(full, s);
+            load(step0, staged[0]);
+            load(clamp(step0 + 1), staged[1]);
+            plain_step(s, lds0 + kRestPlace);
+        } else {
+            load(step0, staged[0]);
+            load(clamp(step0 + 1), staged[1]);
+        }
         write(staged[0], lds0);
         load(clamp(step0 + 2), staged[0]);
         write(staged[1], lds0 + S::kPlace);
@@ -394,8 +413,6 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads == 256 && S::kParts == 3 ?
         }
         if (step < step1) one_step(std::integral_constant<int, 0>{}, step);
     }
-    if (last && a.rows % kDeep) plain_step(full);
-
     // lane l holds rows 8 q + 4 (l / kBlock) .. + 3 (of X's block), q = 0 .. kPieces - 1, of column l mod kBlock (of dY's)
     auto each_piece = [&](auto&& f) __attribute__((always_inline)) {
 #pragma unroll
