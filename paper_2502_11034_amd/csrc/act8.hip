@@ -47,7 +47,14 @@ struct Place {
 template <bool WHOLE, class T>
 __device__ __forceinline__ Vector<T> fetch(const T* row, const Args& a, int32_t col)
 {
-    return WHOLE ? load_whole(row + col) : load_vector(row, col, a.cols, 0);
+    return WHOLE ? load_whole(row + col) : load_ahead(row, col, a.cols, 0);
+}
+// What was fetched, with zeros from the row's end on.
+template <bool WHOLE, class T>
+__device__ __forceinline__ Vector<T> settled(Vector<T> v, const Args& a, int32_t col)
+{
+    if constexpr (!WHOLE) settle(v, col, a.cols, 0);
+    return v;
 }
 template <bool WHOLE, class T>
 __device__ __forceinline__ void put(T* row, const Args& a, int32_t col, const Vector<T>& v)
@@ -184,7 +191,7 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const Args a)
         a, [&](const Place& at) { return fetch<WHOLE>(row_of<T>(a.x, at.row), a, at.col); },
         [&](const Place& at, const Vector<T>& in) {
             float x[N];
-            widen(in, x);
+            widen(settled<WHOLE>(in, a, at.col), x);
             pack_vector(a, a.a, at, x);
         });
 }
@@ -217,8 +224,8 @@ __global__ __launch_bounds__(kThreads) void swiglu_kernel(const Args a)
         },
         [&](const Place& at, const In& in) {
             float g[N], u[N], h[N];
-            widen(in.gate, g);
-            widen(in.up, u);
+            widen(settled<WHOLE>(in.gate, a, at.col), g);
+            widen(settled<WHOLE>(in.up, a, at.col), u);
 #pragma unroll
             for (int i = 0; i < N; ++i) h[i] = g[i] * sigmoid(g[i]) * u[i];
             put<WHOLE>(out_row<T>(a.z, at.row), a, at.col, narrow<T>(h));
@@ -245,7 +252,7 @@ __global__ __launch_bounds__(kThreads) void swiglu_backward_kernel(const Args a)
         },
         [&](const Place& at, const In& in) {
             float g[N], u[N], d[N], dg[N], h[N];
-            widen(in.d_out, d);
+            widen(settled<WHOLE>(in.d_out, a, at.col), d);
             unpack_vector(in.gate, g);
             unpack_vector(in.up, u);
 #pragma unroll

@@ -315,8 +315,9 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads == 256 && S::kParts == 3 ?
     };
 
     // a step from the place at `place`, whose staged units are loaded
-    auto plain_step = [&](const Staged& s, uint32_t place) __attribute__((always_inline)) {
+    auto plain_step = [&](const Staged& s, uint32_t place, auto&& meanwhile) __attribute__((always_inline)) {
         write(s, place);
+        meanwhile();
         __syncthreads();
 #pragma unroll
         for (int f = 0; f < kF; ++f) x[0][f] = read_x(f, place);
@@ -332,17 +333,24 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads == 256 && S::kParts == 3 ?
     constexpr uint32_t kRestPlace = (kPlaces - 1) * S::kPlace;
 
     if constexpr (EDGE) {
-        for (int64_t step = step0; step < step1 + rest; ++step) {
-            Staged s;
-            __syncthreads();
-            load_checked(step, s);
-            plain_step(s, lds0);
-        }
+        // two steps' loads are on their way; a step's writes and the reads of the step before take different places
+        const int64_t end = step1 + rest;
+        Staged staged[2];
+        if (step0 < end) load_checked(step0, staged[0]);
+        if (step0 + 1 < end) load_checked(step0 + 1, staged[1]);
+        for (int64_t step = step0; step < end; step += 2)
+            static_for<2>([&](auto P) __attribute__((always_inline)) {
+                constexpr int p = decltype(P)::value;
+                if (step + p >= end) return;
+                plain_step(staged[p], lds0 + p * S::kPlace, [&] {
+                    if (step + p + 2 < end) load_checked(step + p + 2, staged[p]);
+                });
+            });
     } else if (step0 == step1) {
         if (rest) {
             Staged s;
             load_checked(full, s);
-            plain_step(s, lds0 + kRestPlace);
+            plain_step(s, lds0 + kRestPlace, [] {});
         }
     } else {
         Staged staged[2];
@@ -352,7 +360,7 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads == 256 && S::kParts == 3 ?
             load_checked(full, s);
             load(step0, staged[0]);
             load(clamp(step0 + 1), staged[1]);
-            plain_step(s, lds0 + kRestPlace);
+            plain_step(s, lds0 + kRestPlace, [] {});
         } else {
             load(step0, staged[0]);
             load(clamp(step0 + 1), staged[1]);
@@ -447,7 +455,16 @@ __global__ __launch_bounds__(S::kThreads) void join_kernel(const WgradArgs a)
     const int64_t o0 = EDGE ? o_least : min(o_least, (int64_t)a.n_out - BM), i0 = EDGE ? i_least : min(i_least, (int64_t)a.ld - BN);
     const f32x4* from = reinterpret_cast<const f32x4*>(a.workspace) + (size_t)n_tile * a.split * (BM * BN / 4) + (size_t)piece * S::kThreads + tid;
     f32x4 sum = from[0];
-    for (int p = 1; p < a.split; ++p) sum += from[(size_t)p * (BM * BN / 4)];
+    int p = 1;
+    constexpr int kTogether = 4;                       // loads on their way
+    for (; p + kTogether <= a.split; p += kTogether) {
+        f32x4 v[kTogether];
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u) v[u] = from[(size_t)(p + u) * (BM * BN / 4)];
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u) sum += v[u];
+    }
+    for (; p < a.split; ++p) sum += from[(size_t)p * (BM * BN / 4)];
     store_results(a, o0 + (wm * S::kTM + m) * kBlock + lane % kBlock, o_least, i0 + (wn * kTN + n) * kBlock + q * 8 + lane / kBlock * 4, i_least, sum);
 }
 

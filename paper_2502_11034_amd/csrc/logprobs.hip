@@ -172,17 +172,19 @@ struct TopList {
             merge(lane < n ? lds[lane] : 0, n);
         }
     }
-    // A value of each lane, or none.  Ones that equal the bar wait too: they may have come with the list's last, a lower index.
+    // A value of each lane, or none.  Of ones that equal a full list's last only those of lower indices wait.
     __device__ __forceinline__ void offer(float z, uint32_t index, bool there)
     {
         uint64_t mask = __ballot(there && !(z < bar));
         if (!mask) return;
+        const uint64_t own = key(z, index);
+        if (count == k) mask = __ballot(there && own > of_lane(mine, k - 1));
         if (waiting + __builtin_popcountll(mask) > 64) {
             flush();
-            mask = __ballot(there && !(z < bar));
+            mask = __ballot(there && (count == k ? own > of_lane(mine, k - 1) : !(z < bar)));
         }
         const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
-        if (mask >> (threadIdx.x & 63) & 1) lds[waiting + before] = key(z, index);
+        if (mask >> (threadIdx.x & 63) & 1) lds[waiting + before] = own;
         waiting += __builtin_popcountll(mask);
     }
 
@@ -309,7 +311,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const ForwardArgs a)
     };
     // The bar of the workgroup's lists from its first values, the largest of each lane: the k-th largest of those is no larger than
     // the row's k-th.  Then all lists together get about top_k values of the first group, and as many of each later one.
-    __shared__ float lane_most[TOP ? kThreads + 1 : 1];
+    __shared__ float lane_most[kThreads + 1];
     auto begin = [&](float m) __attribute__((always_inline)) {
         lane_most[tid] = m;
         __syncthreads();
@@ -357,7 +359,8 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const ForwardArgs a)
     }
     for (; v0 < last; v0 += kThreads) {
         const int i = v0 + tid, count = i < last ? min(N, a.vocab - i * N) : 0;
-        const Vector<T> v = load_vector(z, (int64_t)i * N, count > 0 ? a.vocab : 0, masked<T>());
+        // lanes past the part's end hold masked values
+        const Vector<T> v = load_vector(z, i < last ? (int64_t)i * N : (int64_t)a.vocab, a.vocab, masked<T>());
         if constexpr (TOP) {
             if (v0 == first) {
                 float x[N];
@@ -515,10 +518,12 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(const Backw
             for (int u = 0; u < kBackwardVectors; ++u) store_whole(d_z + col + u * kThreads * N, one(v[u], (uint32_t)col + u * kThreads * N));
         } else {
 #pragma unroll
-            for (int u = 0; u < kBackwardVectors; ++u) v[u] = load_vector(z, (int64_t)col + u * kThreads * N, a.vocab, masked<T>());
+            for (int u = 0; u < kBackwardVectors; ++u) v[u] = load_ahead(z, (int64_t)col + u * kThreads * N, a.vocab, masked<T>());
 #pragma unroll
-            for (int u = 0; u < kBackwardVectors; ++u)
+            for (int u = 0; u < kBackwardVectors; ++u) {
+                settle(v[u], (int64_t)col + u * kThreads * N, a.vocab, masked<T>());
                 store_vector(d_z, (int64_t)col + u * kThreads * N, a.vocab, one(v[u], (uint32_t)col + u * kThreads * N));
+            }
         }
     }
 }

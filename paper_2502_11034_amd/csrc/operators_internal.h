@@ -77,42 +77,76 @@ __device__ __forceinline__ Vector<T> narrow(const float (&x)[16 / sizeof(T)])
     return v;
 }
 
-// The 16 bytes at column `col` of a row of n columns, `fill` (a word's bits) from its end on.
+// The 16 bytes at column `col` of a row of n columns, in two steps.  First a load that needs no branch where a row has 16 bytes: the last
+// vector of a row that ends inside it is loaded from the row's last 16 bytes; then, where it is used, the values below `col` are
+// shifted out and `fill` (a word's bits) takes the places from the row's end on.  (Loading the end one by one costs a wave the memory's
+// latency several times, and with short rows every wave has an end.)
 template <class T>
-__device__ __forceinline__ Vector<T> load_vector(const T* row, int64_t col, int64_t n, uint32_t fill)
+__device__ __forceinline__ Vector<T> load_ahead(const T* row, int64_t col, int64_t n, uint32_t fill)
 {
     constexpr int N = 16 / sizeof(T);
+    if (n >= N) return load_whole(row + (col < n - N ? col : n - N));
     Vector<T> v;
-    if (col + N <= n) {
-        v = load_whole(row + col);
-    } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (sizeof(T) == 4) {
-                v.w[i] = col + i < n ? __float_as_uint(row[col + i]) : fill;
-            } else {
-                const uint32_t lo = col + 2 * i < n ? row[col + 2 * i] : fill & 0xFFFFu;
-                const uint32_t hi = col + 2 * i + 1 < n ? row[col + 2 * i + 1] : fill >> 16;
-                v.w[i] = lo | hi << 16;
-            }
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            v.w[i] = col + i < n ? __float_as_uint(row[col + i]) : fill;
+        } else {
+            const uint32_t lo = col + 2 * i < n ? row[col + 2 * i] : fill & 0xFFFFu;
+            const uint32_t hi = col + 2 * i + 1 < n ? row[col + 2 * i + 1] : fill >> 16;
+            v.w[i] = lo | hi << 16;
         }
     }
     return v;
 }
+template <class T>
+__device__ __forceinline__ void settle(Vector<T>& v, int64_t col, int64_t n, uint32_t fill)
+{
+    constexpr int N = 16 / sizeof(T);
+    if (n < N || col + N <= n) return;
+    const int beyond = col < n ? (int)(col + N - n) : N;          // values past the row's end
+    const int words = sizeof(T) == 4 ? beyond : beyond / 2;
+    if (sizeof(T) == 2 && (beyond & 1)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v.w[i] = v.w[i] >> 16 | (i < 3 ? v.w[i + 1] : fill) << 16;
+    }
+    if (words & 1) v.w = u32x4{v.w[1], v.w[2], v.w[3], fill};
+    if (words & 2) v.w = u32x4{v.w[2], v.w[3], fill, fill};
+    if (words & 4) v.w = u32x4{fill, fill, fill, fill};
+}
+template <class T>
+__device__ __forceinline__ Vector<T> load_vector(const T* row, int64_t col, int64_t n, uint32_t fill)
+{
+    Vector<T> v = load_ahead(row, col, n, fill);
+    settle(v, col, n, fill);
+    return v;
+}
 
+// The end of a row is stored in pieces of four, two and one values.
 template <class T>
 __device__ __forceinline__ void store_vector(T* row, int64_t col, int64_t n, const Vector<T>& v)
 {
     constexpr int N = 16 / sizeof(T);
+    typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+    typedef uint32_t u32_any __attribute__((aligned(2)));
     if (col + N <= n) {
         store_whole(row + col, v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if (col + i < n) {
-                if constexpr (sizeof(T) == 4) row[col + i] = __uint_as_float(v.w[i]);
-                else row[col + i] = (uint16_t)(v.w[i / 2] >> (16 * (i & 1)));
-            }
+    } else if (col < n) {
+        T* p = row + col;
+        u32x4 w = v.w;
+        const int left = (int)(n - col), words = sizeof(T) == 4 ? left : left / 2;
+        if (words & 2) {
+            *reinterpret_cast<u32x2_any*>(p) = u32x2_any{w[0], w[1]};
+            p += 8 / sizeof(T);
+            w = u32x4{w[2], w[3], 0, 0};
+        }
+        if (words & 1) {
+            *reinterpret_cast<u32_any*>(p) = w[0];
+            p += 4 / sizeof(T);
+            w[0] = w[1];
+        }
+        if constexpr (sizeof(T) == 2) {
+            if (left & 1) *p = (uint16_t)w[0];
         }
     }
 }
