@@ -494,7 +494,11 @@ Plan plan_of(int64_t rows, int64_t n_out, int64_t n_in, int32_t dtype)
     p.tiles_in = (n_in + p.bn - 1) / p.bn;
     const int64_t all = p.tiles_out * p.tiles_in, round = p.bn == 256 ? kUnits : 2 * kUnits, steps = rows / kDeep;
     p.rest = all % round;
-    p.split = p.rest ? std::max<int64_t>(1, std::min(round / p.rest, steps / 8)) : 1;
+    // A part has four steps at least, and eight where there are few: what another workgroup saves has to pay for the partial sums and the second
+    // kernel (us with eight everywhere, with four everywhere: 660 tokens 74 x 125 15.2, 10.0; 1000 tokens 300 x 900 fp32 22.4, 19.2;
+    // 256 tokens 768 x 768 8.3, 10.2; 300 tokens 2000 x 2000 12.0, 26.7).
+    const int64_t most = steps < 16 ? steps / 8 : steps / 4;
+    p.split = p.rest ? std::max<int64_t>(1, std::min(round / p.rest, most)) : 1;
     if (p.split == 1) p.rest = 0;
     p.whole = all - p.rest;
     return p;
