@@ -481,8 +481,10 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(const Backw
 {
     constexpr int N = 16 / sizeof(T);
     for (uint64_t item = blockIdx.x; item < a.items; item += gridDim.x) {
-        const int64_t row = (int64_t)(item / a.row_blocks);
-        const uint32_t block = (uint32_t)(item - (uint64_t)row * a.row_blocks);
+        // last rows first: the forward pass has left them in the memory-side cache
+        const uint64_t back = a.items - 1 - item;
+        const int64_t row = (int64_t)(back / a.row_blocks);
+        const uint32_t block = (uint32_t)(back - (uint64_t)row * a.row_blocks);
         const T* z = static_cast<const T*>(a.logits) + row * a.ld;
         T* d_z = static_cast<T*>(a.d_logits) + row * a.ld_d;
         const float stat = a.stats[2 * row];
@@ -500,8 +502,10 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(const Backw
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const float logp = a.scale * (x[i] - most) - log_sum;
-                const float p = __builtin_exp2f(logp * kLog2e);        // down to subnormal numbers, which factors may raise
-                x[i] = p * fmaf(k1, fmaxf(logp, kMaskedLogp), k0);     // p is 0 from far above kMaskedLogp on
+                // p as the square of the root, which is no subnormal number (the instruction would make those 0, and factors may raise them);
+                // 0 from far above kMaskedLogp on
+                const float root = exp2_fast(logp * (0.5f * kLog2e));
+                x[i] = root * (root * fmaf(k1, fmaxf(logp, kMaskedLogp), k0));
             }
             if ((uint32_t)target - col < (uint32_t)N) {
 #pragma unroll
