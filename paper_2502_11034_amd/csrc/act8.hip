@@ -183,6 +183,9 @@ __device__ __forceinline__ void each_vector(const Args& a, Load&& load, Finish&&
     }
 }
 
+// Elementwise kernels all: bound by memory on long calls, by a load's and a store's latency on short ones (2 to 3 us).  Lanes take
+// neighbouring 16-byte vectors, so that the 4 (bf16) or 8 (fp32) lanes of a block of 32 are neighbours and find its largest value without LDS.
+// 16384 x 4096 bf16: packed in 41 us (5.0 TB/s), unpacked in 30 (6.7, from the memory-side cache).
 template <class T, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void pack_kernel(const Args a)
 {
@@ -209,7 +212,7 @@ __global__ __launch_bounds__(kThreads) void unpack_kernel(const Args a)
         });
 }
 
-// x: gate, y: up, z: out
+// x: gate, y: up, z: out.  Gate and up are read once for the product and both checkpoints: 8192 x 14336 bf16 169 us (5.6 TB/s).
 template <class T, bool WHOLE, bool PACK>
 __global__ __launch_bounds__(kThreads) void swiglu_kernel(const Args a)
 {
@@ -236,7 +239,7 @@ __global__ __launch_bounds__(kThreads) void swiglu_kernel(const Args a)
         });
 }
 
-// x: d_out, y: d_gate, z: d_up, w: out (or null)
+// x: d_out, y: d_gate, z: d_up, w: out (or null).  8192 x 14336 bf16 165 us (5.7 TB/s).
 template <class T, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void swiglu_backward_kernel(const Args a)
 {

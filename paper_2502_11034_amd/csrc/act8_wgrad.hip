@@ -159,6 +159,11 @@ struct Tile {
 // the registers it was loaded to into its place, and those take step k + 4.  One barrier a step: what it orders is the writes of k + 2
 // before their reads in the next step; the reads of a place are done a step before it is written again.  Loads past the last step take
 // the last one again: a loop without conditions lets the compiler count what is outstanding.
+//
+// What bounds large calls is power, and what the two waves of a SIMD wait for each other: 8192 tokens 14336 x 4096 bf16 816 us (1.18 PFLOP/s;
+// 923 back to back, where a library product of bf16 matrices lying like these takes 1049), the matrix cores busy 53 % of the time at
+// some 1.9 GHz, LDS 40 %; with zeros for values 738.  Reads beyond the L2s are 4.5 times the operands, 1.5 TB/s.  Small calls are a chain of
+// latencies: 123 tokens 768 x 768 8 us.
 template <class S, class T, bool EDGE>
 __global__ __launch_bounds__(S::kThreads, S::kThreads == 256 && S::kParts == 3 ? 1 : 2) void wgrad_kernel(const WgradArgs a)
 {
@@ -441,7 +446,8 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads == 256 && S::kParts == 3 ?
     }
 }
 
-// Adds the parts of the split tiles, in order: a workgroup takes one piece of four results of every lane.
+// Adds the parts of the split tiles, in order: a workgroup takes one piece of four results of every lane.  Bound by memory and latency: 128
+// tiles of 256 x 256 in two parts 17 us.
 template <class S, bool EDGE>
 __global__ __launch_bounds__(S::kThreads) void join_kernel(const WgradArgs a)
 {

@@ -274,7 +274,11 @@ __device__ __forceinline__ void write_row(const ForwardArgs& a, int64_t row, con
 
 constexpr int kAhead = 4;        // 16-byte vectors of a lane in a group
 
-// One workgroup per part of a row.
+// One workgroup per part of a row, one pass: each lane keeps a running sum of exponentials (and of z - M times them), lanes and waves are
+// joined at the end.  A row is one part unless there are too few rows to fill the chip.  Bound by memory on long calls, with the vector
+// unit busy two thirds of the time (the exponential is a quarter of its instructions' time and a row's largest value another eighth): 4096 x
+// 128256 bf16 208 us (5.1 TB/s), 1024 x 50257 with top 8 29 us (3.5 TB/s from the memory-side cache; 22 without the list), one row of 128256
+// with top 5 in 31 parts 7 us, of which a load's latency and the list's joining are all but one.
 template <class T, bool ENTROPY, bool TOP, bool SPLIT>
 __global__ __launch_bounds__(kThreads) void logprobs_kernel(const ForwardArgs a)
 {
@@ -427,7 +431,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const ForwardArgs a)
     }
 }
 
-// One wave per row joins the row's parts, at most 64, one in each lane.
+// One wave per row joins the row's parts, at most 64, one in each lane.  3.6 us for a row of 31 parts with top 5: a chain of latencies.
 template <class T, bool ENTROPY, bool TOP>
 __global__ __launch_bounds__(64) void join_parts_kernel(const ForwardArgs a)
 {
@@ -473,6 +477,8 @@ struct BackwardArgs {
     uint64_t       items;
 };
 
+// Gradient of the logits, elementwise: a lane has four vectors loaded before its first store.  Bound by memory: 4096 x 128256 bf16 read and
+// written in 350 us (6.0 TB/s), the vector unit busy for two thirds of that.
 constexpr float kMaskedLogp = -1e4f;
 constexpr int kBackwardVectors = 4;  // per lane and item
 
