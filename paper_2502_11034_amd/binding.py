@@ -271,9 +271,9 @@ def _type(dtype):
 def _matrix(t, name, shape=None, dtype=None):
     """(pointer, dtype code, leading dimension, shape) of a 2-D tensor."""
     own = t.shape
-    if len(own) != 2 or (shape is not None and own != shape):
+    if (len(own) != 2) if shape is None else (own != shape):
         raise ValueError("%s: shape %s, expected %s" % (name, tuple(own), "2-D" if shape is None else tuple(shape)))
-    code = _type(t.dtype)[0]
+    code = (_KNOWN.get(t.dtype) or _type(t.dtype))[0]
     if code is None or (dtype is not None and code != dtype):
         raise TypeError("%s: dtype %s" % (name, t.dtype))
     ld, step = t.stride()
@@ -288,7 +288,7 @@ def _dense(t, shape, dtype, name):
         return None
     if t.shape != shape:
         raise ValueError("%s: shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
-    if _type(t.dtype)[1] != dtype:
+    if (_KNOWN.get(t.dtype) or _type(t.dtype))[1] != dtype:
         raise TypeError("%s: dtype %s, expected %s" % (name, t.dtype, dtype))
     if not t.is_contiguous():
         raise ValueError("%s is not contiguous" % name)
@@ -312,7 +312,7 @@ def _bytes(t, least, name):
 def _on_device(where, *tensors):
     """A kernel that is given host memory would fault the GPU."""
     for t in tensors:
-        if t is not None and not t.is_cuda:
+        if not (t is None or t.is_cuda):
             raise AdagcError(ADAGC_ERR_INVALID_ARG, where + " (a tensor is not in device memory)")
 
 
