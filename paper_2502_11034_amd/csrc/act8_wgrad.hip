@@ -498,12 +498,14 @@ Plan plan_of(int64_t rows, int64_t n_out, int64_t n_in, int32_t dtype)
     p.bn = large || wide ? 256 : 128;
     p.tiles_out = (n_out + p.bm - 1) / p.bm;
     p.tiles_in = (n_in + p.bn - 1) / p.bn;
-    const int64_t all = p.tiles_out * p.tiles_in, round = p.bn == 256 ? kUnits : 2 * kUnits, steps = rows / kDeep;
+    const int64_t all = p.tiles_out * p.tiles_in, steps = rows / kDeep;
+    // the smaller tile's workgroups with bf16 dY share a compute unit in pairs; the others fill its LDS
+    const int64_t round = dtype == ADAGC_BF16 && !large ? 2 * kUnits : kUnits;
     p.rest = all % round;
     // A part has four steps at least, and eight where there are few: what another workgroup saves has to pay for the partial sums and the second
     // kernel (us with eight everywhere, with four everywhere: 660 tokens 74 x 125 15.2, 10.0; 1000 tokens 300 x 900 fp32 22.4, 19.2;
     // 256 tokens 768 x 768 8.3, 10.2; 300 tokens 2000 x 2000 12.0, 26.7).
-    // In the checked loop of matrices smaller than a tile a step takes twice as long: parts of two steps (215 tokens 2947 x 84 fp32 17.7 -> 13.6).
+    // In the checked loop of matrices smaller than a tile a step takes twice as long: parts of two steps (215 tokens 2947 x 84 fp32 17.7 -> 13.8).
     const bool checked = n_out < p.bm || act8_ld(n_in) < p.bn;
     const int64_t most = steps >= 16 ? steps / 4 : checked ? steps / 2 : steps / 8;
     p.split = p.rest ? std::max<int64_t>(1, std::min(round / p.rest, most)) : 1;

@@ -112,7 +112,10 @@ struct Running {
 struct TopList {
     uint64_t  mine = 0;                          // this lane's
     int       count = 0, waiting = 0;            // in the list, in LDS
-    float     bar = NAN;                         // only larger values come in (the last one's, once the list is full); NaN: any value
+    // Values of -inf do not come in: a row with too few others has its list filled up at the end (write_row), which spares masked parts of rows
+    // the sorting of equal values.
+    float     bar = -INFINITY;                   // a later vector has to have a larger value: just below the least that counts, or the full list's last
+    float     below = -INFINITY;                 // values that come in are larger: just below the least that counts, or just below the full list's last
     uint64_t* lds;                               // 64 of the wave's own
     int       k;
 
@@ -130,6 +133,8 @@ struct TopList {
         const uint32_t b = (uint32_t)(key >> 32);
         return __uint_as_float((b & 0x80000000u) ? b & 0x7FFFFFFFu : ~b);
     }
+    // The largest value below that with the upper half `bits` of a key; 0 and -0 count as one value.
+    static __device__ __forceinline__ float just_below(uint32_t bits) { return value((uint64_t)(bits - (bits == 0x80000000u ? 2 : 1)) << 32); }
     static __device__ __forceinline__ uint32_t index(uint64_t key) { return 0xFFFFFFFFu - (uint32_t)key; }
     static __device__ __forceinline__ uint64_t of_lane(uint64_t x, int lane)
     {
@@ -161,7 +166,11 @@ struct TopList {
         count = min(k, count + __builtin_popcountll(__ballot(there)));
         mine = lane < count ? lds[lane] : 0;
         in_order();
-        if (count == k) bar = value(of_lane(mine, k - 1));
+        if (count == k) {
+            const uint64_t last = of_lane(mine, k - 1);
+            bar = value(last);
+            below = just_below((uint32_t)(last >> 32));
+        }
     }
     __device__ __forceinline__ void flush()
     {
@@ -175,13 +184,13 @@ struct TopList {
     // A value of each lane, or none.  Of ones that equal a full list's last only those of lower indices wait.
     __device__ __forceinline__ void offer(float z, uint32_t index, bool there)
     {
-        uint64_t mask = __ballot(there && !(z < bar));
+        uint64_t mask = __ballot(there && !(z <= below));
         if (!mask) return;
         const uint64_t own = key(z, index);
         if (count == k) mask = __ballot(there && own > of_lane(mine, k - 1));
         if (waiting + __builtin_popcountll(mask) > 64) {
             flush();
-            mask = __ballot(there && (count == k ? own > of_lane(mine, k - 1) : !(z < bar)));
+            mask = __ballot(there && (count == k ? own > of_lane(mine, k - 1) : !(z <= below)));
         }
         const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
         if (mask >> (threadIdx.x & 63) & 1) lds[waiting + before] = own;
@@ -189,7 +198,7 @@ struct TopList {
     }
 
     // The bar for a list that gets none of what lies below the k-th largest of 64 J values (J of each lane, 0 < k <= 64 J): just below
-    // that, found bit by bit, its upper half being enough; NaN if it is -inf or NaN, for then any value may come in.
+    // that, found bit by bit, its upper half being enough; -inf if it is -inf or NaN.
     template <int J>
     static __device__ __forceinline__ float bar_of(const float (&values)[J], int k)
     {
@@ -203,7 +212,7 @@ struct TopList {
             if (above >= k) at |= bit;
         }
         const float kth = value((uint64_t)at << 32);
-        return kth > -INFINITY ? value((uint64_t)(at - (kth == 0.f ? 2 : 1)) << 32) : NAN;      // 0 and -0 count as one value
+        return kth > -INFINITY ? just_below(at) : -INFINITY;
     }
 };
 
@@ -265,10 +274,24 @@ __device__ __forceinline__ void write_row(const ForwardArgs& a, int64_t row, con
             a.stats[2 * row + 1] = log_sum;
         }
     }
-    if (TOP && lane < a.top_k) {
-        const float z = TopList::value(top.mine);
-        a.top_logprob[row * a.top_k + lane] = none ? -INFINITY : a.scale * (z - r.most) - log_sum;
-        a.top_index[row * a.top_k + lane] = (int32_t)TopList::index(top.mine);
+    if constexpr (TOP) {
+        auto put = [&](int place, float z, int32_t index) __attribute__((always_inline)) {
+            a.top_logprob[row * a.top_k + place] = none ? -INFINITY : a.scale * (z - r.most) - log_sum;
+            a.top_index[row * a.top_k + place] = index;
+        };
+        const bool there = lane < a.top_k && top.mine != 0;
+        if (there) put(lane, TopList::value(top.mine), (int32_t)TopList::index(top.mine));
+        // all others are -inf: the first of them in order
+        const T* z = static_cast<const T*>(a.logits) + row * a.ld;
+        int have = __builtin_popcountll(__ballot(there));
+        for (int64_t j0 = 0; have < a.top_k && j0 < a.vocab; j0 += 64) {
+            const int64_t j = j0 + lane;
+            const bool is = j < a.vocab && to_float(z[j]) == -INFINITY;
+            const uint64_t mask = __ballot(is);
+            const int place = have + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+            if (is && place < a.top_k) put(place, -INFINITY, (int32_t)j);
+            have += __builtin_popcountll(mask);
+        }
     }
 }
 
@@ -327,7 +350,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const ForwardArgs a)
             if (lane == 0) lane_most[kThreads] = bar;
         }
         __syncthreads();
-        top.bar = lane_most[kThreads];
+        top.bar = top.below = lane_most[kThreads];
     };
     // Whole waves go round together.  A group's loads are on their way while the group before is worked on (the last group loads
     // itself again: a loop without conditions).
@@ -451,7 +474,7 @@ __global__ __launch_bounds__(64) void join_parts_kernel(const ForwardArgs a)
         const uint64_t* keys = a.part_keys + row * a.parts * a.top_k;
         const uint64_t first = has ? keys[lane * a.top_k] : 0;
         const float largest[1] = {first ? TopList::value(first) : -INFINITY};
-        top.bar = TopList::bar_of(largest, a.top_k);
+        top.bar = top.below = TopList::bar_of(largest, a.top_k);
         for (int j = 0; j < a.parts * a.top_k; j += 64) {
             const uint64_t key = j + lane < a.parts * a.top_k ? keys[j + lane] : 0;
             top.offer(TopList::value(key), TopList::index(key), key != 0);

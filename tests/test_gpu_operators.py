@@ -183,6 +183,28 @@ def test_logprobs_ties_and_order():
             assert torch.equal(out["top_index"].cpu().long(), O.top(rows.to(dtype), 64))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [7, 1100])                            # rows in several parts and in one
+def test_logprobs_top_of_mostly_masked_rows(dtype, rows):
+    """Fewer tokens than alternatives asked for, parts without any, ones of the type's lowest value, and masks in front of the rest."""
+    dtype, vocab, k = TYPES[dtype], 40007, 20
+    g = gen(17)
+    z = torch.full((7, vocab), -math.inf, dtype=dtype)
+    z[1, torch.randperm(vocab, generator=g)[:5]] = torch.randn(5, generator=g).to(dtype)
+    z[2, torch.randperm(vocab, generator=g)[:19]] = torch.finfo(dtype).min
+    z[3, 7000:] = torch.randn(vocab - 7000, generator=g).to(dtype)
+    z[4, :30000] = torch.randn(30000, generator=g).to(dtype)
+    z[5, vocab - 3:] = 1.0
+    z[6, ::2] = torch.finfo(dtype).min
+    z[6, 3] = math.nan
+    z = z.repeat(-(-rows // 7), 1)[:rows]
+    _, out = run_logprobs(z, torch.zeros(rows, dtype=torch.int64), 1.0, k)
+    assert torch.equal(out["top_index"].cpu().long(), O.top(z[:7], k).repeat(-(-rows // 7), 1)[:rows])
+    logp = out["top_logprob"].cpu()
+    assert (logp[0] == -math.inf).all() and torch.isnan(logp[6]).all()
+    assert (logp[1, 5:] == -math.inf).all() and torch.isfinite(logp[1, :5]).all()
+
+
 @pytest.mark.parametrize("scale", [1e-3, 50.0])
 def test_logprobs_scales(scale):
     z, t = make_logits(6, 5003, torch.float32, 7, size=4.0)
