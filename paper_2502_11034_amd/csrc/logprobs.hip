@@ -501,7 +501,7 @@ struct BackwardArgs {
 };
 
 // Gradient of the logits, elementwise: a lane has four vectors loaded before its first store.  Bound by memory: 4096 x 128256 bf16 read and
-// written in 350 us (6.0 TB/s), the vector unit busy for two thirds of that.
+// written in 350 us (6.0 TB/s), the vector unit busy for half of that.
 constexpr float kMaskedLogp = -1e4f;
 constexpr int kBackwardVectors = 4;  // per lane and item
 
