@@ -326,7 +326,7 @@ def _size(rc, where):
 
 @functools.lru_cache(maxsize=1024)
 def adagc_token_logprobs_workspace_bytes(rows, vocab, top_k=0):
-    return _size(lib().adagc_token_logprobs_workspace_bytes(rows, vocab, top_k), "adagc_token_logprobs_workspace_bytes")
+    return _size(lib().adagc_token_logprobs_workspace_bytes(int(rows), int(vocab), int(top_k)), "adagc_token_logprobs_workspace_bytes")
 
 
 def adagc_token_logprobs(logits, targets=None, logprob=None, entropy=None, stats=None, top_logprob=None, top_index=None, scale=1.0,
@@ -371,7 +371,7 @@ def adagc_token_logprobs_backward(logits, targets, stats, entropy, d_logprob, d_
 @functools.lru_cache(maxsize=1024)
 def adagc_act8_bytes(rows, cols):
     """Bytes of a checkpoint of a rows x cols matrix."""
-    return _size(lib().adagc_act8_bytes(rows, cols), "adagc_act8_bytes")
+    return _size(lib().adagc_act8_bytes(int(rows), int(cols)), "adagc_act8_bytes")
 
 
 def adagc_act8_pack(x, ckpt, stream=None):
@@ -429,7 +429,7 @@ def adagc_swiglu_backward(d_out, gate_ckpt, up_ckpt, d_gate, d_up, out=None, str
 
 @functools.lru_cache(maxsize=1024)
 def adagc_act8_wgrad_workspace_bytes(rows, n_out, n_in, dtype):
-    return _size(lib().adagc_act8_wgrad_workspace_bytes(rows, n_out, n_in, dtype), "adagc_act8_wgrad_workspace_bytes")
+    return _size(lib().adagc_act8_wgrad_workspace_bytes(int(rows), int(n_out), int(n_in), int(dtype)), "adagc_act8_wgrad_workspace_bytes")
 
 
 def adagc_act8_wgrad(d_out, ckpt, d_weight, accumulate=False, workspace=None, stream=None):

@@ -118,6 +118,13 @@ def test_sizes():
         assert 0 <= B.adagc_act8_wgrad_workspace_bytes(rows, n_out, n_in, B.ADAGC_BF16) <= 1 << 31
 
 
+def test_sizes_take_numpy_integers():
+    np = pytest.importorskip("numpy")
+    assert B.adagc_act8_bytes(np.int64(3), np.int32(33)) == 3 * 66
+    assert B.adagc_token_logprobs_workspace_bytes(np.int64(4096), np.int64(128256), np.int64(5)) == 0
+    assert B.adagc_act8_wgrad_workspace_bytes(np.int64(0), np.int64(5), np.int64(5), np.int64(1)) == 0
+
+
 def test_binding_refuses_tensors_that_do_not_fit():
     bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)
     f = lambda *s: torch.zeros(*s)
