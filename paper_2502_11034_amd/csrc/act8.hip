@@ -142,10 +142,29 @@ __device__ __forceinline__ void unpack_vector(const Packed& p, float (&x)[N])
     }
 }
 
-// 1 / (1 + exp(-g))
-__device__ __forceinline__ float sigmoid(float g)
+// t = 1 / (1 + exp(-g)) as p w, w a power of two, and 1 - t.  p is a normal number also where t is too small for one (g from -87 down to
+// -167, which leave normal results of large factors; below, t counts as 0), so products are taken with p first and with w at the end.
+// FINE, for fp32 values: the exponential's argument |g| log2 e is carried in two numbers, and the reciprocal gets a Newton step, so that t is
+// off by 8 * 2^-24 of itself at most.  With the argument rounded to one number that is 2 |g| more, 2^-16 of t at the least: nothing
+// beside the 2^-8 of bf16 results, and 8192 x 14336 bf16 takes 1 % less (forward 175 against 177 us, back 171 against 173).
+struct Gate {
+    float p, w, rest;
+};
+template <bool FINE>
+__device__ __forceinline__ Gate sigmoid(float g)
 {
-    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(g * -1.44269504088896340736f));
+#pragma clang fp contract(off)      // high + 116 is exact, of the product as it was rounded
+    constexpr float kC = -1.44269504088896340736f, kLow = (float)(-1.44269504088896340736 - (double)kC), kLn2 = 0.69314718055994530942f;
+    const float size = FINE ? fminf(fabsf(g), 200.f) : fabsf(g);     // an infinite argument has no rest
+    const float high = size * kC;
+    const bool far = g < 0.f && high < -126.f;
+    const float w = far ? 0x1p-116f : 1.f;
+    float e = __builtin_amdgcn_exp2f(far ? high + 116.f : high);     // exp(-|g|) / w
+    if constexpr (FINE) e = fmaf(e, fmaf(size, kLow, fmaf(size, kC, -high)) * kLn2, e);
+    const float d = fmaf(e, w, 1.f);
+    float q = __builtin_amdgcn_rcpf(d);
+    if constexpr (FINE) q = fmaf(fmaf(-d, q, 1.f), q, q);
+    return g < 0.f ? Gate{e * q, w, q} : Gate{q, 1.f, e * q};
 }
 
 // finish(place, load(place)) for every vector; a lane's loads come before its first store, of which the compiler could not tell that
@@ -230,7 +249,10 @@ __global__ __launch_bounds__(kThreads) void swiglu_kernel(const Args a)
             widen(settled<WHOLE>(in.gate, a, at.col), g);
             widen(settled<WHOLE>(in.up, a, at.col), u);
 #pragma unroll
-            for (int i = 0; i < N; ++i) h[i] = g[i] * sigmoid(g[i]) * u[i];
+            for (int i = 0; i < N; ++i) {
+                const Gate t = sigmoid<sizeof(T) == 4>(g[i]);
+                h[i] = g[i] * t.p * u[i] * t.w;
+            }
             put<WHOLE>(out_row<T>(a.z, at.row), a, at.col, narrow<T>(h));
             if constexpr (PACK) {
                 pack_vector(a, a.a, at, g);
@@ -260,10 +282,11 @@ __global__ __launch_bounds__(kThreads) void swiglu_backward_kernel(const Args a)
             unpack_vector(in.up, u);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float t = sigmoid(g[i]), silu = g[i] * t;
-                dg[i] = d[i] * u[i] * (t + silu * (1.f - t));
-                h[i] = silu * u[i];
-                d[i] *= silu;
+                const Gate t = sigmoid<sizeof(T) == 4>(g[i]);
+                const float silu = g[i] * t.p;
+                dg[i] = d[i] * (u[i] * (t.p * fmaf(g[i], t.rest, 1.f))) * t.w;
+                h[i] = silu * u[i] * t.w;
+                d[i] = d[i] * silu * t.w;
             }
             put<WHOLE>(out_row<T>(a.y, at.row), a, at.col, narrow<T>(dg));
             put<WHOLE>(out_row<T>(a.z, at.row), a, at.col, narrow<T>(d));

@@ -1,0 +1,50 @@
+"""Corners of the operators around the step: results next to the ends of fp32's range, and instantiations that ordinary sizes seldom reach."""
+import pytest
+import torch
+
+import operators_oracle as O
+from paper_2502_11034_amd import binding as B
+from test_gpu_operators import DEV, Framed, gen, near
+
+pytestmark = pytest.mark.gpu
+U = O.U32
+
+
+# ------------------------------------------------------------------------------------------------ gated activation
+
+def gate_off(g, dtype):
+    """What t = 1 / (1 + exp(-g)) may be off by, in half steps of fp32 of itself.  The same number for every g in fp32: the exponential's
+    instruction a step (2), its correction 1, then 1 + e one and e's share, the reciprocal after a Newton step 1, their product 1.  For
+    bf16 values the argument |g| log2 e is one rounded number times a rounded constant (2 |g|), and the reciprocal's step (2) stays."""
+    return 8.0 if dtype == torch.float32 else 9.0 + 2.0 * g.abs()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [1.5, 2.0 ** 100])
+def test_gates_far_from_zero(dtype, size):
+    """Relative error independent of the gate, and no zeros where the product is a normal number: silu(-88) = -5.3e-37."""
+    dtype = torch.float32 if dtype == "f32" else torch.bfloat16
+    step = torch.linspace(-160, 90, 64 * 100).view(64, 100)
+    step[0, :8] = torch.tensor([-88.0, -87.5, -88.7, -89.0, -91.0, -1.2784645, -0.0, 1e-30])
+    gate = step.to(dtype)
+    up = torch.full_like(gate, size)
+    out = Framed(64, 100, dtype)
+    ckpts = [torch.empty(B.adagc_act8_bytes(64, 100), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    B.adagc_swiglu(gate.to(DEV), up.to(DEV), out.t, *ckpts)
+    g, u = gate.double(), up.double()
+    want = g * torch.sigmoid(g) * u
+    near(out.result(), want, want.abs() * (gate_off(g, dtype) + 4) * U + 2.0 ** -126, dtype)        # three more products
+
+    g, u = (O.values(c.cpu(), 64, 100) for c in ckpts)
+    t = torch.sigmoid(g)
+    d_out = torch.randn(64, 100, generator=gen(50)).to(dtype)
+    d = d_out.double()
+    d_gate, d_up, again = (Framed(64, 100, dtype) for _ in range(3))
+    B.adagc_swiglu_backward(d_out.to(DEV), *ckpts, d_gate.t, d_up.t, again.t)
+    rest = torch.sigmoid(-g)                                                                  # 1 - t
+    slope = 1 + g * rest
+    near(again.result(), g * t * u, (g * t * u).abs() * (gate_off(g, dtype) + 4) * U + 2.0 ** -126, dtype)
+    near(d_up.result(), d * g * t, (d * g * t).abs() * (gate_off(g, dtype) + 4) * U + 2.0 ** -126, dtype)
+    # d and u times t times the slope, in which g rest is off by as much as t and one product
+    off = (d * u).abs() * t * U * (slope.abs() * (gate_off(g, dtype) + 5) + (g * rest).abs() * (gate_off(g, dtype) + 1))
+    near(d_gate.result(), d * u * t * slope, off + 2.0 ** -126, dtype)
