@@ -521,10 +521,23 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(const Backw
         const float most = stat == -INFINITY ? 0.f : stat, log_sum = stat == -INFINITY ? INFINITY : a.stats[2 * row + 1];
         const int64_t t = a.targets ? a.targets[row] : -1;
         const int target = t >= 0 && t < a.vocab && stat != -INFINITY ? (int)t : -1;
-        const float d_lp = t >= 0 && t < a.vocab ? a.d_logprob[row] : 0.f;
-        const float d_h = a.d_entropy ? a.d_entropy[row] : 0.f;
+        float d_lp = t >= 0 && t < a.vocab ? a.d_logprob[row] : 0.f;
+        float d_h = a.d_entropy ? a.d_entropy[row] : 0.f;
         const float h = a.d_entropy ? a.entropy[row] : 0.f;
-        const float k0 = -a.scale * (d_lp + d_h * h), k1 = -a.scale * d_h;
+        // Gradients with which scale (d_lp + d_h (logp + h)) might be no number where p takes it back to one, or to 0: the larger is moved
+        // to 2^99 or above and the scale next to 1 first, results by `after` powers of two last.
+        const float size = fmaxf(fabsf(d_lp), fabsf(d_h));
+        const bool huge = size > 0x1p100f || size > 0x1p100f / a.scale;
+        float scale = a.scale;
+        int after = 0;
+        if (huge) {
+            const int of_size = __builtin_amdgcn_frexp_expf(size), of_scale = __builtin_amdgcn_frexp_expf(scale);
+            d_lp = __builtin_ldexpf(d_lp, 100 - of_size);
+            d_h = __builtin_ldexpf(d_h, 100 - of_size);
+            scale = __builtin_ldexpf(scale, -of_scale);
+            after = of_size + of_scale - 100;
+        }
+        const float k0 = -scale * (d_lp + d_h * h), k1 = -scale * d_h;
         auto one = [&](const Vector<T>& v, uint32_t col) __attribute__((always_inline)) {
             float x[N];
             widen(v, x);
@@ -538,7 +551,11 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(const Backw
             }
             if ((uint32_t)target - col < (uint32_t)N) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) x[i] += (uint32_t)target == col + i ? a.scale * d_lp : 0.f;
+                for (int i = 0; i < N; ++i) x[i] += (uint32_t)target == col + i ? scale * d_lp : 0.f;
+            }
+            if (huge) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] = __builtin_ldexpf(x[i], after);
             }
             return narrow<T>(x);
         };

@@ -1,4 +1,6 @@
 """Corners of the operators around the step: results next to the ends of fp32's range, and instantiations that ordinary sizes seldom reach."""
+import math
+
 import pytest
 import torch
 
@@ -48,3 +50,36 @@ def test_gates_far_from_zero(dtype, size):
     # d and u times t times the slope, in which g rest is off by as much as t and one product
     off = (d * u).abs() * t * U * (slope.abs() * (gate_off(g, dtype) + 5) + (g * rest).abs() * (gate_off(g, dtype) + 1))
     near(d_gate.result(), d * u * t * slope, off + 2.0 ** -126, dtype)
+
+
+# ------------------------------------------------------------------------------------------------ gradient of the logits
+
+def gradient(z, t, scale, d_logprob, d_entropy, in_place=False):
+    rows, vocab = z.shape
+    zd = Framed(rows, vocab, z.dtype, data=z)
+    logprob, entropy, stats = (torch.empty(s, device=DEV) for s in ((rows,), (rows,), (rows, 2)))
+    B.adagc_token_logprobs(zd.t, t.to(DEV), logprob, entropy, stats, scale=scale)
+    d = zd if in_place else Framed(rows, vocab, z.dtype)
+    B.adagc_token_logprobs_backward(zd.t, t.to(DEV), stats, entropy, d_logprob.to(DEV), d_entropy.to(DEV), d.t, scale=scale)
+    return d.result()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale, size", [(1.0, 3.5e34), (1.0, 3e38), (0.5, 1e37), (2.0 ** 100, 3e4), (2.0 ** 100, 1e36), (2.0 ** 100, 1e-30),
+                                         (2.0 ** -100, 3e38), (2.0 ** -100, 1.0)])
+def test_gradients_of_any_size(dtype, scale, size):
+    """Wherever scale and gradients are numbers: masked and vanishing tokens get 0, the others what the formula gives, infinite only
+    where that is."""
+    dtype, g = torch.float32 if dtype == "f32" else torch.bfloat16, gen(51)
+    z = torch.randn(6, 300, generator=g).to(dtype)
+    z[:, ::3] = -math.inf
+    z[1, 5:] = -math.inf
+    z[2, 7] = 100.0
+    t = torch.tensor([1, 2, 7, -1, 4, 299])
+    dl, dh = ((torch.rand(6, generator=g) / 2 + 0.5) * size * torch.randn(6, generator=g).sign() for _ in range(2))
+    got = gradient(z, t, scale, dl, dh)
+    assert not got[z == -math.inf].any()
+    want, off = O.logprobs_backward(z, t, scale, dl, dh)
+    most = torch.finfo(dtype).max
+    want = torch.where(want.abs() > most, want.sign() * math.inf, want)
+    near(got, want, off, dtype)
