@@ -521,8 +521,9 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(const Backw
         const float most = stat == -INFINITY ? 0.f : stat, log_sum = stat == -INFINITY ? INFINITY : a.stats[2 * row + 1];
         const int64_t t = a.targets ? a.targets[row] : -1;
         const int target = t >= 0 && t < a.vocab && stat != -INFINITY ? (int)t : -1;
-        float d_lp = t >= 0 && t < a.vocab ? a.d_logprob[row] : 0.f;
-        float d_h = a.d_entropy ? a.d_entropy[row] : 0.f;
+        // a row of nothing but masked values asks for no gradient, which may be no number (of a ratio of its probabilities, for one)
+        float d_lp = target >= 0 ? a.d_logprob[row] : 0.f;
+        float d_h = a.d_entropy && stat != -INFINITY ? a.d_entropy[row] : 0.f;
         const float h = a.d_entropy ? a.entropy[row] : 0.f;
         // Gradients with which scale (d_lp + d_h (logp + h)) might be no number where p takes it back to one, or to 0: the larger is moved
         // to 2^99 or above and the scale next to 1 first, results by `after` powers of two last.

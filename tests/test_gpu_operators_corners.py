@@ -83,3 +83,17 @@ def test_gradients_of_any_size(dtype, scale, size):
     most = torch.finfo(dtype).max
     want = torch.where(want.abs() > most, want.sign() * math.inf, want)
     near(got, want, off, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("odd", [math.nan, math.inf, -math.inf])
+def test_rows_of_nothing_get_no_gradient(dtype, odd):
+    """All of a masked row's gradient is 0, also where the gradients asked for are no numbers; the other rows do not notice."""
+    z = torch.randn(3, 1030, generator=gen(52)).to(torch.float32 if dtype == "f32" else torch.bfloat16)
+    z[1] = -math.inf
+    t, dl, dh = torch.tensor([5, 6, -1]), torch.tensor([1.0, odd, odd]), torch.tensor([0.5, odd, -0.5])
+    want, off = O.logprobs_backward(z, t, 1.0, torch.tensor([1.0, 0.0, 0.0]), torch.tensor([0.5, 0.0, -0.5]))
+    for in_place in (False, True):
+        got = gradient(z, t, 1.0, dl, dh, in_place)
+        near(got, want, off, z.dtype)
+        assert not got[1].any()
