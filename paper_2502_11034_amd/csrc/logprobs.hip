@@ -256,6 +256,11 @@ __device__ __forceinline__ void write_row(const ForwardArgs& a, int64_t row, con
 {
     const int lane = threadIdx.x & 63;
     const bool none = r.most == -INFINITY && r.sum == 0.f;
+    // scale (z - M), also where the difference is beyond fp32's range and the product is not
+    auto relative = [&](float z) __attribute__((always_inline)) {
+        const float d = z - r.most;
+        return d == -INFINITY && z != -INFINITY ? 2.f * a.scale * (0.5f * z - 0.5f * r.most) : a.scale * d;
+    };
     // relative to ref, which is the maximum here
     const float log_sum = none ? 0.f : logf(r.sum);
     if (lane == 0) {
@@ -264,7 +269,7 @@ __device__ __forceinline__ void write_row(const ForwardArgs& a, int64_t row, con
             float v = 0.f;
             if (t >= 0 && t < a.vocab) {
                 const float z = to_float(static_cast<const T*>(a.logits)[row * a.ld + t]);
-                v = none ? -INFINITY : a.scale * (z - r.most) - log_sum;
+                v = none ? -INFINITY : relative(z) - log_sum;
             }
             a.logprob[row] = v;
         }
@@ -276,7 +281,7 @@ __device__ __forceinline__ void write_row(const ForwardArgs& a, int64_t row, con
     }
     if constexpr (TOP) {
         auto put = [&](int place, float z, int32_t index) __attribute__((always_inline)) {
-            a.top_logprob[row * a.top_k + place] = none ? -INFINITY : a.scale * (z - r.most) - log_sum;
+            a.top_logprob[row * a.top_k + place] = none ? -INFINITY : relative(z) - log_sum;
             a.top_index[row * a.top_k + place] = index;
         };
         const bool there = lane < a.top_k && top.mine != 0;

@@ -6,7 +6,7 @@ import torch
 
 import operators_oracle as O
 from paper_2502_11034_amd import binding as B
-from test_gpu_operators import DEV, Framed, gen, near
+from test_gpu_operators import DEV, Framed, check_logprobs, gen, near
 
 pytestmark = pytest.mark.gpu
 U = O.U32
@@ -97,3 +97,17 @@ def test_rows_of_nothing_get_no_gradient(dtype, odd):
         got = gradient(z, t, 1.0, dl, dh, in_place)
         near(got, want, off, z.dtype)
         assert not got[1].any()
+
+
+# ------------------------------------------------------------------------------------------------ log-probabilities
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [9, 20011])                     # a row in one part and in several
+@pytest.mark.parametrize("scale", [2.0 ** -100, 1e-20, 0.25])
+def test_differences_beyond_the_range(dtype, vocab, scale):
+    """A token of the type's lowest value beside one of its largest: the difference is no fp32 number, scale times it may be one."""
+    dtype = torch.float32 if dtype == "f32" else torch.bfloat16
+    z = torch.full((2, vocab), -math.inf, dtype=dtype)
+    z[:, 3:7] = torch.tensor([torch.finfo(dtype).min, 1.0, torch.finfo(dtype).max, -2.0 ** 127], dtype=dtype)
+    t = torch.tensor([3, 6])
+    check_logprobs(z, t, scale, 4)
