@@ -527,7 +527,7 @@ int adagc_swiglu_backward(const void* d_out, int64_t ld_d_out, int32_t dtype, co
  *   d_weight   DEVICE weight_dtype[n_out][ld_weight], n_in values a row; zero rows of d_out make it 0 (or leave it)
  *   workspace  DEVICE, adagc_act8_wgrad_workspace_bytes of it (0: may be NULL), 16-byte aligned, contents without meaning
  * The result does not depend on what else runs: sums are taken in a fixed order.
- * Errors: INVALID_ARG, TOO_LARGE, HIP.
+ * Errors: INVALID_ARG, TOO_LARGE (also, and from the workspace's size too, where d_weight is some 2^24 tiles of 128 x 128 values or more), HIP.
  */
 int64_t adagc_act8_wgrad_workspace_bytes(int64_t rows, int64_t n_out, int64_t n_in, int32_t dtype);
 int adagc_act8_wgrad(const void* d_out, int32_t dtype, int64_t ld_d_out, const void* ckpt, int64_t rows, int64_t n_out, int64_t n_in,

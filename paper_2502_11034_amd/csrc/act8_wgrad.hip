@@ -487,6 +487,7 @@ struct Plan {
     int     bm, bn;
     int64_t tiles_out, tiles_in, whole, rest, split;
     int64_t workspace() const { return split > 1 ? rest * split * bm * bn * 4 : 0; }
+    bool    launchable() const { return (whole + rest * split) * (bm + bn > 256 ? 512 : 256) <= UINT32_MAX; }      // lanes
 };
 Plan plan_of(int64_t rows, int64_t n_out, int64_t n_in, int32_t dtype)
 {
@@ -542,7 +543,8 @@ using namespace adagc;
 extern "C" int64_t adagc_act8_wgrad_workspace_bytes(int64_t rows, int64_t n_out, int64_t n_in, int32_t dtype)
 {
     if (const int rc = check(rows, n_out, n_in, dtype)) return rc;
-    return plan_of(rows, n_out, n_in, dtype).workspace();
+    const Plan p = plan_of(rows, n_out, n_in, dtype);
+    return p.launchable() ? p.workspace() : (int64_t)ADAGC_ERR_TOO_LARGE;
 }
 
 extern "C" int adagc_act8_wgrad(const void* d_out, int32_t dtype, int64_t ld_d_out, const void* ckpt, int64_t rows, int64_t n_out,
@@ -557,7 +559,7 @@ extern "C" int adagc_act8_wgrad(const void* d_out, int32_t dtype, int64_t ld_d_o
         return ADAGC_ERR_INVALID_ARG;
     if (ld_weight > kMaxLd || (rows > 0 && ld_d_out > kMaxLd)) return ADAGC_ERR_TOO_LARGE;
     const Plan p = plan_of(rows, n_out, n_in, dtype);
-    if (p.whole + p.rest * p.split > (1 << 22)) return ADAGC_ERR_TOO_LARGE;
+    if (!p.launchable()) return ADAGC_ERR_TOO_LARGE;
     const int64_t need = p.workspace();
     if (need > 0 && (!workspace || workspace_bytes < need || misaligned(workspace, 16))) return ADAGC_ERR_INVALID_ARG;
     WgradArgs a{};

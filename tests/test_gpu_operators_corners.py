@@ -6,7 +6,7 @@ import torch
 
 import operators_oracle as O
 from paper_2502_11034_amd import binding as B
-from test_gpu_operators import DEV, Framed, check_logprobs, gen, near
+from test_gpu_operators import DEV, FILL, Framed, check_logprobs, gen, near
 
 pytestmark = pytest.mark.gpu
 U = O.U32
@@ -111,3 +111,22 @@ def test_differences_beyond_the_range(dtype, vocab, scale):
     z[:, 3:7] = torch.tensor([torch.finfo(dtype).min, 1.0, torch.finfo(dtype).max, -2.0 ** 127], dtype=dtype)
     t = torch.tensor([3, 6])
     check_logprobs(z, t, scale, 4)
+
+
+# ------------------------------------------------------------------------------------------------ weight gradient
+
+@pytest.mark.parametrize("thin", ["n_in", "n_out"])
+def test_wgrad_of_more_tiles_than_two_to_22(thin):
+    """One token, so that dW is the product itself: 2^29 + 1 outputs of one input, and one output of as many inputs."""
+    n = 2 ** 29 + 1
+    long = (torch.arange(n, dtype=torch.int32, device=DEV) % 15 - 7).to(torch.bfloat16)       # exact next to a block's 7
+    n_out, n_in = (n, 1) if thin == "n_in" else (1, n)
+    d_out, x = (long[None], torch.full((1, 1), 2.0, dtype=torch.bfloat16, device=DEV))
+    if thin == "n_out":
+        d_out, x = x, d_out
+    ckpt = torch.empty(B.adagc_act8_bytes(1, n_in), dtype=torch.uint8, device=DEV)
+    B.adagc_act8_pack(x, ckpt)
+    w = torch.full((n_out, n_in), FILL, dtype=torch.bfloat16, device=DEV)
+    size = B.adagc_act8_wgrad_workspace_bytes(1, n_out, n_in, B.ADAGC_BF16)
+    B.adagc_act8_wgrad(d_out, ckpt, w, workspace=torch.empty(max(1, size), dtype=torch.uint8, device=DEV))
+    assert all(torch.equal(a, 2 * b) for a, b in zip(w.view(-1).split(2 ** 27), long.split(2 ** 27)))
