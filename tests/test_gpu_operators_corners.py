@@ -6,7 +6,7 @@ import torch
 
 import operators_oracle as O
 from paper_2502_11034_amd import binding as B
-from test_gpu_operators import DEV, FILL, Framed, check_logprobs, gen, near
+from test_gpu_operators import DEV, FILL, Framed, check_logprobs, gen, near, run_wgrad
 
 pytestmark = pytest.mark.gpu
 U = O.U32
@@ -130,3 +130,39 @@ def test_wgrad_of_more_tiles_than_two_to_22(thin):
     size = B.adagc_act8_wgrad_workspace_bytes(1, n_out, n_in, B.ADAGC_BF16)
     B.adagc_act8_wgrad(d_out, ckpt, w, workspace=torch.empty(max(1, size), dtype=torch.uint8, device=DEV))
     assert all(torch.equal(a, 2 * b) for a, b in zip(w.view(-1).split(2 ** 27), long.split(2 ** 27)))
+
+
+@pytest.mark.parametrize("dw", ["f32", "bf16"])
+@pytest.mark.parametrize("rows, n_out, n_in, ld_d, offset, ld_w, accumulate", [
+    (96, 128, 128, None, 0, None, False),              # three steps: one that the loop itself has staged
+    (165, 200, 200, 203, 1, 201, True),                # five, and tokens after them
+    (480, 129, 97, None, 0, None, False),              # fifteen, not split
+    (1000, 130, 150, 131, 3, 151, True),               # 31 in seven parts
+    (4097, 300, 224, None, 0, 229, False),             # 128 in 32 parts, and a token after them
+    (2200, 700, 255, 701, 0, None, True),
+])
+def test_wgrad_of_fp32_gradients_and_narrow_inputs(dw, rows, n_out, n_in, ld_d, offset, ld_w, accumulate):
+    """fp32 gradients of layers with 97 to 255 inputs have tiles, a main loop and a joining kernel of their own."""
+    g = gen(rows + n_out)
+    d_out = torch.randn(rows, n_out, generator=g) * torch.exp(2 * torch.randn(rows, 1, generator=g))
+    x = (torch.randn(rows, n_in, generator=g) * torch.exp(torch.randn(1, n_in, generator=g))).to(torch.bfloat16)
+    dw = torch.float32 if dw == "f32" else torch.bfloat16
+    start = torch.randn(n_out, n_in, generator=g).to(dw) if accumulate else None
+    got, held = run_wgrad(d_out, x, dw, ld_d, offset, ld_w, start)
+    want, off = O.wgrad(d_out, held)
+    if accumulate:
+        want = want + start.double()
+        off = off + 2 * U * (want.abs() + off)
+    near(got, want, off, dw)
+
+
+@pytest.mark.parametrize("rows", [31, 32, 64, 97, 160, 224, 511, 512, 2085])
+def test_wgrad_of_fp32_gradients_and_narrow_inputs_is_exact(rows):
+    """Whole numbers, every sum of which is one in fp32: no token is lost or taken twice, whatever the number of steps and parts."""
+    g = gen(rows)
+    d_out = torch.randint(-2 ** 9, 2 ** 9 + 1, (rows, 333), generator=g).float() * 2.0 ** -3        # two bf16 terms
+    x = torch.randint(-8, 9, (rows, 200), generator=g).to(torch.bfloat16)
+    x[:, ::32] = 8                                     # blocks of one scale hold these exactly
+    got, held = run_wgrad(d_out, x, torch.float32)
+    assert torch.equal(held, x.double())
+    assert torch.equal(got.double(), d_out.double().t() @ x.double())
