@@ -32,9 +32,8 @@ struct Checkpoint {
 struct Args {
     Matrix     x, y, z, w;       // as the kernel has them
     Checkpoint a, b;
-    int64_t    rows;
     int32_t    cols, ld;         // of the checkpoints
-    uint32_t   row_vectors;      // vectors of a row of ld elements
+    uint32_t   row_vectors;      // vectors of a row of ld elements: four at least
     uint32_t   reciprocal;       // 2^32 / row_vectors, rounded down
     uint64_t   vectors;
 };
@@ -303,11 +302,10 @@ Checkpoint checkpoint(const void* p, int64_t rows, int64_t cols)
 Args arguments(int64_t rows, int64_t cols, int32_t dtype)
 {
     Args a{};
-    a.rows = rows;
     a.cols = (int32_t)cols;
     a.ld = (int32_t)act8_ld(cols);
     a.row_vectors = (uint32_t)((int64_t)a.ld * dtype_size(dtype) / 16);
-    a.reciprocal = a.row_vectors == 1 ? UINT32_MAX : (uint32_t)((1ull << 32) / a.row_vectors);
+    a.reciprocal = (uint32_t)((1ull << 32) / a.row_vectors);
     a.vectors = (uint64_t)rows * a.row_vectors;
     return a;
 }

@@ -498,7 +498,6 @@ struct BackwardArgs {
     const float*   d_logprob;
     const float*   d_entropy;
     int64_t        ld, ld_d;
-    int64_t        rows;
     int32_t        vocab;
     float          scale;
     uint32_t       row_blocks;    // workgroup items per row
@@ -693,7 +692,6 @@ extern "C" int adagc_token_logprobs_backward(const void* logits, int32_t dtype, 
     a.d_entropy = d_entropy;
     a.ld = ld;
     a.ld_d = ld_d;
-    a.rows = rows;
     a.vocab = (int32_t)vocab;
     a.scale = scale;
     const int64_t per_block = (int64_t)kThreads * kBackwardVectors * (16 / dtype_size(dtype));
