@@ -141,29 +141,47 @@ __device__ __forceinline__ void unpack_vector(const Packed& p, float (&x)[N])
     }
 }
 
-// t = 1 / (1 + exp(-g)) as p w, w a power of two, and 1 - t.  p is a normal number also where t is too small for one (g from -87 down to
-// -167, which leave normal results of large factors; below, t counts as 0), so products are taken with p first and with w at the end.
-// FINE, for fp32 values: the exponential's argument |g| log2 e is carried in two numbers, and the reciprocal gets a Newton step, so that t is
-// off by 8 * 2^-24 of itself at most.  With the argument rounded to one number that is 2 |g| more, 2^-16 of t at the least: nothing
-// beside the 2^-8 of bf16 results, and 8192 x 14336 bf16 takes 1 % less (forward 175 against 177 us, back 171 against 173).
+// t = 1 / (1 + exp(-g)) as p w, w a power of two, and 1 - t.
+// FAR, for gates below kFar, where t is exp(g) in all its bits and next to the least normal number or below it (large factors make normal
+// results of those too): p is exp(g) 2^116 (0 below -167).  Products are taken with p first and with w last.  Other gates' results are
+// the same either way.
+// FINE, for fp32 values: what the exponential's argument g log2 e loses by its rounding is multiplied in after, so that t is off by
+// 8 * 2^-24 of itself at most.  Without, that is 2 |g| more, 2^-16 of t at the least: nothing beside the 2^-8 of bf16 results.  The
+// five instructions a value cost 2048 x 4096 fp32 5 % forward, from the memory-side cache (19.5 -> 20.4 us), 8192 x 4096 1.5 % (87.9 -> 89.2).
 struct Gate {
     float p, w, rest;
 };
-template <bool FINE>
+constexpr float kFar = -87.f;
+template <bool FINE, bool FAR>
 __device__ __forceinline__ Gate sigmoid(float g)
 {
-#pragma clang fp contract(off)      // high + 116 is exact, of the product as it was rounded
+#pragma clang fp contract(off)      // `high` is the product as it was rounded, everywhere
     constexpr float kC = -1.44269504088896340736f, kLow = (float)(-1.44269504088896340736 - (double)kC), kLn2 = 0.69314718055994530942f;
-    const float size = FINE ? fminf(fabsf(g), 200.f) : fabsf(g);     // an infinite argument has no rest
-    const float high = size * kC;
-    const bool far = g < 0.f && high < -126.f;
-    const float w = far ? 0x1p-116f : 1.f;
-    float e = __builtin_amdgcn_exp2f(far ? high + 116.f : high);     // exp(-|g|) / w
-    if constexpr (FINE) e = fmaf(e, fmaf(size, kLow, fmaf(size, kC, -high)) * kLn2, e);
-    const float d = fmaf(e, w, 1.f);
-    float q = __builtin_amdgcn_rcpf(d);
-    if constexpr (FINE) q = fmaf(fmaf(-d, q, 1.f), q, q);
-    return g < 0.f ? Gate{e * q, w, q} : Gate{q, 1.f, e * q};
+    const float x = FINE ? __builtin_amdgcn_fmed3f(g, -200.f, 200.f) : g;     // an infinite argument has no rest
+    const float high = x * kC;
+    float e = __builtin_amdgcn_exp2f(high), low = 0.f;
+    if constexpr (FINE) {
+        low = fmaf(x, kLow, fmaf(x, kC, -high)) * kLn2;
+        e = fmaf(e, low, e);
+    }
+    const float t = __builtin_amdgcn_rcpf(1.f + e);
+    Gate gate{t, 1.f, e * t};
+    if constexpr (FAR) {
+        float p = __builtin_amdgcn_exp2f(116.f - high);
+        if constexpr (FINE) p = fmaf(p, -low, p);
+        if (g < kFar) gate = Gate{p, 0x1p-116f, 1.f};
+    }
+    return gate;
+}
+// f(constant whether FAR) for a lane's gates, of which hardly any is: the wave is asked.
+template <int N, class F>
+__device__ __forceinline__ void for_gates(const float (&g)[N], F&& f)
+{
+    float least = g[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) least = fminf(least, g[i]);
+    if (__builtin_expect(__ballot(least < kFar) != 0, 0)) f(std::true_type{});
+    else f(std::false_type{});
 }
 
 // finish(place, load(place)) for every vector; a lane's loads come before its first store, of which the compiler could not tell that
@@ -247,11 +265,13 @@ __global__ __launch_bounds__(kThreads) void swiglu_kernel(const Args a)
             float g[N], u[N], h[N];
             widen(settled<WHOLE>(in.gate, a, at.col), g);
             widen(settled<WHOLE>(in.up, a, at.col), u);
+            for_gates(g, [&](auto FAR) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const Gate t = sigmoid<sizeof(T) == 4>(g[i]);
-                h[i] = g[i] * t.p * u[i] * t.w;
-            }
+                for (int i = 0; i < N; ++i) {
+                    const Gate t = sigmoid<sizeof(T) == 4, decltype(FAR)::value>(g[i]);
+                    h[i] = g[i] * t.p * u[i] * t.w;
+                }
+            });
             put<WHOLE>(out_row<T>(a.z, at.row), a, at.col, narrow<T>(h));
             if constexpr (PACK) {
                 pack_vector(a, a.a, at, g);
@@ -279,14 +299,16 @@ __global__ __launch_bounds__(kThreads) void swiglu_backward_kernel(const Args a)
             widen(settled<WHOLE>(in.d_out, a, at.col), d);
             unpack_vector(in.gate, g);
             unpack_vector(in.up, u);
+            for_gates(g, [&](auto FAR) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const Gate t = sigmoid<sizeof(T) == 4>(g[i]);
-                const float silu = g[i] * t.p;
-                dg[i] = d[i] * (u[i] * (t.p * fmaf(g[i], t.rest, 1.f))) * t.w;
-                h[i] = silu * u[i] * t.w;
-                d[i] = d[i] * silu * t.w;
-            }
+                for (int i = 0; i < N; ++i) {
+                    const Gate t = sigmoid<sizeof(T) == 4, decltype(FAR)::value>(g[i]);
+                    const float silu = g[i] * t.p;
+                    dg[i] = d[i] * (u[i] * (t.p * fmaf(g[i], t.rest, 1.f))) * t.w;
+                    h[i] = silu * u[i] * t.w;
+                    d[i] = d[i] * silu * t.w;
+                }
+            });
             put<WHOLE>(out_row<T>(a.y, at.row), a, at.col, narrow<T>(dg));
             put<WHOLE>(out_row<T>(a.z, at.row), a, at.col, narrow<T>(d));
             if (a.w.p) put<WHOLE>(out_row<T>(a.w, at.row), a, at.col, narrow<T>(h));

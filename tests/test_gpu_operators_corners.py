@@ -16,8 +16,8 @@ U = O.U32
 
 def gate_off(g, dtype):
     """What t = 1 / (1 + exp(-g)) may be off by, in half steps of fp32 of itself.  The same number for every g in fp32: the exponential's
-    instruction a step (2), its correction 1, then 1 + e one and e's share, the reciprocal after a Newton step 1, their product 1.  For
-    bf16 values the argument |g| log2 e is one rounded number times a rounded constant (2 |g|), and the reciprocal's step (2) stays."""
+    instruction a step (2) and its correction 1, the sum 1, the reciprocal's instruction a step (2); 1 - t has a product more.  For
+    bf16 values the argument g log2 e is one rounded number times a rounded constant: 2 |g| more."""
     return 8.0 if dtype == torch.float32 else 9.0 + 2.0 * g.abs()
 
 
