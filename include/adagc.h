@@ -454,6 +454,8 @@ int adagc_muon_gemm_nt_batched(const void* P, int64_t ldp, const void* Q, int64_
  *   top_logprob  DEVICE fp32[rows][top_k], largest first                     (NULL if top_k = 0)
  *   top_index    DEVICE int32[rows][top_k]; of equal logits the lowest index comes first, NaN before everything else
  *   workspace    DEVICE, adagc_token_logprobs_workspace_bytes of it (0: may be NULL), 16-byte aligned, contents before and after without meaning
+ * Arithmetic is fp32: an exponential is off by about 2 |scale (z_j - M)| * 2^-24 of itself (the small ones by more, which weigh less), L by
+ * (vocab / 256 + 130) * 2^-24 at most.
  * At least one output is wanted.  A row whose logits are all -inf has log-probabilities -inf, entropy 0, M = -inf, L = 0.  A row
  * with a NaN or +inf has NaN log-probabilities and entropy.
  * Errors: INVALID_ARG, TOO_LARGE (also more than 2^24 - 1 rows), HIP.
@@ -467,7 +469,8 @@ int adagc_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int64_
  * Gradient of the logits of adagc_token_logprobs for the gradients of its log-probabilities and entropies:
  *     d_z_j = scale ( d_logprob (1[j = target] - p_j) - d_entropy p_j (logp_j + entropy) ),   p_j = exp(logp_j),
  * without the d_logprob part for rows without a target, p_j (logp_j + entropy) being 0 where p_j = 0 (masked tokens), and 0 for all of a
- * row of -inf.
+ * row of -inf, whatever its d_logprob and d_entropy.  Results are infinite only where the formula's leave the type's range; a p_j is off
+ * by about (5 |logp_j| + 10) * 2^-24 of itself, beside what L is off by.
  *   logits, targets, scale   as the forward call had them
  *   stats, entropy           DEVICE, the forward call's (entropy NULL if d_entropy is)
  *   d_logprob                DEVICE fp32[rows], or NULL for none (then targets may be NULL)

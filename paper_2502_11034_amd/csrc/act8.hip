@@ -2,9 +2,9 @@
 //
 // Blocks of 32 values of a row share a power of two: e is the smallest exponent, at least -100, with largest / 2^e <= 448, the
 // largest e4m3 number, and a code is the e4m3 number nearest to x / 2^e (ties to even).  Nothing saturates (but what would be rounded
-// to 2^128 is held as 1.875 * 2^127), and a value is off by at most 2^-4 of itself down to 2^-15 of the block's largest.  The scale
-// being a power of two, what a code stands for has 4 significant bits and is exact in bf16 and in fp32.  Infinities and NaN are
-// kept as NaN; the block's scale is that of its finite values.
+// to 2^128 is held as 1.875 * 2^127), and a value is off by at most 2^-4 of itself down to 2^-6 * 2^e, which is 2^-13 of the block's largest at
+// most, and by at most 2^-10 * 2^e below.  The scale being a power of two, what a code stands for has 4 significant bits and is exact in
+// bf16 and in fp32.  Infinities and NaN are kept as NaN; the block's scale is that of its finite values.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -221,7 +221,7 @@ __device__ __forceinline__ void each_vector(const Args& a, Load&& load, Finish&&
 
 // Elementwise kernels all: bound by memory on long calls, by a load's and a store's latency on short ones (2 to 3 us).  Lanes take
 // neighbouring 16-byte vectors, so that the 4 (bf16) or 8 (fp32) lanes of a block of 32 are neighbours and find its largest value without LDS.
-// 16384 x 4096 bf16: packed in 41 us (5.0 TB/s), unpacked in 30 (6.7, from the memory-side cache).
+// 16384 x 4096 bf16: packed in 41 us (4.9 TB/s), unpacked in 30 (6.7, from the memory-side cache); fp32 60 (5.6) and 58 (5.8).
 template <class T, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void pack_kernel(const Args a)
 {
@@ -248,7 +248,8 @@ __global__ __launch_bounds__(kThreads) void unpack_kernel(const Args a)
         });
 }
 
-// x: gate, y: up, z: out.  Gate and up are read once for the product and both checkpoints: 8192 x 14336 bf16 169 us (5.6 TB/s).
+// x: gate, y: up, z: out.  Gate and up are read once for the product and both checkpoints: 8192 x 14336 bf16 170 us (5.6 TB/s), without
+// checkpoints 126 (5.6); 8192 x 4096 fp32 89 (5.3) and 72 (5.6).
 template <class T, bool WHOLE, bool PACK>
 __global__ __launch_bounds__(kThreads) void swiglu_kernel(const Args a)
 {
@@ -280,7 +281,7 @@ __global__ __launch_bounds__(kThreads) void swiglu_kernel(const Args a)
         });
 }
 
-// x: d_out, y: d_gate, z: d_up, w: out (or null).  8192 x 14336 bf16 165 us (5.7 TB/s).
+// x: d_out, y: d_gate, z: d_up, w: out (or null).  8192 x 14336 bf16 167 us (5.7 TB/s), with `out` 210 (5.6); 8192 x 4096 fp32 83 (5.7).
 template <class T, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void swiglu_backward_kernel(const Args a)
 {

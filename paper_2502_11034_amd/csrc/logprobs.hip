@@ -305,8 +305,9 @@ constexpr int kAhead = 4;        // 16-byte vectors of a lane in a group
 // One workgroup per part of a row, one pass: each lane keeps a running sum of exponentials (and of z - M times them), lanes and waves are
 // joined at the end.  A row is one part unless there are too few rows to fill the chip.  Bound by memory on long calls, with the vector
 // unit busy two thirds of the time (the exponential is a quarter of its instructions' time and a row's largest value another eighth): 4096 x
-// 128256 bf16 208 us (5.1 TB/s), 1024 x 50257 with top 8 29 us (3.5 TB/s from the memory-side cache; 22 without the list), one row of 128256
-// with top 5 in 31 parts 7 us, of which a load's latency and the list's joining are all but one.
+// 128256 bf16 208 us (5.1 TB/s), 1024 x 50257 with top 8 29 us (3.5 TB/s from the memory-side cache; 22 without the list, 25 with top 1, 36 with
+// top 20, 72 with top 64).  One row of 128256 with top 5 in 31 parts 7 us: the 518 vectors of a part go round three times, each time waiting for
+// their loads, the last time for 6 lanes; then the lists are joined.
 template <class T, bool ENTROPY, bool TOP, bool SPLIT>
 __global__ __launch_bounds__(kThreads) void logprobs_kernel(const ForwardArgs a)
 {
@@ -505,7 +506,7 @@ struct BackwardArgs {
 };
 
 // Gradient of the logits, elementwise: a lane has four vectors loaded before its first store.  Bound by memory: 4096 x 128256 bf16 read and
-// written in 350 us (6.0 TB/s), the vector unit busy for half of that.
+// written in 356 us (5.9 TB/s), the vector unit busy for half of that.
 constexpr float kMaskedLogp = -1e4f;
 constexpr int kBackwardVectors = 4;  // per lane and item
 
