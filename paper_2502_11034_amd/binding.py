@@ -322,11 +322,23 @@ def _size(rc, where):
     return rc
 
 
+def _integers(where, *sizes):
+    """(value, bits) each as an int; ctypes would take one beyond its bits without its upper ones."""
+    out = []
+    for n, bits in sizes:
+        n = int(n)
+        if n >> (bits - 1) not in (0, -1):
+            raise AdagcError(ADAGC_ERR_INVALID_ARG, where)
+        out.append(n)
+    return out
+
+
 # Sizes are functions of the arguments alone and are asked for at every call.
 
 @functools.lru_cache(maxsize=1024)
 def adagc_token_logprobs_workspace_bytes(rows, vocab, top_k=0):
-    return _size(lib().adagc_token_logprobs_workspace_bytes(int(rows), int(vocab), int(top_k)), "adagc_token_logprobs_workspace_bytes")
+    where = "adagc_token_logprobs_workspace_bytes"
+    return _size(lib().adagc_token_logprobs_workspace_bytes(*_integers(where, (rows, 64), (vocab, 64), (top_k, 32))), where)
 
 
 def adagc_token_logprobs(logits, targets=None, logprob=None, entropy=None, stats=None, top_logprob=None, top_index=None, scale=1.0,
@@ -371,7 +383,7 @@ def adagc_token_logprobs_backward(logits, targets, stats, entropy, d_logprob, d_
 @functools.lru_cache(maxsize=1024)
 def adagc_act8_bytes(rows, cols):
     """Bytes of a checkpoint of a rows x cols matrix."""
-    return _size(lib().adagc_act8_bytes(int(rows), int(cols)), "adagc_act8_bytes")
+    return _size(lib().adagc_act8_bytes(*_integers("adagc_act8_bytes", (rows, 64), (cols, 64))), "adagc_act8_bytes")
 
 
 def adagc_act8_pack(x, ckpt, stream=None):
@@ -429,7 +441,8 @@ def adagc_swiglu_backward(d_out, gate_ckpt, up_ckpt, d_gate, d_up, out=None, str
 
 @functools.lru_cache(maxsize=1024)
 def adagc_act8_wgrad_workspace_bytes(rows, n_out, n_in, dtype):
-    return _size(lib().adagc_act8_wgrad_workspace_bytes(int(rows), int(n_out), int(n_in), int(dtype)), "adagc_act8_wgrad_workspace_bytes")
+    where = "adagc_act8_wgrad_workspace_bytes"
+    return _size(lib().adagc_act8_wgrad_workspace_bytes(*_integers(where, (rows, 64), (n_out, 64), (n_in, 64), (dtype, 32))), where)
 
 
 def adagc_act8_wgrad(d_out, ckpt, d_weight, accumulate=False, workspace=None, stream=None):
