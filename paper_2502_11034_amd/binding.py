@@ -8,6 +8,7 @@ PyTorch is used by callers for device memory and streams; this module only reads
 import ctypes
 import functools
 import os
+import sys
 
 import numpy as np
 
@@ -34,6 +35,9 @@ EXPORTS = [
     "adagc_muon_workspace_bytes", "adagc_muon_step",
     "adagc_token_logprobs_workspace_bytes", "adagc_token_logprobs", "adagc_token_logprobs_backward", "adagc_act8_bytes", "adagc_act8_pack",
     "adagc_act8_unpack", "adagc_swiglu", "adagc_swiglu_backward", "adagc_act8_wgrad_workspace_bytes", "adagc_act8_wgrad",
+    "adagc_linear_logprobs_workspace_bytes", "adagc_linear_logprobs", "adagc_linear_logprobs_backward_workspace_bytes",
+    "adagc_linear_logprobs_backward", "adagc_gated_linear_workspace_bytes", "adagc_gated_linear", "adagc_gated_linear_backward_workspace_bytes",
+    "adagc_gated_linear_backward", "adagc_dropout",
     "adagc_strerror",
 ]
 
@@ -158,6 +162,25 @@ def lib():
     L.adagc_act8_wgrad_workspace_bytes.argtypes = [i64, i64, i64, i32]
     L.adagc_act8_wgrad.restype = ctypes.c_int
     L.adagc_act8_wgrad.argtypes = [vp, i32, i64, vp, i64, i64, i64, vp, i32, i64, i32, vp, i64, vp]
+    L.adagc_linear_logprobs_workspace_bytes.restype = i64
+    L.adagc_linear_logprobs_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    L.adagc_linear_logprobs.restype = ctypes.c_int
+    L.adagc_linear_logprobs.argtypes = [vp, i64, vp, i64, i32, i64, i64, i64, vp, f32, vp, vp, vp, i64, vp]
+    L.adagc_linear_logprobs_backward_workspace_bytes.restype = i64
+    L.adagc_linear_logprobs_backward_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    L.adagc_linear_logprobs_backward.restype = ctypes.c_int
+    L.adagc_linear_logprobs_backward.argtypes = [vp, i64, vp, i64, i32, i64, i64, i64, vp, f32, vp, vp, vp, i64, vp, i32, i64, i32, vp, i64, vp]
+    L.adagc_gated_linear_workspace_bytes.restype = i64
+    L.adagc_gated_linear_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    L.adagc_gated_linear.restype = ctypes.c_int
+    L.adagc_gated_linear.argtypes = [vp, i64, vp, i64, vp, i64, i32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    L.adagc_gated_linear_backward_workspace_bytes.restype = i64
+    L.adagc_gated_linear_backward_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    L.adagc_gated_linear_backward.restype = ctypes.c_int
+    L.adagc_gated_linear_backward.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64,
+                                              i32, i32, vp, i64, vp, i64, vp]
+    L.adagc_dropout.restype = ctypes.c_int
+    L.adagc_dropout.argtypes = [vp, i64, vp, i64, i32, i64, i64, ctypes.c_double, vp, vp, i64, vp]
     L.adagc_strerror.restype = ctypes.c_char_p
     L.adagc_strerror.argtypes = [ctypes.c_int]
     _lib = L
@@ -459,6 +482,159 @@ def adagc_act8_wgrad(d_out, ckpt, d_weight, accumulate=False, workspace=None, st
     if rc:
         raise AdagcError(rc, "adagc_act8_wgrad")
 
+
+def _one_device(where, *tensors):
+    """A kernel that is given host memory, or runs on another device than its data's, would fault the GPU."""
+    device = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise AdagcError(ADAGC_ERR_INVALID_ARG, where + " (a tensor is not in device memory)")
+        if device is None:
+            device = sys.modules["torch"].cuda.current_device()
+        if t.get_device() != device:
+            raise AdagcError(ADAGC_ERR_INVALID_ARG, where + " (a tensor is not in the current device's memory)")
+
+
+@functools.lru_cache(maxsize=1024)
+def adagc_linear_logprobs_workspace_bytes(rows, vocab, dim, dtype):
+    where = "adagc_linear_logprobs_workspace_bytes"
+    return _size(lib().adagc_linear_logprobs_workspace_bytes(*_integers(where, (rows, 64), (vocab, 64), (dim, 64), (dtype, 32))), where)
+
+
+@functools.lru_cache(maxsize=1024)
+def adagc_linear_logprobs_backward_workspace_bytes(rows, vocab, dim, dtype):
+    where = "adagc_linear_logprobs_backward_workspace_bytes"
+    return _size(lib().adagc_linear_logprobs_backward_workspace_bytes(*_integers(where, (rows, 64), (vocab, 64), (dim, 64), (dtype, 32))), where)
+
+
+def adagc_linear_logprobs(x, weight, targets=None, logprob=None, stats=None, scale=1.0, workspace=None, stream=None):
+    """Log-probabilities of targets (int64 [rows]) for the logits x weight^T, x [rows, dim], weight [vocab, dim], without the logits; the
+    outputs that are given are written.  stats: fp32 [rows, 2]; workspace: adagc_linear_logprobs_workspace_bytes(rows, vocab, dim, dtype) bytes."""
+    p, dtype, ld, (rows, dim) = _matrix(x, "x")
+    w, _, ld_w, (vocab, w_dim) = _matrix(weight, "weight", None, dtype)
+    if w_dim != dim:
+        raise ValueError("weight: %d columns, expected %d" % (w_dim, dim))
+    ws, ws_bytes = _bytes(workspace, adagc_linear_logprobs_workspace_bytes(rows, vocab, dim, dtype) if rows else 0, "workspace")
+    t = _dense(targets, (rows,), "torch.int64", "targets")
+    lp = _dense(logprob, (rows,), "torch.float32", "logprob")
+    st = _dense(stats, (rows, 2), "torch.float32", "stats")
+    _one_device("adagc_linear_logprobs", x, weight, targets, logprob, stats, workspace)
+    rc = lib().adagc_linear_logprobs(p, ld, w, ld_w, dtype, rows, vocab, dim, t, scale, lp, st, ws, ws_bytes, stream)
+    if rc:
+        raise AdagcError(rc, "adagc_linear_logprobs")
+
+
+def adagc_linear_logprobs_backward(x, weight, targets, stats, d_logprob, d_x=None, d_weight=None, scale=1.0, accumulate=False, workspace=None,
+                                   stream=None):
+    """Writes d_x [rows, dim] and (adds to, with accumulate) d_weight [vocab, dim], fp32 or bf16, for d_logprob fp32 [rows]; workspace:
+    adagc_linear_logprobs_backward_workspace_bytes(rows, vocab, dim, dtype) bytes."""
+    p, dtype, ld, shape = _matrix(x, "x")
+    rows, dim = shape
+    w, _, ld_w, w_shape = _matrix(weight, "weight", None, dtype)
+    vocab, w_dim = w_shape
+    if w_dim != dim:
+        raise ValueError("weight: %d columns, expected %d" % (w_dim, dim))
+    dx, ld_dx, dw, weight_dtype, ld_dw = None, 0, None, 0, 0
+    if d_x is not None:
+        dx, _, ld_dx, _ = _matrix(d_x, "d_x", shape, dtype)
+    if d_weight is not None:
+        dw, weight_dtype, ld_dw, _ = _matrix(d_weight, "d_weight", w_shape)
+    ws, ws_bytes = _bytes(workspace, adagc_linear_logprobs_backward_workspace_bytes(rows, vocab, dim, dtype), "workspace")
+    t = _dense(targets, (rows,), "torch.int64", "targets")
+    st = _dense(stats, (rows, 2), "torch.float32", "stats")
+    dl = _dense(d_logprob, (rows,), "torch.float32", "d_logprob")
+    _one_device("adagc_linear_logprobs_backward", x, weight, targets, stats, d_logprob, d_x, d_weight, workspace)
+    rc = lib().adagc_linear_logprobs_backward(p, ld, w, ld_w, dtype, rows, vocab, dim, t, scale, st, dl, dx, ld_dx, dw, weight_dtype, ld_dw,
+                                              1 if accumulate else 0, ws, ws_bytes, stream)
+    if rc:
+        raise AdagcError(rc, "adagc_linear_logprobs_backward")
+
+
+@functools.lru_cache(maxsize=1024)
+def adagc_gated_linear_workspace_bytes(rows, dim, hidden, dtype):
+    where = "adagc_gated_linear_workspace_bytes"
+    return _size(lib().adagc_gated_linear_workspace_bytes(*_integers(where, (rows, 64), (dim, 64), (hidden, 64), (dtype, 32))), where)
+
+
+@functools.lru_cache(maxsize=1024)
+def adagc_gated_linear_backward_workspace_bytes(rows, dim, hidden, dtype):
+    where = "adagc_gated_linear_backward_workspace_bytes"
+    return _size(lib().adagc_gated_linear_backward_workspace_bytes(*_integers(where, (rows, 64), (dim, 64), (hidden, 64), (dtype, 32))), where)
+
+
+def adagc_gated_linear(x, w_gate, w_up, out, gate=None, up=None, workspace=None, stream=None):
+    """out [rows, hidden] = silu(x w_gate^T) (x w_up^T) for x [rows, dim], weights [hidden, dim]; both products are left in gate and up, if given.
+    workspace: adagc_gated_linear_workspace_bytes(rows, dim, hidden, dtype) bytes."""
+    p, dtype, ld, (rows, dim) = _matrix(x, "x")
+    wg, _, ld_wg, w_shape = _matrix(w_gate, "w_gate", None, dtype)
+    hidden, w_dim = w_shape
+    if w_dim != dim:
+        raise ValueError("w_gate: %d columns, expected %d" % (w_dim, dim))
+    wu, _, ld_wu, _ = _matrix(w_up, "w_up", w_shape, dtype)
+    shape = (rows, hidden)
+    o, _, ld_o, _ = _matrix(out, "out", shape, dtype)
+    g, ld_g, u, ld_u = None, 0, None, 0
+    if gate is not None:
+        g, _, ld_g, _ = _matrix(gate, "gate", shape, dtype)
+    if up is not None:
+        u, _, ld_u, _ = _matrix(up, "up", shape, dtype)
+    ws, ws_bytes = _bytes(workspace, adagc_gated_linear_workspace_bytes(rows, dim, hidden, dtype), "workspace")
+    _one_device("adagc_gated_linear", x, w_gate, w_up, out, gate, up, workspace)
+    rc = lib().adagc_gated_linear(p, ld, wg, ld_wg, wu, ld_wu, dtype, rows, dim, hidden, o, ld_o, g, ld_g, u, ld_u, ws, ws_bytes, stream)
+    if rc:
+        raise AdagcError(rc, "adagc_gated_linear")
+
+
+def adagc_gated_linear_backward(d_out, x, w_gate, w_up, d_x=None, d_w_gate=None, d_w_up=None, gate=None, up=None, out=None, accumulate=False,
+                                workspace=None, stream=None):
+    """Writes d_x [rows, dim], (adds to, with accumulate) d_w_gate and d_w_up [hidden, dim], fp32 or bf16, and, if given, out again, for d_out
+    [rows, hidden]; gate and up: as the forward call left them, or None: both products are made again.  workspace:
+    adagc_gated_linear_backward_workspace_bytes(rows, dim, hidden, dtype) bytes."""
+    p, dtype, ld, x_shape = _matrix(x, "x")
+    rows, dim = x_shape
+    wg, _, ld_wg, w_shape = _matrix(w_gate, "w_gate", None, dtype)
+    hidden, w_dim = w_shape
+    if w_dim != dim:
+        raise ValueError("w_gate: %d columns, expected %d" % (w_dim, dim))
+    wu, _, ld_wu, _ = _matrix(w_up, "w_up", w_shape, dtype)
+    shape = (rows, hidden)
+    d, _, ld_d, _ = _matrix(d_out, "d_out", shape, dtype)
+    g, ld_g, u, ld_u, o, ld_o, dx, ld_dx = None, 0, None, 0, None, 0, None, 0
+    dwg, weight_dtype, ld_dwg, dwu, ld_dwu = None, 0, 0, None, 0
+    if gate is not None:
+        g, _, ld_g, _ = _matrix(gate, "gate", shape, dtype)
+    if up is not None:
+        u, _, ld_u, _ = _matrix(up, "up", shape, dtype)
+    if out is not None:
+        o, _, ld_o, _ = _matrix(out, "out", shape, dtype)
+    if d_x is not None:
+        dx, _, ld_dx, _ = _matrix(d_x, "d_x", x_shape, dtype)
+    if d_w_gate is not None:
+        dwg, weight_dtype, ld_dwg, _ = _matrix(d_w_gate, "d_w_gate", w_shape)
+    if d_w_up is not None:
+        dwu, _, ld_dwu, _ = _matrix(d_w_up, "d_w_up", w_shape, weight_dtype if d_w_gate is not None else None)
+    ws, ws_bytes = _bytes(workspace, adagc_gated_linear_backward_workspace_bytes(rows, dim, hidden, dtype), "workspace")
+    _one_device("adagc_gated_linear_backward", d_out, x, w_gate, w_up, d_x, d_w_gate, d_w_up, gate, up, out, workspace)
+    rc = lib().adagc_gated_linear_backward(d, ld_d, p, ld, wg, ld_wg, wu, ld_wu, dtype, rows, dim, hidden, g, ld_g, u, ld_u, dx, ld_dx, dwg, ld_dwg,
+                                           dwu, ld_dwu, weight_dtype, 1 if accumulate else 0, o, ld_o, ws, ws_bytes, stream)
+    if rc:
+        raise AdagcError(rc, "adagc_gated_linear_backward")
+
+
+def adagc_dropout(x, out, rng, p, residual=None, stream=None):
+    """out = (residual +) x / (1 - p) where a value is kept, all [rows, cols] of one type; rng: int64 [2] on the device, seed and offset."""
+    a, dtype, ld, shape = _matrix(x, "x")
+    o, _, ld_o, _ = _matrix(out, "out", shape, dtype)
+    r, ld_r = None, 0
+    if residual is not None:
+        r, _, ld_r, _ = _matrix(residual, "residual", shape, dtype)
+    state = _dense(rng, (2,), "torch.int64", "rng")
+    _one_device("adagc_dropout", x, out, rng, residual)
+    rc = lib().adagc_dropout(a, ld, r, ld_r, dtype, shape[0], shape[1], p, state, o, ld_o, stream)
+    if rc:
+        raise AdagcError(rc, "adagc_dropout")
 
 ADAGC_STATIC_MAX_TENSORS = 32768
 ADAGC_STATIC_MAX_CHUNKS = 524288

@@ -7,10 +7,11 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libadagc.so")
 SOURCES = ["api.cpp", "segment_table.cpp", "kernels.hip", "static_step.hip", "muon_gemm.hip", "muon.hip", "muon_plan.cpp",
-           "logprobs.hip", "act8.hip", "act8_wgrad.hip"]
+           "logprobs.hip", "act8.hip", "act8_wgrad.hip", "product.hip", "linear_logprobs.hip", "gated_linear.hip",
+           "dropout.hip"]
 HEADERS = [os.path.join(ROOT, "include", "adagc.h"), os.path.join(CSRC, "adagc_internal.h"), os.path.join(CSRC, "adagc_device.h"), os.path.join(CSRC, "muon_internal.h"),
            os.path.join(CSRC, "muon_plan.h"), os.path.join(CSRC, "walk_lines.h"), os.path.join(CSRC, "operators_internal.h"),
-           os.path.join(CSRC, "act8_device.h")]
+           os.path.join(CSRC, "act8_device.h"), os.path.join(CSRC, "product_device.h")]
 
 
 def hipcc():

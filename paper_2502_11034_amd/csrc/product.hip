@@ -1,0 +1,11 @@
+// The products with a plain result of the operators' backward passes, both types, Y along and across k (product_device.h).
+#include "product_device.h"
+
+namespace adagc {
+namespace product {
+template int run_plain<float, false>(PlainArgs, hipStream_t);
+template int run_plain<float, true>(PlainArgs, hipStream_t);
+template int run_plain<uint16_t, false>(PlainArgs, hipStream_t);
+template int run_plain<uint16_t, true>(PlainArgs, hipStream_t);
+}  // namespace product
+}  // namespace adagc

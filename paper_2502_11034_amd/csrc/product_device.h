@@ -1,0 +1,813 @@
+// The tile loop of the matrix products behind the operators that make their intermediate results again instead of keeping them
+// (linear_logprobs.hip, gated_linear.hip), and a product with a plain result.
+//
+// A block tile's sums  acc[row][col] += sum_k Y[row][k] X[col][k]  on the matrix cores, fp32 accumulation.  Each operand lies in memory
+// either with k consecutive ("along": rows of k) or with k as the slow index ("across": k rows of consecutive rows or columns of the
+// result).  bf16 products are exact in fp32, fp32 ones are rounded by the matrix cores' fp32 instruction.
+#ifndef ADAGC_PRODUCT_DEVICE_H
+#define ADAGC_PRODUCT_DEVICE_H
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <type_traits>
+#include <utility>
+
+#include "operators_internal.h"
+
+namespace adagc {
+
+typedef __bf16 bf16x8_p __attribute__((ext_vector_type(8)));
+typedef float f32x4_p __attribute__((ext_vector_type(4)));
+typedef short s16x4_p __attribute__((ext_vector_type(4)));
+
+namespace product {
+
+#define ADAGC_P_LDS __attribute__((address_space(3)))
+// s_waitcnt for "at most n vector-memory operations of this wave still outstanding", nothing else waited for
+#define ADAGC_P_WAIT_VMEM(n) __builtin_amdgcn_s_waitcnt(((n) & 0xF) | (((n) >> 4) << 14) | (7 << 4) | (0xF << 8))
+// s_waitcnt for "at most n LDS accesses of this wave still outstanding", nothing else waited for
+#define ADAGC_P_WAIT_LDS(n) __builtin_amdgcn_s_waitcnt(0xF | (3 << 14) | (7 << 4) | ((n) << 8))
+// nothing is moved across this point by the compiler's instruction scheduler
+#define ADAGC_P_FENCE() __builtin_amdgcn_sched_barrier(0)
+
+// f(integral_constant 0), ..., f(integral_constant N-1)
+template <class F, int... I>
+__device__ __forceinline__ void each_impl(F&& f, std::integer_sequence<int, I...>)
+{
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void each(F&& f)
+{
+    each_impl(f, std::make_integer_sequence<int, N>{});
+}
+
+// Compute units: a round of a launch is as many workgroups of the large tile.
+constexpr int kUnits = 256;
+constexpr int kPlaces = 3;                 // of LDS, that steps staged through registers go round in
+constexpr int kRing = 5;                   // of LDS, that steps loaded straight into it go round in
+constexpr int kStepBytes = 64;             // of k, a step
+
+// BM x BN tile (BM rows of Y), kWM x kWN waves of kTM x kTN blocks of 16 x 16.  A step is 64 bytes of k: 32 bf16 or 16 fp32 numbers, so that
+// an operand's tile has the same bytes and a lane's fragment the same 16 with both types.  DIRECT: operands go from global memory straight into
+// LDS, which wants rows at multiples of 16 bytes; otherwise through registers, rows at any element.
+template <class T, int BM_, int BN_, int kWM_, int kWN_, bool DIRECT_>
+struct Tile {
+    static constexpr int BM = BM_, BN = BN_, kWM = kWM_, kWN = kWN_;
+    static constexpr int kThreads = 64 * kWM * kWN;
+    static constexpr int kTM = BM / kWM / 16, kTN = BN / kWN / 16;
+    static constexpr int kDeep = kStepBytes / (int)sizeof(T);
+    static constexpr int kY = BM * kStepBytes, kX = BN * kStepBytes, kPlace = kY + kX;      // bytes
+    static constexpr int kYUnits = kY / 16 / kThreads, kXUnits = kX / 16 / kThreads;       // of 16 bytes, a lane's
+    static constexpr int kLoads = kYUnits + kXUnits;
+    static constexpr bool kDirect = DIRECT_;
+    static constexpr int kLds = (DIRECT_ ? kRing : kPlaces) * kPlace;
+    static_assert(kY % (16 * kThreads) == 0 && kX % (16 * kThreads) == 0, "operand tiles are dealt evenly");
+};
+
+// 16 bytes per lane from global memory straight into LDS: lane i's, at base + off_i bytes (base: the same in all lanes), land at
+// lds_at + 16 i (the same in all lanes).  The instruction takes the LDS address from M0 and wants a wait state after M0 is written; M0 is put
+// back afterwards.  Inline assembly rather than the compiler's builtin so that the compiler does not track these loads: it would turn every wait
+// for an LDS read into a wait for all of them.  The waits for these loads are explicit (ADAGC_P_WAIT_VMEM) wherever their data is needed.
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t off, uint32_t lds_at)
+{
+    uint32_t saved_m0;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+                 : "=&s"(saved_m0)
+                 : "s"(lds_at), "v"(off), "s"(base)
+                 : "memory");
+}
+
+// A value that is the same in all lanes, in scalar registers.
+__device__ __forceinline__ int64_t scalar(int64_t v)
+{
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+template <class T>
+__device__ __forceinline__ const T* scalar(const T* p)
+{
+    return reinterpret_cast<const T*>(scalar((int64_t)reinterpret_cast<uintptr_t>(p)));
+}
+
+// Number n of a launch of tiles_m x tiles_n: 8 XCDs, each with its own L2, get workgroups in turn; the 32 that one of them has in a round are
+// neighbours, in bands of 8 tiles along m.
+__device__ __forceinline__ void place_of_tile(int n, int tiles_m, int tiles_n, int* tm, int* tn)
+{
+    const int all = tiles_m * tiles_n, round = n / kUnits * kUnits, in_round = min(all - round, kUnits);
+    int at = n - round;
+    if (in_round == kUnits) at = at % 8 * (kUnits / 8) + at / 8;
+    at += round;
+    const int band = at / (8 * tiles_n), in_band = at - band * 8 * tiles_n;
+    const int high = min(8, tiles_m - 8 * band);
+    *tn = __builtin_amdgcn_readfirstlane(in_band / high);          // the same in all lanes: kept in scalar registers
+    *tm = __builtin_amdgcn_readfirstlane(8 * band + in_band - *tn * high);
+}
+
+// How one operand's tile (B rows or columns of the result) is loaded, staged in LDS and read: kUnits units of 16 bytes for a lane.
+//
+// Along: LDS rows of 64 bytes, one for a row of the result; the 16-byte vector v of row r is at position v ^ ((r / 4) mod 4), so that the 16
+// rows that 16 lanes read one vector of lie in different banks.
+// Across, bf16: LDS rows of B numbers, one for each k; 16 lanes read 4 rows of 16 columns and get a column each (ds_read_b64_tr_b16); the
+// 32-byte units of a row are permuted so that the eight that half a wave takes (rows 0 .. 3 and 8 .. 11) lie in different banks.
+// Across, fp32: the same with 64-byte units, read number by number.
+template <class T, int B, int kThreads, int kUnits, int kBlocks, bool ACROSS>
+struct Side {
+    static constexpr int kE = 16 / (int)sizeof(T);                 // numbers in a vector
+    static constexpr int kDeep = kStepBytes / (int)sizeof(T);
+    static constexpr int kVectors = ACROSS ? B / kE : 4;            // of a row in LDS
+    static constexpr int kPitch = kVectors * 16;                    // bytes
+    static constexpr bool kHalf = sizeof(T) == 2;
+
+    const T* row[ACROSS ? 1 : kUnits];     // along: a unit's address at k = 0, less its vector
+    uint32_t lane_at;                      // across: bytes from the step's address, unit 0
+    uint32_t off[kUnits];                  // straight into LDS: bytes from the step's address, which is the same in all lanes
+    int64_t  ld;
+    uint32_t write_at, read_at;
+
+    static __device__ __forceinline__ int row_of(int tid, int u) { return (tid + u * kThreads) / kVectors; }
+    static __device__ __forceinline__ int vector_of(int tid, int u) { return (tid + u * kThreads) % kVectors; }
+    static __device__ __forceinline__ uint32_t place(int r, int v)
+    {
+        if constexpr (!ACROSS) return (uint32_t)(r * kPitch + (v ^ ((r >> 2) & 3)) * 16);
+        else if constexpr (kHalf) return (uint32_t)(r * kPitch + ((v >> 1) ^ ((r & 3) | ((r >> 3) & 1) << 2)) * 32 + (v & 1) * 16);
+        else return (uint32_t)(r * kPitch + ((v >> 2) ^ ((r >> 2) & 3)) * 64 + (v & 3) * 16);
+    }
+    // lds0: the tile's first byte in a place, wave_block: the wave's first block
+    __device__ __forceinline__ void set_places(int tid, uint32_t lds0, int wave_block)
+    {
+        write_at = lds0 + place(row_of(tid, 0), vector_of(tid, 0));
+        const int l = tid & 63;
+        if constexpr (!ACROSS) {
+            read_at = lds0 + place(l & 15, l >> 4) + (uint32_t)(wave_block * 16 * kPitch);
+        } else if constexpr (kHalf) {
+            const int r = 8 * (l >> 4) + ((l >> 2) & 3);
+            read_at = lds0 + (uint32_t)(r * kPitch + (wave_block ^ ((r & 3) | ((r >> 3) & 1) << 2)) * 32 + (l & 3) * 8);
+        } else {
+            const int r = 4 * (l >> 4);
+            read_at = lds0 + (uint32_t)(r * kPitch + (wave_block ^ ((r >> 2) & 3)) * 64 + (l & 15) * 4);
+        }
+    }
+    // along: row_at(r): the address of row r of the tile (rows beyond the matrix: any of its rows)
+    template <class F>
+    __device__ __forceinline__ void set_rows(int tid, F&& row_at)
+    {
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) row[u] = row_at(row_of(tid, u)) + vector_of(tid, u) * kE;
+    }
+    // across: k rows from `at` on, B whole columns of them inside the matrix, kDeep * ld_ numbers within 32 bits of bytes
+    __device__ __forceinline__ void set_columns(int tid, const T* at, int64_t ld_)
+    {
+        row[0] = at;
+        ld = ld_;
+        lane_at = (uint32_t)(row_of(tid, 0) * (uint32_t)ld_ + (uint32_t)vector_of(tid, 0) * kE) * (uint32_t)sizeof(T);
+    }
+    __device__ __forceinline__ u32x4 load(int64_t step, int u) const
+    {
+        if constexpr (!ACROSS) {
+            return load_whole(row[u] + step * kDeep).w;
+        } else {
+            const uint8_t* at = reinterpret_cast<const uint8_t*>(row[0] + (step * kDeep + u * (kThreads / kVectors)) * ld);
+            return load_whole(reinterpret_cast<const T*>(at + lane_at)).w;
+        }
+    }
+    // the same where k or (across) the columns may end inside: zeros there
+    __device__ __forceinline__ u32x4 load_checked(int tid, int64_t step, int u, int64_t k, int64_t columns) const
+    {
+        if constexpr (!ACROSS) {
+            const int v = vector_of(tid, u);
+            return load_vector(row[u] - v * kE, step * kDeep + v * kE, k, 0).w;
+        } else {
+            const int64_t t = step * kDeep + row_of(tid, u);
+            return load_vector(row[0] + t * ld, vector_of(tid, u) * kE, t < k ? columns : 0, 0).w;
+        }
+    }
+    // Straight into LDS: position i of row r gets vector unplaced(r, i), so that vector v is where place(r, v) says.
+    static __device__ __forceinline__ int unplaced(int r, int i) { return (int)(place(r, i) % (uint32_t)kPitch) / 16; }      // its own inverse
+    // along: rows of one matrix within 32 bits of bytes from `at`; number_of(r): the number of row r of the tile, from `at` (a row inside the matrix)
+    template <class F>
+    __device__ __forceinline__ void set_rows_direct(int tid, const T* at, int64_t ld_, F&& number_of)
+    {
+        row[0] = scalar(at);
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const int r = row_of(tid, u);
+            off[u] = ((uint32_t)number_of(r) * (uint32_t)ld_ + (uint32_t)unplaced(r, vector_of(tid, u)) * kE) * (uint32_t)sizeof(T);
+        }
+    }
+    __device__ __forceinline__ void set_columns_direct(int tid, const T* at, int64_t ld_)
+    {
+        row[0] = scalar(at);
+        ld = scalar(ld_);
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const int r = row_of(tid, u);
+            off[u] = ((uint32_t)r * (uint32_t)ld_ + (uint32_t)unplaced(r, vector_of(tid, u)) * kE) * (uint32_t)sizeof(T);
+        }
+    }
+    __device__ __forceinline__ void load_direct(int step, int u, uint32_t lds_at) const
+    {
+        load_to_lds(row[0] + (ACROSS ? (int64_t)(step * kDeep) * ld : step * kDeep), off[u], lds_at + (uint32_t)(u * kThreads * 16));
+    }
+    __device__ __forceinline__ void write(int u, uint32_t place, const u32x4& w) const
+    {
+        // a unit's rows are kRows below the last one's: at the same place of the permutation but for fp32 across, where 8 rows flip a bit of it
+        constexpr int kRows = kThreads / kVectors;
+        static_assert(kRows % 16 == 0 || (ACROSS && !kHalf && kRows == 8 && kUnits <= 2), "the permutation of a unit's rows");
+        const uint32_t at = kRows % 16 && u ? write_at ^ 128u : write_at;
+        *reinterpret_cast<ADAGC_P_LDS u32x4*>(at + place + (uint32_t)(u * kRows * kPitch)) = w;
+    }
+    __device__ __forceinline__ u32x4 read(int block, uint32_t place) const
+    {
+        if constexpr (!ACROSS) {
+            return *reinterpret_cast<const ADAGC_P_LDS u32x4*>(read_at + place + (uint32_t)(block * 16 * kPitch));
+        } else if constexpr (kHalf) {
+            static_assert((kBlocks & (kBlocks - 1)) == 0, "blocks are exclusive-ored into an address");
+            const uint32_t at = (read_at ^ (uint32_t)(block * 32)) + place;
+            const s16x4_p a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ADAGC_P_LDS s16x4_p*>(at));
+            const s16x4_p b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ADAGC_P_LDS s16x4_p*>(at + 4 * kPitch));
+            return __builtin_bit_cast(u32x4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            const uint32_t at = (read_at ^ (uint32_t)(block * 64)) + place;
+            u32x4 w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = *reinterpret_cast<const ADAGC_P_LDS uint32_t*>(at + (uint32_t)(j * kPitch));
+            return w;
+        }
+    }
+};
+
+// sum += x y^T of one block: lane l gets columns 4 (l / 16) .. + 3 of row l mod 16.
+template <class T>
+__device__ __forceinline__ void multiply(const u32x4& x, const u32x4& y, f32x4_p& sum)
+{
+    if constexpr (sizeof(T) == 2) {
+        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_p, x), __builtin_bit_cast(bf16x8_p, y), sum, 0, 0, 0);
+    } else {
+        // four k of every four: both operands give the same ones
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x[j]), __uint_as_float(y[j]), sum, 0, 0, 0);
+    }
+}
+
+template <class S>
+using Sums = f32x4_p[S::kTM][S::kTN];
+
+template <class S>
+__device__ __forceinline__ void clear(Sums<S>& acc)
+{
+#pragma unroll
+    for (int m = 0; m < S::kTM; ++m)
+#pragma unroll
+        for (int n = 0; n < S::kTN; ++n) acc[m][n] = f32x4_p{0.f, 0.f, 0.f, 0.f};
+}
+
+// Steps step0 .. step1 - 1 of k, and with `rest` the numbers after the last whole step (number `full`).  CHECKED: every load looks where the
+// operands end.
+//
+// Main loop.  A step's operands are staged in a place of LDS; while step i is multiplied from registers, step i + 1 is read to registers
+// from its place (each fragment of Y as soon as its multiplications are issued, those of X to a second set), step i + 2 goes from the
+// registers it was loaded to into its place, and those take step i + 4.  One barrier a step: what it orders is the writes of i + 2
+// before their reads in the next step; the reads of a place are done a step before it is written again.  Loads past the last step take
+// the last one again: a loop without conditions lets the compiler count what is outstanding.  All waves leave with LDS free to use.
+template <class S, class T, bool CHECKED, class SideY, class SideX>
+__device__ __forceinline__ void accumulate(Sums<S>& acc, const SideY& sy, const SideX& sx, int64_t step0, int64_t step1, bool rest, int64_t full,
+                                           int64_t k, int64_t columns_y, int64_t columns_x)
+{
+    constexpr int kTM = S::kTM, kTN = S::kTN, kYU = S::kYUnits, kXU = S::kXUnits;
+    const int tid = threadIdx.x;
+    struct Staged {
+        u32x4 y[kYU], x[kXU];
+    };
+    auto load = [&](int64_t step, Staged& s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < kYU; ++u) s.y[u] = sy.load(step, u);
+#pragma unroll
+        for (int u = 0; u < kXU; ++u) s.x[u] = sx.load(step, u);
+    };
+    auto load_checked = [&](int64_t step, Staged& s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < kYU; ++u) s.y[u] = sy.load_checked(tid, step, u, k, columns_y);
+#pragma unroll
+        for (int u = 0; u < kXU; ++u) s.x[u] = sx.load_checked(tid, step, u, k, columns_x);
+    };
+    auto write = [&](const Staged& s, uint32_t place) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < kYU; ++u) sy.write(u, place, s.y[u]);
+#pragma unroll
+        for (int u = 0; u < kXU; ++u) sx.write(u, place, s.x[u]);
+    };
+    u32x4 y[kTM], x[2][kTN];
+    auto plain_step = [&](const Staged& s, uint32_t place, auto&& meanwhile) __attribute__((always_inline)) {
+        write(s, place);
+        meanwhile();
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < kTN; ++n) x[0][n] = sx.read(n, place);
+#pragma unroll
+        for (int m = 0; m < kTM; ++m) {
+            y[0] = sy.read(m, place);
+#pragma unroll
+            for (int n = 0; n < kTN; ++n) multiply<T>(x[0][n], y[0], acc[m][n]);
+        }
+    };
+    constexpr uint32_t kRestPlace = (kPlaces - 1) * S::kPlace;
+
+    if constexpr (CHECKED) {
+        // two steps' loads are on their way; a step's writes and the reads of the step before take different places
+        const int64_t end = step1 + rest;
+        Staged staged[2];
+        if (step0 < end) load_checked(step0, staged[0]);
+        if (step0 + 1 < end) load_checked(step0 + 1, staged[1]);
+        for (int64_t step = step0; step < end; step += 2)
+            each<2>([&](auto P) __attribute__((always_inline)) {
+                constexpr int p = decltype(P)::value;
+                if (step + p >= end) return;
+                plain_step(staged[p], p * S::kPlace, [&] {
+                    if (step + p + 2 < end) load_checked(step + p + 2, staged[p]);
+                });
+            });
+    } else if (S::kDirect || step0 == step1) {
+        if (rest) {
+            Staged s;
+            load_checked(full, s);
+            plain_step(s, kRestPlace, [] {});
+        }
+    } else {
+        // what is left over comes first (with the main loop's first loads on their way at the same time registers would be short)
+        Staged staged[2];
+        auto clamp = [&](int64_t step) { return min(step, step1 - 1); };
+        if (rest) {
+            load_checked(full, staged[0]);
+            plain_step(staged[0], kRestPlace, [] {});
+            ADAGC_P_FENCE();
+        }
+        load(step0, staged[0]);
+        load(clamp(step0 + 1), staged[1]);
+        write(staged[0], 0);
+        load(clamp(step0 + 2), staged[0]);
+        write(staged[1], S::kPlace);
+        load(clamp(step0 + 3), staged[1]);
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < kTN; ++n) x[0][n] = sx.read(n, 0);
+#pragma unroll
+        for (int m = 0; m < kTM; ++m) y[m] = sy.read(m, 0);
+        uint32_t next = S::kPlace;                 // the place of step i + 1
+        auto after = [](uint32_t place) { return place == (kPlaces - 1) * S::kPlace ? 0u : place + S::kPlace; };
+        auto one_step = [&](auto PARITY, int64_t step) __attribute__((always_inline)) {
+            constexpr int p = decltype(PARITY)::value;
+            constexpr int kSlots = kTM * kTN, kMoves = kYU + kXU;
+            const uint32_t to_place = after(next);
+            const int64_t ahead = clamp(step + 4);
+            each<kSlots>([&](auto SLOT) __attribute__((always_inline)) {
+                constexpr int slot = decltype(SLOT)::value, m = slot / kTN, n = slot % kTN;
+                multiply<T>(x[p][n], y[m], acc[m][n]);
+                ADAGC_P_FENCE();
+                if constexpr (slot % 2 == 0 && slot / 2 < kTN) x[p ^ 1][slot / 2] = sx.read(slot / 2, next);
+                if constexpr (n == kTN - 1) y[m] = sy.read(m, next);
+                each<kMoves>([&](auto N) __attribute__((always_inline)) {
+                    constexpr int w = decltype(N)::value;
+                    if constexpr (kSlots / 4 + w * (kSlots / 4) / kMoves + 1 == slot) {
+                        if constexpr (w < kYU) sy.write(w, to_place, staged[p].y[w]);
+                        else sx.write(w - kYU, to_place, staged[p].x[w - kYU]);
+                    }
+                    if constexpr (kSlots / 2 + 2 + w * (kSlots / 4) / kMoves == slot) {
+                        if constexpr (w < kYU) staged[p].y[w] = sy.load(ahead, w);
+                        else staged[p].x[w - kYU] = sx.load(ahead, w - kYU);
+                    }
+                });
+                ADAGC_P_FENCE();
+            });
+            // the writes, in the first half of the step, are done; the fragments read since (one access each at least) may still be on their way
+            ADAGC_P_WAIT_LDS(kTM / 2 - 1);
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            ADAGC_P_FENCE();
+            next = to_place;
+        };
+        int64_t step = step0;
+        for (; step + 1 < step1; step += 2) {
+            one_step(std::integral_constant<int, 0>{}, step);
+            one_step(std::integral_constant<int, 1>{}, step + 1);
+        }
+        if (step < step1) one_step(std::integral_constant<int, 0>{}, step);
+    }
+    __syncthreads();
+}
+
+// The same with operands that go straight into LDS, whole steps only, into a ring of five places.  While step i is multiplied from registers,
+// step i + 1 is read to registers and step i + 4 is loaded into the place of step i - 1, whose reads were waited for by the
+// multiplications before the last barrier: no wait for LDS is needed there, and a load has two steps and a half to arrive.
+template <class S, class T, class SideY, class SideX>
+__device__ __forceinline__ void accumulate_direct(Sums<S>& acc, const SideY& sy, const SideX& sx, uint32_t lds0, int64_t step0, int64_t step1)
+{
+    constexpr int kTM = S::kTM, kTN = S::kTN, kYU = S::kYUnits, kLoads = S::kLoads, kAhead = kRing - 1;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const uint32_t lds_wave = lds0 + (uint32_t)wave * 1024u;
+    const int first = __builtin_amdgcn_readfirstlane((int)step0), steps = __builtin_amdgcn_readfirstlane((int)(step1 - step0));
+    if (steps <= 0) return;
+    auto load = [&](int step, int u, uint32_t place) __attribute__((always_inline)) {
+        if (u < kYU) sy.load_direct(first + step, u, lds_wave + place);
+        else sx.load_direct(first + step, u - kYU, lds_wave + place + S::kY);
+    };
+    auto meet = []() __attribute__((always_inline)) {
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        ADAGC_P_FENCE();
+    };
+    u32x4 y[kTM], x[2][kTN];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+        if (i < steps)
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) load(i, u, i * S::kPlace);
+    if (steps >= kAhead) ADAGC_P_WAIT_VMEM(2 * kLoads);        // the first two are there
+    else ADAGC_P_WAIT_VMEM(0);
+    meet();
+#pragma unroll
+    for (int n = 0; n < kTN; ++n) x[0][n] = sx.read(n, 0);
+#pragma unroll
+    for (int m = 0; m < kTM; ++m) y[m] = sy.read(m, 0);
+    uint32_t here = 0;                             // the place of step i
+    auto one_step = [&](auto PARITY, auto WHOLE, int i) __attribute__((always_inline)) {
+        constexpr int p = decltype(PARITY)::value;
+        constexpr bool whole = decltype(WHOLE)::value;     // step i + kAhead exists
+        constexpr int kSlots = kTM * kTN;
+        const uint32_t next = here == (kRing - 1) * S::kPlace ? 0u : here + S::kPlace;
+        const uint32_t before = here == 0 ? (kRing - 1) * S::kPlace : here - S::kPlace;
+        each<kSlots>([&](auto SLOT) __attribute__((always_inline)) {
+            constexpr int slot = decltype(SLOT)::value, m = slot / kTN, n = slot % kTN;
+            multiply<T>(x[p][n], y[m], acc[m][n]);
+            ADAGC_P_FENCE();
+            if constexpr (slot % 2 == 0 && slot / 2 < kTN) x[p ^ 1][slot / 2] = sx.read(slot / 2, next);
+            if constexpr (n == kTN - 1) y[m] = sy.read(m, next);
+            each<kLoads>([&](auto N) __attribute__((always_inline)) {
+                constexpr int u = decltype(N)::value;
+                if constexpr (1 + u * kSlots / kLoads == slot) {
+                    if (whole || i + kAhead < steps) load(i + kAhead, u, before);
+                }
+            });
+            ADAGC_P_FENCE();
+        });
+        // the loads of step i + 2 have to be there: those of two more steps may be on their way, as far as there are any
+        const int more = steps - 3 - i;
+        if (whole || more >= 2) ADAGC_P_WAIT_VMEM(2 * kLoads);
+        else if (more == 1) ADAGC_P_WAIT_VMEM(kLoads);
+        else ADAGC_P_WAIT_VMEM(0);
+        meet();
+        here = next;
+    };
+    int i = 0;
+    for (; i + 1 + kAhead < steps; i += 2) {
+        one_step(std::integral_constant<int, 0>{}, std::true_type{}, i);
+        one_step(std::integral_constant<int, 1>{}, std::true_type{}, i + 1);
+    }
+    // the fragments of the step after the last one are read from some place of the ring and not used
+    for (; i < steps; i += 2) {
+        one_step(std::integral_constant<int, 0>{}, std::false_type{}, i);
+        if (i + 1 < steps) one_step(std::integral_constant<int, 1>{}, std::false_type{}, i + 1);
+    }
+    __syncthreads();
+}
+
+// f(m, n, row, column, sums of 4 consecutive columns): rows and columns within the tile
+template <class S, class F>
+__device__ __forceinline__ void each_piece(const Sums<S>& acc, F&& f)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / S::kWN, wn = wave % S::kWN;
+#pragma unroll
+    for (int m = 0; m < S::kTM; ++m)
+#pragma unroll
+        for (int n = 0; n < S::kTN; ++n)
+            f(m, n, (wm * S::kTM + m) * 16 + lane % 16, (wn * S::kTN + n) * 16 + lane / 16 * 4, acc[m][n]);
+}
+
+// Four consecutive results from column `col` of a row that ends at `end` on; those before `least` are left as they are.
+template <class T>
+__device__ __forceinline__ void store4(T* row, int64_t col, int64_t least, int64_t end, const f32x4_p& v)
+{
+    typedef uint32_t u32x2_of_bf16 __attribute__((ext_vector_type(2), aligned(2)));
+    if (col >= least && col + 4 <= end) {
+        if constexpr (sizeof(T) == 4) {
+            store_whole(row + col, {__builtin_bit_cast(u32x4, v)});
+        } else {
+            const f32x2_t lo = {v[0], v[1]}, hi = {v[2], v[3]};
+            *reinterpret_cast<u32x2_of_bf16*>(row + col) =
+                u32x2_of_bf16{__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2_t)), __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2_t))};
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (col + r >= least && col + r < end) {
+                if constexpr (sizeof(T) == 4) row[col + r] = v[r];
+                else row[col + r] = __builtin_bit_cast(uint16_t, (__bf16)v[r]);
+            }
+    }
+}
+// The four there; 0 outside.
+template <class T>
+__device__ __forceinline__ f32x4_p load4(const T* row, int64_t col, int64_t least, int64_t end)
+{
+    typedef uint32_t u32x2_of_bf16 __attribute__((ext_vector_type(2), aligned(2)));
+    f32x4_p v = {0.f, 0.f, 0.f, 0.f};
+    if (col >= least && col + 4 <= end) {
+        if constexpr (sizeof(T) == 4) {
+            v = __builtin_bit_cast(f32x4_p, load_whole(row + col).w);
+        } else {
+            const u32x2_of_bf16 two = *reinterpret_cast<const u32x2_of_bf16*>(row + col);
+            v = f32x4_p{__uint_as_float(two[0] << 16), __uint_as_float(two[0] & 0xFFFF0000u), __uint_as_float(two[1] << 16), __uint_as_float(two[1] & 0xFFFF0000u)};
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (col + r >= least && col + r < end) v[r] = to_float(row[col + r]);
+    }
+    return v;
+}
+
+using Large = Tile<uint16_t, 256, 256, 2, 4, true>;
+using Small = Tile<uint16_t, 128, 128, 2, 2, true>;
+template <class T> using Staged = Tile<T, 128, 128, 2, 2, false>;
+
+// Rows of an operand start at multiples of 16 bytes.
+inline bool rows_aligned(const void* p, int64_t ld, int32_t dtype) { return !misaligned(p, 16) && ld * dtype_size(dtype) % 16 == 0; }
+
+
+// Tiles for a product of rows along k; n: of both matrices where there are two.
+struct AlongPlan {
+    bool    large, direct;
+    int64_t tiles_m, tiles_n;
+    bool    launchable() const { return tiles_m * tiles_n * (large ? 512 : 256) <= UINT32_MAX; }      // lanes
+};
+inline AlongPlan along_plan(int64_t m, int64_t n, int32_t dtype, bool aligned, int64_t ld_y, int64_t ld_x)
+{
+    AlongPlan p{};
+    auto tiles = [&](int64_t size) { return ((m + size - 1) / size) * ((n + size - 1) / size); };
+    // fp32: the matrix cores' fp32 rate is a sixteenth, which the small tile and staging keep up with
+    p.direct = aligned && dtype == ADAGC_BF16 && ld_y < (int64_t)1 << 23 && ld_x < (int64_t)1 << 23;          // 256 rows are within 32 bits
+    p.large = p.direct && tiles(256) >= kUnits / 2;
+    const int size = p.large ? 256 : 128;
+    p.tiles_m = (m + size - 1) / size;
+    p.tiles_n = (n + size - 1) / size;
+    return p;
+}
+
+// ---------------------------------------------------------------------------------------- both operands along k
+
+// Rows of Y, and of X or, as the gated projections take them, of two matrices in turn: blocks of 16 columns of the result belong to x[0] and
+// x[1] alternately, so that a lane has both results of a place next to each other.
+struct AlongArgs {
+    const void* y;
+    const void* x[2];
+    int64_t     ld_y, ld_x[2];
+    int64_t     m, n, k;          // n: rows of one X
+    int32_t     tiles_m, tiles_n;
+};
+
+// The sums of the tile whose first row is m0 and whose first row of X (or of each) is n0.
+template <class S, class T, bool PAIR>
+__device__ __forceinline__ void along_tile(Sums<S>& acc, const AlongArgs& a, uint32_t lds0, int64_t m0, int64_t n0)
+{
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t full = a.k / S::kDeep;
+    const bool rest = a.k % S::kDeep;
+    const T* y = static_cast<const T*>(a.y);
+    Side<T, S::BM, S::kThreads, S::kYUnits, S::kTM, false> sy;
+    Side<T, S::BN, S::kThreads, S::kXUnits, S::kTN, false> sx;
+    sy.set_places(tid, lds0, wave / S::kWN * S::kTM);
+    sx.set_places(tid, lds0 + S::kY, wave % S::kWN * S::kTN);
+    clear<S>(acc);
+    auto row_of_x = [&](int r) __attribute__((always_inline)) { return min(n0 + (PAIR ? (r >> 5) * 16 + (r & 15) : r), a.n - 1); };
+    if (!S::kDirect || rest) {
+        sy.set_rows(tid, [&](int r) { return y + min(m0 + r, a.m - 1) * a.ld_y; });
+        sx.set_rows(tid, [&](int r) {
+            const bool second = PAIR && (r >> 4 & 1);
+            return static_cast<const T*>(second ? a.x[1] : a.x[0]) + row_of_x(r) * (second ? a.ld_x[1] : a.ld_x[0]);
+        });
+        accumulate<S, T, false>(acc, sy, sx, S::kDirect ? full : 0, full, rest, full, a.k, 0, 0);
+    }
+    if constexpr (S::kDirect) {
+        // a load of a wave is 16 rows, and a lane's units are an even number of them apart: with two matrices, all of one
+        static_assert(S::kThreads / 64 % 2 == 0);
+        const bool second = PAIR && (wave & 1);
+        const int64_t ld_x = second ? a.ld_x[1] : a.ld_x[0];
+        sy.set_rows_direct(tid, y + m0 * a.ld_y, a.ld_y, [&](int r) { return min(m0 + r, a.m - 1) - m0; });
+        sx.set_rows_direct(tid, static_cast<const T*>(second ? a.x[1] : a.x[0]) + n0 * ld_x, ld_x, [&](int r) { return row_of_x(r) - n0; });
+        accumulate_direct<S, T>(acc, sy, sx, lds0, 0, full);
+    }
+}
+
+// ---------------------------------------------------------------------------------------- a product with a plain result
+
+// out = (add +) factor times the sum over up to two pairs of operands, or two products side by side.
+struct PlainArgs {
+    const void* y[2];
+    const void* x[2];
+    int64_t     ld_y, ld_x[2];
+    void*       out[2];
+    int64_t     ld_out[2];
+    const void* add[2];           // NULL: nothing
+    int64_t     ld_add[2];
+    int64_t     m, n, k;
+    int64_t     m_readable;       // Y across k: columns of it that may be read, m or more
+    float*      workspace;        // partial sums of the split tiles
+    float       factor;
+    int32_t     pairs;            // 1, or 2: both pairs' products are summed
+    int32_t     products;         // 1, or 2: out[0], out[1] of the two pairs
+    int32_t     out_bf16, add_bf16;
+    int32_t     tiles_m, tiles_n; // of one product
+    int32_t     whole;            // tiles computed by one workgroup each; the others by `split`
+    int32_t     split;
+};
+
+__device__ __forceinline__ void store_plain(const PlainArgs& a, int product, int64_t row, int64_t row_least, int64_t col, int64_t col_least, f32x4_p v)
+{
+    if (row < row_least || row >= a.m || col >= a.n) return;
+    v *= a.factor;
+    const void* add = product ? a.add[1] : a.add[0];
+    void* out = product ? a.out[1] : a.out[0];
+    if (add) {
+        const int64_t at = row * (product ? a.ld_add[1] : a.ld_add[0]);
+        v += a.add_bf16 ? load4(static_cast<const uint16_t*>(add) + at, col, col_least, a.n) : load4(static_cast<const float*>(add) + at, col, col_least, a.n);
+    }
+    const int64_t at = row * (product ? a.ld_out[1] : a.ld_out[0]);
+    if (a.out_bf16) store4(static_cast<uint16_t*>(out) + at, col, col_least, a.n, v);
+    else store4(static_cast<float*>(out) + at, col, col_least, a.n, v);
+}
+
+// The first row or column that a tile computes and the first that it stores: the last tile across columns begins a tile before the end, so that
+// every tile is whole.
+template <bool SHIFT>
+__device__ __forceinline__ int64_t first_of_tile(int tile, int size, int64_t n)
+{
+    const int64_t first = (int64_t)tile * size;
+    return SHIFT ? min(first, n - size) : first;
+}
+
+// Y along k or across it, X across it (the products of a backward pass).  CHECKED: a side across k is smaller than a tile, or its rows are too
+// far apart for 32-bit offsets.
+template <class S, class T, bool ACROSS_Y, bool CHECKED>
+__global__ __launch_bounds__(S::kThreads, 2) void plain_kernel(const PlainArgs a)
+{
+    static_assert(!(CHECKED && S::kDirect));
+    __shared__ __attribute__((aligned(512))) uint8_t lds[S::kLds];
+    const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>(&lds[0]);      // low half of the flat address = LDS offset
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int item = (int)blockIdx.x;
+    int tile = item, part = 0;
+    const bool alone = item < a.whole;
+    if (!alone) {
+        tile = __builtin_amdgcn_readfirstlane(a.whole + (item - a.whole) / a.split);
+        part = __builtin_amdgcn_readfirstlane((item - a.whole) % a.split);
+    }
+    const int per_product = a.tiles_m * a.tiles_n, product = __builtin_amdgcn_readfirstlane(tile / per_product);
+    int tm, tn;
+    place_of_tile(tile - product * per_product, a.tiles_m, a.tiles_n, &tm, &tn);
+    const int64_t m0 = first_of_tile<ACROSS_Y && !CHECKED>(tm, S::BM, ACROSS_Y ? a.m_readable : a.m), n0 = first_of_tile<!CHECKED>(tn, S::BN, a.n);
+    const int64_t full = a.k / S::kDeep;
+    int64_t step0 = 0, step1 = full;
+    if (!alone) {
+        step0 = full * part / a.split;
+        step1 = full * (part + 1) / a.split;
+    }
+    const bool rest = (alone || part == a.split - 1) && a.k % S::kDeep;
+
+    Side<T, S::BM, S::kThreads, S::kYUnits, S::kTM, ACROSS_Y> sy;
+    Side<T, S::BN, S::kThreads, S::kXUnits, S::kTN, true> sx;
+    sy.set_places(tid, lds0, wave / S::kWN * S::kTM);
+    sx.set_places(tid, lds0 + S::kY, wave % S::kWN * S::kTN);
+    Sums<S> acc;
+    clear<S>(acc);
+    for (int pair = product; pair < product + a.pairs; ++pair) {
+        const T* y = static_cast<const T*>(pair ? a.y[1] : a.y[0]);         // (an index would put the arguments into memory)
+        const T* x = static_cast<const T*>(pair ? a.x[1] : a.x[0]) + n0;
+        const int64_t ld_x = pair ? a.ld_x[1] : a.ld_x[0];
+        if (!S::kDirect || rest) {
+            if constexpr (ACROSS_Y) sy.set_columns(tid, y + m0, a.ld_y);
+            else sy.set_rows(tid, [&](int r) { return y + min(m0 + r, a.m - 1) * a.ld_y; });
+            sx.set_columns(tid, x, ld_x);
+            accumulate<S, T, CHECKED>(acc, sy, sx, S::kDirect ? full : step0, S::kDirect ? full : step1, rest, full, a.k, (ACROSS_Y ? a.m_readable : a.m) - m0, a.n - n0);
+        }
+        if constexpr (S::kDirect) {
+            if constexpr (ACROSS_Y) sy.set_columns_direct(tid, y + m0, a.ld_y);
+            else sy.set_rows_direct(tid, y + m0 * a.ld_y, a.ld_y, [&](int r) { return min(m0 + r, a.m - 1) - m0; });
+            sx.set_columns_direct(tid, x, ld_x);
+            accumulate_direct<S, T>(acc, sy, sx, lds0, step0, step1);
+        }
+    }
+    const int64_t m_least = (int64_t)tm * S::BM, n_least = (int64_t)tn * S::BN;
+    if (alone) {
+        each_piece<S>(acc, [&](int, int, int r, int c, const f32x4_p& v) __attribute__((always_inline)) {
+            store_plain(a, product, m0 + r, m_least, n0 + c, n_least, v);
+        });
+    } else {
+        f32x4_p* to = reinterpret_cast<f32x4_p*>(a.workspace) + (size_t)(item - a.whole) * (S::BM * S::BN / 4) + tid;
+        each_piece<S>(acc, [&](int m, int n, int, int, const f32x4_p& v) __attribute__((always_inline)) { to[(m * S::kTN + n) * S::kThreads] = v; });
+    }
+}
+
+// Adds the parts of the split tiles, in order: a workgroup takes one block of every wave.
+template <class S, bool ACROSS_Y, bool CHECKED>
+__global__ __launch_bounds__(S::kThreads) void plain_join_kernel(const PlainArgs a)
+{
+    constexpr int kBlocks = S::kTM * S::kTN;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / S::kWN, wn = wave % S::kWN;
+    const int n_tile = (int)blockIdx.x / kBlocks, block = (int)blockIdx.x % kBlocks, m = block / S::kTN, n = block % S::kTN;
+    const int tile = a.whole + n_tile, per_product = a.tiles_m * a.tiles_n, product = tile / per_product;
+    int tm, tn;
+    place_of_tile(tile - product * per_product, a.tiles_m, a.tiles_n, &tm, &tn);
+    const int64_t m0 = first_of_tile<ACROSS_Y && !CHECKED>(tm, S::BM, ACROSS_Y ? a.m_readable : a.m), n0 = first_of_tile<!CHECKED>(tn, S::BN, a.n);
+    const f32x4_p* from = reinterpret_cast<const f32x4_p*>(a.workspace) + (size_t)n_tile * a.split * (S::BM * S::BN / 4) + (size_t)block * S::kThreads + tid;
+    f32x4_p sum = from[0];
+    int p = 1;
+    constexpr int kTogether = 4;                       // loads on their way
+    for (; p + kTogether <= a.split; p += kTogether) {
+        f32x4_p v[kTogether];
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u) v[u] = from[(size_t)(p + u) * (S::BM * S::BN / 4)];
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u) sum += v[u];
+    }
+    for (; p < a.split; ++p) sum += from[(size_t)p * (S::BM * S::BN / 4)];
+    store_plain(a, product, m0 + (wm * S::kTM + m) * 16 + lane % 16, (int64_t)tm * S::BM, n0 + (wn * S::kTN + n) * 16 + lane / 16 * 4, (int64_t)tn * S::BN, sum);
+}
+
+// How a product is cut: tiles, and those of the last, partial round of workgroups also along k, so that they fill the chip too.
+struct PlainPlan {
+    int     size;                 // 256 or 128
+    bool    checked, direct;
+    int64_t tiles_m, tiles_n, whole, rest, split;
+    int64_t workspace() const { return split > 1 ? rest * split * size * size * 4 : 0; }
+    bool    launchable() const { return (whole + rest * split) * (size == 256 ? 512 : 256) <= UINT32_MAX; }      // lanes
+};
+// m: with Y across k, of its readable columns; pairs: of operands that are summed; products: side by side; aligned: the rows of both operands
+// are, and so is m.  A workspace is sized for both.
+inline PlainPlan plain_plan(int64_t m, int64_t n, int64_t k, int32_t dtype, bool across_y, int64_t ld_y, int64_t ld_x, int pairs, int products, bool aligned)
+{
+    PlainPlan p{};
+    auto tiles = [&](int64_t size) { return products * ((m + size - 1) / size) * ((n + size - 1) / size); };
+    // 32 rows across, 256 along k are not within 32 bits
+    const bool far = ld_x >= (int64_t)1 << 24 || (across_y && ld_y >= (int64_t)1 << 24);
+    // fp32: the matrix cores' fp32 rate is a sixteenth, which the small tile and staging keep up with
+    p.direct = aligned && !far && dtype == ADAGC_BF16 && (across_y || ld_y < (int64_t)1 << 23) && n >= 128 && n % 8 == 0 &&
+               (!across_y || m >= 128);      // (m: of what is readable, a multiple of 8)
+    const bool large = p.direct && m >= 256 && n >= 256 && tiles(256) >= kUnits / 2;
+    p.size = large ? 256 : 128;
+    p.checked = far || n < p.size || (across_y && m < p.size);
+    p.tiles_m = (m + p.size - 1) / p.size;
+    p.tiles_n = (n + p.size - 1) / p.size;
+    const int64_t all = tiles(p.size), steps = k / (kStepBytes / dtype_size(dtype));
+    const int64_t round = large ? kUnits : 2 * kUnits;      // the small tile's workgroups share a compute unit in pairs
+    p.rest = all % round;
+    // a part has eight steps at least (of each pair)
+    p.split = p.rest ? std::max<int64_t>(1, std::min(round / p.rest, steps * pairs / 8)) : 1;
+    p.split = std::min(p.split, std::max<int64_t>(1, steps));
+    if (p.split == 1) p.rest = 0;
+    p.whole = all - p.rest;
+    return p;
+}
+
+template <class S, class T, bool ACROSS_Y, bool CHECKED>
+int launch_plain(const PlainArgs& a, const PlainPlan& p, hipStream_t s)
+{
+    plain_kernel<S, T, ACROSS_Y, CHECKED><<<dim3((uint32_t)(p.whole + p.rest * p.split)), dim3(S::kThreads), 0, s>>>(a);
+    if (p.rest) plain_join_kernel<S, ACROSS_Y, CHECKED><<<dim3((uint32_t)(p.rest * S::kTM * S::kTN)), dim3(S::kThreads), 0, s>>>(a);
+    return hipGetLastError() == hipSuccess ? ADAGC_OK : ADAGC_ERR_HIP;
+}
+// Fills in how the product is cut and launches it.
+template <class T, bool ACROSS_Y>
+int run_plain(PlainArgs a, hipStream_t s)
+{
+    constexpr int32_t dtype = sizeof(T) == 4 ? ADAGC_F32 : ADAGC_BF16;
+    const int both = std::max(a.pairs, a.products);
+    const int64_t m = ACROSS_Y ? a.m_readable : a.m;
+    bool aligned = !ACROSS_Y || m % 8 == 0;
+    int64_t ld_x = 0;
+    for (int i = 0; i < both; ++i) {
+        aligned = aligned && rows_aligned(a.y[i], a.ld_y, dtype) && rows_aligned(a.x[i], a.ld_x[i], dtype);
+        ld_x = std::max(ld_x, a.ld_x[i]);
+    }
+    const PlainPlan p = plain_plan(m, a.n, a.k, dtype, ACROSS_Y, a.ld_y, ld_x, a.pairs, a.products, aligned);
+    a.tiles_m = (int32_t)p.tiles_m;
+    a.tiles_n = (int32_t)p.tiles_n;
+    a.whole = (int32_t)p.whole;
+    a.split = (int32_t)p.split;
+    if constexpr (sizeof(T) == 2) {
+        if (p.size == 256) return launch_plain<Large, T, ACROSS_Y, false>(a, p, s);
+        if (p.direct) return launch_plain<Small, T, ACROSS_Y, false>(a, p, s);
+    }
+    return p.checked ? launch_plain<Staged<T>, T, ACROSS_Y, true>(a, p, s) : launch_plain<Staged<T>, T, ACROSS_Y, false>(a, p, s);
+}
+
+// instantiated in product.hip
+extern template int run_plain<float, false>(PlainArgs, hipStream_t);
+extern template int run_plain<float, true>(PlainArgs, hipStream_t);
+extern template int run_plain<uint16_t, false>(PlainArgs, hipStream_t);
+extern template int run_plain<uint16_t, true>(PlainArgs, hipStream_t);
+
+}  // namespace product
+}  // namespace adagc
+#endif
