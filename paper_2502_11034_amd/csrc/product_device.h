@@ -47,7 +47,7 @@ __device__ __forceinline__ void each(F&& f)
 // Compute units: a round of a launch is as many workgroups of the large tile.
 constexpr int kUnits = 256;
 constexpr int kPlaces = 3;                 // of LDS, that steps staged through registers go round in
-constexpr int kRing = 5;                   // of LDS, that steps loaded straight into it go round in
+constexpr int kRing = 5;                   // of LDS, that operand tiles of two steps loaded straight into it go round in
 constexpr int kStepBytes = 64;             // of k, a step
 
 // BM x BN tile (BM rows of Y), kWM x kWN waves of kTM x kTN blocks of 16 x 16.  A step is 64 bytes of k: 32 bf16 or 16 fp32 numbers, so that
@@ -61,9 +61,10 @@ struct Tile {
     static constexpr int kDeep = kStepBytes / (int)sizeof(T);
     static constexpr int kY = BM * kStepBytes, kX = BN * kStepBytes, kPlace = kY + kX;      // bytes
     static constexpr int kYUnits = kY / 16 / kThreads, kXUnits = kX / 16 / kThreads;       // of 16 bytes, a lane's
-    static constexpr int kLoads = kYUnits + kXUnits;
     static constexpr bool kDirect = DIRECT_;
+    static constexpr int kYLoads = 2 * kYUnits, kXLoads = 2 * kXUnits;                     // straight into LDS, of two steps, a lane's
     static constexpr int kLds = (DIRECT_ ? kRing : kPlaces) * kPlace;
+    static_assert(!DIRECT_ || BM_ == BN_, "a place of the ring takes either operand");
     static_assert(kY % (16 * kThreads) == 0 && kX % (16 * kThreads) == 0, "operand tiles are dealt evenly");
 };
 
@@ -106,24 +107,26 @@ __device__ __forceinline__ void place_of_tile(int n, int tiles_m, int tiles_n, i
     *tm = __builtin_amdgcn_readfirstlane(8 * band + in_band - *tn * high);
 }
 
-// How one operand's tile (B rows or columns of the result) is loaded, staged in LDS and read: kUnits units of 16 bytes for a lane.
+// How one operand's tile (B rows or columns of the result) is loaded, staged in LDS and read: kUnits units of 16 bytes a step for a lane.
 //
-// Along: LDS rows of 64 bytes, one for a row of the result; the 16-byte vector v of row r is at position v ^ ((r / 4) mod 4), so that the 16
-// rows that 16 lanes read one vector of lie in different banks.
+// Along: LDS rows of a step's 64 bytes (DIRECT: of two steps' 128), one for a row of the result.  The 16-byte vector v of row r is at position
+// v ^ f((r / 4) mod 4), f = 0, 3, 2, 1 (DIRECT: v ^ ((r / 2) mod 8)): the 16 lanes that read at a time (vector v of rows 0 .. 3 and 12 .. 15
+// with v ^ 1 of rows 4 .. 11) so meet different banks.  (With f = 0, 1, 2, 3, which separates 16 rows of one vector, half of the LDS
+// cycles were conflicts.)
 // Across, bf16: LDS rows of B numbers, one for each k; 16 lanes read 4 rows of 16 columns and get a column each (ds_read_b64_tr_b16); the
 // 32-byte units of a row are permuted so that the eight that half a wave takes (rows 0 .. 3 and 8 .. 11) lie in different banks.
 // Across, fp32: the same with 64-byte units, read number by number.
-template <class T, int B, int kThreads, int kUnits, int kBlocks, bool ACROSS>
+template <class T, int B, int kThreads, int kUnits, int kBlocks, bool ACROSS, bool DIRECT>
 struct Side {
     static constexpr int kE = 16 / (int)sizeof(T);                 // numbers in a vector
     static constexpr int kDeep = kStepBytes / (int)sizeof(T);
-    static constexpr int kVectors = ACROSS ? B / kE : 4;            // of a row in LDS
-    static constexpr int kPitch = kVectors * 16;                    // bytes
+    static constexpr int kVectors = ACROSS ? B / kE : 4;            // of a row and a step
+    static constexpr int kPitch = ACROSS ? B * (int)sizeof(T) : DIRECT ? 2 * kStepBytes : kStepBytes;      // bytes of a row in LDS
     static constexpr bool kHalf = sizeof(T) == 2;
+    static_assert(!DIRECT || kHalf);
 
     const T* row[ACROSS ? 1 : kUnits];     // along: a unit's address at k = 0, less its vector
     uint32_t lane_at;                      // across: bytes from the step's address, unit 0
-    uint32_t off[kUnits];                  // straight into LDS: bytes from the step's address, which is the same in all lanes
     int64_t  ld;
     uint32_t write_at, read_at;
 
@@ -131,11 +134,12 @@ struct Side {
     static __device__ __forceinline__ int vector_of(int tid, int u) { return (tid + u * kThreads) % kVectors; }
     static __device__ __forceinline__ uint32_t place(int r, int v)
     {
-        if constexpr (!ACROSS) return (uint32_t)(r * kPitch + (v ^ ((r >> 2) & 3)) * 16);
+        if constexpr (!ACROSS && DIRECT) return (uint32_t)(r * kPitch + (v ^ ((r >> 1) & 7)) * 16);
+        else if constexpr (!ACROSS) return (uint32_t)(r * kPitch + (v ^ ((r >> 2) & 3) ^ ((r >> 1) & 2)) * 16);
         else if constexpr (kHalf) return (uint32_t)(r * kPitch + ((v >> 1) ^ ((r & 3) | ((r >> 3) & 1) << 2)) * 32 + (v & 1) * 16);
         else return (uint32_t)(r * kPitch + ((v >> 2) ^ ((r >> 2) & 3)) * 64 + (v & 3) * 16);
     }
-    // lds0: the tile's first byte in a place, wave_block: the wave's first block
+    // lds0: the first byte of the tile's place, wave_block: the wave's first block
     __device__ __forceinline__ void set_places(int tid, uint32_t lds0, int wave_block)
     {
         write_at = lds0 + place(row_of(tid, 0), vector_of(tid, 0));
@@ -150,6 +154,8 @@ struct Side {
             read_at = lds0 + (uint32_t)(r * kPitch + (wave_block ^ ((r >> 2) & 3)) * 64 + (l & 15) * 4);
         }
     }
+
+    // ---- through registers
     // along: row_at(r): the address of row r of the tile (rows beyond the matrix: any of its rows)
     template <class F>
     __device__ __forceinline__ void set_rows(int tid, F&& row_at)
@@ -184,33 +190,6 @@ struct Side {
             return load_vector(row[0] + t * ld, vector_of(tid, u) * kE, t < k ? columns : 0, 0).w;
         }
     }
-    // Straight into LDS: position i of row r gets vector unplaced(r, i), so that vector v is where place(r, v) says.
-    static __device__ __forceinline__ int unplaced(int r, int i) { return (int)(place(r, i) % (uint32_t)kPitch) / 16; }      // its own inverse
-    // along: rows of one matrix within 32 bits of bytes from `at`; number_of(r): the number of row r of the tile, from `at` (a row inside the matrix)
-    template <class F>
-    __device__ __forceinline__ void set_rows_direct(int tid, const T* at, int64_t ld_, F&& number_of)
-    {
-        row[0] = scalar(at);
-#pragma unroll
-        for (int u = 0; u < kUnits; ++u) {
-            const int r = row_of(tid, u);
-            off[u] = ((uint32_t)number_of(r) * (uint32_t)ld_ + (uint32_t)unplaced(r, vector_of(tid, u)) * kE) * (uint32_t)sizeof(T);
-        }
-    }
-    __device__ __forceinline__ void set_columns_direct(int tid, const T* at, int64_t ld_)
-    {
-        row[0] = scalar(at);
-        ld = scalar(ld_);
-#pragma unroll
-        for (int u = 0; u < kUnits; ++u) {
-            const int r = row_of(tid, u);
-            off[u] = ((uint32_t)r * (uint32_t)ld_ + (uint32_t)unplaced(r, vector_of(tid, u)) * kE) * (uint32_t)sizeof(T);
-        }
-    }
-    __device__ __forceinline__ void load_direct(int step, int u, uint32_t lds_at) const
-    {
-        load_to_lds(row[0] + (ACROSS ? (int64_t)(step * kDeep) * ld : step * kDeep), off[u], lds_at + (uint32_t)(u * kThreads * 16));
-    }
     __device__ __forceinline__ void write(int u, uint32_t place, const u32x4& w) const
     {
         // a unit's rows are kRows below the last one's: at the same place of the permutation but for fp32 across, where 8 rows flip a bit of it
@@ -219,13 +198,49 @@ struct Side {
         const uint32_t at = kRows % 16 && u ? write_at ^ 128u : write_at;
         *reinterpret_cast<ADAGC_P_LDS u32x4*>(at + place + (uint32_t)(u * kRows * kPitch)) = w;
     }
-    __device__ __forceinline__ u32x4 read(int block, uint32_t place) const
+
+    // ---- straight into LDS, two steps at a time: a lane's kLoads vectors, kAlong of a row
+    static constexpr int kLoads = 2 * kUnits, kAlong = ACROSS ? kVectors : 8;
+    uint32_t off[ACROSS ? 1 : kLoads];     // bytes from the first step's address, which is the same in all lanes
+    const T* base;
+
+    // Position i of row r gets vector unplaced(r, i), so that vector v is where place(r, v) says (its own inverse).
+    static __device__ __forceinline__ int unplaced(int r, int i) { return (int)(place(r, i) % (uint32_t)kPitch) / 16; }
+    // along: rows of one matrix within 32 bits of bytes from `at`; number_of(r): the number of row r of the tile, from `at` (a row inside the matrix)
+    template <class F>
+    __device__ __forceinline__ void set_rows_direct(int tid, const T* at, int64_t ld_, F&& number_of)
+    {
+        base = scalar(at);
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) {
+            const int i = tid + u * kThreads, r = i / kAlong;
+            off[u] = ((uint32_t)number_of(r) * (uint32_t)ld_ + (uint32_t)unplaced(r, i % kAlong) * kE) * (uint32_t)sizeof(T);
+        }
+    }
+    __device__ __forceinline__ void set_columns_direct(int tid, const T* at, int64_t ld_)
+    {
+        base = scalar(at);
+        ld = scalar(ld_);
+        const int r = tid / kAlong;
+        off[0] = ((uint32_t)r * (uint32_t)ld_ + (uint32_t)unplaced(r, tid % kAlong) * kE) * (uint32_t)sizeof(T);
+    }
+    __device__ __forceinline__ void load_direct(int two_steps, int u, uint32_t lds_at) const
+    {
+        constexpr int kRows = kThreads / kAlong;       // of a load, across: the permutation repeats after 16
+        static_assert(!ACROSS || kRows % 16 == 0);
+        if constexpr (ACROSS) load_to_lds(base + (int64_t)(two_steps * 2 * kDeep + u * kRows) * ld, off[0], lds_at + (uint32_t)(u * kThreads * 16));
+        else load_to_lds(base + (int64_t)two_steps * 2 * kDeep, off[u], lds_at + (uint32_t)(u * kThreads * 16));
+    }
+
+    // second: of two steps in a place
+    __device__ __forceinline__ u32x4 read(int block, uint32_t place, bool second = false) const
     {
         if constexpr (!ACROSS) {
-            return *reinterpret_cast<const ADAGC_P_LDS u32x4*>(read_at + place + (uint32_t)(block * 16 * kPitch));
+            const uint32_t at = DIRECT && second ? read_at ^ 64u : read_at;
+            return *reinterpret_cast<const ADAGC_P_LDS u32x4*>(at + place + (uint32_t)(block * 16 * kPitch));
         } else if constexpr (kHalf) {
             static_assert((kBlocks & (kBlocks - 1)) == 0, "blocks are exclusive-ored into an address");
-            const uint32_t at = (read_at ^ (uint32_t)(block * 32)) + place;
+            const uint32_t at = (read_at ^ (uint32_t)(block * 32)) + place + (second ? kDeep * kPitch : 0);
             const s16x4_p a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ADAGC_P_LDS s16x4_p*>(at));
             const s16x4_p b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ADAGC_P_LDS s16x4_p*>(at + 4 * kPitch));
             return __builtin_bit_cast(u32x4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -329,7 +344,7 @@ __device__ __forceinline__ void accumulate(Sums<S>& acc, const SideY& sy, const 
                     if (step + p + 2 < end) load_checked(step + p + 2, staged[p]);
                 });
             });
-    } else if (S::kDirect || step0 == step1) {
+    } else if (step0 == step1) {
         if (rest) {
             Staged s;
             load_checked(full, s);
@@ -398,77 +413,123 @@ __device__ __forceinline__ void accumulate(Sums<S>& acc, const SideY& sy, const 
     __syncthreads();
 }
 
-// The same with operands that go straight into LDS, whole steps only, into a ring of five places.  While step i is multiplied from registers,
-// step i + 1 is read to registers and step i + 4 is loaded into the place of step i - 1, whose reads were waited for by the
-// multiplications before the last barrier: no wait for LDS is needed there, and a load has two steps and a half to arrive.
+// What is left over after `first` steps, a step at a time: for the tiles whose whole pairs of steps go straight into LDS.
 template <class S, class T, class SideY, class SideX>
-__device__ __forceinline__ void accumulate_direct(Sums<S>& acc, const SideY& sy, const SideX& sx, uint32_t lds0, int64_t step0, int64_t step1)
+__device__ __forceinline__ void accumulate_rest(Sums<S>& acc, const SideY& sy, const SideX& sx, int64_t first, int64_t k, int64_t columns_y, int64_t columns_x)
 {
-    constexpr int kTM = S::kTM, kTN = S::kTN, kYU = S::kYUnits, kLoads = S::kLoads, kAhead = kRing - 1;
+    const int tid = threadIdx.x;
+    constexpr uint32_t kXPlace = S::kXLoads * S::kThreads * 16;            // the next place of the ring
+    for (int64_t step = first; step * S::kDeep < k; ++step) {
+        u32x4 w[S::kYUnits + S::kXUnits];
+#pragma unroll
+        for (int u = 0; u < S::kYUnits; ++u) w[u] = sy.load_checked(tid, step, u, k, columns_y);
+#pragma unroll
+        for (int u = 0; u < S::kXUnits; ++u) w[S::kYUnits + u] = sx.load_checked(tid, step, u, k, columns_x);
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < S::kYUnits; ++u) sy.write(u, 0, w[u]);
+#pragma unroll
+        for (int u = 0; u < S::kXUnits; ++u) sx.write(u, kXPlace, w[S::kYUnits + u]);
+        __syncthreads();
+        u32x4 x[S::kTN];
+#pragma unroll
+        for (int n = 0; n < S::kTN; ++n) x[n] = sx.read(n, kXPlace);
+#pragma unroll
+        for (int m = 0; m < S::kTM; ++m) {
+            const u32x4 y = sy.read(m, 0);
+#pragma unroll
+            for (int n = 0; n < S::kTN; ++n) multiply<T>(x[n], y, acc[m][n]);
+        }
+    }
+    __syncthreads();
+}
+
+// Pairs of steps pair0 .. pair1 - 1 with operands that go straight into LDS, into a ring of five places.  A place holds one operand's tile of two
+// steps, so that a row along k is loaded 128 bytes at a time: with the 64 of one step the L2s had twice the requests.
+//
+// While a step is multiplied from registers, the next one is read to registers.  In the first step of pair d the X of pair d + 2 is loaded into
+// the place of the Y of pair d - 1, in the second its Y into the place of the X of pair d.  What a place held before has been read by then: the
+// Y were waited for by the multiplications before the last barrier, and the X, which are read first, by a wait for all but the later LDS
+// reads.  A load has one and a half or two and a half steps to arrive.
+template <class S, class T, class SideY, class SideX>
+__device__ __forceinline__ void accumulate_direct(Sums<S>& acc, const SideY& sy, const SideX& sx, uint32_t lds0, int64_t pair0, int64_t pair1)
+{
+    constexpr int kTM = S::kTM, kTN = S::kTN, kLoads = S::kYLoads, kSize = S::kPlace, kEnd = kRing * kSize;      // kSize: one operand, two steps
+    static_assert(S::kYLoads == S::kXLoads && kLoads * S::kThreads * 16 == kSize);
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const uint32_t lds_wave = lds0 + (uint32_t)wave * 1024u;
-    const int first = __builtin_amdgcn_readfirstlane((int)step0), steps = __builtin_amdgcn_readfirstlane((int)(step1 - step0));
-    if (steps <= 0) return;
-    auto load = [&](int step, int u, uint32_t place) __attribute__((always_inline)) {
-        if (u < kYU) sy.load_direct(first + step, u, lds_wave + place);
-        else sx.load_direct(first + step, u - kYU, lds_wave + place + S::kY);
-    };
+    const int first = __builtin_amdgcn_readfirstlane((int)pair0), pairs = __builtin_amdgcn_readfirstlane((int)(pair1 - pair0));
+    if (pairs <= 0) return;
+    auto load_y = [&](int d, int u, uint32_t place) __attribute__((always_inline)) { sy.load_direct(first + d, u, lds_wave + place); };
+    auto load_x = [&](int d, int u, uint32_t place) __attribute__((always_inline)) { sx.load_direct(first + d, u, lds_wave + place); };
     auto meet = []() __attribute__((always_inline)) {
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         ADAGC_P_FENCE();
     };
+    auto later = [](uint32_t place, int n) { return place + (uint32_t)(n * kSize) >= (uint32_t)kEnd ? place + (uint32_t)(n * kSize) - kEnd : place + (uint32_t)(n * kSize); };
     u32x4 y[kTM], x[2][kTN];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-        if (i < steps)
+    for (int d = 0; d < 2; ++d)
+        if (d < pairs) {
 #pragma unroll
-            for (int u = 0; u < kLoads; ++u) load(i, u, i * S::kPlace);
-    if (steps >= kAhead) ADAGC_P_WAIT_VMEM(2 * kLoads);        // the first two are there
+            for (int u = 0; u < kLoads; ++u) load_x(d, u, 2 * d * kSize);
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) load_y(d, u, (2 * d + 1) * kSize);
+        }
+    if (pairs > 1) ADAGC_P_WAIT_VMEM(2 * kLoads);
     else ADAGC_P_WAIT_VMEM(0);
     meet();
 #pragma unroll
     for (int n = 0; n < kTN; ++n) x[0][n] = sx.read(n, 0);
 #pragma unroll
-    for (int m = 0; m < kTM; ++m) y[m] = sy.read(m, 0);
-    uint32_t here = 0;                             // the place of step i
-    auto one_step = [&](auto PARITY, auto WHOLE, int i) __attribute__((always_inline)) {
-        constexpr int p = decltype(PARITY)::value;
-        constexpr bool whole = decltype(WHOLE)::value;     // step i + kAhead exists
+    for (int m = 0; m < kTM; ++m) y[m] = sy.read(m, kSize);
+    uint32_t here = 0;                             // the place of X of pair d; its Y's is the next one
+    auto one_step = [&](auto SECOND, auto MORE, int d) __attribute__((always_inline)) {
+        constexpr int second = decltype(SECOND)::value;
+        constexpr bool more = decltype(MORE)::value;       // pair d + 2 exists
         constexpr int kSlots = kTM * kTN;
-        const uint32_t next = here == (kRing - 1) * S::kPlace ? 0u : here + S::kPlace;
-        const uint32_t before = here == 0 ? (kRing - 1) * S::kPlace : here - S::kPlace;
+        // of the step that is read: the second one of pair d, the first one of pair d + 1
+        const uint32_t from_x = second ? later(here, 2) : here, from_y = later(here, second ? 3 : 1);
+        const uint32_t to = second ? here : later(here, 4);
         each<kSlots>([&](auto SLOT) __attribute__((always_inline)) {
             constexpr int slot = decltype(SLOT)::value, m = slot / kTN, n = slot % kTN;
-            multiply<T>(x[p][n], y[m], acc[m][n]);
+            multiply<T>(x[second][n], y[m], acc[m][n]);
             ADAGC_P_FENCE();
-            if constexpr (slot % 2 == 0 && slot / 2 < kTN) x[p ^ 1][slot / 2] = sx.read(slot / 2, next);
-            if constexpr (n == kTN - 1) y[m] = sy.read(m, next);
-            each<kLoads>([&](auto N) __attribute__((always_inline)) {
-                constexpr int u = decltype(N)::value;
-                if constexpr (1 + u * kSlots / kLoads == slot) {
-                    if (whole || i + kAhead < steps) load(i + kAhead, u, before);
-                }
-            });
+            if constexpr (slot % 2 == 0 && slot / 2 < kTN) x[second ^ 1][slot / 2] = sx.read(slot / 2, from_x, !second);
+            if constexpr (n == kTN - 1) y[m] = sy.read(m, from_y, !second);
+            if constexpr (more) {
+                each<kLoads>([&](auto N) __attribute__((always_inline)) {
+                    constexpr int u = decltype(N)::value;
+                    if constexpr (1 + u * kSlots / kLoads == slot) {
+                        if constexpr (second) load_y(d + 2, u, to);
+                        else load_x(d + 2, u, to);
+                    }
+                });
+            }
             ADAGC_P_FENCE();
         });
-        // the loads of step i + 2 have to be there: those of two more steps may be on their way, as far as there are any
-        const int more = steps - 3 - i;
-        if (whole || more >= 2) ADAGC_P_WAIT_VMEM(2 * kLoads);
-        else if (more == 1) ADAGC_P_WAIT_VMEM(kLoads);
-        else ADAGC_P_WAIT_VMEM(0);
+        if constexpr (!second) {
+            // pair d + 1 has to be there, and X of pair d read: kTM - 1 fragments of Y, one access each at least, are read after it
+            if constexpr (more) ADAGC_P_WAIT_VMEM(kLoads);
+            else ADAGC_P_WAIT_VMEM(0);
+            ADAGC_P_WAIT_LDS(kTM - 1);
+        }
         meet();
-        here = next;
     };
-    int i = 0;
-    for (; i + 1 + kAhead < steps; i += 2) {
-        one_step(std::integral_constant<int, 0>{}, std::true_type{}, i);
-        one_step(std::integral_constant<int, 1>{}, std::true_type{}, i + 1);
+    constexpr std::integral_constant<int, 0> even{};
+    constexpr std::integral_constant<int, 1> odd{};
+    int d = 0;
+    for (; d + 2 < pairs; ++d) {
+        one_step(even, std::true_type{}, d);
+        one_step(odd, std::true_type{}, d);
+        here = later(here, 2);
     }
     // the fragments of the step after the last one are read from some place of the ring and not used
-    for (; i < steps; i += 2) {
-        one_step(std::integral_constant<int, 0>{}, std::false_type{}, i);
-        if (i + 1 < steps) one_step(std::integral_constant<int, 1>{}, std::false_type{}, i + 1);
+    for (; d < pairs; ++d) {
+        one_step(even, std::false_type{}, d);
+        one_step(odd, std::false_type{}, d);
+        here = later(here, 2);
     }
     __syncthreads();
 }
@@ -572,31 +633,31 @@ template <class S, class T, bool PAIR>
 __device__ __forceinline__ void along_tile(Sums<S>& acc, const AlongArgs& a, uint32_t lds0, int64_t m0, int64_t n0)
 {
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t full = a.k / S::kDeep;
-    const bool rest = a.k % S::kDeep;
     const T* y = static_cast<const T*>(a.y);
-    Side<T, S::BM, S::kThreads, S::kYUnits, S::kTM, false> sy;
-    Side<T, S::BN, S::kThreads, S::kXUnits, S::kTN, false> sx;
+    Side<T, S::BM, S::kThreads, S::kYUnits, S::kTM, false, S::kDirect> sy;
+    Side<T, S::BN, S::kThreads, S::kXUnits, S::kTN, false, S::kDirect> sx;
     sy.set_places(tid, lds0, wave / S::kWN * S::kTM);
-    sx.set_places(tid, lds0 + S::kY, wave % S::kWN * S::kTN);
+    sx.set_places(tid, S::kDirect ? lds0 : lds0 + S::kY, wave % S::kWN * S::kTN);
     clear<S>(acc);
     auto row_of_x = [&](int r) __attribute__((always_inline)) { return min(n0 + (PAIR ? (r >> 5) * 16 + (r & 15) : r), a.n - 1); };
-    if (!S::kDirect || rest) {
+    const int64_t pairs = a.k / (2 * S::kDeep), full = a.k / S::kDeep;
+    if (!S::kDirect || a.k % (2 * S::kDeep)) {
         sy.set_rows(tid, [&](int r) { return y + min(m0 + r, a.m - 1) * a.ld_y; });
         sx.set_rows(tid, [&](int r) {
             const bool second = PAIR && (r >> 4 & 1);
             return static_cast<const T*>(second ? a.x[1] : a.x[0]) + row_of_x(r) * (second ? a.ld_x[1] : a.ld_x[0]);
         });
-        accumulate<S, T, false>(acc, sy, sx, S::kDirect ? full : 0, full, rest, full, a.k, 0, 0);
+        if constexpr (S::kDirect) accumulate_rest<S, T>(acc, sy, sx, 2 * pairs, a.k, 0, 0);
+        else accumulate<S, T, false>(acc, sy, sx, 0, full, a.k % S::kDeep, full, a.k, 0, 0);
     }
     if constexpr (S::kDirect) {
-        // a load of a wave is 16 rows, and a lane's units are an even number of them apart: with two matrices, all of one
-        static_assert(S::kThreads / 64 % 2 == 0);
-        const bool second = PAIR && (wave & 1);
+        // a load of a wave is 8 rows, and a lane's are a multiple of 32 apart: with two matrices, all of one
+        static_assert(S::kThreads / 8 % 32 == 0);
+        const bool second = PAIR && (wave >> 1 & 1);
         const int64_t ld_x = second ? a.ld_x[1] : a.ld_x[0];
         sy.set_rows_direct(tid, y + m0 * a.ld_y, a.ld_y, [&](int r) { return min(m0 + r, a.m - 1) - m0; });
         sx.set_rows_direct(tid, static_cast<const T*>(second ? a.x[1] : a.x[0]) + n0 * ld_x, ld_x, [&](int r) { return row_of_x(r) - n0; });
-        accumulate_direct<S, T>(acc, sy, sx, lds0, 0, full);
+        accumulate_direct<S, T>(acc, sy, sx, lds0, 0, pairs);
     }
 }
 
@@ -667,18 +728,18 @@ __global__ __launch_bounds__(S::kThreads, 2) void plain_kernel(const PlainArgs a
     int tm, tn;
     place_of_tile(tile - product * per_product, a.tiles_m, a.tiles_n, &tm, &tn);
     const int64_t m0 = first_of_tile<ACROSS_Y && !CHECKED>(tm, S::BM, ACROSS_Y ? a.m_readable : a.m), n0 = first_of_tile<!CHECKED>(tn, S::BN, a.n);
-    const int64_t full = a.k / S::kDeep;
+    const int64_t full = a.k / (S::kDirect ? 2 * S::kDeep : S::kDeep);          // steps, or pairs of them
     int64_t step0 = 0, step1 = full;
     if (!alone) {
         step0 = full * part / a.split;
         step1 = full * (part + 1) / a.split;
     }
-    const bool rest = (alone || part == a.split - 1) && a.k % S::kDeep;
+    const bool rest = (alone || part == a.split - 1) && a.k % (S::kDirect ? 2 * S::kDeep : S::kDeep);
 
-    Side<T, S::BM, S::kThreads, S::kYUnits, S::kTM, ACROSS_Y> sy;
-    Side<T, S::BN, S::kThreads, S::kXUnits, S::kTN, true> sx;
+    Side<T, S::BM, S::kThreads, S::kYUnits, S::kTM, ACROSS_Y, S::kDirect> sy;
+    Side<T, S::BN, S::kThreads, S::kXUnits, S::kTN, true, S::kDirect> sx;
     sy.set_places(tid, lds0, wave / S::kWN * S::kTM);
-    sx.set_places(tid, lds0 + S::kY, wave % S::kWN * S::kTN);
+    sx.set_places(tid, S::kDirect ? lds0 : lds0 + S::kY, wave % S::kWN * S::kTN);
     Sums<S> acc;
     clear<S>(acc);
     for (int pair = product; pair < product + a.pairs; ++pair) {
@@ -689,7 +750,9 @@ __global__ __launch_bounds__(S::kThreads, 2) void plain_kernel(const PlainArgs a
             if constexpr (ACROSS_Y) sy.set_columns(tid, y + m0, a.ld_y);
             else sy.set_rows(tid, [&](int r) { return y + min(m0 + r, a.m - 1) * a.ld_y; });
             sx.set_columns(tid, x, ld_x);
-            accumulate<S, T, CHECKED>(acc, sy, sx, S::kDirect ? full : step0, S::kDirect ? full : step1, rest, full, a.k, (ACROSS_Y ? a.m_readable : a.m) - m0, a.n - n0);
+            const int64_t columns_y = (ACROSS_Y ? a.m_readable : a.m) - m0, columns_x = a.n - n0;
+            if constexpr (S::kDirect) accumulate_rest<S, T>(acc, sy, sx, 2 * full, a.k, columns_y, columns_x);
+            else accumulate<S, T, CHECKED>(acc, sy, sx, step0, step1, rest, full, a.k, columns_y, columns_x);
         }
         if constexpr (S::kDirect) {
             if constexpr (ACROSS_Y) sy.set_columns_direct(tid, y + m0, a.ld_y);
@@ -759,12 +822,12 @@ inline PlainPlan plain_plan(int64_t m, int64_t n, int64_t k, int32_t dtype, bool
     p.checked = far || n < p.size || (across_y && m < p.size);
     p.tiles_m = (m + p.size - 1) / p.size;
     p.tiles_n = (n + p.size - 1) / p.size;
-    const int64_t all = tiles(p.size), steps = k / (kStepBytes / dtype_size(dtype));
+    const int64_t all = tiles(p.size), steps = k / (kStepBytes / dtype_size(dtype)) / (p.direct ? 2 : 1) * (p.direct ? 2 : 1);
     const int64_t round = large ? kUnits : 2 * kUnits;      // the small tile's workgroups share a compute unit in pairs
     p.rest = all % round;
     // a part has eight steps at least (of each pair)
     p.split = p.rest ? std::max<int64_t>(1, std::min(round / p.rest, steps * pairs / 8)) : 1;
-    p.split = std::min(p.split, std::max<int64_t>(1, steps));
+    p.split = std::min(p.split, std::max<int64_t>(1, steps / 2));
     if (p.split == 1) p.rest = 0;
     p.whole = all - p.rest;
     return p;
