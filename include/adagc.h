@@ -563,7 +563,7 @@ int adagc_linear_logprobs(const void* x, int64_t ld_x, const void* weight, int64
 /*
  * Its gradients for the gradient d of the log-probabilities, the logits made again in pieces of the vocabulary: with p_j = exp(logp_j),
  *     d_z_j = d (1[j = target] - p_j),   d_x = scale d_z W,   d_weight = scale d_z^T x   (+ d_weight with accumulate = 1),
- * d_z being 0 for rows without a target and for rows of nothing but -inf.  With bf16 data d_z is rounded to bf16 before the products (off by
+ * d_z being 0 for rows without a target, rows of nothing but -inf and rows whose d is 0.  With bf16 data d_z is rounded to bf16 before the products (off by
  * 2^-9 of itself at most, rounded to nearest even); sums are fp32.
  *   x, weight, targets, scale   as the forward call had them
  *   stats      DEVICE, the forward call's

@@ -42,53 +42,81 @@ template <class S, class T, bool BACKWARD>
 __global__ __launch_bounds__(S::kThreads, 2) void gated_kernel(const GatedArgs a)
 {
     __shared__ __attribute__((aligned(512))) uint8_t lds[S::kLds];
-    const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>(&lds[0]);
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    int tm, tn;
-    place_of_tile((int)blockIdx.x, a.p.tiles_m, a.p.tiles_n, &tm, &tn);
-    const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * (S::BN / 2);
-    Sums<S> acc;
-    along_tile<S, T, true>(acc, a.p, lds0, m0, n0);
-
-    const int first_row = wave / S::kWN * S::kTM * 16 + lane % 16, first_col = wave % S::kWN * (S::kTN / 2) * 16 + lane / 16 * 4;
+    along_tiles<S, T, true>(a.p, lds, [](int64_t, int64_t) {}, [&](Sums<S>& acc, int64_t m0, int64_t n0, uint8_t*) __attribute__((always_inline)) {
+        const int t = thread_anew(), lane = t & 63, wave = t >> 6;
+        const int first_row = wave / S::kWN * S::kTM * 16 + lane % 16, first_col = wave % S::kWN * (S::kTN / 2) * 16 + lane / 16 * 4;
+        const int64_t row0 = m0 + first_row, col0 = n0 + first_col;
+        auto results = [&](int m, int n, f32x4_p& o) __attribute__((always_inline)) {
+            const f32x4_p &g = acc[m][n], &u = acc[m][n + 1];
 #pragma unroll
-    for (int m = 0; m < S::kTM; ++m) {
-        const int64_t row = m0 + first_row + m * 16;
-        if (row >= a.p.m) continue;
-#pragma unroll
-        for (int n = 0; n < S::kTN; n += 2) {
-            const int64_t col = n0 + first_col + n * 8;
-            if (col >= a.p.n) continue;
-            const f32x4_p g = acc[m][n], u = acc[m][n + 1];
-            f32x4_p o;
-            if constexpr (BACKWARD) {
-                const f32x4_p d = load4(static_cast<const T*>(a.d_out) + row * a.ld_d_out, col, 0, a.p.n);
-                f32x4_p dg, du;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float of_gate, of_up;
-                    slopes(g[r], u[r], &of_gate, &of_up);
-                    o[r] = of_up * u[r];
-                    dg[r] = d[r] * of_gate;
-                    du[r] = d[r] * of_up;
-                }
-                store4(static_cast<T*>(a.gate) + row * a.ld_gate, col, 0, a.p.n, dg);
-                store4(static_cast<T*>(a.up) + row * a.ld_up, col, 0, a.p.n, du);
-            } else {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float t, rest;
-                    sigmoid(g[r], &t, &rest);
-                    o[r] = silu(g[r], t) * u[r];
-                }
-                if (a.gate) {
-                    store4(static_cast<T*>(a.gate) + row * a.ld_gate, col, 0, a.p.n, g);
-                    store4(static_cast<T*>(a.up) + row * a.ld_up, col, 0, a.p.n, u);
-                }
+            for (int r = 0; r < 4; ++r) {
+                float t, rest;
+                sigmoid(g[r], &t, &rest);
+                o[r] = silu(g[r], t) * u[r];
             }
-            if (!BACKWARD || a.out) store4(static_cast<T*>(a.out) + row * a.ld_out, col, 0, a.p.n, o);
+        };
+        auto gradients = [&](int m, int n, const f32x4_p& d, f32x4_p& o, f32x4_p& dg, f32x4_p& du) __attribute__((always_inline)) {
+            const f32x4_p &g = acc[m][n], &u = acc[m][n + 1];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float of_gate, of_up;
+                slopes(g[r], u[r], &of_gate, &of_up);
+                o[r] = of_up * u[r];
+                dg[r] = d[r] * of_gate;
+                du[r] = d[r] * of_up;
+            }
+        };
+        if (m0 + S::BM <= a.p.m && n0 + S::BN / 2 <= a.p.n) {
+            // a tile inside: one address for each array, no checks
+            T* out = static_cast<T*>(a.out) + row0 * a.ld_out + col0;
+            T *gate = static_cast<T*>(a.gate) + row0 * a.ld_gate + col0, *up = static_cast<T*>(a.up) + row0 * a.ld_up + col0;
+            const T* d_out = static_cast<const T*>(a.d_out) + row0 * a.ld_d_out + col0;
+#pragma unroll
+            for (int m = 0; m < S::kTM; ++m)
+#pragma unroll
+                for (int n = 0; n < S::kTN; n += 2) {
+                    f32x4_p o;
+                    if constexpr (BACKWARD) {
+                        f32x4_p dg, du;
+                        gradients(m, n, load4(d_out + m * 16 * a.ld_d_out + n * 8), o, dg, du);
+                        store4(gate + m * 16 * a.ld_gate + n * 8, dg);
+                        store4(up + m * 16 * a.ld_up + n * 8, du);
+                    } else {
+                        results(m, n, o);
+                        if (a.gate) {
+                            store4(gate + m * 16 * a.ld_gate + n * 8, acc[m][n]);
+                            store4(up + m * 16 * a.ld_up + n * 8, acc[m][n + 1]);
+                        }
+                    }
+                    if (!BACKWARD || a.out) store4(out + m * 16 * a.ld_out + n * 8, o);
+                }
+            return;
         }
-    }
+#pragma unroll
+        for (int m = 0; m < S::kTM; ++m) {
+            const int64_t row = row0 + m * 16;
+            if (row >= a.p.m) continue;
+#pragma unroll
+            for (int n = 0; n < S::kTN; n += 2) {
+                const int64_t col = col0 + n * 8;
+                if (col >= a.p.n) continue;
+                f32x4_p o;
+                if constexpr (BACKWARD) {
+                    f32x4_p dg, du;
+                    gradients(m, n, load4(static_cast<const T*>(a.d_out) + row * a.ld_d_out, col, 0, a.p.n), o, dg, du);
+                    store4(static_cast<T*>(a.gate) + row * a.ld_gate, col, 0, a.p.n, dg);
+                    store4(static_cast<T*>(a.up) + row * a.ld_up, col, 0, a.p.n, du);
+                } else {
+                    results(m, n, o);
+                    if (a.gate) {
+                        store4(static_cast<T*>(a.gate) + row * a.ld_gate, col, 0, a.p.n, acc[m][n]);
+                        store4(static_cast<T*>(a.up) + row * a.ld_up, col, 0, a.p.n, acc[m][n + 1]);
+                    }
+                }
+                if (!BACKWARD || a.out) store4(static_cast<T*>(a.out) + row * a.ld_out, col, 0, a.p.n, o);
+            }
+        }
+    });
 }
 
 struct KeptArgs {
@@ -162,7 +190,7 @@ int projections(GatedArgs a, hipStream_t s)
     a.p.tiles_n = (int32_t)p.tiles_n;
     const dim3 grid((uint32_t)(p.tiles_m * p.tiles_n));
     if constexpr (sizeof(T) == 2) {
-        if (p.large) gated_kernel<Large, T, BACKWARD><<<grid, dim3(Large::kThreads), 0, s>>>(a);
+        if (p.large) gated_kernel<Large, T, BACKWARD><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
         else if (p.direct) gated_kernel<Small, T, BACKWARD><<<grid, dim3(Small::kThreads), 0, s>>>(a);
     }
     if (!p.direct) gated_kernel<Staged<T>, T, BACKWARD><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);

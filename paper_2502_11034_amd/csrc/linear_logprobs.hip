@@ -30,67 +30,82 @@ template <class S, class T>
 __global__ __launch_bounds__(S::kThreads, 2) void stats_kernel(const StatsArgs a)
 {
     __shared__ __attribute__((aligned(512))) uint8_t lds[S::kLds];
-    const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>(&lds[0]);
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    int tm, tn;
-    place_of_tile((int)blockIdx.x, a.p.tiles_m, a.p.tiles_n, &tm, &tn);
-    const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
-    Sums<S> acc;
-    along_tile<S, T, false>(acc, a.p, lds0, m0, n0);
-
     const float c = a.scale * kLog2e;
-    if (n0 + S::BN > a.p.n) {
-        each_piece<S>(acc, [&](int m, int n, int, int col, const f32x4_p&) __attribute__((always_inline)) {
+    int target[S::kTM];            // its column from the lane's first one, if in the wave's columns
+    auto before = [&](int64_t m0, int64_t n0) __attribute__((always_inline)) {
+        const LanePlace<S> at;
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (n0 + col + r >= a.p.n) acc[m][n][r] = -__builtin_inff();
-        });
-    }
-    float2* shared = reinterpret_cast<float2*>(lds);       // [BM][kWN]
-    const int first_row = wave / S::kWN * S::kTM * 16 + lane % 16, first_col = wave % S::kWN * S::kTN * 16 + lane / 16 * 4;
+        for (int m = 0; m < S::kTM; ++m) {
+            const int64_t row = m0 + at.row + m * 16;
+            target[m] = -1;
+            if (a.targets && row < a.p.m) {
+                const int64_t t = a.targets[row];
+                if (t >= n0 + at.col && t < min(n0 + at.col + S::kTN * 16, a.p.n)) target[m] = (int)(t - n0 - at.col);
+            }
+        }
+        settle_now(target);
+    };
+    along_tiles<S, T, false>(a.p, lds, before, [&](Sums<S>& acc, int64_t m0, int64_t n0, uint8_t* scratch) __attribute__((always_inline)) {
+        const LanePlace<S> at;
+        const int tid = thread_anew(), lane = tid & 63, wave = tid >> 6;
+        if (n0 + S::BN > a.p.n) {
+            each_piece<S>(acc, [&](int m, int n, int, int col, const f32x4_p&) __attribute__((always_inline)) {
 #pragma unroll
-    for (int m = 0; m < S::kTM; ++m) {
-        float most = -__builtin_inff();
+                for (int r = 0; r < 4; ++r)
+                    if (n0 + col + r >= a.p.n) acc[m][n][r] = -__builtin_inff();
+            });
+        }
+        float2* shared = reinterpret_cast<float2*>(scratch);       // [BM][kWN]
 #pragma unroll
-        for (int n = 0; n < S::kTN; ++n)
+        for (int m = 0; m < S::kTM; ++m) {
+            float most = -__builtin_inff();
 #pragma unroll
-            for (int r = 0; r < 4; ++r) most = maximum(most, acc[m][n][r]);
-        most = maximum(most, __shfl_xor(most, 16));
-        most = maximum(most, __shfl_xor(most, 32));
-        const float from = most == -__builtin_inff() ? 0.f : most;
-        float sum = 0.f;
+            for (int n = 0; n < S::kTN; ++n)
 #pragma unroll
-        for (int n = 0; n < S::kTN; ++n)
+                for (int r = 0; r < 4; ++r) most = maximum(most, acc[m][n][r]);
+            most = maximum(most, __shfl_xor(most, 16));
+            most = maximum(most, __shfl_xor(most, 32));
+            // relative to from, most c as an fp32 number: an exponent is rounded once, and the sum then put right for what that number is off by
+            const float from = most == -__builtin_inff() ? 0.f : most * c;
+            float sum = 0.f;
+            if (__builtin_fabsf(from) < 0x1p20f) {         // (then it is off by less than 2^-4)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f((acc[m][n][r] - from) * c);
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
-        const int row = first_row + m * 16;
-        if (lane < 16) shared[row * S::kWN + wave % S::kWN] = float2{most, sum};
-        if (a.targets && m0 + row < a.p.m) {
-            const int64_t t = a.targets[m0 + row] - n0 - first_col;
-            if (t >= 0 && t < S::kTN * 16) {               // in this wave's columns, if in the right four of 16
+                for (int n = 0; n < S::kTN; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[m][n][r], c, -from));
+                if (from != 0.f) sum *= __builtin_amdgcn_exp2f(-__builtin_fmaf(most, c, -from));
+            } else {
+#pragma unroll
+                for (int n = 0; n < S::kTN; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f((acc[m][n][r] - most) * c);
+            }
+            sum += __shfl_xor(sum, 16);
+            sum += __shfl_xor(sum, 32);
+            const int row = at.row + m * 16;
+            if (lane < 16) shared[row * S::kWN + wave % S::kWN] = float2{most, sum};
+            if (target[m] >= 0) {
 #pragma unroll
                 for (int n = 0; n < S::kTN; ++n)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        if ((int)t == n * 16 + r && n0 + first_col + t < a.p.n) a.target_logit[m0 + row] = acc[m][n][r];
+                        if (target[m] == n * 16 + r) a.target_logit[m0 + row] = acc[m][n][r];
             }
         }
-    }
-    __syncthreads();
-    if (tid < S::BM && m0 + tid < a.p.m) {
-        float2 part[S::kWN];
-        float most = -__builtin_inff(), sum = 0.f;
+        meet_keeping_loads();
+        if (tid < S::BM && m0 + tid < a.p.m) {
+            float2 part[S::kWN];
+            float most = -__builtin_inff(), sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < S::kWN; ++w) {
-            part[w] = shared[tid * S::kWN + w];
-            most = maximum(most, part[w].x);
+            for (int w = 0; w < S::kWN; ++w) {
+                part[w] = shared[tid * S::kWN + w];
+                most = maximum(most, part[w].x);
+            }
+#pragma unroll
+            for (int w = 0; w < S::kWN; ++w) sum += rescaled(part[w].x, part[w].y, most, c);
+            a.parts[(m0 + tid) * a.p.tiles_n + n0 / S::BN] = float2{most, sum};
         }
-#pragma unroll
-        for (int w = 0; w < S::kWN; ++w) sum += rescaled(part[w].x, part[w].y, most, c);
-        a.parts[(m0 + tid) * a.p.tiles_n + tn] = float2{most, sum};
-    }
+    });
 }
 
 struct JoinArgs {
@@ -159,37 +174,46 @@ template <class S, class T>
 __global__ __launch_bounds__(S::kThreads, 2) void grad_kernel(const GradArgs a)
 {
     __shared__ __attribute__((aligned(512))) uint8_t lds[S::kLds];
-    const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>(&lds[0]);
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    int tm, tn;
-    place_of_tile((int)blockIdx.x, a.p.tiles_m, a.p.tiles_n, &tm, &tn);
-    const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
-    Sums<S> acc;
-    along_tile<S, T, false>(acc, a.p, lds0, m0, n0);
-
     const float c = a.scale * kLog2e;
-    const int first_row = wave / S::kWN * S::kTM * 16 + lane % 16, first_col = wave % S::kWN * S::kTN * 16 + lane / 16 * 4;
+    // of a row: the target's column from the lane's first one (or none of them), M, L in powers of two, d (0: all of the row's gradients are 0)
+    int target[S::kTM];
+    float most[S::kTM], log2_sum[S::kTM], d[S::kTM];
+    auto before = [&](int64_t m0, int64_t n0) __attribute__((always_inline)) {
+        const LanePlace<S> at;
 #pragma unroll
-    for (int m = 0; m < S::kTM; ++m) {
-        const int64_t row = m0 + first_row + m * 16;
-        if (row >= a.p.m) continue;
-        const int64_t target = a.targets[row];
-        const bool has = target >= 0 && target < a.vocab;
-        const float most = a.stats[2 * row], log2_sum = a.stats[2 * row + 1] * kLog2e, d = a.d_logprob[row];
-        const bool zero = !has || most == -__builtin_inff();
-        const int64_t t = target - a.first - n0 - first_col;
-        T* to = static_cast<T*>(a.d_logits) + row * a.ld;
-#pragma unroll
-        for (int n = 0; n < S::kTN; ++n) {
-            f32x4_p v;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float p = __builtin_amdgcn_exp2f((acc[m][n][r] - most) * c - log2_sum);
-                v[r] = zero ? 0.f : ((t == n * 16 + r ? 1.f : 0.f) - p) * d;
-            }
-            store4(to, n0 + first_col + n * 16, 0, a.p.n, v);
+        for (int m = 0; m < S::kTM; ++m) {
+            const int64_t row = min(m0 + at.row + m * 16, a.p.m - 1), t = a.targets[row];
+            most[m] = a.stats[2 * row];
+            log2_sum[m] = a.stats[2 * row + 1] * kLog2e;
+            d[m] = a.d_logprob[row];
+            const int64_t from = t - a.first - n0 - at.col;
+            target[m] = from >= 0 && from < S::kTN * 16 ? (int)from : -1;
+            if (t < 0 || t >= a.vocab || most[m] == -__builtin_inff()) d[m] = 0.f;
         }
-    }
+        settle_now(target);
+        settle_now(most);
+        settle_now(log2_sum);
+        settle_now(d);
+    };
+    along_tiles<S, T, false>(a.p, lds, before, [&](Sums<S>& acc, int64_t m0, int64_t n0, uint8_t*) __attribute__((always_inline)) {
+        const LanePlace<S> at;
+#pragma unroll
+        for (int m = 0; m < S::kTM; ++m) {
+            const int64_t row = m0 + at.row + m * 16;
+            if (row >= a.p.m) continue;
+            T* to = static_cast<T*>(a.d_logits) + row * a.ld + n0 + at.col;
+#pragma unroll
+            for (int n = 0; n < S::kTN; ++n) {
+                f32x4_p v;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float p = __builtin_amdgcn_exp2f((acc[m][n][r] - most[m]) * c - log2_sum[m]);
+                    v[r] = d[m] == 0.f ? 0.f : ((target[m] == n * 16 + r ? 1.f : 0.f) - p) * d[m];
+                }
+                store4(to + n * 16, v);            // (columns past the piece's end are within ld, and not read)
+            }
+        }
+    });
 }
 
 int check(int64_t rows, int64_t vocab, int64_t dim, int32_t dtype)
@@ -219,7 +243,7 @@ Pieces pieces_of(int64_t rows, int64_t vocab, int64_t dim, int32_t dtype)
     p.number = (vocab + most - 1) / most;
     p.size = p.number == 1 ? vocab : ((vocab + p.number - 1) / p.number + 255) / 256 * 256;
     p.number = (vocab + p.size - 1) / p.size;
-    p.ld = (p.size + 127) / 128 * 128;
+    p.ld = (p.size + 255) / 256 * 256;
     p.d_logits = up16(rows * p.ld * dtype_size(dtype));
     p.sums = p.number > 1 && dtype == ADAGC_BF16 ? up16(rows * dim * 4) : 0;
     for (const int64_t n : {p.size, vocab - (p.number - 1) * p.size})
@@ -263,7 +287,7 @@ int forward(StatsArgs a, const JoinArgs& join, hipStream_t s)
     const AlongPlan p = plan_of(&a.p, sizeof(T) == 4 ? ADAGC_F32 : ADAGC_BF16);
     const dim3 grid((uint32_t)(p.tiles_m * p.tiles_n));
     if constexpr (sizeof(T) == 2) {
-        if (p.large) stats_kernel<Large, T><<<grid, dim3(Large::kThreads), 0, s>>>(a);
+        if (p.large) stats_kernel<Large, T><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
         else if (p.direct) stats_kernel<Small, T><<<grid, dim3(Small::kThreads), 0, s>>>(a);
     }
     if (!p.direct) stats_kernel<Staged<T>, T><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
@@ -279,7 +303,7 @@ int gradient(GradArgs a, hipStream_t s)
     const AlongPlan p = plan_of(&a.p, sizeof(T) == 4 ? ADAGC_F32 : ADAGC_BF16);
     const dim3 grid((uint32_t)(p.tiles_m * p.tiles_n));
     if constexpr (sizeof(T) == 2) {
-        if (p.large) grad_kernel<Large, T><<<grid, dim3(Large::kThreads), 0, s>>>(a);
+        if (p.large) grad_kernel<Large, T><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
         else if (p.direct) grad_kernel<Small, T><<<grid, dim3(Small::kThreads), 0, s>>>(a);
     }
     if (!p.direct) grad_kernel<Staged<T>, T><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
