@@ -119,6 +119,44 @@ __global__ __launch_bounds__(S::kThreads, 2) void gated_kernel(const GatedArgs a
     });
 }
 
+// Few rows: a thread for each result.
+template <class T, int TM, bool BACKWARD>
+__global__ __launch_bounds__(kThinThreads, 4) void thin_gated_kernel(const GatedArgs a)
+{
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kThinLds<TM>];
+    constexpr int kColumns = kThinColumns / 2;
+    float d = 0.f;
+    auto before = [&](int64_t n0) __attribute__((always_inline)) {
+        const int64_t row = threadIdx.x / kColumns, col = n0 + threadIdx.x % kColumns;
+        if (BACKWARD && row < a.p.m && col < a.p.n) d = to_float(static_cast<const T*>(a.d_out)[row * a.ld_d_out + col]);
+    };
+    thin_tiles<T, TM, true>(a.p, lds, before, [&](int64_t n0, int64_t row, int at, float g, float u) __attribute__((always_inline)) {
+        const int64_t col = n0 + at;
+        if (row >= a.p.m || col >= a.p.n) return;
+        auto store = [](void* to, int64_t at, float v) __attribute__((always_inline)) {
+            if constexpr (sizeof(T) == 4) static_cast<T*>(to)[at] = v;
+            else static_cast<T*>(to)[at] = __builtin_bit_cast(uint16_t, (__bf16)v);
+        };
+        float o;
+        if constexpr (BACKWARD) {
+            float of_gate, of_up;
+            slopes(g, u, &of_gate, &of_up);
+            o = of_up * u;
+            store(a.gate, row * a.ld_gate + col, d * of_gate);
+            store(a.up, row * a.ld_up + col, d * of_up);
+        } else {
+            float t, rest;
+            sigmoid(g, &t, &rest);
+            o = silu(g, t) * u;
+            if (a.gate) {
+                store(a.gate, row * a.ld_gate + col, g);
+                store(a.up, row * a.ld_up + col, u);
+            }
+        }
+        if (!BACKWARD || a.out) store(a.out, row * a.ld_out + col, o);
+    });
+}
+
 struct KeptArgs {
     const void *d_out, *gate, *up;
     void *      d_gate, *d_up, *out;
@@ -189,11 +227,15 @@ int projections(GatedArgs a, hipStream_t s)
     a.p.tiles_m = (int32_t)p.tiles_m;
     a.p.tiles_n = (int32_t)p.tiles_n;
     const dim3 grid((uint32_t)(p.tiles_m * p.tiles_n));
-    if constexpr (sizeof(T) == 2) {
+    const bool few = thin(a.p, sizeof(T) == 4 ? ADAGC_F32 : ADAGC_BF16);
+    if (few) {
+        const dim3 blocks((uint32_t)std::min<int64_t>((a.p.n + kThinColumns / 2 - 1) / (kThinColumns / 2), kThinGrid));
+        for_rows(a.p.m, [&](auto TM) { thin_gated_kernel<T, decltype(TM)::value, BACKWARD><<<blocks, dim3(kThinThreads), 0, s>>>(a); });
+    } else if constexpr (sizeof(T) == 2) {
         if (p.large) gated_kernel<Large, T, BACKWARD><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
         else if (p.direct) gated_kernel<Small, T, BACKWARD><<<grid, dim3(Small::kThreads), 0, s>>>(a);
     }
-    if (!p.direct) gated_kernel<Staged<T>, T, BACKWARD><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+    if (!few && !p.direct) gated_kernel<Staged<T>, T, BACKWARD><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
     return hipGetLastError() == hipSuccess ? ADAGC_OK : ADAGC_ERR_HIP;
 }
 

@@ -108,6 +108,29 @@ __global__ __launch_bounds__(S::kThreads, 2) void stats_kernel(const StatsArgs a
     });
 }
 
+// Few rows: a thread for each value.
+template <class T, int TM>
+__global__ __launch_bounds__(kThinThreads, 4) void thin_stats_kernel(const StatsArgs a)
+{
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kThinLds<TM>];
+    const int own_row = threadIdx.x / kThinColumns;
+    const int64_t target = a.targets && own_row < a.p.m ? a.targets[own_row] : -1;
+    const float c = a.scale * kLog2e;
+    thin_tiles<T, TM, false>(a.p, lds, [](int64_t) {}, [&](int64_t n0, int row, int at, float z, float) __attribute__((always_inline)) {
+        if (row >= a.p.m) return;                          // (whole halves of waves)
+        const int64_t col = n0 + at;
+        if (col >= a.p.n) z = -__builtin_inff();
+        float most = z;
+#pragma unroll
+        for (int d = 1; d < kThinColumns; d *= 2) most = maximum(most, __shfl_xor(most, d));
+        float sum = __builtin_amdgcn_exp2f((z - (most == -__builtin_inff() ? 0.f : most)) * c);
+#pragma unroll
+        for (int d = 1; d < kThinColumns; d *= 2) sum += __shfl_xor(sum, d);
+        if (at == 0) a.parts[row * (int64_t)a.p.tiles_n + n0 / kThinColumns] = float2{most, sum};
+        if (target == col && col < a.p.n) a.target_logit[row] = z;
+    });
+}
+
 struct JoinArgs {
     const float2*  parts;
     const float*   target_logit;
@@ -216,6 +239,24 @@ __global__ __launch_bounds__(S::kThreads, 2) void grad_kernel(const GradArgs a)
     });
 }
 
+template <class T, int TM>
+__global__ __launch_bounds__(kThinThreads, 4) void thin_grad_kernel(const GradArgs a)
+{
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kThinLds<TM>];
+    const int64_t own_row = min((int64_t)threadIdx.x / kThinColumns, a.p.m - 1), target = a.targets[own_row];
+    const float most = a.stats[2 * own_row], log2_sum = a.stats[2 * own_row + 1] * kLog2e, c = a.scale * kLog2e;
+    const float d = target < 0 || target >= a.vocab || most == -__builtin_inff() ? 0.f : a.d_logprob[own_row];
+    thin_tiles<T, TM, false>(a.p, lds, [](int64_t) {}, [&](int64_t n0, int row, int at, float z, float) __attribute__((always_inline)) {
+        if (row >= a.p.m) return;
+        const int64_t col = n0 + at;                       // (columns past the piece's end are within ld, and not read)
+        const float p = __builtin_amdgcn_exp2f((z - most) * c - log2_sum);
+        const float v = d == 0.f ? 0.f : ((target - a.first == col ? 1.f : 0.f) - p) * d;
+        T* to = static_cast<T*>(a.d_logits) + row * a.ld + col;
+        if constexpr (sizeof(T) == 4) *to = v;
+        else *to = __builtin_bit_cast(uint16_t, (__bf16)v);
+    });
+}
+
 int check(int64_t rows, int64_t vocab, int64_t dim, int32_t dtype)
 {
     if (rows < 0 || vocab < 1 || dim < 1 || !known_dtype(dtype)) return ADAGC_ERR_INVALID_ARG;
@@ -225,9 +266,11 @@ int check(int64_t rows, int64_t vocab, int64_t dim, int32_t dtype)
 bool scale_in_range(float scale) { return scale >= 0x1p-100f && scale <= 0x1p100f; }
 int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 
+// at most: of the smallest tile
+int64_t parts_of_row(int64_t rows, int64_t vocab) { return rows <= kThinRows ? (vocab + kThinColumns - 1) / kThinColumns : (vocab + 127) / 128; }
 int64_t forward_workspace(int64_t rows, int64_t vocab)
 {
-    return up16(rows * ((vocab + 127) / 128) * 8) + rows * 4;          // the small tile's parts
+    return up16(rows * parts_of_row(rows, vocab) * 8) + rows * 4;
 }
 
 // Pieces of the vocabulary: 2^26 gradients of logits a piece, which the memory-side cache holds as bf16, and 2048 columns at least.
@@ -286,11 +329,15 @@ int forward(StatsArgs a, const JoinArgs& join, hipStream_t s)
 {
     const AlongPlan p = plan_of(&a.p, sizeof(T) == 4 ? ADAGC_F32 : ADAGC_BF16);
     const dim3 grid((uint32_t)(p.tiles_m * p.tiles_n));
-    if constexpr (sizeof(T) == 2) {
+    const bool few = thin(a.p, sizeof(T) == 4 ? ADAGC_F32 : ADAGC_BF16);
+    if (few) {
+        a.p.tiles_n = (int32_t)((a.p.n + kThinColumns - 1) / kThinColumns);
+        for_rows(a.p.m, [&](auto TM) { thin_stats_kernel<T, decltype(TM)::value><<<dim3(std::min(a.p.tiles_n, kThinGrid)), dim3(kThinThreads), 0, s>>>(a); });
+    } else if constexpr (sizeof(T) == 2) {
         if (p.large) stats_kernel<Large, T><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
         else if (p.direct) stats_kernel<Small, T><<<grid, dim3(Small::kThreads), 0, s>>>(a);
     }
-    if (!p.direct) stats_kernel<Staged<T>, T><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+    if (!few && !p.direct) stats_kernel<Staged<T>, T><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
     JoinArgs j = join;
     j.tiles = a.p.tiles_n;
     join_kernel<<<dim3((uint32_t)a.p.m), dim3(kJoin), 0, s>>>(j);
@@ -302,11 +349,15 @@ int gradient(GradArgs a, hipStream_t s)
 {
     const AlongPlan p = plan_of(&a.p, sizeof(T) == 4 ? ADAGC_F32 : ADAGC_BF16);
     const dim3 grid((uint32_t)(p.tiles_m * p.tiles_n));
-    if constexpr (sizeof(T) == 2) {
+    const bool few = thin(a.p, sizeof(T) == 4 ? ADAGC_F32 : ADAGC_BF16);
+    if (few) {
+        const dim3 blocks((uint32_t)std::min<int64_t>((a.p.n + kThinColumns - 1) / kThinColumns, kThinGrid));
+        for_rows(a.p.m, [&](auto TM) { thin_grad_kernel<T, decltype(TM)::value><<<blocks, dim3(kThinThreads), 0, s>>>(a); });
+    } else if constexpr (sizeof(T) == 2) {
         if (p.large) grad_kernel<Large, T><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
         else if (p.direct) grad_kernel<Small, T><<<grid, dim3(Small::kThreads), 0, s>>>(a);
     }
-    if (!p.direct) grad_kernel<Staged<T>, T><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+    if (!few && !p.direct) grad_kernel<Staged<T>, T><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
     return hipGetLastError() == hipSuccess ? ADAGC_OK : ADAGC_ERR_HIP;
 }
 
@@ -414,7 +465,7 @@ extern "C" int adagc_linear_logprobs(const void* x, int64_t ld_x, const void* we
     a.targets = logprob ? targets : nullptr;
     a.scale = scale;
     a.parts = static_cast<float2*>(workspace);
-    a.target_logit = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + up16(rows * ((vocab + 127) / 128) * 8));
+    a.target_logit = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + up16(rows * parts_of_row(rows, vocab) * 8));
     JoinArgs j{};
     j.parts = a.parts;
     j.target_logit = a.target_logit;

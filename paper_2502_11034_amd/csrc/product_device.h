@@ -766,6 +766,148 @@ __device__ __forceinline__ void meet_keeping_loads()
     ADAGC_P_FENCE();
 }
 
+// ---- few rows
+//
+// Up to 16 rows of Y: memory bounds it, the rows of X that go past once.  A workgroup of 8 waves has 32 rows of X at a time (of two matrices 16
+// each) and all of Y; its waves share k out and their sums meet in LDS, in their order.  Operands go from memory to registers as the matrix
+// cores want them, a batch on its way while one is multiplied, the next rows' first one while the sums meet.
+//
+// A load takes 128 bytes each of 8 rows, whole lines of the cache (of the instruction's natural 16 rows 64 bytes each, lines came from
+// memory twice where they had left the L2 between the halves: one row, 128256 x 4096 bf16 215 - 255 us, with loads past the caches 296).  So an
+// operand of 16 rows is 8 rows with the first 64 bytes and the same 8 with the second; of the 16 x 16 results the quadrants that belong together
+// are added, the others not used.
+constexpr int kThinRows = 16, kThinColumns = 32, kThinWaves = 8, kThinThreads = 64 * kThinWaves, kThinBlocks = kThinColumns / 8;
+template <int TM>
+constexpr int kThinLds = kThinWaves * TM * kThinBlocks * 64 * 16;
+constexpr int kThinGrid = 2 * kUnits;      // workgroups that fill the chip
+
+// The workgroup's rows of X; k is a vector at least.  before(n0): loads for finish; finish(n0, row, col, sum, sum_of_second): of row `row` of Y with row n0 + col of X (of
+// each), a thread for each: all threads call it, those with row 8 TM or more, or beyond the matrices, with nothing.
+template <class T, int TM, bool PAIR, class Before, class Finish>
+__device__ __forceinline__ void thin_tiles(const AlongArgs& a, uint8_t* lds, Before&& before, Finish&& finish)
+{
+    constexpr int kE = 16 / (int)sizeof(T), kDeep = 2 * kStepBytes / (int)sizeof(T), kU = 1, kB = kThinBlocks;
+    constexpr int kColumns = PAIR ? kThinColumns / 2 : kThinColumns;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lane_k = (lane / 8 % 2 * 4 + lane / 16) * kE, k = (int)a.k;
+    const int full = k / kDeep, steps = (k + kDeep - 1) / kDeep;           // the last one may be cut
+    const int first = __builtin_amdgcn_readfirstlane((int)((int64_t)steps * wave / kThinWaves));
+    const int own = __builtin_amdgcn_readfirstlane((int)((int64_t)steps * (wave + 1) / kThinWaves)) - first;
+    const T *y[TM], *x[kB];
+#pragma unroll
+    for (int m = 0; m < TM; ++m) y[m] = static_cast<const T*>(a.y) + min((int64_t)(m * 8 + lane % 8), a.m - 1) * a.ld_y;
+    auto aim = [&](int64_t n0) __attribute__((always_inline)) {
+        const int l = thread_anew();
+#pragma unroll
+        for (int n = 0; n < kB; ++n) {
+            const bool second = PAIR && (n & 1);
+            const int64_t row = min(n0 + (PAIR ? n / 2 : n) * 8 + l % 8, a.n - 1);
+            x[n] = static_cast<const T*>(second ? a.x[1] : a.x[0]) + row * (second ? a.ld_x[1] : a.ld_x[0]);
+        }
+    };
+    struct Batch {
+        u32x4 y[kU][TM], x[kU][kB];
+    };
+    // a batch's steps that do not exist are the last one again, and not multiplied
+    auto load = [&](int i, Batch& b) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            const int at = min((first + min(i + u, own - 1)) * kDeep + lane_k, k - kE);       // (k's last vector is put right in use)
+#pragma unroll
+            for (int n = 0; n < kB; ++n) b.x[u][n] = load_whole(x[n] + at).w;
+#pragma unroll
+            for (int m = 0; m < TM; ++m) b.y[u][m] = load_whole(y[m] + at).w;
+        }
+    };
+    f32x4_p acc[TM][kB];
+    auto use = [&](int i, Batch& b) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < kU; ++u)
+            if (i + u < own) {
+                if (first + i + u == full) {
+                    const int l = thread_anew() & 63, col = full * kDeep + (l / 8 % 2 * 4 + l / 16) * kE;
+                    auto cut = [&](u32x4& w) __attribute__((always_inline)) {
+                        Vector<T> v{w};
+                        settle(v, col, k, 0);
+                        w = v.w;
+                    };
+#pragma unroll
+                    for (int m = 0; m < TM; ++m) cut(b.y[u][m]);
+#pragma unroll
+                    for (int n = 0; n < kB; ++n) cut(b.x[u][n]);
+                }
+#pragma unroll
+                for (int m = 0; m < TM; ++m)
+#pragma unroll
+                    for (int n = 0; n < kB; ++n) multiply<T>(b.x[u][n], b.y[u][m], acc[m][n]);
+            }
+    };
+    const int64_t step = (int64_t)gridDim.x * kColumns;
+    int64_t n0 = (int64_t)blockIdx.x * kColumns;
+    Batch b[2];
+    aim(n0);
+    if (own > 0) load(0, b[0]);
+    while (true) {
+#pragma unroll
+        for (int m = 0; m < TM; ++m)
+#pragma unroll
+            for (int n = 0; n < kB; ++n) acc[m][n] = f32x4_p{0.f, 0.f, 0.f, 0.f};
+        before(n0);
+        const int64_t next = n0 + step;
+        if (own > 0) {
+            int i = 0;
+            for (; i + 2 * kU < own; i += 2 * kU) {
+                load(i + kU, b[1]);
+                use(i, b[0]);
+                load(i + 2 * kU, b[0]);
+                use(i + kU, b[1]);
+            }
+            if (i + kU < own) load(i + kU, b[1]);
+            use(i, b[0]);
+            if (next < a.n) {
+                aim(next);
+                load(0, b[0]);
+            }
+            if (i + kU < own) use(i + kU, b[1]);
+        } else if (next < a.n) {
+            aim(next);
+        }
+        // value r of lane l: row (l mod 16) mod 8 of Y, row (4 (l / 16) + r) mod 8 of X; valid where both are in the same half
+        float* parts = reinterpret_cast<float*>(lds);
+        const int own_part = thread_anew() & 63;
+#pragma unroll
+        for (int m = 0; m < TM; ++m)
+#pragma unroll
+            for (int n = 0; n < kB; ++n) reinterpret_cast<f32x4_p*>(parts)[((wave * TM + m) * kB + n) * 64 + own_part] = acc[m][n];
+        meet_keeping_loads();
+        const int t = thread_anew(), row = t / kColumns, col = t % kColumns;
+        float sum[2] = {0.f, 0.f};
+        if (row < 8 * TM) {
+#pragma unroll
+            for (int p = 0; p < (PAIR ? 2 : 1); ++p) {
+                const int block = PAIR ? col / 8 * 2 + p : col / 8;
+                const float* from = parts + ((row / 8 * kB + block) * 64 + col % 8 / 4 * 16 + row % 8) * 4 + col % 4;
+#pragma unroll
+                for (int w = 0; w < kThinWaves; ++w) sum[p] += from[w * TM * kB * 256] + from[w * TM * kB * 256 + 40 * 4];
+            }
+        }
+        if (next < a.n) meet_keeping_loads();
+        finish(n0, row, col, sum[0], sum[1]);
+        if (next >= a.n) break;
+        n0 = next;
+    }
+}
+
+inline bool thin(const AlongArgs& a, int32_t dtype) { return a.m <= kThinRows && a.k >= 16 / dtype_size(dtype); }
+
+// f(integral_constant blocks of 8 rows) for up to kThinRows rows
+template <class F>
+inline void for_rows(int64_t rows, F&& f)
+{
+    if (rows <= 8) f(std::integral_constant<int, 1>{});
+    else f(std::integral_constant<int, 2>{});
+}
+
 // ---------------------------------------------------------------------------------------- a product with a plain result
 
 // out = (add +) factor times the sum over up to two pairs of operands, or two products side by side.
