@@ -232,10 +232,15 @@ int projections(GatedArgs a, hipStream_t s)
         const dim3 blocks((uint32_t)std::min<int64_t>((a.p.n + kThinColumns / 2 - 1) / (kThinColumns / 2), kThinGrid));
         for_rows(a.p.m, [&](auto TM) { thin_gated_kernel<T, decltype(TM)::value, BACKWARD><<<blocks, dim3(kThinThreads), 0, s>>>(a); });
     } else if constexpr (sizeof(T) == 2) {
-        if (p.large) gated_kernel<Large, T, BACKWARD><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
+        if (p.size == 256) gated_kernel<Large, T, BACKWARD><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
         else if (p.direct) gated_kernel<Small, T, BACKWARD><<<grid, dim3(Small::kThreads), 0, s>>>(a);
     }
-    if (!few && !p.direct) gated_kernel<Staged<T>, T, BACKWARD><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+    if (!few && !p.direct) {
+        if constexpr (sizeof(T) == 4) {
+            if (p.size == 64) gated_kernel<Smallest, T, BACKWARD><<<grid, dim3(Smallest::kThreads), 0, s>>>(a);
+        }
+        if (p.size == 128) gated_kernel<Staged<T>, T, BACKWARD><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+    }
     return hipGetLastError() == hipSuccess ? ADAGC_OK : ADAGC_ERR_HIP;
 }
 

@@ -266,8 +266,12 @@ int check(int64_t rows, int64_t vocab, int64_t dim, int32_t dtype)
 bool scale_in_range(float scale) { return scale >= 0x1p-100f && scale <= 0x1p100f; }
 int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 
-// at most: of the smallest tile
-int64_t parts_of_row(int64_t rows, int64_t vocab) { return rows <= kThinRows ? (vocab + kThinColumns - 1) / kThinColumns : (vocab + 127) / 128; }
+// at most: of the smallest tile that a call of this size may take
+int64_t parts_of_row(int64_t rows, int64_t vocab)
+{
+    const int64_t tile = rows <= kThinRows ? kThinColumns : ((rows + 127) / 128) * ((vocab + 127) / 128) < 4 * kUnits ? 64 : 128;
+    return (vocab + tile - 1) / tile;
+}
 int64_t forward_workspace(int64_t rows, int64_t vocab)
 {
     return up16(rows * parts_of_row(rows, vocab) * 8) + rows * 4;
@@ -334,10 +338,15 @@ int forward(StatsArgs a, const JoinArgs& join, hipStream_t s)
         a.p.tiles_n = (int32_t)((a.p.n + kThinColumns - 1) / kThinColumns);
         for_rows(a.p.m, [&](auto TM) { thin_stats_kernel<T, decltype(TM)::value><<<dim3(std::min(a.p.tiles_n, kThinGrid)), dim3(kThinThreads), 0, s>>>(a); });
     } else if constexpr (sizeof(T) == 2) {
-        if (p.large) stats_kernel<Large, T><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
+        if (p.size == 256) stats_kernel<Large, T><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
         else if (p.direct) stats_kernel<Small, T><<<grid, dim3(Small::kThreads), 0, s>>>(a);
     }
-    if (!few && !p.direct) stats_kernel<Staged<T>, T><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+    if (!few && !p.direct) {
+        if constexpr (sizeof(T) == 4) {
+            if (p.size == 64) stats_kernel<Smallest, T><<<grid, dim3(Smallest::kThreads), 0, s>>>(a);
+        }
+        if (p.size == 128) stats_kernel<Staged<T>, T><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+    }
     JoinArgs j = join;
     j.tiles = a.p.tiles_n;
     join_kernel<<<dim3((uint32_t)a.p.m), dim3(kJoin), 0, s>>>(j);
@@ -354,10 +363,15 @@ int gradient(GradArgs a, hipStream_t s)
         const dim3 blocks((uint32_t)std::min<int64_t>((a.p.n + kThinColumns - 1) / kThinColumns, kThinGrid));
         for_rows(a.p.m, [&](auto TM) { thin_grad_kernel<T, decltype(TM)::value><<<blocks, dim3(kThinThreads), 0, s>>>(a); });
     } else if constexpr (sizeof(T) == 2) {
-        if (p.large) grad_kernel<Large, T><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
+        if (p.size == 256) grad_kernel<Large, T><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
         else if (p.direct) grad_kernel<Small, T><<<grid, dim3(Small::kThreads), 0, s>>>(a);
     }
-    if (!few && !p.direct) grad_kernel<Staged<T>, T><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+    if (!few && !p.direct) {
+        if constexpr (sizeof(T) == 4) {
+            if (p.size == 64) grad_kernel<Smallest, T><<<grid, dim3(Smallest::kThreads), 0, s>>>(a);
+        }
+        if (p.size == 128) grad_kernel<Staged<T>, T><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+    }
     return hipGetLastError() == hipSuccess ? ADAGC_OK : ADAGC_ERR_HIP;
 }
 

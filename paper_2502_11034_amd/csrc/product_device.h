@@ -401,11 +401,12 @@ __device__ __forceinline__ void accumulate(Sums<S>& acc, const SideY& sy, const 
                 if constexpr (n == kTN - 1) y[m] = sy.read(m, next);
                 each<kMoves>([&](auto N) __attribute__((always_inline)) {
                     constexpr int w = decltype(N)::value;
-                    if constexpr (kSlots / 4 + w * (kSlots / 4) / kMoves + 1 == slot) {
+                    constexpr int kLate = kSlots >= 16 ? 1 : 0;
+                    if constexpr (kSlots / 4 + w * (kSlots / 4) / kMoves + kLate == slot) {
                         if constexpr (w < kYU) sy.write(w, to_place, staged[p].y[w]);
                         else sx.write(w - kYU, to_place, staged[p].x[w - kYU]);
                     }
-                    if constexpr (kSlots / 2 + 2 + w * (kSlots / 4) / kMoves == slot) {
+                    if constexpr (kSlots / 2 + w * (kSlots / 4) / kMoves + 1 + kLate == slot) {
                         if constexpr (w < kYU) staged[p].y[w] = sy.load(ahead, w);
                         else staged[p].x[w - kYU] = sx.load(ahead, w - kYU);
                     }
@@ -632,6 +633,7 @@ __device__ __forceinline__ f32x4_p load4(const T* row, int64_t col, int64_t leas
 using Large = Tile<uint16_t, 256, 256, 2, 4, true>;
 using Small = Tile<uint16_t, 128, 128, 2, 2, true>;
 template <class T> using Staged = Tile<T, 128, 128, 2, 2, false>;
+using Smallest = Tile<float, 64, 64, 2, 2, false>;
 
 // Rows of an operand start at multiples of 16 bytes.
 inline bool rows_aligned(const void* p, int64_t ld, int32_t dtype) { return !misaligned(p, 16) && ld * dtype_size(dtype) % 16 == 0; }
@@ -639,20 +641,26 @@ inline bool rows_aligned(const void* p, int64_t ld, int32_t dtype) { return !mis
 
 // Tiles for a product of rows along k; n: of both matrices where there are two.
 struct AlongPlan {
-    bool    large, direct;
+    int     size;                 // 256, 128 or 64
+    bool    direct;
     int64_t tiles_m, tiles_n;
-    bool    launchable() const { return tiles_m * tiles_n * (large ? 512 : 256) <= UINT32_MAX; }      // lanes
 };
+// fp32: the matrix cores' fp32 rate is a sixteenth, which staging keeps up with; the 64-tile as long as the others would be few (333 x 5462 x 765,
+// 129 tiles of 128, 64 us)
+template <class F>
+inline int tile_size(bool direct, int32_t dtype, F&& tiles)
+{
+    if (direct) return tiles(256) >= kUnits / 2 ? 256 : 128;
+    return dtype == ADAGC_F32 && tiles(128) < 4 * kUnits ? 64 : 128;
+}
 inline AlongPlan along_plan(int64_t m, int64_t n, int32_t dtype, bool aligned, int64_t ld_y, int64_t ld_x)
 {
     AlongPlan p{};
     auto tiles = [&](int64_t size) { return ((m + size - 1) / size) * ((n + size - 1) / size); };
-    // fp32: the matrix cores' fp32 rate is a sixteenth, which the small tile and staging keep up with
     p.direct = aligned && dtype == ADAGC_BF16 && ld_y < (int64_t)1 << 23 && ld_x < (int64_t)1 << 23;          // 256 rows are within 32 bits
-    p.large = p.direct && tiles(256) >= kUnits / 2;
-    const int size = p.large ? 256 : 128;
-    p.tiles_m = (m + size - 1) / size;
-    p.tiles_n = (n + size - 1) / size;
+    p.size = tile_size(p.direct, dtype, tiles);
+    p.tiles_m = (m + p.size - 1) / p.size;
+    p.tiles_n = (n + p.size - 1) / p.size;
     return p;
 }
 
@@ -1134,7 +1142,7 @@ __global__ __launch_bounds__(S::kThreads) void plain_join_kernel(const PlainArgs
 
 // How a product is cut: tiles, and those of the last, partial round of workgroups also along k, so that they fill the chip too.
 struct PlainPlan {
-    int     size;                 // 256 or 128
+    int     size;                 // 256, 128 or 64
     bool    checked, direct;
     int64_t tiles_m, tiles_n, whole, rest, split;
     int64_t workspace() const { return split > 1 ? rest * split * size * size * 4 : 0; }
@@ -1148,16 +1156,16 @@ inline PlainPlan plain_plan(int64_t m, int64_t n, int64_t k, int32_t dtype, bool
     auto tiles = [&](int64_t size) { return products * ((m + size - 1) / size) * ((n + size - 1) / size); };
     // 32 rows across, 256 along k are not within 32 bits
     const bool far = ld_x >= (int64_t)1 << 24 || (across_y && ld_y >= (int64_t)1 << 24);
-    // fp32: the matrix cores' fp32 rate is a sixteenth, which the small tile and staging keep up with
     p.direct = aligned && !far && dtype == ADAGC_BF16 && (across_y || ld_y < (int64_t)1 << 23) && n >= 128 && n % 8 == 0 &&
                (!across_y || m >= 128);      // (m: of what is readable, a multiple of 8)
-    const bool large = p.direct && m >= 256 && n >= 256 && tiles(256) >= kUnits / 2;
-    p.size = large ? 256 : 128;
+    p.size = tile_size(p.direct, dtype, tiles);
+    if (p.size == 256 && (m < 256 || n < 256)) p.size = 128;
+    const bool large = p.size == 256;
     p.checked = far || n < p.size || (across_y && m < p.size);
     p.tiles_m = (m + p.size - 1) / p.size;
     p.tiles_n = (n + p.size - 1) / p.size;
     const int64_t all = tiles(p.size), steps = k / (kStepBytes / dtype_size(dtype)) / (p.direct ? 2 : 1) * (p.direct ? 2 : 1);
-    const int64_t round = large ? kUnits : 2 * kUnits;      // the small tile's workgroups share a compute unit in pairs
+    const int64_t round = large ? kUnits : 2 * kUnits;      // the smaller tiles' workgroups share a compute unit in pairs
     p.rest = all % round;
     // a part has eight steps at least (of each pair)
     p.split = p.rest ? std::max<int64_t>(1, std::min(round / p.rest, steps * pairs / 8)) : 1;
@@ -1195,6 +1203,8 @@ int run_plain(PlainArgs a, hipStream_t s)
     if constexpr (sizeof(T) == 2) {
         if (p.size == 256) return launch_plain<Large, T, ACROSS_Y, false>(a, p, s);
         if (p.direct) return launch_plain<Small, T, ACROSS_Y, false>(a, p, s);
+    } else {
+        if (p.size == 64) return p.checked ? launch_plain<Smallest, T, ACROSS_Y, true>(a, p, s) : launch_plain<Smallest, T, ACROSS_Y, false>(a, p, s);
     }
     return p.checked ? launch_plain<Staged<T>, T, ACROSS_Y, true>(a, p, s) : launch_plain<Staged<T>, T, ACROSS_Y, false>(a, p, s);
 }
