@@ -32,13 +32,25 @@ __device__ __forceinline__ void slopes(float g, float u, float* of_gate, float* 
 
 struct GatedArgs {
     AlongArgs   p;
-    void*       out;               // T; backward: or NULL
-    void *      gate, *up;         // T, or both NULL; backward: d_g and d_u
-    const void* d_out;             // T
+    void*       out;               // O; backward: or NULL
+    void *      gate, *up;         // O, or both NULL; backward: d_g and d_u, in kParts of bf16 if there are as many
+    const void* d_out;             // O
     int64_t     ld_out, ld_gate, ld_up, ld_d_out;
+    int64_t     part, rows;        // d_g and d_u in parts: elements from part to part; rows with those filled with zeros
 };
 
-template <class S, class T, bool BACKWARD>
+// Four of d_g or d_u in parts.
+__device__ __forceinline__ void store_parts(uint16_t* to, int64_t part, const f32x4_p& v)
+{
+    uint32_t bits[kParts][2];
+    split4(v, bits);
+#pragma unroll
+    for (int p = 0; p < kParts; ++p) *reinterpret_cast<u32x2_of_bf16*>(to + p * part) = u32x2_of_bf16{bits[p][0], bits[p][1]};
+}
+
+// T: of the operands; O: of what else is read and written.  PARTS: of d_g and d_u, 1 or kParts, the latter with zeros in rows past the last one
+// and columns past the last one.
+template <class S, class T, class O, bool BACKWARD, int PARTS>
 __global__ __launch_bounds__(S::kThreads, 2) void gated_kernel(const GatedArgs a)
 {
     __shared__ __attribute__((aligned(512))) uint8_t lds[S::kLds];
@@ -66,11 +78,34 @@ __global__ __launch_bounds__(S::kThreads, 2) void gated_kernel(const GatedArgs a
                 du[r] = d[r] * of_up;
             }
         };
+        if constexpr (PARTS > 1) {
+            uint16_t *gate = static_cast<uint16_t*>(a.gate) + row0 * a.ld_gate + col0, *up = static_cast<uint16_t*>(a.up) + row0 * a.ld_up + col0;
+#pragma unroll
+            for (int m = 0; m < S::kTM; ++m) {
+                const int64_t row = row0 + m * 16;
+                if (row >= a.rows) continue;
+#pragma unroll
+                for (int n = 0; n < S::kTN; n += 2) {
+                    const int64_t col = col0 + n * 8;
+                    if (col >= a.ld_gate) continue;
+                    const f32x4_p none = {0.f, 0.f, 0.f, 0.f};
+                    f32x4_p o, dg, du;
+                    gradients(m, n, row < a.p.m ? load4(static_cast<const O*>(a.d_out) + row * a.ld_d_out, col, 0, a.p.n) : none, o, dg, du);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (row >= a.p.m || col + r >= a.p.n) dg[r] = du[r] = 0.f;
+                    store_parts(gate + m * 16 * a.ld_gate + n * 8, a.part, dg);
+                    store_parts(up + m * 16 * a.ld_up + n * 8, a.part, du);
+                    if (a.out && row < a.p.m) store4(static_cast<O*>(a.out) + row * a.ld_out, col, 0, a.p.n, o);
+                }
+            }
+            return;
+        }
         if (m0 + S::BM <= a.p.m && n0 + S::BN / 2 <= a.p.n) {
             // a tile inside: one address for each array, no checks
-            T* out = static_cast<T*>(a.out) + row0 * a.ld_out + col0;
-            T *gate = static_cast<T*>(a.gate) + row0 * a.ld_gate + col0, *up = static_cast<T*>(a.up) + row0 * a.ld_up + col0;
-            const T* d_out = static_cast<const T*>(a.d_out) + row0 * a.ld_d_out + col0;
+            O* out = static_cast<O*>(a.out) + row0 * a.ld_out + col0;
+            O *gate = static_cast<O*>(a.gate) + row0 * a.ld_gate + col0, *up = static_cast<O*>(a.up) + row0 * a.ld_up + col0;
+            const O* d_out = static_cast<const O*>(a.d_out) + row0 * a.ld_d_out + col0;
 #pragma unroll
             for (int m = 0; m < S::kTM; ++m)
 #pragma unroll
@@ -103,17 +138,17 @@ __global__ __launch_bounds__(S::kThreads, 2) void gated_kernel(const GatedArgs a
                 f32x4_p o;
                 if constexpr (BACKWARD) {
                     f32x4_p dg, du;
-                    gradients(m, n, load4(static_cast<const T*>(a.d_out) + row * a.ld_d_out, col, 0, a.p.n), o, dg, du);
-                    store4(static_cast<T*>(a.gate) + row * a.ld_gate, col, 0, a.p.n, dg);
-                    store4(static_cast<T*>(a.up) + row * a.ld_up, col, 0, a.p.n, du);
+                    gradients(m, n, load4(static_cast<const O*>(a.d_out) + row * a.ld_d_out, col, 0, a.p.n), o, dg, du);
+                    store4(static_cast<O*>(a.gate) + row * a.ld_gate, col, 0, a.p.n, dg);
+                    store4(static_cast<O*>(a.up) + row * a.ld_up, col, 0, a.p.n, du);
                 } else {
                     results(m, n, o);
                     if (a.gate) {
-                        store4(static_cast<T*>(a.gate) + row * a.ld_gate, col, 0, a.p.n, acc[m][n]);
-                        store4(static_cast<T*>(a.up) + row * a.ld_up, col, 0, a.p.n, acc[m][n + 1]);
+                        store4(static_cast<O*>(a.gate) + row * a.ld_gate, col, 0, a.p.n, acc[m][n]);
+                        store4(static_cast<O*>(a.up) + row * a.ld_up, col, 0, a.p.n, acc[m][n + 1]);
                     }
                 }
-                if (!BACKWARD || a.out) store4(static_cast<T*>(a.out) + row * a.ld_out, col, 0, a.p.n, o);
+                if (!BACKWARD || a.out) store4(static_cast<O*>(a.out) + row * a.ld_out, col, 0, a.p.n, o);
             }
         }
     });
@@ -161,13 +196,14 @@ struct KeptArgs {
     const void *d_out, *gate, *up;
     void *      d_gate, *d_up, *out;
     int64_t     ld_d_out, ld_gate, ld_up, ld_d, ld_out;
-    int64_t     cols, vectors;      // vectors of a row
+    int64_t     rows, cols, vectors;       // vectors of a row
     int64_t     all;                // of all rows
+    int64_t     part;               // d_g and d_u in parts: elements from part to part
 };
 
 // d_g and d_u from g and u that were kept: 16 bytes of each for a lane.  Bound by memory.
 constexpr int kKept = 256;
-template <class T>
+template <class T, int PARTS>
 __global__ __launch_bounds__(kKept) void kept_kernel(const KeptArgs a)
 {
     constexpr int N = 16 / sizeof(T);
@@ -175,9 +211,10 @@ __global__ __launch_bounds__(kKept) void kept_kernel(const KeptArgs a)
     if (i >= a.all) return;
     const int64_t row = i / a.vectors, col = (i - row * a.vectors) * N;
     float d[N], g[N], u[N], dg[N], du[N], o[N];
-    widen(load_vector(static_cast<const T*>(a.d_out) + row * a.ld_d_out, col, a.cols, 0), d);
-    widen(load_vector(static_cast<const T*>(a.gate) + row * a.ld_gate, col, a.cols, 0), g);
-    widen(load_vector(static_cast<const T*>(a.up) + row * a.ld_up, col, a.cols, 0), u);
+    const int64_t cols = PARTS > 1 && row >= a.rows ? 0 : a.cols;          // (0 times what is there past the end is 0)
+    widen(load_vector(static_cast<const T*>(a.d_out) + row * a.ld_d_out, col, cols, 0), d);
+    widen(load_vector(static_cast<const T*>(a.gate) + row * a.ld_gate, col, cols, 0), g);
+    widen(load_vector(static_cast<const T*>(a.up) + row * a.ld_up, col, cols, 0), u);
 #pragma unroll
     for (int r = 0; r < N; ++r) {
         float of_gate, of_up;
@@ -186,62 +223,109 @@ __global__ __launch_bounds__(kKept) void kept_kernel(const KeptArgs a)
         dg[r] = d[r] * of_gate;
         du[r] = d[r] * of_up;
     }
-    store_vector(static_cast<T*>(a.d_gate) + row * a.ld_d, col, a.cols, narrow<T>(dg));
-    store_vector(static_cast<T*>(a.d_up) + row * a.ld_d, col, a.cols, narrow<T>(du));
-    if (a.out) store_vector(static_cast<T*>(a.out) + row * a.ld_out, col, a.cols, narrow<T>(o));
+    if constexpr (PARTS > 1) {
+        store_parts(static_cast<uint16_t*>(a.d_gate) + row * a.ld_d + col, a.part, f32x4_p{dg[0], dg[1], dg[2], dg[3]});
+        store_parts(static_cast<uint16_t*>(a.d_up) + row * a.ld_d + col, a.part, f32x4_p{du[0], du[1], du[2], du[3]});
+    } else {
+        store_vector(static_cast<T*>(a.d_gate) + row * a.ld_d, col, cols, narrow<T>(dg));
+        store_vector(static_cast<T*>(a.d_up) + row * a.ld_d, col, cols, narrow<T>(du));
+    }
+    if (a.out) store_vector(static_cast<T*>(a.out) + row * a.ld_out, col, cols, narrow<T>(o));
 }
 
 int check(int64_t rows, int64_t dim, int64_t hidden, int32_t dtype)
 {
     if (rows < 0 || dim < 1 || hidden < 1 || !known_dtype(dtype)) return ADAGC_ERR_INVALID_ARG;
     if (rows > (1 << 24) - 1 || dim > kMaxCols || hidden > kMaxCols / 2) return ADAGC_ERR_TOO_LARGE;
-    const int64_t m = (rows + 127) / 128, k = (dim + 127) / 128, n = (hidden + 63) / 64;
-    if (std::max({m * n, m * k, n * k}) >= 1 << 23) return ADAGC_ERR_TOO_LARGE;
-    if (rows * ((hidden * dtype_size(dtype) + 15) / 16) > (int64_t)UINT32_MAX - kKept) return ADAGC_ERR_TOO_LARGE;       // lanes
+    const int64_t m = (rows + 63) / 64, k = (dim + 63) / 64, n = (hidden + 31) / 32;
+    // lanes of a launch are within 32 bits
+    if (std::max(m * n, n * k) >= 1 << 23 || m * k >= 1 << 22 || m * 64 * (n * 32 / 4) > (int64_t)UINT32_MAX - kKept) return ADAGC_ERR_TOO_LARGE;
     return ADAGC_OK;
 }
 int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 
-// d_g and d_u, rows x ld each, then partial sums
-struct Space {
-    int64_t ld, gradients, partial;
-    int64_t all() const { return 2 * gradients + partial; }
+// What a call needs, in bytes: operands laid out anew; backward: d_g and d_u, rows x ld each, and partial sums of a product.
+struct Work {
+    Layout  layout;
+    int64_t x, weight;                             // weight: of each
+    int64_t ld, rows, gradients, partial;
+    int64_t forward() const { return x + 2 * weight; }
+    int64_t backward() const { return 2 * gradients + partial + x + 2 * weight; }
 };
-Space space_of(int64_t rows, int64_t dim, int64_t hidden, int32_t dtype)
+Work work_of(int64_t rows, int64_t dim, int64_t hidden, int32_t dtype)
 {
-    Space s{};
-    s.ld = (hidden + 63) / 64 * 64;
-    s.gradients = up16(rows * s.ld * dtype_size(dtype));
+    Work w{};
+    w.layout = layout_of(rows, hidden, dim, dtype);
+    if (w.layout.anew) {
+        w.x = w.layout.bytes(rows);
+        w.weight = w.layout.bytes(hidden);
+    }
+    const bool parts = w.layout.parts > 1;
+    w.ld = (hidden + 63) / 64 * 64;
+    w.rows = parts ? Layout::rows_of(rows) : rows;
+    w.gradients = up16(w.rows * w.ld * (parts ? 2 * kParts : dtype_size(dtype)));
+    const int32_t type = w.layout.anew ? ADAGC_BF16 : dtype;
+    const int64_t columns = w.layout.anew ? (dim + 7) / 8 * 8 : dim;
     for (const bool aligned : {false, true})
-        s.partial = std::max({s.partial, plain_plan((hidden + 7) / 8 * 8, dim, rows, dtype, true, s.ld, dim, 1, 2, aligned).workspace(),
-                              plain_plan(rows, dim, hidden, dtype, false, s.ld, dim, 2, 1, aligned).workspace()});
-    return s;
+        w.partial = std::max({w.partial, plain_plan((hidden + 7) / 8 * 8, columns, w.rows, type, true, w.ld, columns, w.layout.segments, 2, aligned).workspace(),
+                              plain_plan(rows, columns, parts ? w.ld : hidden, type, false, w.ld, columns, 2 * w.layout.segments, 1, aligned).workspace()});
+    return w;
 }
 
-template <class T, bool BACKWARD>
+int launched() { return hipGetLastError() == hipSuccess ? ADAGC_OK : ADAGC_ERR_HIP; }
+
+// Lays x and both weights out anew, if the call does that.
+template <class T>
+int lay_operands(const Work& w, AlongArgs* p, uint8_t* space, hipStream_t s)
+{
+    p->segments = w.layout.segments;
+    if (!w.layout.anew || p->m == 0) return ADAGC_OK;
+    if (const int rc = lay<T>(p->y, p->ld_y, p->m, p->k, w.layout, space, s)) return rc;
+    p->y = space;
+    for (int i = 0; i < 2; ++i) {
+        uint8_t* to = space + w.x + i * w.weight;
+        if (const int rc = lay<T>(p->x[i], p->ld_x[i], p->n, p->k, w.layout, to, s)) return rc;
+        p->x[i] = to;
+    }
+    p->ld_y = p->ld_x[0] = p->ld_x[1] = p->k = w.layout.ld;
+    p->part_y = w.layout.part(p->m);
+    p->part_x = w.layout.part(p->n);
+    return ADAGC_OK;
+}
+
+// T: of the operands, as they are or laid out anew; O: of the call's data
+template <class T, class O, bool BACKWARD>
 int projections(GatedArgs a, hipStream_t s)
 {
     constexpr int32_t dtype = sizeof(T) == 4 ? ADAGC_F32 : ADAGC_BF16;
+    if constexpr (sizeof(T) == sizeof(O)) {
+        if (thin(a.p, dtype)) {
+            const dim3 blocks((uint32_t)std::min<int64_t>((a.p.n + kThinColumns / 2 - 1) / (kThinColumns / 2), kThinGrid));
+            for_rows(a.p.m, [&](auto TM) { thin_gated_kernel<T, decltype(TM)::value, BACKWARD><<<blocks, dim3(kThinThreads), 0, s>>>(a); });
+            return launched();
+        }
+    }
     const bool aligned = rows_aligned(a.p.y, a.p.ld_y, dtype) && rows_aligned(a.p.x[0], a.p.ld_x[0], dtype) && rows_aligned(a.p.x[1], a.p.ld_x[1], dtype);
     const AlongPlan p = along_plan(a.p.m, 2 * a.p.n, dtype, aligned, a.p.ld_y, std::max(a.p.ld_x[0], a.p.ld_x[1]));
     a.p.tiles_m = (int32_t)p.tiles_m;
     a.p.tiles_n = (int32_t)p.tiles_n;
     const dim3 grid((uint32_t)(p.tiles_m * p.tiles_n));
-    const bool few = thin(a.p, sizeof(T) == 4 ? ADAGC_F32 : ADAGC_BF16);
-    if (few) {
-        const dim3 blocks((uint32_t)std::min<int64_t>((a.p.n + kThinColumns / 2 - 1) / (kThinColumns / 2), kThinGrid));
-        for_rows(a.p.m, [&](auto TM) { thin_gated_kernel<T, decltype(TM)::value, BACKWARD><<<blocks, dim3(kThinThreads), 0, s>>>(a); });
-    } else if constexpr (sizeof(T) == 2) {
-        if (p.size == 256) gated_kernel<Large, T, BACKWARD><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
-        else if (p.direct) gated_kernel<Small, T, BACKWARD><<<grid, dim3(Small::kThreads), 0, s>>>(a);
+    if constexpr (sizeof(T) == 2) {
+        constexpr int kOf = BACKWARD && sizeof(O) == 4 ? kParts : 1;       // (fp32 data is laid out in parts)
+        if (p.size == 256) gated_kernel<Large, T, O, BACKWARD, kOf><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
+        else if (p.direct) gated_kernel<Small, T, O, BACKWARD, kOf><<<grid, dim3(Small::kThreads), 0, s>>>(a);
     }
-    if (!few && !p.direct) {
-        if constexpr (sizeof(T) == 4) {
-            if (p.size == 64) gated_kernel<Smallest, T, BACKWARD><<<grid, dim3(Smallest::kThreads), 0, s>>>(a);
-        }
-        if (p.size == 128) gated_kernel<Staged<T>, T, BACKWARD><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+    if constexpr (sizeof(T) == sizeof(O)) {
+        if (!p.direct) gated_kernel<Staged<T>, T, O, BACKWARD, 1><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
     }
-    return hipGetLastError() == hipSuccess ? ADAGC_OK : ADAGC_ERR_HIP;
+    return launched();
+}
+
+template <class T>
+int forward(const Work& w, GatedArgs a, uint8_t* workspace, hipStream_t s)
+{
+    if (const int rc = lay_operands<T>(w, &a.p, workspace, s)) return rc;
+    return w.layout.anew ? projections<uint16_t, T, false>(a, s) : projections<T, T, false>(a, s);
 }
 
 struct Backward {
@@ -256,14 +340,15 @@ struct Backward {
 };
 
 template <class T>
-int backward(Backward b, uint8_t* workspace, hipStream_t s)
+int backward(const Work& w, Backward b, uint8_t* workspace, hipStream_t s)
 {
     constexpr int32_t dtype = sizeof(T) == 4 ? ADAGC_F32 : ADAGC_BF16;
+    const int64_t rows = b.g.p.m, hidden = b.g.p.n, dim = b.g.p.k;
+    const bool anew = w.layout.anew, parts = w.layout.parts > 1;
+    uint8_t *d_gate = workspace, *d_up = workspace + w.gradients;
+    const int64_t part = w.rows * w.ld;
+    if (const int rc = lay_operands<T>(w, &b.g.p, workspace + 2 * w.gradients + w.partial, s)) return rc;
     const AlongArgs& p = b.g.p;
-    const int64_t rows = p.m, hidden = p.n, dim = p.k;
-    const Space space = space_of(rows, dim, hidden, dtype);
-    T *d_gate = reinterpret_cast<T*>(workspace), *d_up = reinterpret_cast<T*>(workspace + space.gradients);
-    float* partial = reinterpret_cast<float*>(workspace + 2 * space.gradients);
     if (rows > 0 && b.gate) {
         KeptArgs k{};
         k.d_out = b.g.d_out;
@@ -274,66 +359,74 @@ int backward(Backward b, uint8_t* workspace, hipStream_t s)
         k.ld_up = b.ld_up;
         k.d_gate = d_gate;
         k.d_up = d_up;
-        k.ld_d = space.ld;
+        k.ld_d = w.ld;
+        k.part = part;
         k.out = b.g.out;
         k.ld_out = b.g.ld_out;
+        k.rows = rows;
         k.cols = hidden;
-        k.vectors = (hidden * (int64_t)sizeof(T) + 15) / 16;
-        k.all = rows * k.vectors;
-        kept_kernel<T><<<dim3((uint32_t)((k.all + kKept - 1) / kKept)), dim3(kKept), 0, s>>>(k);
-        if (hipGetLastError() != hipSuccess) return ADAGC_ERR_HIP;
+        k.vectors = ((parts ? w.ld : hidden) * (int64_t)sizeof(T) + 15) / 16;
+        k.all = w.rows * k.vectors;
+        const dim3 grid((uint32_t)((k.all + kKept - 1) / kKept));
+        if constexpr (sizeof(T) == 4) {
+            if (parts) kept_kernel<T, kParts><<<grid, dim3(kKept), 0, s>>>(k);
+        }
+        if (!parts) kept_kernel<T, 1><<<grid, dim3(kKept), 0, s>>>(k);
+        if (const int rc = launched()) return rc;
     } else if (rows > 0) {
         b.g.gate = d_gate;
         b.g.up = d_up;
-        b.g.ld_gate = b.g.ld_up = space.ld;
-        if (const int rc = projections<T, true>(b.g, s)) return rc;
+        b.g.ld_gate = b.g.ld_up = w.ld;
+        b.g.part = part;
+        b.g.rows = w.rows;
+        if (const int rc = anew ? projections<uint16_t, T, true>(b.g, s) : projections<T, T, true>(b.g, s)) return rc;
     }
+    PlainArgs both{};
+    both.y[0] = d_gate;
+    both.y[1] = d_up;
+    both.ld_y = w.ld;
+    both.part_y = part;
+    both.segments = w.layout.segments;
+    both.n = dim;
+    both.n_readable = anew ? (dim + 7) / 8 * 8 : dim;
+    both.workspace = reinterpret_cast<float*>(workspace + 2 * w.gradients);
+    both.factor = 1.f;
     if (b.d_w_gate) {
-        PlainArgs w{};
-        w.y[0] = d_gate;
-        w.y[1] = d_up;
-        w.ld_y = space.ld;
-        w.x[0] = w.x[1] = p.y;
-        w.ld_x[0] = w.ld_x[1] = p.ld_y;
-        w.out[0] = b.d_w_gate;
-        w.out[1] = b.d_w_up;
-        w.ld_out[0] = w.ld_add[0] = b.ld_d_w_gate;
-        w.ld_out[1] = w.ld_add[1] = b.ld_d_w_up;
+        PlainArgs a = both;
+        a.x[0] = a.x[1] = p.y;
+        a.ld_x[0] = a.ld_x[1] = p.ld_y;
+        a.part_x = p.part_y;
+        a.out[0] = b.d_w_gate;
+        a.out[1] = b.d_w_up;
+        a.ld_out[0] = a.ld_add[0] = b.ld_d_w_gate;
+        a.ld_out[1] = a.ld_add[1] = b.ld_d_w_up;
         if (b.accumulate) {
-            w.add[0] = b.d_w_gate;
-            w.add[1] = b.d_w_up;
+            a.add[0] = b.d_w_gate;
+            a.add[1] = b.d_w_up;
         }
-        w.m = hidden;
-        w.m_readable = (hidden + 7) / 8 * 8;
-        w.n = dim;
-        w.k = rows;
-        w.workspace = partial;
-        w.factor = 1.f;
-        w.pairs = 1;
-        w.products = 2;
-        w.out_bf16 = w.add_bf16 = b.weight_dtype == ADAGC_BF16;
-        if (const int rc = run_plain<T, true>(w, s)) return rc;
+        a.m = hidden;
+        a.m_readable = (hidden + 7) / 8 * 8;
+        a.k = w.rows;
+        a.pairs = 1;
+        a.products = 2;
+        a.out_bf16 = a.add_bf16 = b.weight_dtype == ADAGC_BF16;
+        if (const int rc = anew ? run_plain<uint16_t, true>(a, s) : run_plain<T, true>(a, s)) return rc;
     }
     if (b.d_x && rows > 0) {
-        PlainArgs x{};
-        x.y[0] = d_gate;
-        x.y[1] = d_up;
-        x.ld_y = space.ld;
-        x.x[0] = p.x[0];
-        x.x[1] = p.x[1];
-        x.ld_x[0] = p.ld_x[0];
-        x.ld_x[1] = p.ld_x[1];
-        x.out[0] = b.d_x;
-        x.ld_out[0] = b.ld_d_x;
-        x.m = x.m_readable = rows;
-        x.n = dim;
-        x.k = hidden;
-        x.workspace = partial;
-        x.factor = 1.f;
-        x.pairs = 2;
-        x.products = 1;
-        x.out_bf16 = dtype == ADAGC_BF16;
-        if (const int rc = run_plain<T, false>(x, s)) return rc;
+        PlainArgs a = both;
+        a.x[0] = p.x[0];
+        a.x[1] = p.x[1];
+        a.ld_x[0] = p.ld_x[0];
+        a.ld_x[1] = p.ld_x[1];
+        a.part_x = p.part_x;
+        a.out[0] = b.d_x;
+        a.ld_out[0] = b.ld_d_x;
+        a.m = a.m_readable = rows;
+        a.k = parts ? w.ld : hidden;
+        a.pairs = 2;
+        a.products = 1;
+        a.out_bf16 = dtype == ADAGC_BF16;
+        if (const int rc = anew ? run_plain<uint16_t, false>(a, s) : run_plain<T, false>(a, s)) return rc;
     }
     return ADAGC_OK;
 }
@@ -346,7 +439,7 @@ using namespace adagc;
 extern "C" int64_t adagc_gated_linear_workspace_bytes(int64_t rows, int64_t dim, int64_t hidden, int32_t dtype)
 {
     if (const int rc = check(rows, dim, hidden, dtype)) return rc;
-    return 0;
+    return work_of(rows, dim, hidden, dtype).forward();
 }
 
 extern "C" int adagc_gated_linear(const void* x, int64_t ld_x, const void* w_gate, int64_t ld_w_gate, const void* w_up, int64_t ld_w_up, int32_t dtype,
@@ -362,10 +455,11 @@ extern "C" int adagc_gated_linear(const void* x, int64_t ld_x, const void* w_gat
         return ADAGC_ERR_INVALID_ARG;
     if (gate && (ld_gate < hidden || ld_up < hidden || misaligned(gate, size) || misaligned(up, size))) return ADAGC_ERR_INVALID_ARG;
     if (std::max({ld_x, ld_w_gate, ld_w_up, ld_out}) > kMaxLd || (gate && std::max(ld_gate, ld_up) > kMaxLd)) return ADAGC_ERR_TOO_LARGE;
-    const int64_t need = adagc_gated_linear_workspace_bytes(rows, dim, hidden, dtype);
+    const Work w = work_of(rows, dim, hidden, dtype);
+    const int64_t need = w.forward();
     if (need > 0 && (!workspace || workspace_bytes < need || misaligned(workspace, 16))) return ADAGC_ERR_INVALID_ARG;
     GatedArgs a{};
-    a.p = {x, {w_gate, w_up}, ld_x, {ld_w_gate, ld_w_up}, rows, hidden, dim, 0, 0};
+    a.p = {x, {w_gate, w_up}, ld_x, {ld_w_gate, ld_w_up}, rows, hidden, dim, 0, 0, 1, 0, 0};
     a.out = out;
     a.ld_out = ld_out;
     a.gate = gate;
@@ -373,13 +467,14 @@ extern "C" int adagc_gated_linear(const void* x, int64_t ld_x, const void* w_gat
     a.ld_gate = ld_gate;
     a.ld_up = ld_up;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    return dtype == ADAGC_F32 ? projections<float, false>(a, s) : projections<uint16_t, false>(a, s);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    return dtype == ADAGC_F32 ? forward<float>(w, a, ws, s) : forward<uint16_t>(w, a, ws, s);
 }
 
 extern "C" int64_t adagc_gated_linear_backward_workspace_bytes(int64_t rows, int64_t dim, int64_t hidden, int32_t dtype)
 {
     if (const int rc = check(rows, dim, hidden, dtype)) return rc;
-    return space_of(rows, dim, hidden, dtype).all();
+    return work_of(rows, dim, hidden, dtype).backward();
 }
 
 extern "C" int adagc_gated_linear_backward(const void* d_out, int64_t ld_d_out, const void* x, int64_t ld_x, const void* w_gate, int64_t ld_w_gate,
@@ -405,10 +500,11 @@ extern "C" int adagc_gated_linear_backward(const void* d_out, int64_t ld_d_out, 
             return ADAGC_ERR_TOO_LARGE;
     }
     if (d_w_gate && std::max(ld_d_w_gate, ld_d_w_up) > kMaxLd) return ADAGC_ERR_TOO_LARGE;
-    const int64_t need = space_of(rows, dim, hidden, dtype).all();
+    const Work w = work_of(rows, dim, hidden, dtype);
+    const int64_t need = w.backward();
     if (need > 0 && (!workspace || workspace_bytes < need || misaligned(workspace, 16))) return ADAGC_ERR_INVALID_ARG;
     Backward b{};
-    b.g.p = {x, {w_gate, w_up}, ld_x, {ld_w_gate, ld_w_up}, rows, hidden, dim, 0, 0};
+    b.g.p = {x, {w_gate, w_up}, ld_x, {ld_w_gate, ld_w_up}, rows, hidden, dim, 0, 0, 1, 0, 0};
     b.g.out = out;
     b.g.ld_out = ld_out;
     b.g.d_out = d_out;
@@ -427,5 +523,5 @@ extern "C" int adagc_gated_linear_backward(const void* d_out, int64_t ld_d_out, 
     b.accumulate = accumulate;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    return dtype == ADAGC_F32 ? backward<float>(b, ws, s) : backward<uint16_t>(b, ws, s);
+    return dtype == ADAGC_F32 ? backward<float>(w, b, ws, s) : backward<uint16_t>(w, b, ws, s);
 }

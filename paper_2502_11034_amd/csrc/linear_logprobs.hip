@@ -16,10 +16,12 @@ using namespace product;
 constexpr float kLog2e = 1.44269504088896340736f;
 
 struct StatsArgs {
-    AlongArgs      p;
+    AlongArgs      p;              // n: of a piece of the vocabulary
     const int64_t* targets;        // or NULL
     float          scale;
-    float2*        parts;          // [rows][tiles_n]: maximum, sum
+    float2*        parts;          // [rows][pitch]: maximum, sum of each tile
+    int64_t        pitch;
+    int64_t        first;          // of the vocabulary
     float*         target_logit;   // [rows]
 };
 
@@ -39,7 +41,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void stats_kernel(const StatsArgs a
             const int64_t row = m0 + at.row + m * 16;
             target[m] = -1;
             if (a.targets && row < a.p.m) {
-                const int64_t t = a.targets[row];
+                const int64_t t = a.targets[row] - a.first;
                 if (t >= n0 + at.col && t < min(n0 + at.col + S::kTN * 16, a.p.n)) target[m] = (int)(t - n0 - at.col);
             }
         }
@@ -103,7 +105,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void stats_kernel(const StatsArgs a
             }
 #pragma unroll
             for (int w = 0; w < S::kWN; ++w) sum += rescaled(part[w].x, part[w].y, most, c);
-            a.parts[(m0 + tid) * a.p.tiles_n + n0 / S::BN] = float2{most, sum};
+            a.parts[(m0 + tid) * a.pitch + n0 / S::BN] = float2{most, sum};
         }
     });
 }
@@ -126,7 +128,7 @@ __global__ __launch_bounds__(kThinThreads, 4) void thin_stats_kernel(const Stats
         float sum = __builtin_amdgcn_exp2f((z - (most == -__builtin_inff() ? 0.f : most)) * c);
 #pragma unroll
         for (int d = 1; d < kThinColumns; d *= 2) sum += __shfl_xor(sum, d);
-        if (at == 0) a.parts[row * (int64_t)a.p.tiles_n + n0 / kThinColumns] = float2{most, sum};
+        if (at == 0) a.parts[row * a.pitch + n0 / kThinColumns] = float2{most, sum};
         if (target == col && col < a.p.n) a.target_logit[row] = z;
     });
 }
@@ -137,7 +139,7 @@ struct JoinArgs {
     const int64_t* targets;
     float          scale;
     int64_t        vocab;
-    int32_t        tiles;
+    int64_t        pitch, tiles;
     float*         logprob;        // or NULL
     float2*        stats;          // or NULL
 };
@@ -149,17 +151,17 @@ __global__ __launch_bounds__(kJoin) void join_kernel(const JoinArgs a)
     __shared__ float most_of[kJoin / 64], sum_of[kJoin / 64];
     const int64_t row = blockIdx.x;
     const int tid = threadIdx.x;
-    const float2* parts = a.parts + row * a.tiles;
+    const float2* parts = a.parts + row * a.pitch;
     const float c = a.scale * kLog2e;
     float most = -__builtin_inff(), sum = 0.f;
-    for (int i = tid; i < a.tiles; i += kJoin) most = maximum(most, parts[i].x);
+    for (int64_t i = tid; i < a.tiles; i += kJoin) most = maximum(most, parts[i].x);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) most = maximum(most, __shfl_xor(most, d));
     if (tid % 64 == 0) most_of[tid / 64] = most;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kJoin / 64; ++w) most = maximum(most, most_of[w]);
-    for (int i = tid; i < a.tiles; i += kJoin) sum += rescaled(parts[i].x, parts[i].y, most, c);
+    for (int64_t i = tid; i < a.tiles; i += kJoin) sum += rescaled(parts[i].x, parts[i].y, most, c);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
     if (tid % 64 == 0) sum_of[tid / 64] = sum;
@@ -189,11 +191,13 @@ struct GradArgs {
     float          scale;
     int64_t        first;          // of the vocabulary
     int64_t        vocab;
-    void*          d_logits;       // T[rows][ld]
+    void*          d_logits;       // T[rows][ld], or kParts of them in bf16
     int64_t        ld;
+    int64_t        part, rows;     // in parts: elements from part to part; rows with those filled with zeros
 };
 
-template <class S, class T>
+// PARTS: 1, or kParts, with zeros in rows past the last one and columns past the piece's end.
+template <class S, class T, int PARTS>
 __global__ __launch_bounds__(S::kThreads, 2) void grad_kernel(const GradArgs a)
 {
     __shared__ __attribute__((aligned(512))) uint8_t lds[S::kLds];
@@ -223,17 +227,28 @@ __global__ __launch_bounds__(S::kThreads, 2) void grad_kernel(const GradArgs a)
 #pragma unroll
         for (int m = 0; m < S::kTM; ++m) {
             const int64_t row = m0 + at.row + m * 16;
-            if (row >= a.p.m) continue;
+            if (row >= (PARTS == 1 ? a.p.m : a.rows)) continue;
             T* to = static_cast<T*>(a.d_logits) + row * a.ld + n0 + at.col;
 #pragma unroll
             for (int n = 0; n < S::kTN; ++n) {
+                if (PARTS > 1 && n0 + at.col + n * 16 >= a.ld) continue;
                 f32x4_p v;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float p = __builtin_amdgcn_exp2f((acc[m][n][r] - most[m]) * c - log2_sum[m]);
                     v[r] = d[m] == 0.f ? 0.f : ((target[m] == n * 16 + r ? 1.f : 0.f) - p) * d[m];
                 }
-                store4(to + n * 16, v);            // (columns past the piece's end are within ld, and not read)
+                if constexpr (PARTS == 1) {
+                    store4(to + n * 16, v);        // (columns past the piece's end are within ld, and not read)
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (row >= a.p.m || n0 + at.col + n * 16 + r >= a.p.n) v[r] = 0.f;
+                    uint32_t bits[kParts][2];
+                    split4(v, bits);
+#pragma unroll
+                    for (int p = 0; p < kParts; ++p) *reinterpret_cast<u32x2_of_bf16*>(to + p * a.part + n * 16) = u32x2_of_bf16{bits[p][0], bits[p][1]};
+                }
             }
         }
     });
@@ -266,58 +281,102 @@ int check(int64_t rows, int64_t vocab, int64_t dim, int32_t dtype)
 bool scale_in_range(float scale) { return scale >= 0x1p-100f && scale <= 0x1p100f; }
 int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 
-// at most: of the smallest tile that a call of this size may take
-int64_t parts_of_row(int64_t rows, int64_t vocab)
-{
-    const int64_t tile = rows <= kThinRows ? kThinColumns : ((rows + 127) / 128) * ((vocab + 127) / 128) < 4 * kUnits ? 64 : 128;
-    return (vocab + tile - 1) / tile;
-}
-int64_t forward_workspace(int64_t rows, int64_t vocab)
-{
-    return up16(rows * parts_of_row(rows, vocab) * 8) + rows * 4;
-}
-
-// Pieces of the vocabulary: 2^26 gradients of logits a piece, which the memory-side cache holds as bf16, and 2048 columns at least.
-struct Pieces {
-    int64_t size, number, ld;
-    int64_t d_logits, sums, partial;       // bytes
-    int64_t all() const { return d_logits + sums + partial; }
+// What a call needs, in bytes, and how it goes through the vocabulary.
+//
+// The backward pass and operands that are laid out anew go in pieces: 2^26 gradients of logits, which the memory-side cache holds as bf16 (as three
+// parts half as many), and as many weights, laid out, at most; 2048 columns at least.
+struct Work {
+    Layout  layout;
+    int64_t size, number;                          // of a piece, of pieces
+    int64_t pitch, parts, targets;                 // forward: tiles of a row at most; their parts, the targets' logits
+    int64_t ld, d_logits, sums, partial;           // backward: the gradients of a piece's logits; sums of dx in fp32; partial sums of a product
+    int64_t x, weight;                             // operands laid out
+    int64_t forward() const { return parts + targets + x + weight; }
+    int64_t backward() const { return d_logits + sums + partial + x + weight; }
 };
-Pieces pieces_of(int64_t rows, int64_t vocab, int64_t dim, int32_t dtype)
+// Columns of a piece, so many at most: the weight's gradient takes 256-tiles in whole rounds of the compute units where that many fill some.
+int64_t piece_of(int64_t vocab, int64_t dim, int64_t most)
 {
-    Pieces p{};
-    const int64_t most = std::max<int64_t>(2048, ((int64_t)1 << 26) / std::max<int64_t>(rows, 1) / 256 * 256);
-    p.number = (vocab + most - 1) / most;
-    p.size = p.number == 1 ? vocab : ((vocab + p.number - 1) / p.number + 255) / 256 * 256;
-    p.number = (vocab + p.size - 1) / p.size;
-    p.ld = (p.size + 255) / 256 * 256;
-    p.d_logits = up16(rows * p.ld * dtype_size(dtype));
-    p.sums = p.number > 1 && dtype == ADAGC_BF16 ? up16(rows * dim * 4) : 0;
-    for (const int64_t n : {p.size, vocab - (p.number - 1) * p.size})
+    if (vocab <= most) return vocab;
+    const int64_t wide = (dim + 255) / 256, rounds = most / 256 * wide / kUnits;
+    return rounds ? rounds * kUnits / wide * 256 : most;
+}
+Work work_of(int64_t rows, int64_t vocab, int64_t dim, int32_t dtype, bool backward)
+{
+    Work w{};
+    w.layout = layout_of(rows, vocab, dim, dtype);
+    const int64_t cap = (int64_t)1 << (w.layout.parts > 1 ? 25 : 26);
+    int64_t most = std::max<int64_t>(2048, cap / std::max<int64_t>(rows, 1) / 256 * 256);
+    if (w.layout.anew) most = std::max<int64_t>(2048, std::min(backward ? most : INT64_MAX, cap / w.layout.ld / 256 * 256));
+    w.size = backward || w.layout.anew ? piece_of(vocab, dim, most) : vocab;
+    w.number = (vocab + w.size - 1) / w.size;
+    const int64_t tile = rows <= kThinRows ? kThinColumns : dtype == ADAGC_F32 && !w.layout.anew ? 64 : 128;
+    w.pitch = (vocab + tile - 1) / tile + w.number;
+    w.parts = up16(rows * w.pitch * 8);
+    w.targets = up16(rows * 4);
+    w.ld = (w.size + 255) / 256 * 256;
+    const int dz_size = w.layout.parts > 1 ? 2 * kParts : dtype_size(dtype);
+    w.d_logits = up16((w.layout.parts > 1 ? Layout::rows_of(rows) : rows) * w.ld * dz_size);
+    w.sums = w.number > 1 && dtype == ADAGC_BF16 ? up16(rows * dim * 4) : 0;
+    if (w.layout.anew) {
+        w.x = w.layout.bytes(rows);
+        w.weight = w.layout.bytes(w.size);
+    }
+    if (!backward) return w;
+    const int32_t type = w.layout.anew ? ADAGC_BF16 : dtype;
+    const int64_t columns = w.layout.anew ? (dim + 7) / 8 * 8 : dim;
+    for (const int64_t n : {w.size, vocab - (w.number - 1) * w.size})
         for (const bool aligned : {false, true}) {
-            const int64_t readable = (n + 7) / 8 * 8;
-            p.partial = std::max({p.partial, plain_plan(readable, dim, rows, dtype, true, p.ld, dim, 1, 1, aligned).workspace(),
-                                  plain_plan(rows, dim, n, dtype, false, p.ld, dim, 1, 1, aligned).workspace()});
+            const int64_t readable = (n + 7) / 8 * 8, k = w.layout.parts > 1 ? Layout::rows_of(rows) : rows;
+            w.partial = std::max({w.partial, plain_plan(readable, columns, k, type, true, w.ld, columns, w.layout.segments, 1, aligned).workspace(),
+                                  plain_plan(rows, columns, w.layout.parts > 1 ? Layout::rows_of(n) : n, type, false, w.ld, columns, w.layout.segments, 1, aligned).workspace()});
         }
-    return p;
+    return w;
 }
 bool launchable(int64_t rows, int64_t vocab, int64_t dim)
 {
-    const int64_t tiles = ((rows + 127) / 128) * ((vocab + 127) / 128), weight = ((vocab + 127) / 128) * ((dim + 127) / 128),
-                  input = ((rows + 127) / 128) * ((dim + 127) / 128);
-    return std::max({tiles, weight, input}) < 1 << 23;
+    const int64_t tiles = ((rows + 63) / 64) * ((vocab + 63) / 64), weight = ((vocab + 63) / 64) * ((dim + 63) / 64), input = ((rows + 63) / 64) * ((dim + 63) / 64);
+    return std::max(tiles, weight) < 1 << 23 && input < 1 << 22;       // lanes of a launch are within 32 bits
 }
 
-AlongArgs along_args(const void* x, int64_t ld_x, const void* weight, int64_t ld_weight, int64_t rows, int64_t vocab, int64_t dim)
+// A piece's operands, laid out by the time its kernels run.
+struct Operands {
+    const void *x, *weight;
+    int64_t     ld_x, ld_weight;
+};
+template <class T>
+int lay_x(const Work& w, int64_t rows, int64_t dim, Operands* o, uint8_t* space, hipStream_t s)
+{
+    if (!w.layout.anew || rows == 0) return ADAGC_OK;
+    if (const int rc = lay<T>(o->x, o->ld_x, rows, dim, w.layout, space, s)) return rc;
+    o->x = space;
+    o->ld_x = w.layout.ld;
+    return ADAGC_OK;
+}
+// first, n: the piece
+template <class T>
+int lay_weight(const Work& w, int64_t first, int64_t n, int64_t dim, Operands* o, uint8_t* space, hipStream_t s)
+{
+    o->weight = static_cast<const T*>(o->weight) + first * o->ld_weight;
+    if (!w.layout.anew) return ADAGC_OK;
+    if (const int rc = lay<T>(o->weight, o->ld_weight, n, dim, w.layout, space, s)) return rc;
+    o->weight = space;
+    o->ld_weight = w.layout.ld;
+    return ADAGC_OK;
+}
+AlongArgs along_args(const Operands& o, const Work& w, int64_t rows, int64_t n, int64_t dim)
 {
     AlongArgs p{};
-    p.y = x;
-    p.ld_y = ld_x;
-    p.x[0] = p.x[1] = weight;
-    p.ld_x[0] = p.ld_x[1] = ld_weight;
+    p.y = o.x;
+    p.ld_y = o.ld_x;
+    p.x[0] = p.x[1] = o.weight;
+    p.ld_x[0] = p.ld_x[1] = o.ld_weight;
     p.m = rows;
-    p.n = vocab;
-    p.k = dim;
+    p.n = n;
+    p.k = w.layout.anew ? w.layout.ld : dim;
+    p.part_y = w.layout.part(rows);
+    p.part_x = w.layout.part(n);
+    p.segments = w.layout.segments;
     return p;
 }
 AlongPlan plan_of(AlongArgs* p, int32_t dtype)
@@ -327,52 +386,72 @@ AlongPlan plan_of(AlongArgs* p, int32_t dtype)
     p->tiles_n = (int32_t)plan.tiles_n;
     return plan;
 }
+int launched() { return hipGetLastError() == hipSuccess ? ADAGC_OK : ADAGC_ERR_HIP; }
 
+// One piece; *tiles: the parts of a row that it adds.
 template <class T>
-int forward(StatsArgs a, const JoinArgs& join, hipStream_t s)
+int stats_of(StatsArgs a, int64_t* tiles, hipStream_t s)
 {
-    const AlongPlan p = plan_of(&a.p, sizeof(T) == 4 ? ADAGC_F32 : ADAGC_BF16);
+    constexpr int32_t dtype = sizeof(T) == 4 ? ADAGC_F32 : ADAGC_BF16;
+    if (thin(a.p, dtype)) {
+        *tiles = (a.p.n + kThinColumns - 1) / kThinColumns;
+        for_rows(a.p.m, [&](auto TM) {
+            thin_stats_kernel<T, decltype(TM)::value><<<dim3((uint32_t)std::min<int64_t>(*tiles, kThinGrid)), dim3(kThinThreads), 0, s>>>(a);
+        });
+        return launched();
+    }
+    const AlongPlan p = plan_of(&a.p, dtype);
+    *tiles = p.tiles_n;
     const dim3 grid((uint32_t)(p.tiles_m * p.tiles_n));
-    const bool few = thin(a.p, sizeof(T) == 4 ? ADAGC_F32 : ADAGC_BF16);
-    if (few) {
-        a.p.tiles_n = (int32_t)((a.p.n + kThinColumns - 1) / kThinColumns);
-        for_rows(a.p.m, [&](auto TM) { thin_stats_kernel<T, decltype(TM)::value><<<dim3(std::min(a.p.tiles_n, kThinGrid)), dim3(kThinThreads), 0, s>>>(a); });
-    } else if constexpr (sizeof(T) == 2) {
+    if constexpr (sizeof(T) == 2) {
         if (p.size == 256) stats_kernel<Large, T><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
         else if (p.direct) stats_kernel<Small, T><<<grid, dim3(Small::kThreads), 0, s>>>(a);
     }
-    if (!few && !p.direct) {
-        if constexpr (sizeof(T) == 4) {
-            if (p.size == 64) stats_kernel<Smallest, T><<<grid, dim3(Smallest::kThreads), 0, s>>>(a);
-        }
-        if (p.size == 128) stats_kernel<Staged<T>, T><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
-    }
-    JoinArgs j = join;
-    j.tiles = a.p.tiles_n;
-    join_kernel<<<dim3((uint32_t)a.p.m), dim3(kJoin), 0, s>>>(j);
-    return hipGetLastError() == hipSuccess ? ADAGC_OK : ADAGC_ERR_HIP;
+    if (!p.direct) stats_kernel<Staged<T>, T><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+    return launched();
 }
 
 template <class T>
-int gradient(GradArgs a, hipStream_t s)
+int forward(const Work& w, Operands o, int64_t rows, int64_t vocab, int64_t dim, StatsArgs a, JoinArgs join, uint8_t* workspace, hipStream_t s)
 {
-    const AlongPlan p = plan_of(&a.p, sizeof(T) == 4 ? ADAGC_F32 : ADAGC_BF16);
-    const dim3 grid((uint32_t)(p.tiles_m * p.tiles_n));
-    const bool few = thin(a.p, sizeof(T) == 4 ? ADAGC_F32 : ADAGC_BF16);
-    if (few) {
+    uint8_t* laid = workspace + w.parts + w.targets;
+    if (const int rc = lay_x<T>(w, rows, dim, &o, laid, s)) return rc;
+    for (int64_t first = 0; first < vocab; first += w.size) {
+        const int64_t n = std::min(w.size, vocab - first);
+        Operands piece = o;
+        if (const int rc = lay_weight<T>(w, first, n, dim, &piece, laid + w.x, s)) return rc;
+        StatsArgs b = a;
+        b.p = along_args(piece, w, rows, n, dim);
+        b.first = first;
+        b.parts += join.tiles;
+        int64_t tiles = 0;
+        if (const int rc = w.layout.anew ? stats_of<uint16_t>(b, &tiles, s) : stats_of<T>(b, &tiles, s)) return rc;
+        join.tiles += tiles;
+    }
+    join_kernel<<<dim3((uint32_t)rows), dim3(kJoin), 0, s>>>(join);
+    return launched();
+}
+
+template <class T>
+int gradient(GradArgs a, int parts, hipStream_t s)
+{
+    constexpr int32_t dtype = sizeof(T) == 4 ? ADAGC_F32 : ADAGC_BF16;
+    if (parts == 1 && thin(a.p, dtype)) {
         const dim3 blocks((uint32_t)std::min<int64_t>((a.p.n + kThinColumns - 1) / kThinColumns, kThinGrid));
         for_rows(a.p.m, [&](auto TM) { thin_grad_kernel<T, decltype(TM)::value><<<blocks, dim3(kThinThreads), 0, s>>>(a); });
-    } else if constexpr (sizeof(T) == 2) {
-        if (p.size == 256) grad_kernel<Large, T><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
-        else if (p.direct) grad_kernel<Small, T><<<grid, dim3(Small::kThreads), 0, s>>>(a);
+        return launched();
     }
-    if (!few && !p.direct) {
-        if constexpr (sizeof(T) == 4) {
-            if (p.size == 64) grad_kernel<Smallest, T><<<grid, dim3(Smallest::kThreads), 0, s>>>(a);
-        }
-        if (p.size == 128) grad_kernel<Staged<T>, T><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+    const AlongPlan p = plan_of(&a.p, dtype);
+    const dim3 grid((uint32_t)(p.tiles_m * p.tiles_n));
+    if constexpr (sizeof(T) == 2) {
+        const dim3 large(grid_of<Large>(p.tiles_m * p.tiles_n));
+        if (p.size == 256 && parts > 1) grad_kernel<Large, T, kParts><<<large, dim3(Large::kThreads), 0, s>>>(a);
+        else if (p.size == 256) grad_kernel<Large, T, 1><<<large, dim3(Large::kThreads), 0, s>>>(a);
+        else if (p.direct && parts > 1) grad_kernel<Small, T, kParts><<<grid, dim3(Small::kThreads), 0, s>>>(a);
+        else if (p.direct) grad_kernel<Small, T, 1><<<grid, dim3(Small::kThreads), 0, s>>>(a);
     }
-    return hipGetLastError() == hipSuccess ? ADAGC_OK : ADAGC_ERR_HIP;
+    if (!p.direct) grad_kernel<Staged<T>, T, 1><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+    return launched();
 }
 
 struct Outputs {
@@ -385,66 +464,71 @@ struct Outputs {
 };
 
 template <class T>
-int backward(const GradArgs& all, const Outputs& o, uint8_t* workspace, hipStream_t s)
+int backward(const Work& w, Operands o, int64_t rows, int64_t vocab, int64_t dim, const GradArgs& all, const Outputs& out, uint8_t* workspace, hipStream_t s)
 {
     constexpr int32_t dtype = sizeof(T) == 4 ? ADAGC_F32 : ADAGC_BF16;
-    const int64_t rows = all.p.m, vocab = all.vocab, dim = all.p.k;
-    const Pieces pieces = pieces_of(rows, vocab, dim, dtype);
-    float* sums = reinterpret_cast<float*>(workspace + pieces.d_logits);
-    float* partial = reinterpret_cast<float*>(workspace + pieces.d_logits + pieces.sums);
-    const int w_size = dtype_size(o.weight_dtype);
-    for (int64_t i = 0; i < pieces.number; ++i) {
-        const int64_t first = i * pieces.size, n = std::min(pieces.size, vocab - first);
-        const T* weight = static_cast<const T*>(all.p.x[0]) + first * all.p.ld_x[0];
+    float* sums = reinterpret_cast<float*>(workspace + w.d_logits);
+    float* partial = reinterpret_cast<float*>(workspace + w.d_logits + w.sums);
+    uint8_t* laid = workspace + w.d_logits + w.sums + w.partial;
+    const bool anew = w.layout.anew, parts = w.layout.parts > 1;
+    const int w_size = dtype_size(out.weight_dtype);
+    const int64_t rows_dz = parts ? Layout::rows_of(rows) : rows, columns = anew ? (dim + 7) / 8 * 8 : dim;
+    if (const int rc = lay_x<T>(w, rows, dim, &o, laid, s)) return rc;
+    auto product_across = [&](const PlainArgs& a) { return anew ? run_plain<uint16_t, true>(a, s) : run_plain<T, true>(a, s); };
+    auto product_along = [&](const PlainArgs& a) { return anew ? run_plain<uint16_t, false>(a, s) : run_plain<T, false>(a, s); };
+    for (int64_t first = 0; first < vocab; first += w.size) {
+        const int64_t n = std::min(w.size, vocab - first);
+        Operands piece = o;
+        PlainArgs both{};
+        both.y[0] = workspace;
+        both.ld_y = w.ld;
+        both.part_y = rows_dz * w.ld;
+        both.segments = w.layout.segments;
+        both.n = dim;
+        both.n_readable = columns;
+        both.workspace = partial;
+        both.factor = all.scale;
+        both.pairs = both.products = 1;
         if (rows > 0) {
+            if (const int rc = lay_weight<T>(w, first, n, dim, &piece, laid + w.x, s)) return rc;
             GradArgs a = all;
-            a.p.x[0] = a.p.x[1] = weight;
-            a.p.n = n;
+            a.p = along_args(piece, w, rows, n, dim);
             a.first = first;
             a.d_logits = workspace;
-            a.ld = pieces.ld;
-            if (const int rc = gradient<T>(a, s)) return rc;
+            a.ld = w.ld;
+            a.part = both.part_y;
+            a.rows = rows_dz;
+            if (const int rc = anew ? gradient<uint16_t>(a, w.layout.parts, s) : gradient<T>(a, 1, s)) return rc;
         }
-        if (o.d_weight) {
-            PlainArgs w{};
-            w.y[0] = workspace;
-            w.ld_y = pieces.ld;
-            w.x[0] = all.p.y;
-            w.ld_x[0] = all.p.ld_y;
-            w.out[0] = static_cast<uint8_t*>(o.d_weight) + first * o.ld_d_weight * w_size;
-            w.ld_out[0] = o.ld_d_weight;
-            w.add[0] = o.accumulate ? w.out[0] : nullptr;
-            w.ld_add[0] = o.ld_d_weight;
-            w.m = n;
-            w.m_readable = (n + 7) / 8 * 8;
-            w.n = dim;
-            w.k = rows;
-            w.workspace = partial;
-            w.factor = all.scale;
-            w.pairs = w.products = 1;
-            w.out_bf16 = w.add_bf16 = o.weight_dtype == ADAGC_BF16;
-            if (const int rc = run_plain<T, true>(w, s)) return rc;
+        if (out.d_weight) {
+            PlainArgs a = both;
+            a.x[0] = piece.x;
+            a.ld_x[0] = piece.ld_x;
+            a.part_x = w.layout.part(rows);
+            a.out[0] = static_cast<uint8_t*>(out.d_weight) + first * out.ld_d_weight * w_size;
+            a.ld_out[0] = out.ld_d_weight;
+            a.add[0] = out.accumulate ? a.out[0] : nullptr;
+            a.ld_add[0] = out.ld_d_weight;
+            a.m = n;
+            a.m_readable = (n + 7) / 8 * 8;
+            a.k = rows_dz;
+            a.out_bf16 = a.add_bf16 = out.weight_dtype == ADAGC_BF16;
+            if (const int rc = product_across(a)) return rc;
         }
-        if (o.d_x && rows > 0) {
-            const bool last = i == pieces.number - 1;
-            PlainArgs x{};
-            x.y[0] = workspace;
-            x.ld_y = pieces.ld;
-            x.x[0] = weight;
-            x.ld_x[0] = all.p.ld_x[0];
-            const bool direct = last || dtype == ADAGC_F32;
-            x.out[0] = direct ? o.d_x : sums;
-            x.ld_out[0] = direct ? o.ld_d_x : dim;
-            x.out_bf16 = direct && dtype == ADAGC_BF16;
-            x.add[0] = i == 0 ? nullptr : dtype == ADAGC_F32 ? o.d_x : sums;
-            x.ld_add[0] = dtype == ADAGC_F32 ? o.ld_d_x : dim;
-            x.m = x.m_readable = rows;
-            x.n = dim;
-            x.k = n;
-            x.workspace = partial;
-            x.factor = all.scale;
-            x.pairs = x.products = 1;
-            if (const int rc = run_plain<T, false>(x, s)) return rc;
+        if (out.d_x && rows > 0) {
+            PlainArgs a = both;
+            a.x[0] = piece.weight;
+            a.ld_x[0] = piece.ld_weight;
+            a.part_x = w.layout.part(n);
+            const bool direct = first + n == vocab || dtype == ADAGC_F32;
+            a.out[0] = direct ? out.d_x : sums;
+            a.ld_out[0] = direct ? out.ld_d_x : dim;
+            a.out_bf16 = direct && dtype == ADAGC_BF16;
+            a.add[0] = first == 0 ? nullptr : dtype == ADAGC_F32 ? out.d_x : sums;
+            a.ld_add[0] = dtype == ADAGC_F32 ? out.ld_d_x : dim;
+            a.m = a.m_readable = rows;
+            a.k = parts ? Layout::rows_of(n) : n;
+            if (const int rc = product_along(a)) return rc;
         }
     }
     return ADAGC_OK;
@@ -458,7 +542,7 @@ using namespace adagc;
 extern "C" int64_t adagc_linear_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int64_t dim, int32_t dtype)
 {
     if (const int rc = check(rows, vocab, dim, dtype)) return rc;
-    return launchable(rows, vocab, 1) ? forward_workspace(rows, vocab) : (int64_t)ADAGC_ERR_TOO_LARGE;
+    return launchable(rows, vocab, dim) ? work_of(rows, vocab, dim, dtype, false).forward() : (int64_t)ADAGC_ERR_TOO_LARGE;
 }
 
 extern "C" int adagc_linear_logprobs(const void* x, int64_t ld_x, const void* weight, int64_t ld_weight, int32_t dtype, int64_t rows, int64_t vocab,
@@ -472,30 +556,34 @@ extern "C" int adagc_linear_logprobs(const void* x, int64_t ld_x, const void* we
     if (!x || !weight || ld_x < dim || ld_weight < dim || misaligned(x, size) || misaligned(weight, size) || (logprob && !targets) ||
         misaligned(targets, 8) || misaligned(logprob, 4) || misaligned(stats, 4))
         return ADAGC_ERR_INVALID_ARG;
-    if (ld_x > kMaxLd || ld_weight > kMaxLd || !launchable(rows, vocab, 1)) return ADAGC_ERR_TOO_LARGE;
-    if (!workspace || workspace_bytes < forward_workspace(rows, vocab) || misaligned(workspace, 16)) return ADAGC_ERR_INVALID_ARG;
+    if (ld_x > kMaxLd || ld_weight > kMaxLd || !launchable(rows, vocab, dim)) return ADAGC_ERR_TOO_LARGE;
+    const Work w = work_of(rows, vocab, dim, dtype, false);
+    if (!workspace || workspace_bytes < w.forward() || misaligned(workspace, 16)) return ADAGC_ERR_INVALID_ARG;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
     StatsArgs a{};
-    a.p = along_args(x, ld_x, weight, ld_weight, rows, vocab, dim);
     a.targets = logprob ? targets : nullptr;
     a.scale = scale;
-    a.parts = static_cast<float2*>(workspace);
-    a.target_logit = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + up16(rows * parts_of_row(rows, vocab) * 8));
+    a.parts = reinterpret_cast<float2*>(ws);
+    a.pitch = w.pitch;
+    a.target_logit = reinterpret_cast<float*>(ws + w.parts);
     JoinArgs j{};
     j.parts = a.parts;
+    j.pitch = w.pitch;
     j.target_logit = a.target_logit;
     j.targets = targets;
     j.scale = scale;
     j.vocab = vocab;
     j.logprob = logprob;
     j.stats = reinterpret_cast<float2*>(stats);
+    const Operands o = {x, weight, ld_x, ld_weight};
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    return dtype == ADAGC_F32 ? forward<float>(a, j, s) : forward<uint16_t>(a, j, s);
+    return dtype == ADAGC_F32 ? forward<float>(w, o, rows, vocab, dim, a, j, ws, s) : forward<uint16_t>(w, o, rows, vocab, dim, a, j, ws, s);
 }
 
 extern "C" int64_t adagc_linear_logprobs_backward_workspace_bytes(int64_t rows, int64_t vocab, int64_t dim, int32_t dtype)
 {
     if (const int rc = check(rows, vocab, dim, dtype)) return rc;
-    return launchable(rows, vocab, dim) ? pieces_of(rows, vocab, dim, dtype).all() : (int64_t)ADAGC_ERR_TOO_LARGE;
+    return launchable(rows, vocab, dim) ? work_of(rows, vocab, dim, dtype, true).backward() : (int64_t)ADAGC_ERR_TOO_LARGE;
 }
 
 extern "C" int adagc_linear_logprobs_backward(const void* x, int64_t ld_x, const void* weight, int64_t ld_weight, int32_t dtype, int64_t rows,
@@ -513,17 +601,18 @@ extern "C" int adagc_linear_logprobs_backward(const void* x, int64_t ld_x, const
         return ADAGC_ERR_INVALID_ARG;
     if ((d_weight && ld_d_weight > kMaxLd) || (rows > 0 && (ld_x > kMaxLd || ld_weight > kMaxLd || (d_x && ld_d_x > kMaxLd))) || !launchable(rows, vocab, dim))
         return ADAGC_ERR_TOO_LARGE;
-    const int64_t need = pieces_of(rows, vocab, dim, dtype).all();
+    const Work w = work_of(rows, vocab, dim, dtype, true);
+    const int64_t need = w.backward();
     if (need > 0 && (!workspace || workspace_bytes < need || misaligned(workspace, 16))) return ADAGC_ERR_INVALID_ARG;
     GradArgs a{};
-    a.p = along_args(x, ld_x, weight, ld_weight, rows, vocab, dim);
     a.targets = targets;
     a.stats = stats;
     a.d_logprob = d_logprob;
     a.scale = scale;
     a.vocab = vocab;
-    const Outputs o = {d_x, ld_d_x, d_weight, weight_dtype, ld_d_weight, accumulate};
+    const Operands o = {x, weight, ld_x, ld_weight};
+    const Outputs out = {d_x, ld_d_x, d_weight, weight_dtype, ld_d_weight, accumulate};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    return dtype == ADAGC_F32 ? backward<float>(a, o, ws, s) : backward<uint16_t>(a, o, ws, s);
+    return dtype == ADAGC_F32 ? backward<float>(w, o, rows, vocab, dim, a, out, ws, s) : backward<uint16_t>(w, o, rows, vocab, dim, a, out, ws, s);
 }

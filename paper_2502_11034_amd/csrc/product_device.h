@@ -632,8 +632,7 @@ __device__ __forceinline__ f32x4_p load4(const T* row, int64_t col, int64_t leas
 
 using Large = Tile<uint16_t, 256, 256, 2, 4, true>;
 using Small = Tile<uint16_t, 128, 128, 2, 2, true>;
-template <class T> using Staged = Tile<T, 128, 128, 2, 2, false>;
-using Smallest = Tile<float, 64, 64, 2, 2, false>;
+template <class T> using Staged = Tile<T, sizeof(T) == 4 ? 64 : 128, sizeof(T) == 4 ? 64 : 128, 2, 2, false>;
 
 // Rows of an operand start at multiples of 16 bytes.
 inline bool rows_aligned(const void* p, int64_t ld, int32_t dtype) { return !misaligned(p, 16) && ld * dtype_size(dtype) % 16 == 0; }
@@ -645,13 +644,11 @@ struct AlongPlan {
     bool    direct;
     int64_t tiles_m, tiles_n;
 };
-// fp32: the matrix cores' fp32 rate is a sixteenth, which staging keeps up with; the 64-tile as long as the others would be few (333 x 5462 x 765,
-// 129 tiles of 128, 64 us)
+// fp32 as it is: the matrix cores' rate is a sixteenth, which staging and a small tile keep up with.
 template <class F>
 inline int tile_size(bool direct, int32_t dtype, F&& tiles)
 {
-    if (direct) return tiles(256) >= kUnits / 2 ? 256 : 128;
-    return dtype == ADAGC_F32 && tiles(128) < 4 * kUnits ? 64 : 128;
+    return direct && tiles(256) >= kUnits / 2 ? 256 : dtype == ADAGC_F32 ? 64 : 128;
 }
 inline AlongPlan along_plan(int64_t m, int64_t n, int32_t dtype, bool aligned, int64_t ld_y, int64_t ld_x)
 {
@@ -666,6 +663,34 @@ inline AlongPlan along_plan(int64_t m, int64_t n, int32_t dtype, bool aligned, i
 
 // ---------------------------------------------------------------------------------------- both operands along k
 
+// fp32 operands in three bf16 parts, hi + mid + lo, each the nearest to what the ones before it leave (8 + 8 + 8 significant bits, exact but
+// next to the type's ends): of the nine products of parts the six that count, smallest first; the others are some 2^-26 of the whole.  The
+// matrix cores' bf16 rate is 16 times the fp32 one.  Segment s takes parts part_of_y(s), part_of_x(s); a single segment takes the last one's.
+constexpr int kSegments = 6, kParts = 3;
+__device__ __forceinline__ int part_of_y(int s) { return 0x001102 >> (4 * s) & 15; }
+__device__ __forceinline__ int part_of_x(int s) { return 0x010120 >> (4 * s) & 15; }
+
+// Four values in parts: bits of bf16 pairs.  What is not finite is in the first part alone; what rounds beyond bf16's range keeps its largest number.
+__device__ __forceinline__ void split4(const f32x4_p& v, uint32_t (&bits)[kParts][2])
+{
+    float left[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+    for (int p = 0; p < kParts; ++p)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const f32x2_t two = {left[2 * i], left[2 * i + 1]};
+            uint32_t w = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, bf16x2_t));
+            if (p == 0) {
+                if ((w & 0x7FFFu) == 0x7F80u && __builtin_isfinite(left[2 * i])) w -= 1;
+                if ((w & 0x7FFF0000u) == 0x7F800000u && __builtin_isfinite(left[2 * i + 1])) w -= 0x10000u;
+            }
+            bits[p][i] = w;
+            const float lo = left[2 * i] - __uint_as_float(w << 16), hi = left[2 * i + 1] - __uint_as_float(w & 0xFFFF0000u);
+            left[2 * i] = __builtin_isfinite(left[2 * i]) ? lo : 0.f;
+            left[2 * i + 1] = __builtin_isfinite(left[2 * i + 1]) ? hi : 0.f;
+        }
+}
+
 // Rows of Y, and of X or, as the gated projections take them, of two matrices in turn: blocks of 16 columns of the result belong to x[0] and
 // x[1] alternately, so that a lane has both results of a place next to each other.
 struct AlongArgs {
@@ -673,6 +698,8 @@ struct AlongArgs {
     const void* x[2];
     int64_t     ld_y, ld_x[2];
     int64_t     m, n, k;          // n: rows of one X
+    int64_t     part_y, part_x;   // operands in parts: elements from part to part
+    int32_t     segments;         // products that are summed: 1, or kSegments of operands in three parts
     int32_t     tiles_m, tiles_n;
 };
 
@@ -717,43 +744,51 @@ __device__ __forceinline__ void along_tiles(const AlongArgs& a, uint8_t* lds, Be
         finish(acc, m0, n0, lds);
     } else {
         const int pairs = (int)(a.k / (2 * S::kDeep)), tiles = a.tiles_m * a.tiles_n;
-        const bool rest = a.k % (2 * S::kDeep);
-        auto aim = [&]() __attribute__((always_inline)) {
+        const bool rest = a.k % (2 * S::kDeep);        // (not with several segments)
+        auto aim = [&](int segment) __attribute__((always_inline)) {
             // a load of a wave is 8 rows, and a lane's are a multiple of 32 apart: with two matrices, all of one
             static_assert(S::kThreads / 8 % 32 == 0);
             const int tid = thread_anew();
             const bool second = PAIR && (wave >> 1 & 1);
             const int64_t ld_x = second ? a.ld_x[1] : a.ld_x[0];
-            sy.set_rows_direct(tid, y + m0 * a.ld_y, a.ld_y, [&](int r) { return min(m0 + r, a.m - 1) - m0; });
-            sx.set_rows_direct(tid, static_cast<const T*>(second ? a.x[1] : a.x[0]) + n0 * ld_x, ld_x, [&](int r) { return row_of_x(r) - n0; });
+            sy.set_rows_direct(tid, y + part_of_y(segment) * a.part_y + m0 * a.ld_y, a.ld_y, [&](int r) { return min(m0 + r, a.m - 1) - m0; });
+            sx.set_rows_direct(tid, static_cast<const T*>(second ? a.x[1] : a.x[0]) + part_of_x(segment) * a.part_x + n0 * ld_x, ld_x,
+                               [&](int r) { return row_of_x(r) - n0; });
         };
-        int n = (int)blockIdx.x;
+        const int first = kSegments - a.segments;
+        int n = (int)blockIdx.x, segment = first;
         to_tile(n);
         if (!rest) {
-            aim();
+            aim(segment);
             start_direct<S>(sy, sx, lds0, 0, pairs);
         }
+        clear<S>(acc);
         while (true) {
-            clear<S>(acc);
             if (rest) {
                 aim_staged();
                 accumulate_rest<S, T>(acc, sy, sx, 2 * pairs, a.k, 0, 0);
-                aim();
+                aim(segment);
                 start_direct<S>(sy, sx, lds0, 0, pairs);
             }
             accumulate_direct<S, T>(acc, sy, sx, lds0, 0, pairs);
+            const bool last = segment == kSegments - 1;
             const int64_t m_now = m0, n_now = n0;
-            before(m_now, n_now);
-            n += (int)gridDim.x;
-            if (n < tiles) {
-                to_tile(n);
-                if (!rest) {
-                    aim();
-                    start_direct<S>(sy, sx, lds0, 0, pairs);
-                }
+            if (!last) {
+                ++segment;
+            } else {
+                before(m_now, n_now);
+                n += (int)gridDim.x;
+                segment = first;
+                if (n < tiles) to_tile(n);
             }
+            if ((!last || n < tiles) && !rest) {
+                aim(segment);
+                start_direct<S>(sy, sx, lds0, 0, pairs);
+            }
+            if (!last) continue;
             finish(acc, m_now, n_now, lds + (kRing - 1) * S::kPlace);
             if (n >= tiles) break;
+            clear<S>(acc);
         }
     }
 }
@@ -929,6 +964,9 @@ struct PlainArgs {
     int64_t     ld_add[2];
     int64_t     m, n, k;
     int64_t     m_readable;       // Y across k: columns of it that may be read, m or more
+    int64_t     n_readable;       // columns of X that may be read, n or more
+    int64_t     part_y, part_x;   // operands in parts: elements from part to part
+    int32_t     segments;         // products that are summed for a pair: 1, or kSegments of operands in three parts
     float*      workspace;        // partial sums of the split tiles
     float       factor;
     int32_t     pairs;            // 1, or 2: both pairs' products are summed
@@ -981,6 +1019,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void plain_kernel(const PlainArgs a
     const int full = (int)(a.k / kTogether), items = a.whole + (a.tiles_m * a.tiles_n * a.products - a.whole) * a.split;
     const bool uneven = a.k % kTogether;
     const int64_t m_readable = ACROSS_Y ? a.m_readable : a.m;
+    const int turns = a.pairs * a.segments, first_segment = kSegments - a.segments;       // of a tile: segments of one pair after the other
     struct Place {
         int     item, product;
         int64_t m0, n0, m_least, n_least;
@@ -1006,27 +1045,35 @@ __global__ __launch_bounds__(S::kThreads, 2) void plain_kernel(const PlainArgs a
         int tm, tn;
         place_of_tile(tile - p.product * per_product, a.tiles_m, a.tiles_n, &tm, &tn);
         p.m0 = scalar(first_of_tile<ACROSS_Y && !CHECKED>(tm, S::BM, m_readable));
-        p.n0 = scalar(first_of_tile<!CHECKED>(tn, S::BN, a.n));
+        p.n0 = scalar(first_of_tile<!CHECKED>(tn, S::BN, a.n_readable));
         p.m_least = (int64_t)tm * S::BM;
         p.n_least = (int64_t)tn * S::BN;
         return p;
     };
-    auto y_of = [&](int pair) { return static_cast<const T*>(pair ? a.y[1] : a.y[0]); };          // (an index would put the arguments into memory)
-    auto x_of = [&](int pair) { return static_cast<const T*>(pair ? a.x[1] : a.x[0]); };
-    auto ld_x_of = [&](int pair) { return pair ? a.ld_x[1] : a.ld_x[0]; };
-    auto aim_staged = [&](const Place& p, int pair) __attribute__((always_inline)) {
-        const int tid = thread_anew();
-        const T* y = y_of(pair);
+    // (an index would put the arguments into memory)
+    auto pair_of = [&](const Place& p, int turn) __attribute__((always_inline)) { return p.product || turn >= a.segments; };
+    auto segment_of = [&](int turn) __attribute__((always_inline)) { return first_segment + (turn >= a.segments ? turn - a.segments : turn); };
+    auto y_of = [&](bool second, int segment) __attribute__((always_inline)) {
+        return static_cast<const T*>(second ? a.y[1] : a.y[0]) + part_of_y(segment) * a.part_y;
+    };
+    auto x_of = [&](bool second, int segment) __attribute__((always_inline)) {
+        return static_cast<const T*>(second ? a.x[1] : a.x[0]) + part_of_x(segment) * a.part_x;
+    };
+    auto aim_staged = [&](const Place& p, int turn) __attribute__((always_inline)) {
+        const int tid = thread_anew(), segment = segment_of(turn);
+        const bool second = pair_of(p, turn);
+        const T* y = y_of(second, segment);
         if constexpr (ACROSS_Y) sy.set_columns(tid, y + p.m0, a.ld_y);
         else sy.set_rows(tid, [&](int r) { return y + min(p.m0 + r, a.m - 1) * a.ld_y; });
-        sx.set_columns(tid, x_of(pair) + p.n0, ld_x_of(pair));
+        sx.set_columns(tid, x_of(second, segment) + p.n0, second ? a.ld_x[1] : a.ld_x[0]);
     };
-    auto aim = [&](const Place& p, int pair) __attribute__((always_inline)) {
-        const int tid = thread_anew();
-        const T* y = y_of(pair);
+    auto aim = [&](const Place& p, int turn) __attribute__((always_inline)) {
+        const int tid = thread_anew(), segment = segment_of(turn);
+        const bool second = pair_of(p, turn);
+        const T* y = y_of(second, segment);
         if constexpr (ACROSS_Y) sy.set_columns_direct(tid, y + p.m0, a.ld_y);
         else sy.set_rows_direct(tid, y + p.m0 * a.ld_y, a.ld_y, [&](int r) { return min(p.m0 + r, a.m - 1) - p.m0; });
-        sx.set_columns_direct(tid, x_of(pair) + p.n0, ld_x_of(pair));
+        sx.set_columns_direct(tid, x_of(second, segment) + p.n0, second ? a.ld_x[1] : a.ld_x[0]);
     };
     Sums<S> acc;
     auto finish_inside = [&](const Place& p, auto* out, const auto* add) __attribute__((always_inline)) {
@@ -1071,39 +1118,39 @@ __global__ __launch_bounds__(S::kThreads, 2) void plain_kernel(const PlainArgs a
 
     clear<S>(acc);
     Place now = place_of((int)blockIdx.x);
+    int turn = 0;
     if constexpr (!S::kDirect) {
-        for (int pair = now.product; pair < now.product + a.pairs; ++pair) {
-            aim_staged(now, pair);
-            accumulate<S, T, CHECKED>(acc, sy, sx, step0, step1, rest, full, a.k, m_readable - now.m0, a.n - now.n0);
+        for (; turn < turns; ++turn) {
+            aim_staged(now, turn);
+            accumulate<S, T, CHECKED>(acc, sy, sx, step0, step1, rest, full, a.k, m_readable - now.m0, a.n_readable - now.n0);
         }
         finish(now);
     } else {
-        int pair = now.product;
         if (!uneven) {
-            aim(now, pair);
+            aim(now, turn);
             start_direct<S>(sy, sx, lds0, step0, step1 - step0);
         }
         while (true) {
             if (uneven) {
                 if (rest) {
-                    aim_staged(now, pair);
-                    accumulate_rest<S, T>(acc, sy, sx, 2 * (int64_t)full, a.k, m_readable - now.m0, a.n - now.n0);
+                    aim_staged(now, turn);
+                    accumulate_rest<S, T>(acc, sy, sx, 2 * (int64_t)full, a.k, m_readable - now.m0, a.n_readable - now.n0);
                 }
-                aim(now, pair);
+                aim(now, turn);
                 start_direct<S>(sy, sx, lds0, step0, step1 - step0);
             }
             accumulate_direct<S, T>(acc, sy, sx, lds0, step0, step1 - step0);
-            const bool last = pair + 1 == now.product + a.pairs;
+            const bool last = turn + 1 == turns;
             const int item = now.item + (int)gridDim.x;
             const Place done = now;
             if (!last) {
-                ++pair;
+                ++turn;
             } else if (item < items) {
                 now = place_of(item);
-                pair = now.product;
+                turn = 0;
             }
             if ((!last || item < items) && !uneven) {
-                aim(now, pair);
+                aim(now, turn);
                 start_direct<S>(sy, sx, lds0, step0, step1 - step0);
             }
             if (!last) continue;
@@ -1124,7 +1171,7 @@ __global__ __launch_bounds__(S::kThreads) void plain_join_kernel(const PlainArgs
     const int tile = a.whole + n_tile, per_product = a.tiles_m * a.tiles_n, product = tile / per_product;
     int tm, tn;
     place_of_tile(tile - product * per_product, a.tiles_m, a.tiles_n, &tm, &tn);
-    const int64_t m0 = first_of_tile<ACROSS_Y && !CHECKED>(tm, S::BM, ACROSS_Y ? a.m_readable : a.m), n0 = first_of_tile<!CHECKED>(tn, S::BN, a.n);
+    const int64_t m0 = first_of_tile<ACROSS_Y && !CHECKED>(tm, S::BM, ACROSS_Y ? a.m_readable : a.m), n0 = first_of_tile<!CHECKED>(tn, S::BN, a.n_readable);
     const f32x4_p* from = reinterpret_cast<const f32x4_p*>(a.workspace) + (size_t)n_tile * a.split * (S::BM * S::BN / 4) + (size_t)block * S::kThreads + tid;
     f32x4_p sum = from[0];
     int p = 1;
@@ -1148,8 +1195,8 @@ struct PlainPlan {
     int64_t workspace() const { return split > 1 ? rest * split * size * size * 4 : 0; }
     bool    launchable() const { return (whole + rest * split) * (size == 256 ? 512 : 256) <= UINT32_MAX; }      // lanes
 };
-// m: with Y across k, of its readable columns; pairs: of operands that are summed; products: side by side; aligned: the rows of both operands
-// are, and so is m.  A workspace is sized for both.
+// m (with Y across k) and n: of the readable columns; pairs: of operands that are summed; products: side by side; aligned: the rows of both
+// operands are.  A workspace is sized for both.
 inline PlainPlan plain_plan(int64_t m, int64_t n, int64_t k, int32_t dtype, bool across_y, int64_t ld_y, int64_t ld_x, int pairs, int products, bool aligned)
 {
     PlainPlan p{};
@@ -1157,7 +1204,7 @@ inline PlainPlan plain_plan(int64_t m, int64_t n, int64_t k, int32_t dtype, bool
     // 32 rows across, 256 along k are not within 32 bits
     const bool far = ld_x >= (int64_t)1 << 24 || (across_y && ld_y >= (int64_t)1 << 24);
     p.direct = aligned && !far && dtype == ADAGC_BF16 && (across_y || ld_y < (int64_t)1 << 23) && n >= 128 && n % 8 == 0 &&
-               (!across_y || m >= 128);      // (m: of what is readable, a multiple of 8)
+               (!across_y || (m >= 128 && m % 8 == 0));
     p.size = tile_size(p.direct, dtype, tiles);
     if (p.size == 256 && (m < 256 || n < 256)) p.size = 128;
     const bool large = p.size == 256;
@@ -1189,13 +1236,13 @@ int run_plain(PlainArgs a, hipStream_t s)
     constexpr int32_t dtype = sizeof(T) == 4 ? ADAGC_F32 : ADAGC_BF16;
     const int both = std::max(a.pairs, a.products);
     const int64_t m = ACROSS_Y ? a.m_readable : a.m;
-    bool aligned = !ACROSS_Y || m % 8 == 0;
+    bool aligned = true;
     int64_t ld_x = 0;
     for (int i = 0; i < both; ++i) {
-        aligned = aligned && rows_aligned(a.y[i], a.ld_y, dtype) && rows_aligned(a.x[i], a.ld_x[i], dtype);
+        aligned = aligned && rows_aligned(a.y[i], a.ld_y, dtype) && rows_aligned(a.x[i], a.ld_x[i], dtype);      // (parts are multiples of 16 bytes apart)
         ld_x = std::max(ld_x, a.ld_x[i]);
     }
-    const PlainPlan p = plain_plan(m, a.n, a.k, dtype, ACROSS_Y, a.ld_y, ld_x, a.pairs, a.products, aligned);
+    const PlainPlan p = plain_plan(m, a.n_readable, a.k, dtype, ACROSS_Y, a.ld_y, ld_x, a.pairs * a.segments, a.products, aligned);
     a.tiles_m = (int32_t)p.tiles_m;
     a.tiles_n = (int32_t)p.tiles_n;
     a.whole = (int32_t)p.whole;
@@ -1203,10 +1250,67 @@ int run_plain(PlainArgs a, hipStream_t s)
     if constexpr (sizeof(T) == 2) {
         if (p.size == 256) return launch_plain<Large, T, ACROSS_Y, false>(a, p, s);
         if (p.direct) return launch_plain<Small, T, ACROSS_Y, false>(a, p, s);
-    } else {
-        if (p.size == 64) return p.checked ? launch_plain<Smallest, T, ACROSS_Y, true>(a, p, s) : launch_plain<Smallest, T, ACROSS_Y, false>(a, p, s);
     }
     return p.checked ? launch_plain<Staged<T>, T, ACROSS_Y, true>(a, p, s) : launch_plain<Staged<T>, T, ACROSS_Y, false>(a, p, s);
+}
+
+// ---------------------------------------------------------------------------------------- operands laid out anew
+//
+// fp32 operands in three parts, and bf16 ones whose rows are not multiples of 16 bytes, are copied to the workspace first, rows and columns filled
+// up to multiples of 64 with zeros, and multiplied by the bf16 tiles that load straight into LDS.  For fewer than 128 rows that costs more than it
+// saves.
+struct Layout {
+    bool    anew;
+    int     parts, segments;
+    int64_t ld;                   // of rows of k numbers
+    int64_t bytes(int64_t rows) const { return parts * rows_of(rows) * ld * 2; }
+    int64_t part(int64_t rows) const { return rows_of(rows) * ld; }                // elements
+    static int64_t rows_of(int64_t rows) { return (rows + 63) / 64 * 64; }
+};
+inline Layout layout_of(int64_t rows, int64_t wide, int64_t k, int32_t dtype)
+{
+    Layout l{};
+    l.anew = rows >= 128 && wide >= 128 && k >= 128 && k < (int64_t)1 << 22 && (dtype == ADAGC_F32 || k % 8);
+    l.parts = l.anew && dtype == ADAGC_F32 ? kParts : 1;
+    l.segments = l.parts == 1 ? 1 : kSegments;
+    l.ld = (k + 63) / 64 * 64;
+    return l;
+}
+
+struct LayArgs {
+    const void* from;
+    uint16_t*   to;
+    int64_t     ld_from, ld_to, part, rows, cols, vectors, all;
+};
+constexpr int kLay = 256;
+// 8 numbers of a row for a lane.  Bound by memory.
+template <class T>
+__global__ __launch_bounds__(kLay) void lay_kernel(const LayArgs a)
+{
+    const int64_t i = (int64_t)blockIdx.x * kLay + threadIdx.x;
+    if (i >= a.all) return;
+    const int64_t row = i / a.vectors, col = (i - row * a.vectors) * 8;
+    const T* from = static_cast<const T*>(a.from) + row * a.ld_from;
+    u32x4* to = reinterpret_cast<u32x4*>(a.to + row * a.ld_to + col);
+    const int64_t n = row < a.rows ? a.cols : 0;
+    if constexpr (sizeof(T) == 2) {
+        *to = load_vector(from, col, n, 0).w;
+    } else {
+        uint32_t bits[2][kParts][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) split4(__builtin_bit_cast(f32x4_p, load_vector(from, col + 4 * h, n, 0).w), bits[h]);
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) to[p * (a.part / 8)] = u32x4{bits[0][p][0], bits[0][p][1], bits[1][p][0], bits[1][p][1]};
+    }
+}
+template <class T>
+int lay(const void* from, int64_t ld_from, int64_t rows, int64_t cols, const Layout& l, void* to, hipStream_t s)
+{
+    const int64_t all = Layout::rows_of(rows) * (l.ld / 8);
+    if (all == 0) return ADAGC_OK;
+    lay_kernel<T><<<dim3((uint32_t)((all + kLay - 1) / kLay)), dim3(kLay), 0, s>>>(
+        {from, static_cast<uint16_t*>(to), ld_from, l.ld, l.part(rows), rows, cols, l.ld / 8, all});
+    return hipGetLastError() == hipSuccess ? ADAGC_OK : ADAGC_ERR_HIP;
 }
 
 // instantiated in product.hip
@@ -1214,6 +1318,8 @@ extern template int run_plain<float, false>(PlainArgs, hipStream_t);
 extern template int run_plain<float, true>(PlainArgs, hipStream_t);
 extern template int run_plain<uint16_t, false>(PlainArgs, hipStream_t);
 extern template int run_plain<uint16_t, true>(PlainArgs, hipStream_t);
+extern template int lay<float>(const void*, int64_t, int64_t, int64_t, const Layout&, void*, hipStream_t);
+extern template int lay<uint16_t>(const void*, int64_t, int64_t, int64_t, const Layout&, void*, hipStream_t);
 
 }  // namespace product
 }  // namespace adagc
