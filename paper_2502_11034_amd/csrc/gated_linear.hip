@@ -280,13 +280,11 @@ int lay_operands(const Work& w, AlongArgs* p, uint8_t* space, hipStream_t s)
 {
     p->segments = w.layout.segments;
     if (!w.layout.anew || p->m == 0) return ADAGC_OK;
-    if (const int rc = lay<T>(p->y, p->ld_y, p->m, p->k, w.layout, space, s)) return rc;
+    const LaySource sources[3] = {{p->x[0], p->ld_x[0], p->n, space + w.x}, {p->x[1], p->ld_x[1], p->n, space + w.x + w.weight}, {p->y, p->ld_y, p->m, space}};
+    if (const int rc = lay<T>(sources, 3, p->k, w.layout, s)) return rc;
     p->y = space;
-    for (int i = 0; i < 2; ++i) {
-        uint8_t* to = space + w.x + i * w.weight;
-        if (const int rc = lay<T>(p->x[i], p->ld_x[i], p->n, p->k, w.layout, to, s)) return rc;
-        p->x[i] = to;
-    }
+    p->x[0] = space + w.x;
+    p->x[1] = space + w.x + w.weight;
     p->ld_y = p->ld_x[0] = p->ld_x[1] = p->k = w.layout.ld;
     p->part_y = w.layout.part(p->m);
     p->part_x = w.layout.part(p->n);
@@ -311,9 +309,10 @@ int projections(GatedArgs a, hipStream_t s)
     a.p.tiles_n = (int32_t)p.tiles_n;
     const dim3 grid((uint32_t)(p.tiles_m * p.tiles_n));
     if constexpr (sizeof(T) == 2) {
+        const dim3 small(grid_of<Small>(p.tiles_m * p.tiles_n));
         constexpr int kOf = BACKWARD && sizeof(O) == 4 ? kParts : 1;       // (fp32 data is laid out in parts)
         if (p.size == 256) gated_kernel<Large, T, O, BACKWARD, kOf><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
-        else if (p.direct) gated_kernel<Small, T, O, BACKWARD, kOf><<<grid, dim3(Small::kThreads), 0, s>>>(a);
+        else if (p.direct) gated_kernel<Small, T, O, BACKWARD, kOf><<<small, dim3(Small::kThreads), 0, s>>>(a);
     }
     if constexpr (sizeof(T) == sizeof(O)) {
         if (!p.direct) gated_kernel<Staged<T>, T, O, BACKWARD, 1><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);

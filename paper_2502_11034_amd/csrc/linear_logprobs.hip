@@ -344,24 +344,20 @@ struct Operands {
     const void *x, *weight;
     int64_t     ld_x, ld_weight;
 };
+// The piece of the weights from `first` on, and with the first one x too.
 template <class T>
-int lay_x(const Work& w, int64_t rows, int64_t dim, Operands* o, uint8_t* space, hipStream_t s)
+int lay_piece(const Work& w, int64_t rows, int64_t first, int64_t n, int64_t dim, Operands* all, Operands* piece, uint8_t* space, hipStream_t s)
 {
-    if (!w.layout.anew || rows == 0) return ADAGC_OK;
-    if (const int rc = lay<T>(o->x, o->ld_x, rows, dim, w.layout, space, s)) return rc;
-    o->x = space;
-    o->ld_x = w.layout.ld;
-    return ADAGC_OK;
-}
-// first, n: the piece
-template <class T>
-int lay_weight(const Work& w, int64_t first, int64_t n, int64_t dim, Operands* o, uint8_t* space, hipStream_t s)
-{
-    o->weight = static_cast<const T*>(o->weight) + first * o->ld_weight;
+    const void* weight = static_cast<const T*>(all->weight) + first * all->ld_weight;
+    *piece = *all;
+    piece->weight = weight;
     if (!w.layout.anew) return ADAGC_OK;
-    if (const int rc = lay<T>(o->weight, o->ld_weight, n, dim, w.layout, space, s)) return rc;
-    o->weight = space;
-    o->ld_weight = w.layout.ld;
+    const LaySource sources[2] = {{weight, all->ld_weight, n, space + w.x}, {all->x, all->ld_x, rows, space}};
+    if (const int rc = lay<T>(sources, first == 0 ? 2 : 1, dim, w.layout, s)) return rc;
+    all->x = piece->x = space;
+    all->ld_x = piece->ld_x = w.layout.ld;
+    piece->weight = space + w.x;
+    piece->ld_weight = w.layout.ld;
     return ADAGC_OK;
 }
 AlongArgs along_args(const Operands& o, const Work& w, int64_t rows, int64_t n, int64_t dim)
@@ -404,8 +400,9 @@ int stats_of(StatsArgs a, int64_t* tiles, hipStream_t s)
     *tiles = p.tiles_n;
     const dim3 grid((uint32_t)(p.tiles_m * p.tiles_n));
     if constexpr (sizeof(T) == 2) {
+        const dim3 small(grid_of<Small>(p.tiles_m * p.tiles_n));
         if (p.size == 256) stats_kernel<Large, T><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
-        else if (p.direct) stats_kernel<Small, T><<<grid, dim3(Small::kThreads), 0, s>>>(a);
+        else if (p.direct) stats_kernel<Small, T><<<small, dim3(Small::kThreads), 0, s>>>(a);
     }
     if (!p.direct) stats_kernel<Staged<T>, T><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
     return launched();
@@ -415,11 +412,10 @@ template <class T>
 int forward(const Work& w, Operands o, int64_t rows, int64_t vocab, int64_t dim, StatsArgs a, JoinArgs join, uint8_t* workspace, hipStream_t s)
 {
     uint8_t* laid = workspace + w.parts + w.targets;
-    if (const int rc = lay_x<T>(w, rows, dim, &o, laid, s)) return rc;
     for (int64_t first = 0; first < vocab; first += w.size) {
         const int64_t n = std::min(w.size, vocab - first);
-        Operands piece = o;
-        if (const int rc = lay_weight<T>(w, first, n, dim, &piece, laid + w.x, s)) return rc;
+        Operands piece;
+        if (const int rc = lay_piece<T>(w, rows, first, n, dim, &o, &piece, laid, s)) return rc;
         StatsArgs b = a;
         b.p = along_args(piece, w, rows, n, dim);
         b.first = first;
@@ -444,11 +440,11 @@ int gradient(GradArgs a, int parts, hipStream_t s)
     const AlongPlan p = plan_of(&a.p, dtype);
     const dim3 grid((uint32_t)(p.tiles_m * p.tiles_n));
     if constexpr (sizeof(T) == 2) {
-        const dim3 large(grid_of<Large>(p.tiles_m * p.tiles_n));
+        const dim3 large(grid_of<Large>(p.tiles_m * p.tiles_n)), small(grid_of<Small>(p.tiles_m * p.tiles_n));
         if (p.size == 256 && parts > 1) grad_kernel<Large, T, kParts><<<large, dim3(Large::kThreads), 0, s>>>(a);
         else if (p.size == 256) grad_kernel<Large, T, 1><<<large, dim3(Large::kThreads), 0, s>>>(a);
-        else if (p.direct && parts > 1) grad_kernel<Small, T, kParts><<<grid, dim3(Small::kThreads), 0, s>>>(a);
-        else if (p.direct) grad_kernel<Small, T, 1><<<grid, dim3(Small::kThreads), 0, s>>>(a);
+        else if (p.direct && parts > 1) grad_kernel<Small, T, kParts><<<small, dim3(Small::kThreads), 0, s>>>(a);
+        else if (p.direct) grad_kernel<Small, T, 1><<<small, dim3(Small::kThreads), 0, s>>>(a);
     }
     if (!p.direct) grad_kernel<Staged<T>, T, 1><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
     return launched();
@@ -473,7 +469,6 @@ int backward(const Work& w, Operands o, int64_t rows, int64_t vocab, int64_t dim
     const bool anew = w.layout.anew, parts = w.layout.parts > 1;
     const int w_size = dtype_size(out.weight_dtype);
     const int64_t rows_dz = parts ? Layout::rows_of(rows) : rows, columns = anew ? (dim + 7) / 8 * 8 : dim;
-    if (const int rc = lay_x<T>(w, rows, dim, &o, laid, s)) return rc;
     auto product_across = [&](const PlainArgs& a) { return anew ? run_plain<uint16_t, true>(a, s) : run_plain<T, true>(a, s); };
     auto product_along = [&](const PlainArgs& a) { return anew ? run_plain<uint16_t, false>(a, s) : run_plain<T, false>(a, s); };
     for (int64_t first = 0; first < vocab; first += w.size) {
@@ -490,7 +485,7 @@ int backward(const Work& w, Operands o, int64_t rows, int64_t vocab, int64_t dim
         both.factor = all.scale;
         both.pairs = both.products = 1;
         if (rows > 0) {
-            if (const int rc = lay_weight<T>(w, first, n, dim, &piece, laid + w.x, s)) return rc;
+            if (const int rc = lay_piece<T>(w, rows, first, n, dim, &o, &piece, laid, s)) return rc;
             GradArgs a = all;
             a.p = along_args(piece, w, rows, n, dim);
             a.first = first;

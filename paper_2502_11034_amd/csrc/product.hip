@@ -7,7 +7,7 @@ template int run_plain<float, false>(PlainArgs, hipStream_t);
 template int run_plain<float, true>(PlainArgs, hipStream_t);
 template int run_plain<uint16_t, false>(PlainArgs, hipStream_t);
 template int run_plain<uint16_t, true>(PlainArgs, hipStream_t);
-template int lay<float>(const void*, int64_t, int64_t, int64_t, const Layout&, void*, hipStream_t);
-template int lay<uint16_t>(const void*, int64_t, int64_t, int64_t, const Layout&, void*, hipStream_t);
+template int lay<float>(const LaySource*, int, int64_t, const Layout&, hipStream_t);
+template int lay<uint16_t>(const LaySource*, int, int64_t, const Layout&, hipStream_t);
 }  // namespace product
 }  // namespace adagc

@@ -47,13 +47,12 @@ __device__ __forceinline__ void each(F&& f)
 // Compute units: a round of a launch is as many workgroups of the large tile.
 constexpr int kUnits = 256;
 constexpr int kPlaces = 3;                 // of LDS, that steps staged through registers go round in
-constexpr int kRing = 5;                   // of LDS, that operand tiles of two steps loaded straight into it go round in
 constexpr int kStepBytes = 64;             // of k, a step
 
 // BM x BN tile (BM rows of Y), kWM x kWN waves of kTM x kTN blocks of 16 x 16.  A step is 64 bytes of k: 32 bf16 or 16 fp32 numbers, so that
-// an operand's tile has the same bytes and a lane's fragment the same 16 with both types.  DIRECT: operands go from global memory straight into
-// LDS, which wants rows at multiples of 16 bytes; otherwise through registers, rows at any element.
-template <class T, int BM_, int BN_, int kWM_, int kWN_, bool DIRECT_>
+// an operand's tile has the same bytes and a lane's fragment the same 16 with both types.  RING: operands go from global memory straight into LDS,
+// into a ring of so many places, which wants rows at multiples of 16 bytes; 0: through registers, rows at any element.
+template <class T, int BM_, int BN_, int kWM_, int kWN_, int RING_>
 struct Tile {
     static constexpr int BM = BM_, BN = BN_, kWM = kWM_, kWN = kWN_;
     static constexpr int kThreads = 64 * kWM * kWN;
@@ -61,10 +60,11 @@ struct Tile {
     static constexpr int kDeep = kStepBytes / (int)sizeof(T);
     static constexpr int kY = BM * kStepBytes, kX = BN * kStepBytes, kPlace = kY + kX;      // bytes
     static constexpr int kYUnits = kY / 16 / kThreads, kXUnits = kX / 16 / kThreads;       // of 16 bytes, a lane's
-    static constexpr bool kDirect = DIRECT_;
+    static constexpr bool kDirect = RING_ > 0;
+    static constexpr int kRing = RING_, kAhead = (RING_ - 1) / 2;                          // places of the ring; pairs of steps that loads are ahead
     static constexpr int kYLoads = 2 * kYUnits, kXLoads = 2 * kXUnits;                     // straight into LDS, of two steps, a lane's
-    static constexpr int kLds = (DIRECT_ ? kRing : kPlaces) * kPlace;
-    static_assert(!DIRECT_ || BM_ == BN_, "a place of the ring takes either operand");
+    static constexpr int kLds = (RING_ ? RING_ : kPlaces) * kPlace;
+    static_assert(!RING_ || (BM_ == BN_ && RING_ % 2 == 1 && RING_ >= 5), "a place of the ring takes either operand, X and Y in turn");
     static_assert(kY % (16 * kThreads) == 0 && kX % (16 * kThreads) == 0, "operand tiles are dealt evenly");
 };
 
@@ -122,6 +122,12 @@ __device__ __forceinline__ void place_of_tile(int n, int tiles_m, int tiles_n, i
     *tn = __builtin_amdgcn_readfirstlane(in_band / high);          // the same in all lanes: kept in scalar registers
     *tm = __builtin_amdgcn_readfirstlane(8 * band + in_band - *tn * high);
 }
+
+// fp32 operands in three bf16 parts, hi + mid + lo, each the nearest to what the ones before it leave (8 + 8 + 8 significant bits, exact but
+// next to the type's ends): of the nine products of parts the six that count, smallest first; the others are some 2^-26 of the whole.  The
+// matrix cores' bf16 rate is 16 times the fp32 one.  Segment s takes the parts that digit s of these says; a single segment takes the last one's.
+constexpr int kSegments = 6, kParts = 3;
+constexpr uint32_t kPartsOfY = 0x001102, kPartsOfX = 0x010120;
 
 // How one operand's tile (B rows or columns of the result) is loaded, staged in LDS and read: kUnits units of 16 bytes a step for a lane.
 //
@@ -219,6 +225,11 @@ struct Side {
     static constexpr int kLoads = 2 * kUnits, kAlong = ACROSS ? kVectors : 8;
     uint32_t off[ACROSS ? 1 : kLoads];     // bytes from the first step's address, which is the same in all lanes
     const T* base;
+    // the next pair of steps to load, of a segment's the pairs from `first` on; segments follow each other
+    const T* at;
+    int      first, pairs, left, segment;
+    int64_t  part;
+    uint32_t parts_table;
 
     // Position i of row r gets vector unplaced(r, i), so that vector v is where place(r, v) says (its own inverse).
     static __device__ __forceinline__ int unplaced(int r, int i) { return (int)(place(r, i) % (uint32_t)kPitch) / 16; }
@@ -240,12 +251,34 @@ struct Side {
         const int r = tid / kAlong;
         off[0] = ((uint32_t)r * (uint32_t)ld_ + (uint32_t)unplaced(r, tid % kAlong) * kE) * (uint32_t)sizeof(T);
     }
-    __device__ __forceinline__ void load_direct(int two_steps, int u, uint32_t lds_at) const
+    __device__ __forceinline__ void to_segment()
+    {
+        at = base + (parts_table >> (4 * segment) & 15) * part + (ACROSS ? (int64_t)(first * 2 * kDeep) * ld : (int64_t)first * 2 * kDeep);
+        left = pairs;
+    }
+    __device__ __forceinline__ void set_pairs(int first_, int pairs_, int segments, int64_t part_, uint32_t table)
+    {
+        first = first_;
+        pairs = pairs_;
+        segment = kSegments - segments;
+        part = part_;
+        parts_table = table;
+        to_segment();
+    }
+    __device__ __forceinline__ void load_direct(int u, uint32_t lds_at) const
     {
         constexpr int kRows = kThreads / kAlong;       // of a load, across: the permutation repeats after 16
         static_assert(!ACROSS || kRows % 16 == 0);
-        if constexpr (ACROSS) load_to_lds(base + (int64_t)(two_steps * 2 * kDeep + u * kRows) * ld, off[0], lds_at + (uint32_t)(u * kThreads * 16));
-        else load_to_lds(base + (int64_t)two_steps * 2 * kDeep, off[u], lds_at + (uint32_t)(u * kThreads * 16));
+        if constexpr (ACROSS) load_to_lds(at + (int64_t)(u * kRows) * ld, off[0], lds_at + (uint32_t)(u * kThreads * 16));
+        else load_to_lds(at, off[u], lds_at + (uint32_t)(u * kThreads * 16));
+    }
+    __device__ __forceinline__ void advance()
+    {
+        at += ACROSS ? 2 * kDeep * ld : (int64_t)(2 * kDeep);
+        if (--left == 0) {
+            ++segment;
+            to_segment();
+        }
     }
 
     // second: of two steps in a place
@@ -461,40 +494,41 @@ __device__ __forceinline__ void accumulate_rest(Sums<S>& acc, const SideY& sy, c
     __syncthreads();
 }
 
-// Pairs of steps pair0 .. pair1 - 1 with operands that go straight into LDS, into a ring of five places.  A place holds one operand's tile of two
+// Pairs of steps with operands that go straight into LDS, into a ring of places.  A place holds one operand's tile of two
 // steps, so that a row along k is loaded 128 bytes at a time: with the 64 of one step the L2s had twice the requests.
 //
-// While a step is multiplied from registers, the next one is read to registers.  In the first step of pair d the X of pair d + 2 is loaded into
-// the place of the Y of pair d - 1, in the second its Y into the place of the X of pair d.  What a place held before has been read by then: the
+// While a step is multiplied from registers, the next one is read to registers.  In the first step of pair d the X of pair d + kAhead is
+// loaded into the place of the Y of pair d - 1, in the second its Y into the place of the X of pair d.  What a place held before has been read by then: the
 // Y were waited for by the multiplications before the last barrier, and the X, which are read first, by a wait for all but the later LDS
-// reads.  A load has one and a half or two and a half steps to arrive.
+// reads.  With five places a load has one and a half or two and a half steps to arrive, with nine four more.
 //
-// A workgroup of the large tile has its compute unit for itself: it stays, and starts the next tile's first loads before it deals with the
+// A workgroup with a ring has its compute unit for itself: it stays, and starts the next tile's first loads before it deals with the
 // results of the last one, for which the last place of the ring is free meanwhile.
 template <class S, class SideY, class SideX>
-__device__ __forceinline__ void start_direct(const SideY& sy, const SideX& sx, uint32_t lds0, int first, int pairs)
+__device__ __forceinline__ void start_direct(SideY& sy, SideX& sx, uint32_t lds0, int total)
 {
     const uint32_t lds_wave = lds0 + (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * 1024u;
 #pragma unroll
-    for (int d = 0; d < 2; ++d)
-        if (d < pairs) {
+    for (int d = 0; d < S::kAhead; ++d)
+        if (d < total) {
 #pragma unroll
-            for (int u = 0; u < S::kXLoads; ++u) sx.load_direct(first + d, u, lds_wave + 2 * d * S::kPlace);
+            for (int u = 0; u < S::kXLoads; ++u) sx.load_direct(u, lds_wave + 2 * d * S::kPlace);
+            sx.advance();
 #pragma unroll
-            for (int u = 0; u < S::kYLoads; ++u) sy.load_direct(first + d, u, lds_wave + (2 * d + 1) * S::kPlace);
+            for (int u = 0; u < S::kYLoads; ++u) sy.load_direct(u, lds_wave + (2 * d + 1) * S::kPlace);
+            sy.advance();
         }
 }
 
+// total: pairs of steps of all segments
 template <class S, class T, class SideY, class SideX>
-__device__ __forceinline__ void accumulate_direct(Sums<S>& acc, const SideY& sy, const SideX& sx, uint32_t lds0, int first, int pairs)
+__device__ __forceinline__ void accumulate_direct(Sums<S>& acc, SideY& sy, SideX& sx, uint32_t lds0, int total)
 {
-    constexpr int kTM = S::kTM, kTN = S::kTN, kLoads = S::kYLoads, kSize = S::kPlace, kEnd = kRing * kSize;      // kSize: one operand, two steps
+    constexpr int kTM = S::kTM, kTN = S::kTN, kLoads = S::kYLoads, kSize = S::kPlace, kEnd = S::kRing * kSize, kAhead = S::kAhead;      // kSize: one operand, two steps
     static_assert(S::kYLoads == S::kXLoads && kLoads * S::kThreads * 16 == kSize);
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const uint32_t lds_wave = lds0 + (uint32_t)wave * 1024u;
-    if (pairs <= 0) return;
-    auto load_y = [&](int d, int u, uint32_t place) __attribute__((always_inline)) { sy.load_direct(first + d, u, lds_wave + place); };
-    auto load_x = [&](int d, int u, uint32_t place) __attribute__((always_inline)) { sx.load_direct(first + d, u, lds_wave + place); };
+    if (total <= 0) return;
     auto meet = []() __attribute__((always_inline)) {
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -502,9 +536,16 @@ __device__ __forceinline__ void accumulate_direct(Sums<S>& acc, const SideY& sy,
     };
     auto later = [](uint32_t place, int n) { return place + (uint32_t)(n * kSize) >= (uint32_t)kEnd ? place + (uint32_t)(n * kSize) - kEnd : place + (uint32_t)(n * kSize); };
     u32x4 y[kTM], x[2][kTN];
+    // all but the loads of so many pairs, fewer than kAhead, are there
+    auto wait_but = [](int pairs) __attribute__((always_inline)) {
+        if (kAhead > 3 && pairs >= 3) ADAGC_P_WAIT_VMEM(6 * kLoads);
+        else if (kAhead > 2 && pairs >= 2) ADAGC_P_WAIT_VMEM(4 * kLoads);
+        else if (pairs >= 1) ADAGC_P_WAIT_VMEM(2 * kLoads);
+        else ADAGC_P_WAIT_VMEM(0);
+    };
+    static_assert(kAhead <= 4);
     // (results stored since the loads were started are waited for too: they are younger)
-    if (pairs > 1) ADAGC_P_WAIT_VMEM(2 * kLoads);
-    else ADAGC_P_WAIT_VMEM(0);
+    wait_but(min(total, kAhead) - 1);
     meet();
 #pragma unroll
     for (int n = 0; n < kTN; ++n) x[0][n] = sx.read(n, 0);
@@ -513,11 +554,11 @@ __device__ __forceinline__ void accumulate_direct(Sums<S>& acc, const SideY& sy,
     uint32_t here = 0;                             // the place of X of pair d; its Y's is the next one
     auto one_step = [&](auto SECOND, auto MORE, int d) __attribute__((always_inline)) {
         constexpr int second = decltype(SECOND)::value;
-        constexpr bool more = decltype(MORE)::value;       // pair d + 2 exists
+        constexpr bool more = decltype(MORE)::value;       // pair d + kAhead exists
         constexpr int kSlots = kTM * kTN;
         // of the step that is read: the second one of pair d, the first one of pair d + 1
         const uint32_t from_x = second ? later(here, 2) : here, from_y = later(here, second ? 3 : 1);
-        const uint32_t to = second ? here : later(here, 4);
+        const uint32_t to = second ? here : later(here, 2 * kAhead);
         each<kSlots>([&](auto SLOT) __attribute__((always_inline)) {
             constexpr int slot = decltype(SLOT)::value, m = slot / kTN, n = slot % kTN;
             multiply<T>(x[second][n], y[m], acc[m][n]);
@@ -528,8 +569,12 @@ __device__ __forceinline__ void accumulate_direct(Sums<S>& acc, const SideY& sy,
                 each<kLoads>([&](auto N) __attribute__((always_inline)) {
                     constexpr int u = decltype(N)::value;
                     if constexpr (1 + u * kSlots / kLoads == slot) {
-                        if constexpr (second) load_y(d + 2, u, to);
-                        else load_x(d + 2, u, to);
+                        if constexpr (second) sy.load_direct(u, lds_wave + to);
+                        else sx.load_direct(u, lds_wave + to);
+                        if constexpr (u == kLoads - 1) {
+                            if constexpr (second) sy.advance();
+                            else sx.advance();
+                        }
                     }
                 });
             }
@@ -537,8 +582,8 @@ __device__ __forceinline__ void accumulate_direct(Sums<S>& acc, const SideY& sy,
         });
         if constexpr (!second) {
             // pair d + 1 has to be there, and X of pair d read: kTM - 1 fragments of Y, one access each at least, are read after it
-            if constexpr (more) ADAGC_P_WAIT_VMEM(kLoads);
-            else ADAGC_P_WAIT_VMEM(0);
+            if constexpr (more) ADAGC_P_WAIT_VMEM((2 * kAhead - 3) * kLoads);
+            else wait_but(total - 2 - d);
             ADAGC_P_WAIT_LDS(kTM - 1);
         }
         meet();
@@ -546,13 +591,13 @@ __device__ __forceinline__ void accumulate_direct(Sums<S>& acc, const SideY& sy,
     constexpr std::integral_constant<int, 0> even{};
     constexpr std::integral_constant<int, 1> odd{};
     int d = 0;
-    for (; d + 2 < pairs; ++d) {
+    for (; d + kAhead < total; ++d) {
         one_step(even, std::true_type{}, d);
         one_step(odd, std::true_type{}, d);
         here = later(here, 2);
     }
     // the fragments of the step after the last one are read from some place of the ring and not used
-    for (; d < pairs; ++d) {
+    for (; d < total; ++d) {
         one_step(even, std::false_type{}, d);
         one_step(odd, std::false_type{}, d);
         here = later(here, 2);
@@ -630,9 +675,9 @@ __device__ __forceinline__ f32x4_p load4(const T* row, int64_t col, int64_t leas
     return v;
 }
 
-using Large = Tile<uint16_t, 256, 256, 2, 4, true>;
-using Small = Tile<uint16_t, 128, 128, 2, 2, true>;
-template <class T> using Staged = Tile<T, sizeof(T) == 4 ? 64 : 128, sizeof(T) == 4 ? 64 : 128, 2, 2, false>;
+using Large = Tile<uint16_t, 256, 256, 2, 4, 5>;
+using Small = Tile<uint16_t, 128, 128, 2, 4, 9>;
+template <class T> using Staged = Tile<T, sizeof(T) == 4 ? 64 : 128, sizeof(T) == 4 ? 64 : 128, 2, 2, 0>;
 
 // Rows of an operand start at multiples of 16 bytes.
 inline bool rows_aligned(const void* p, int64_t ld, int32_t dtype) { return !misaligned(p, 16) && ld * dtype_size(dtype) % 16 == 0; }
@@ -662,13 +707,6 @@ inline AlongPlan along_plan(int64_t m, int64_t n, int32_t dtype, bool aligned, i
 }
 
 // ---------------------------------------------------------------------------------------- both operands along k
-
-// fp32 operands in three bf16 parts, hi + mid + lo, each the nearest to what the ones before it leave (8 + 8 + 8 significant bits, exact but
-// next to the type's ends): of the nine products of parts the six that count, smallest first; the others are some 2^-26 of the whole.  The
-// matrix cores' bf16 rate is 16 times the fp32 one.  Segment s takes parts part_of_y(s), part_of_x(s); a single segment takes the last one's.
-constexpr int kSegments = 6, kParts = 3;
-__device__ __forceinline__ int part_of_y(int s) { return 0x001102 >> (4 * s) & 15; }
-__device__ __forceinline__ int part_of_x(int s) { return 0x010120 >> (4 * s) & 15; }
 
 // Four values in parts: bits of bf16 pairs.  What is not finite is in the first part alone; what rounds beyond bf16's range keeps its largest number.
 __device__ __forceinline__ void split4(const f32x4_p& v, uint32_t (&bits)[kParts][2])
@@ -745,50 +783,45 @@ __device__ __forceinline__ void along_tiles(const AlongArgs& a, uint8_t* lds, Be
     } else {
         const int pairs = (int)(a.k / (2 * S::kDeep)), tiles = a.tiles_m * a.tiles_n;
         const bool rest = a.k % (2 * S::kDeep);        // (not with several segments)
-        auto aim = [&](int segment) __attribute__((always_inline)) {
+        auto aim = [&]() __attribute__((always_inline)) {
             // a load of a wave is 8 rows, and a lane's are a multiple of 32 apart: with two matrices, all of one
             static_assert(S::kThreads / 8 % 32 == 0);
             const int tid = thread_anew();
             const bool second = PAIR && (wave >> 1 & 1);
             const int64_t ld_x = second ? a.ld_x[1] : a.ld_x[0];
-            sy.set_rows_direct(tid, y + part_of_y(segment) * a.part_y + m0 * a.ld_y, a.ld_y, [&](int r) { return min(m0 + r, a.m - 1) - m0; });
-            sx.set_rows_direct(tid, static_cast<const T*>(second ? a.x[1] : a.x[0]) + part_of_x(segment) * a.part_x + n0 * ld_x, ld_x,
-                               [&](int r) { return row_of_x(r) - n0; });
+            sy.set_rows_direct(tid, y + m0 * a.ld_y, a.ld_y, [&](int r) { return min(m0 + r, a.m - 1) - m0; });
+            sy.set_pairs(0, pairs, a.segments, a.part_y, kPartsOfY);
+            sx.set_rows_direct(tid, static_cast<const T*>(second ? a.x[1] : a.x[0]) + n0 * ld_x, ld_x, [&](int r) { return row_of_x(r) - n0; });
+            sx.set_pairs(0, pairs, a.segments, a.part_x, kPartsOfX);
         };
-        const int first = kSegments - a.segments;
-        int n = (int)blockIdx.x, segment = first;
+        const int total = pairs * a.segments;
+        int n = (int)blockIdx.x;
         to_tile(n);
         if (!rest) {
-            aim(segment);
-            start_direct<S>(sy, sx, lds0, 0, pairs);
+            aim();
+            start_direct<S>(sy, sx, lds0, total);
         }
-        clear<S>(acc);
         while (true) {
+            clear<S>(acc);
             if (rest) {
                 aim_staged();
                 accumulate_rest<S, T>(acc, sy, sx, 2 * pairs, a.k, 0, 0);
-                aim(segment);
-                start_direct<S>(sy, sx, lds0, 0, pairs);
+                aim();
+                start_direct<S>(sy, sx, lds0, total);
             }
-            accumulate_direct<S, T>(acc, sy, sx, lds0, 0, pairs);
-            const bool last = segment == kSegments - 1;
+            accumulate_direct<S, T>(acc, sy, sx, lds0, total);
             const int64_t m_now = m0, n_now = n0;
-            if (!last) {
-                ++segment;
-            } else {
-                before(m_now, n_now);
-                n += (int)gridDim.x;
-                segment = first;
-                if (n < tiles) to_tile(n);
+            before(m_now, n_now);
+            n += (int)gridDim.x;
+            if (n < tiles) {
+                to_tile(n);
+                if (!rest) {
+                    aim();
+                    start_direct<S>(sy, sx, lds0, total);
+                }
             }
-            if ((!last || n < tiles) && !rest) {
-                aim(segment);
-                start_direct<S>(sy, sx, lds0, 0, pairs);
-            }
-            if (!last) continue;
-            finish(acc, m_now, n_now, lds + (kRing - 1) * S::kPlace);
+            finish(acc, m_now, n_now, lds + (S::kRing - 1) * S::kPlace);
             if (n >= tiles) break;
-            clear<S>(acc);
         }
     }
 }
@@ -797,7 +830,7 @@ __device__ __forceinline__ void along_tiles(const AlongArgs& a, uint8_t* lds, Be
 template <class S>
 inline uint32_t grid_of(int64_t tiles)
 {
-    return (uint32_t)(S::kDirect && S::BM == 256 ? std::min<int64_t>(tiles, kUnits) : tiles);
+    return (uint32_t)(S::kDirect ? std::min<int64_t>(tiles, kUnits) : tiles);
 }
 
 // Waves meet, their LDS accesses done; loads into LDS may be on their way (which __syncthreads would not leave).
@@ -1019,7 +1052,6 @@ __global__ __launch_bounds__(S::kThreads, 2) void plain_kernel(const PlainArgs a
     const int full = (int)(a.k / kTogether), items = a.whole + (a.tiles_m * a.tiles_n * a.products - a.whole) * a.split;
     const bool uneven = a.k % kTogether;
     const int64_t m_readable = ACROSS_Y ? a.m_readable : a.m;
-    const int turns = a.pairs * a.segments, first_segment = kSegments - a.segments;       // of a tile: segments of one pair after the other
     struct Place {
         int     item, product;
         int64_t m0, n0, m_least, n_least;
@@ -1051,29 +1083,24 @@ __global__ __launch_bounds__(S::kThreads, 2) void plain_kernel(const PlainArgs a
         return p;
     };
     // (an index would put the arguments into memory)
-    auto pair_of = [&](const Place& p, int turn) __attribute__((always_inline)) { return p.product || turn >= a.segments; };
-    auto segment_of = [&](int turn) __attribute__((always_inline)) { return first_segment + (turn >= a.segments ? turn - a.segments : turn); };
-    auto y_of = [&](bool second, int segment) __attribute__((always_inline)) {
-        return static_cast<const T*>(second ? a.y[1] : a.y[0]) + part_of_y(segment) * a.part_y;
-    };
-    auto x_of = [&](bool second, int segment) __attribute__((always_inline)) {
-        return static_cast<const T*>(second ? a.x[1] : a.x[0]) + part_of_x(segment) * a.part_x;
-    };
-    auto aim_staged = [&](const Place& p, int turn) __attribute__((always_inline)) {
-        const int tid = thread_anew(), segment = segment_of(turn);
-        const bool second = pair_of(p, turn);
-        const T* y = y_of(second, segment);
+    auto y_of = [&](bool second) __attribute__((always_inline)) { return static_cast<const T*>(second ? a.y[1] : a.y[0]); };
+    auto x_of = [&](bool second) __attribute__((always_inline)) { return static_cast<const T*>(second ? a.x[1] : a.x[0]); };
+    auto aim_staged = [&](const Place& p, bool second) __attribute__((always_inline)) {
+        const int tid = thread_anew();
+        const T* y = y_of(second);
         if constexpr (ACROSS_Y) sy.set_columns(tid, y + p.m0, a.ld_y);
         else sy.set_rows(tid, [&](int r) { return y + min(p.m0 + r, a.m - 1) * a.ld_y; });
-        sx.set_columns(tid, x_of(second, segment) + p.n0, second ? a.ld_x[1] : a.ld_x[0]);
+        sx.set_columns(tid, x_of(second) + p.n0, second ? a.ld_x[1] : a.ld_x[0]);
     };
-    auto aim = [&](const Place& p, int turn) __attribute__((always_inline)) {
-        const int tid = thread_anew(), segment = segment_of(turn);
-        const bool second = pair_of(p, turn);
-        const T* y = y_of(second, segment);
+    // (what is left over after whole pairs of steps comes with a single segment only)
+    auto aim = [&](const Place& p, bool second) __attribute__((always_inline)) {
+        const int tid = thread_anew();
+        const T* y = y_of(second);
         if constexpr (ACROSS_Y) sy.set_columns_direct(tid, y + p.m0, a.ld_y);
         else sy.set_rows_direct(tid, y + p.m0 * a.ld_y, a.ld_y, [&](int r) { return min(p.m0 + r, a.m - 1) - p.m0; });
-        sx.set_columns_direct(tid, x_of(second, segment) + p.n0, second ? a.ld_x[1] : a.ld_x[0]);
+        sx.set_columns_direct(tid, x_of(second) + p.n0, second ? a.ld_x[1] : a.ld_x[0]);
+        sy.set_pairs(step0, step1 - step0, a.segments, a.part_y, kPartsOfY);
+        sx.set_pairs(step0, step1 - step0, a.segments, a.part_x, kPartsOfX);
     };
     Sums<S> acc;
     auto finish_inside = [&](const Place& p, auto* out, const auto* add) __attribute__((always_inline)) {
@@ -1118,40 +1145,40 @@ __global__ __launch_bounds__(S::kThreads, 2) void plain_kernel(const PlainArgs a
 
     clear<S>(acc);
     Place now = place_of((int)blockIdx.x);
-    int turn = 0;
+    int pair = now.product;
     if constexpr (!S::kDirect) {
-        for (; turn < turns; ++turn) {
-            aim_staged(now, turn);
+        for (; pair < now.product + a.pairs; ++pair) {
+            aim_staged(now, pair);
             accumulate<S, T, CHECKED>(acc, sy, sx, step0, step1, rest, full, a.k, m_readable - now.m0, a.n_readable - now.n0);
         }
         finish(now);
     } else {
         if (!uneven) {
-            aim(now, turn);
-            start_direct<S>(sy, sx, lds0, step0, step1 - step0);
+            aim(now, pair);
+            start_direct<S>(sy, sx, lds0, (step1 - step0) * a.segments);
         }
         while (true) {
             if (uneven) {
                 if (rest) {
-                    aim_staged(now, turn);
+                    aim_staged(now, pair);
                     accumulate_rest<S, T>(acc, sy, sx, 2 * (int64_t)full, a.k, m_readable - now.m0, a.n_readable - now.n0);
                 }
-                aim(now, turn);
-                start_direct<S>(sy, sx, lds0, step0, step1 - step0);
+                aim(now, pair);
+                start_direct<S>(sy, sx, lds0, (step1 - step0) * a.segments);
             }
-            accumulate_direct<S, T>(acc, sy, sx, lds0, step0, step1 - step0);
-            const bool last = turn + 1 == turns;
+            accumulate_direct<S, T>(acc, sy, sx, lds0, (step1 - step0) * a.segments);
+            const bool last = pair + 1 == now.product + a.pairs;
             const int item = now.item + (int)gridDim.x;
             const Place done = now;
             if (!last) {
-                ++turn;
+                ++pair;
             } else if (item < items) {
                 now = place_of(item);
-                turn = 0;
+                pair = now.product;
             }
             if ((!last || item < items) && !uneven) {
-                aim(now, turn);
-                start_direct<S>(sy, sx, lds0, step0, step1 - step0);
+                aim(now, pair);
+                start_direct<S>(sy, sx, lds0, (step1 - step0) * a.segments);
             }
             if (!last) continue;
             finish(done);
@@ -1193,7 +1220,7 @@ struct PlainPlan {
     bool    checked, direct;
     int64_t tiles_m, tiles_n, whole, rest, split;
     int64_t workspace() const { return split > 1 ? rest * split * size * size * 4 : 0; }
-    bool    launchable() const { return (whole + rest * split) * (size == 256 ? 512 : 256) <= UINT32_MAX; }      // lanes
+    bool    launchable() const { return (whole + rest * split) * (direct ? 512 : 256) <= UINT32_MAX; }      // lanes
 };
 // m (with Y across k) and n: of the readable columns; pairs: of operands that are summed; products: side by side; aligned: the rows of both
 // operands are.  A workspace is sized for both.
@@ -1207,12 +1234,11 @@ inline PlainPlan plain_plan(int64_t m, int64_t n, int64_t k, int32_t dtype, bool
                (!across_y || (m >= 128 && m % 8 == 0));
     p.size = tile_size(p.direct, dtype, tiles);
     if (p.size == 256 && (m < 256 || n < 256)) p.size = 128;
-    const bool large = p.size == 256;
     p.checked = far || n < p.size || (across_y && m < p.size);
     p.tiles_m = (m + p.size - 1) / p.size;
     p.tiles_n = (n + p.size - 1) / p.size;
     const int64_t all = tiles(p.size), steps = k / (kStepBytes / dtype_size(dtype)) / (p.direct ? 2 : 1) * (p.direct ? 2 : 1);
-    const int64_t round = large ? kUnits : 2 * kUnits;      // the smaller tiles' workgroups share a compute unit in pairs
+    const int64_t round = p.direct ? kUnits : 2 * kUnits;   // a ring fills a compute unit's LDS; the others' workgroups share a unit in pairs
     p.rest = all % round;
     // a part has eight steps at least (of each pair)
     p.split = p.rest ? std::max<int64_t>(1, std::min(round / p.rest, steps * pairs / 8)) : 1;
@@ -1277,22 +1303,31 @@ inline Layout layout_of(int64_t rows, int64_t wide, int64_t k, int32_t dtype)
     return l;
 }
 
+// Up to three matrices in a launch.
 struct LayArgs {
-    const void* from;
-    uint16_t*   to;
-    int64_t     ld_from, ld_to, part, rows, cols, vectors, all;
+    const void* from[3];
+    uint16_t*   to[3];
+    int64_t     ld_from[3], rows[3], part[3];
+    uint32_t    end[3];           // workgroups of the matrix and those before it
+    int64_t     ld_to, cols;
 };
 constexpr int kLay = 256;
 // 8 numbers of a row for a lane.  Bound by memory.
 template <class T>
 __global__ __launch_bounds__(kLay) void lay_kernel(const LayArgs a)
 {
-    const int64_t i = (int64_t)blockIdx.x * kLay + threadIdx.x;
-    if (i >= a.all) return;
-    const int64_t row = i / a.vectors, col = (i - row * a.vectors) * 8;
-    const T* from = static_cast<const T*>(a.from) + row * a.ld_from;
-    u32x4* to = reinterpret_cast<u32x4*>(a.to + row * a.ld_to + col);
-    const int64_t n = row < a.rows ? a.cols : 0;
+    const uint32_t block = blockIdx.x;
+    const bool first = block < a.end[0], second = block < a.end[1];        // (an index would put the arguments into memory)
+    const int64_t rows = first ? a.rows[0] : second ? a.rows[1] : a.rows[2], part = first ? a.part[0] : second ? a.part[1] : a.part[2];
+    const int64_t ld_from = first ? a.ld_from[0] : second ? a.ld_from[1] : a.ld_from[2];
+    const void* source = first ? a.from[0] : second ? a.from[1] : a.from[2];
+    uint16_t* target = first ? a.to[0] : second ? a.to[1] : a.to[2];
+    const int64_t i = (int64_t)(block - (first ? 0 : second ? a.end[0] : a.end[1])) * kLay + threadIdx.x, vectors = a.ld_to / 8;
+    if (i >= part / 8) return;
+    const int64_t row = i / vectors, col = (i - row * vectors) * 8;
+    const T* from = static_cast<const T*>(source) + row * ld_from;
+    u32x4* to = reinterpret_cast<u32x4*>(target + row * a.ld_to + col);
+    const int64_t n = row < rows ? a.cols : 0;
     if constexpr (sizeof(T) == 2) {
         *to = load_vector(from, col, n, 0).w;
     } else {
@@ -1300,16 +1335,35 @@ __global__ __launch_bounds__(kLay) void lay_kernel(const LayArgs a)
 #pragma unroll
         for (int h = 0; h < 2; ++h) split4(__builtin_bit_cast(f32x4_p, load_vector(from, col + 4 * h, n, 0).w), bits[h]);
 #pragma unroll
-        for (int p = 0; p < kParts; ++p) to[p * (a.part / 8)] = u32x4{bits[0][p][0], bits[0][p][1], bits[1][p][0], bits[1][p][1]};
+        for (int p = 0; p < kParts; ++p) to[p * (part / 8)] = u32x4{bits[0][p][0], bits[0][p][1], bits[1][p][0], bits[1][p][1]};
     }
 }
+struct LaySource {
+    const void* from;
+    int64_t     ld, rows;
+    void*       to;
+};
+// `number` matrices of cols columns
 template <class T>
-int lay(const void* from, int64_t ld_from, int64_t rows, int64_t cols, const Layout& l, void* to, hipStream_t s)
+int lay(const LaySource* sources, int number, int64_t cols, const Layout& l, hipStream_t s)
 {
-    const int64_t all = Layout::rows_of(rows) * (l.ld / 8);
-    if (all == 0) return ADAGC_OK;
-    lay_kernel<T><<<dim3((uint32_t)((all + kLay - 1) / kLay)), dim3(kLay), 0, s>>>(
-        {from, static_cast<uint16_t*>(to), ld_from, l.ld, l.part(rows), rows, cols, l.ld / 8, all});
+    LayArgs a{};
+    uint32_t blocks = 0;
+    for (int i = 0; i < 3; ++i) {
+        if (i < number) {
+            a.from[i] = sources[i].from;
+            a.to[i] = static_cast<uint16_t*>(sources[i].to);
+            a.ld_from[i] = sources[i].ld;
+            a.rows[i] = sources[i].rows;
+            a.part[i] = l.part(sources[i].rows);
+            blocks += (uint32_t)((a.part[i] / 8 + kLay - 1) / kLay);
+        }
+        a.end[i] = blocks;
+    }
+    a.ld_to = l.ld;
+    a.cols = cols;
+    if (blocks == 0) return ADAGC_OK;
+    lay_kernel<T><<<dim3(blocks), dim3(kLay), 0, s>>>(a);
     return hipGetLastError() == hipSuccess ? ADAGC_OK : ADAGC_ERR_HIP;
 }
 
@@ -1318,8 +1372,8 @@ extern template int run_plain<float, false>(PlainArgs, hipStream_t);
 extern template int run_plain<float, true>(PlainArgs, hipStream_t);
 extern template int run_plain<uint16_t, false>(PlainArgs, hipStream_t);
 extern template int run_plain<uint16_t, true>(PlainArgs, hipStream_t);
-extern template int lay<float>(const void*, int64_t, int64_t, int64_t, const Layout&, void*, hipStream_t);
-extern template int lay<uint16_t>(const void*, int64_t, int64_t, int64_t, const Layout&, void*, hipStream_t);
+extern template int lay<float>(const LaySource*, int, int64_t, const Layout&, hipStream_t);
+extern template int lay<uint16_t>(const LaySource*, int, int64_t, const Layout&, hipStream_t);
 
 }  // namespace product
 }  // namespace adagc
