@@ -61,10 +61,11 @@ struct Tile {
     static constexpr int kY = BM * kStepBytes, kX = BN * kStepBytes, kPlace = kY + kX;      // bytes
     static constexpr int kYUnits = kY / 16 / kThreads, kXUnits = kX / 16 / kThreads;       // of 16 bytes, a lane's
     static constexpr bool kDirect = RING_ > 0;
-    static constexpr int kRing = RING_, kAhead = (RING_ - 1) / 2;                          // places of the ring; pairs of steps that loads are ahead
+    static constexpr bool kEven = RING_ % 2 == 0;
+    static constexpr int kRing = RING_, kAhead = RING_ / 2;                                // places of the ring; pairs of steps that loads are ahead
     static constexpr int kYLoads = 2 * kYUnits, kXLoads = 2 * kXUnits;                     // straight into LDS, of two steps, a lane's
     static constexpr int kLds = (RING_ ? RING_ : kPlaces) * kPlace;
-    static_assert(!RING_ || (BM_ == BN_ && RING_ % 2 == 1 && RING_ >= 5), "a place of the ring takes either operand, X and Y in turn");
+    static_assert(!RING_ || (BM_ == BN_ && RING_ >= 5), "a place of the ring takes either operand, X and Y in turn");
     static_assert(kY % (16 * kThreads) == 0 && kX % (16 * kThreads) == 0, "operand tiles are dealt evenly");
 };
 
@@ -500,7 +501,11 @@ __device__ __forceinline__ void accumulate_rest(Sums<S>& acc, const SideY& sy, c
 // While a step is multiplied from registers, the next one is read to registers.  In the first step of pair d the X of pair d + kAhead is
 // loaded into the place of the Y of pair d - 1, in the second its Y into the place of the X of pair d.  What a place held before has been read by then: the
 // Y were waited for by the multiplications before the last barrier, and the X, which are read first, by a wait for all but the later LDS
-// reads.  With five places a load has one and a half or two and a half steps to arrive, with nine four more.
+// reads.  With five places a load has one and a half or two and a half steps to arrive.
+//
+// An even number of places, for tiles with registers to spare: fragments of Y too are read to a second set, early in the step, and waited for before
+// the waves meet, which they do once a pair.  In the second step of pair d the X of pair d + kAhead is loaded into the place of its own X, in the
+// first step of pair d + 1 the Y into that of its Y.
 //
 // A workgroup with a ring has its compute unit for itself: it stays, and starts the next tile's first loads before it deals with the
 // results of the last one, for which the last place of the ring is free meanwhile.
@@ -514,6 +519,7 @@ __device__ __forceinline__ void start_direct(SideY& sy, SideX& sx, uint32_t lds0
 #pragma unroll
             for (int u = 0; u < S::kXLoads; ++u) sx.load_direct(u, lds_wave + 2 * d * S::kPlace);
             sx.advance();
+            if (S::kEven && d == S::kAhead - 1) continue;
 #pragma unroll
             for (int u = 0; u < S::kYLoads; ++u) sy.load_direct(u, lds_wave + (2 * d + 1) * S::kPlace);
             sy.advance();
@@ -535,23 +541,95 @@ __device__ __forceinline__ void accumulate_direct(Sums<S>& acc, SideY& sy, SideX
         ADAGC_P_FENCE();
     };
     auto later = [](uint32_t place, int n) { return place + (uint32_t)(n * kSize) >= (uint32_t)kEnd ? place + (uint32_t)(n * kSize) - kEnd : place + (uint32_t)(n * kSize); };
-    u32x4 y[kTM], x[2][kTN];
     // all but the loads of so many pairs, fewer than kAhead, are there
     auto wait_but = [](int pairs) __attribute__((always_inline)) {
-        if (kAhead > 3 && pairs >= 3) ADAGC_P_WAIT_VMEM(6 * kLoads);
+        if (kAhead > 4 && pairs >= 4) ADAGC_P_WAIT_VMEM(8 * kLoads);
+        else if (kAhead > 3 && pairs >= 3) ADAGC_P_WAIT_VMEM(6 * kLoads);
         else if (kAhead > 2 && pairs >= 2) ADAGC_P_WAIT_VMEM(4 * kLoads);
         else if (pairs >= 1) ADAGC_P_WAIT_VMEM(2 * kLoads);
         else ADAGC_P_WAIT_VMEM(0);
     };
-    static_assert(kAhead <= 4);
-    // (results stored since the loads were started are waited for too: they are younger)
+    static_assert(kAhead <= 5);
+    constexpr std::integral_constant<int, 0> even{};
+    constexpr std::integral_constant<int, 1> odd{};
+    uint32_t here = 0;                             // the place of X of pair d; its Y's is the next one
+    int d = 0;
+    if constexpr (S::kEven) {
+        u32x4 y[2][kTM], x[2][kTN];
+        // (results stored since the loads were started are waited for too: they are younger)
+        wait_but(min(total, kAhead - 1) - 1);
+        meet();
+#pragma unroll
+        for (int n = 0; n < kTN; ++n) x[0][n] = sx.read(n, 0);
+#pragma unroll
+        for (int m = 0; m < kTM; ++m) y[0][m] = sy.read(m, kSize);
+        // LOAD: there is something left to load
+        auto one_step = [&](auto SECOND, auto LOAD, int d) __attribute__((always_inline)) {
+            constexpr int second = decltype(SECOND)::value;
+            constexpr int kSlots = kTM * kTN, kReads = kTM + kTN;
+            // of the step that is read: the second one of pair d, the first one of pair d + 1
+            const uint32_t from_x = second ? later(here, 2) : here, from_y = later(here, second ? 3 : 1);
+            const uint32_t to = second ? here : later(here, 2 * kAhead - 1);
+            each<kSlots>([&](auto SLOT) __attribute__((always_inline)) {
+                constexpr int slot = decltype(SLOT)::value, m = slot / kTN, n = slot % kTN;
+                multiply<T>(x[second][n], y[second][m], acc[m][n]);
+                ADAGC_P_FENCE();
+                each<kReads>([&](auto R) __attribute__((always_inline)) {
+                    constexpr int r = decltype(R)::value;
+                    if constexpr (r * (kSlots / 2) / kReads == slot) {
+                        if constexpr (r < kTN) x[second ^ 1][r] = sx.read(r, from_x, !second);
+                        else y[second ^ 1][r - kTN] = sy.read(r - kTN, from_y, !second);
+                    }
+                });
+                if constexpr (decltype(LOAD)::value) {
+                    each<kLoads>([&](auto N) __attribute__((always_inline)) {
+                        constexpr int u = decltype(N)::value;
+                        if constexpr (kSlots / 2 + u * (kSlots / 2) / kLoads == slot) {
+                            if constexpr (second) sx.load_direct(u, lds_wave + to);
+                            else sy.load_direct(u, lds_wave + to);
+                            if constexpr (u == kLoads - 1) {
+                                if constexpr (second) sx.advance();
+                                else sy.advance();
+                            }
+                        }
+                    });
+                }
+                ADAGC_P_FENCE();
+            });
+            if constexpr (!second) {
+                // pair d + 1 has to be there, and pair d read
+                if constexpr (decltype(LOAD)::value) ADAGC_P_WAIT_VMEM(2 * (kAhead - 2) * kLoads);
+                else wait_but(total - 2 - d);
+                ADAGC_P_WAIT_LDS(0);
+                meet();
+            }
+        };
+        for (; d + kAhead < total; ++d) {
+            one_step(even, std::true_type{}, d);
+            one_step(odd, std::true_type{}, d);
+            here = later(here, 2);
+        }
+        if (d + kAhead == total) {                 // the last Y
+            one_step(even, std::true_type{}, d);
+            one_step(odd, std::false_type{}, d);
+            here = later(here, 2);
+            ++d;
+        }
+        for (; d < total; ++d) {
+            one_step(even, std::false_type{}, d);
+            one_step(odd, std::false_type{}, d);
+            here = later(here, 2);
+        }
+        __syncthreads();
+        return;
+    }
+    u32x4 y[kTM], x[2][kTN];
     wait_but(min(total, kAhead) - 1);
     meet();
 #pragma unroll
     for (int n = 0; n < kTN; ++n) x[0][n] = sx.read(n, 0);
 #pragma unroll
     for (int m = 0; m < kTM; ++m) y[m] = sy.read(m, kSize);
-    uint32_t here = 0;                             // the place of X of pair d; its Y's is the next one
     auto one_step = [&](auto SECOND, auto MORE, int d) __attribute__((always_inline)) {
         constexpr int second = decltype(SECOND)::value;
         constexpr bool more = decltype(MORE)::value;       // pair d + kAhead exists
@@ -588,9 +666,6 @@ __device__ __forceinline__ void accumulate_direct(Sums<S>& acc, SideY& sy, SideX
         }
         meet();
     };
-    constexpr std::integral_constant<int, 0> even{};
-    constexpr std::integral_constant<int, 1> odd{};
-    int d = 0;
     for (; d + kAhead < total; ++d) {
         one_step(even, std::true_type{}, d);
         one_step(odd, std::true_type{}, d);
@@ -676,7 +751,7 @@ __device__ __forceinline__ f32x4_p load4(const T* row, int64_t col, int64_t leas
 }
 
 using Large = Tile<uint16_t, 256, 256, 2, 4, 5>;
-using Small = Tile<uint16_t, 128, 128, 2, 4, 9>;
+using Small = Tile<uint16_t, 128, 128, 2, 4, 10>;
 template <class T> using Staged = Tile<T, sizeof(T) == 4 ? 64 : 128, sizeof(T) == 4 ? 64 : 128, 2, 2, 0>;
 
 // Rows of an operand start at multiples of 16 bytes.
