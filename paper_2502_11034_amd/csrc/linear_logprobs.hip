@@ -33,21 +33,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void stats_kernel(const StatsArgs a
 {
     __shared__ __attribute__((aligned(512))) uint8_t lds[S::kLds];
     const float c = a.scale * kLog2e;
-    int target[S::kTM];            // its column from the lane's first one, if in the wave's columns
-    auto before = [&](int64_t m0, int64_t n0) __attribute__((always_inline)) {
-        const LanePlace<S> at;
-#pragma unroll
-        for (int m = 0; m < S::kTM; ++m) {
-            const int64_t row = m0 + at.row + m * 16;
-            target[m] = -1;
-            if (a.targets && row < a.p.m) {
-                const int64_t t = a.targets[row] - a.first;
-                if (t >= n0 + at.col && t < min(n0 + at.col + S::kTN * 16, a.p.n)) target[m] = (int)(t - n0 - at.col);
-            }
-        }
-        settle_now(target);
-    };
-    along_tiles<S, T, false>(a.p, lds, before, [&](Sums<S>& acc, int64_t m0, int64_t n0, uint8_t* scratch) __attribute__((always_inline)) {
+    along_tiles<S, T, false>(a.p, lds, [](int64_t, int64_t) {}, [&](Sums<S>& acc, int64_t m0, int64_t n0, uint8_t* scratch) __attribute__((always_inline)) {
         const LanePlace<S> at;
         const int tid = thread_anew(), lane = tid & 63, wave = tid >> 6;
         if (n0 + S::BN > a.p.n) {
@@ -86,13 +72,24 @@ __global__ __launch_bounds__(S::kThreads, 2) void stats_kernel(const StatsArgs a
             sum += __shfl_xor(sum, 32);
             const int row = at.row + m * 16;
             if (lane < 16) shared[row * S::kWN + wave % S::kWN] = float2{most, sum};
-            if (target[m] >= 0) {
+        }
+        // the targets last: their loads come after the next tile's in the order that loads are waited for in
+        if (a.targets) {
+            int target[S::kTM];            // the column from the lane's first one, if in the wave's columns
 #pragma unroll
-                for (int n = 0; n < S::kTN; ++n)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (target[m] == n * 16 + r) a.target_logit[m0 + row] = acc[m][n][r];
+            for (int m = 0; m < S::kTM; ++m) {
+                const int64_t t = a.targets[min(m0 + at.row + m * 16, a.p.m - 1)] - a.first;
+                target[m] = t >= n0 + at.col && t < min(n0 + at.col + S::kTN * 16, a.p.n) && m0 + at.row + m * 16 < a.p.m ? (int)(t - n0 - at.col) : -1;
             }
+#pragma unroll
+            for (int m = 0; m < S::kTM; ++m)
+                if (target[m] >= 0) {
+#pragma unroll
+                    for (int n = 0; n < S::kTN; ++n)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (target[m] == n * 16 + r) a.target_logit[m0 + at.row + m * 16] = acc[m][n][r];
+                }
         }
         meet_keeping_loads();
         if (tid < S::BM && m0 + tid < a.p.m) {
@@ -298,8 +295,10 @@ struct Work {
 int64_t piece_of(int64_t vocab, int64_t dim, int64_t most)
 {
     if (vocab <= most) return vocab;
-    const int64_t wide = (dim + 255) / 256, rounds = most / 256 * wide / kUnits;
-    return rounds ? rounds * kUnits / wide * 256 : most;
+    const int64_t wide = (dim + 255) / 256;
+    int64_t rounds = most / 256 * wide / kUnits;
+    if (rounds == 0) rounds = 2 * most / 256 * wide / kUnits;
+    return rounds ? std::min(vocab, rounds * kUnits / wide * 256) : most;
 }
 Work work_of(int64_t rows, int64_t vocab, int64_t dim, int32_t dtype, bool backward)
 {
