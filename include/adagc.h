@@ -538,22 +538,28 @@ int adagc_act8_wgrad(const void* d_out, int32_t dtype, int64_t ld_d_out, const v
                      int64_t workspace_bytes, void* stream);
 
 /*
+ * Operators that keep nothing between the passes but their inputs.  As above; products are sums in fp32 of bf16 products, which are exact, or of
+ * fp32 ones: those of 128 rows and more, as three bf16 numbers each, are off by some 2^-26 of themselves (an infinity among their operands may then
+ * give NaN), the others are rounded to fp32.  The workspace sizes are negative error codes for sizes that are refused.  Results do not
+ * depend on what else runs: sums are taken in a fixed order.
+ *
  * Log-probabilities of given tokens straight from the head's input and weights: what adagc_token_logprobs gives for the logits z = x W^T,
  * without the logits.  With M = max_j z_j and L = ln sum_j exp(scale (z_j - M)),
  *     logp_target = scale (z_target - M) - L.
- * Logits are sums of exact products in fp32 (fp32 data: of products rounded to fp32) and are not rounded to the data's type.
+ * Logits are not rounded to the data's type.
  *   x          DEVICE dtype[rows][ld_x], dim values a row
  *   weight     DEVICE dtype[vocab][ld_weight], dim values a row
  *   targets    DEVICE int64[rows] (NULL if logprob is); outside 0 .. vocab-1 (-1, -100): the row has no target
  *   scale      2^-100 .. 2^100
  *   logprob    DEVICE fp32[rows], 0 for rows without a target; or NULL
  *   stats      DEVICE fp32[rows][2]: M and L, which the backward pass takes; or NULL
- *   workspace  DEVICE, adagc_linear_logprobs_workspace_bytes of it, 16-byte aligned, contents before and after without meaning
+ *   workspace  DEVICE, adagc_linear_logprobs_workspace_bytes of it, 16-byte aligned, contents before and after without meaning: 8 bytes
+ *              for each row and 32 to 128 tokens, and where operands are laid out anew (fp32 data; dim no multiple of 8) x and a piece of
+ *              the weight
  * At least one output is wanted.  A row whose logits are all -inf has log-probability -inf, M = -inf, L = 0; a row with a NaN or +inf among its
  * logits has a NaN log-probability.
- * The workspace sizes are negative error codes for sizes that are refused.  Results do not depend on what else runs: sums are taken in a fixed
- * order.
- * Errors: INVALID_ARG, TOO_LARGE (also 2^24 rows or more, and 2^23 tiles of 128 x 128 logits, values of x or of the weight), HIP.
+ * Errors: INVALID_ARG, TOO_LARGE (also 2^24 rows or more, 2^35 logits or values of the weight, 2^34 of x, and half of that where rows and
+ * columns fill their tiles badly), HIP.
  */
 int64_t adagc_linear_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int64_t dim, int32_t dtype);
 int adagc_linear_logprobs(const void* x, int64_t ld_x, const void* weight, int64_t ld_weight, int32_t dtype, int64_t rows, int64_t vocab,
@@ -563,8 +569,8 @@ int adagc_linear_logprobs(const void* x, int64_t ld_x, const void* weight, int64
 /*
  * Its gradients for the gradient d of the log-probabilities, the logits made again in pieces of the vocabulary: with p_j = exp(logp_j),
  *     d_z_j = d (1[j = target] - p_j),   d_x = scale d_z W,   d_weight = scale d_z^T x   (+ d_weight with accumulate = 1),
- * d_z being 0 for rows without a target, rows of nothing but -inf and rows whose d is 0.  With bf16 data d_z is rounded to bf16 before the products (off by
- * 2^-9 of itself at most, rounded to nearest even); sums are fp32.
+ * d_z being 0 for rows without a target, rows of nothing but -inf and rows whose d is 0 (x has to be finite there too: 0 times it is part of
+ * d_weight).  With bf16 data d_z is rounded to bf16 before the products (off by 2^-8 of itself at most, to nearest even); sums are fp32.
  *   x, weight, targets, scale   as the forward call had them
  *   stats      DEVICE, the forward call's
  *   d_logprob  DEVICE fp32[rows]
@@ -581,15 +587,17 @@ int adagc_linear_logprobs_backward(const void* x, int64_t ld_x, const void* weig
                                    int64_t ld_d_weight, int32_t accumulate, void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
- * The gated projections of a feed-forward layer in one pass: with g = x Wg^T and u = x Wu^T (sums in fp32, not rounded to the data's type),
+ * The gated projections of a feed-forward layer in one pass: with g = x Wg^T and u = x Wu^T (not rounded to the data's type),
  *     out = silu(g) u,   silu(g) = g / (1 + exp(-g)).
  *   x             DEVICE dtype[rows][ld_x], dim values a row
  *   w_gate, w_up  DEVICE dtype[hidden][ld_...], dim values a row (halves of one matrix, for instance)
  *   out           DEVICE dtype[rows][ld_out], hidden values a row
- *   gate, up      DEVICE dtype[rows][ld_...]: g and u for the backward pass, or both NULL
- *   workspace     DEVICE, adagc_gated_linear_workspace_bytes of it (0: may be NULL), 16-byte aligned, contents without meaning
+ *   gate, up      DEVICE dtype[rows][ld_...]: g and u for the backward pass, rounded to the type, or both NULL
+ *   workspace     DEVICE, adagc_gated_linear_workspace_bytes of it (0: may be NULL), 16-byte aligned, contents without meaning: room for operands
+ *                 that are laid out anew (fp32 data; dim no multiple of 8)
  * Gates below -88 count as silu(g) = 0.
- * Errors: INVALID_ARG, TOO_LARGE (also 2^24 rows or more, 2^23 tiles of 128 x 128 of any of the matrices, and 2^32 - 256 vectors of 16 bytes), HIP.
+ * Errors: INVALID_ARG, TOO_LARGE (also 2^24 rows or more, 2^34 values of out, 2^33 of a weight, 2^34 of x, and half of that where rows
+ * and columns fill their tiles badly), HIP.
  */
 int64_t adagc_gated_linear_workspace_bytes(int64_t rows, int64_t dim, int64_t hidden, int32_t dtype);
 int adagc_gated_linear(const void* x, int64_t ld_x, const void* w_gate, int64_t ld_w_gate, const void* w_up, int64_t ld_w_up, int32_t dtype,
@@ -600,7 +608,8 @@ int adagc_gated_linear(const void* x, int64_t ld_x, const void* w_gate, int64_t 
  * Its gradients, from g and u as the forward call left them, or (gate and up NULL) with both products made again: with t = 1 / (1 + exp(-g)),
  *     d_g = d_out u t (1 + g (1 - t)),  d_u = d_out g t,  d_x = d_g Wg + d_u Wu,  d_w_gate = d_g^T x,  d_w_up = d_u^T x
  * (the last two added to what is there with accumulate = 1), and, for the next layer's weight gradient, out again.  With bf16 data d_g and
- * d_u are rounded to bf16 before the products (off by 2^-9 of themselves at most); sums are fp32.
+ * d_u are rounded to bf16 before the products (off by 2^-8 of themselves at most); sums are fp32.  Kept products save a third of the
+ * multiplications of a training pass's backward half and cost their own rounding, which the gradients inherit.
  *   d_out             DEVICE dtype[rows][ld_d_out]
  *   d_x               DEVICE dtype[rows][ld_d_x]; or NULL
  *   d_w_gate, d_w_up  DEVICE weight_dtype[hidden][ld_...], zero rows make them 0 (or leave them); or both NULL
@@ -617,11 +626,12 @@ int adagc_gated_linear_backward(const void* d_out, int64_t ld_d_out, const void*
                                 int64_t ld_out, void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
- * Dropout whose mask is never stored: out = (residual +) x / (1 - p) where a value is kept, residual (or 0) where it is not.  The same call
- * on the gradient of out, without residual, is the gradient of x.
- * Value j of row i has word j mod 4 of block number (offset + i ceil(cols / 4) + j / 4) mod 2^64 of Philox4x32-10 (Salmon et al., 2011) with
- * the counter (low word of the number, high word, 0, 0) and the seed as key (low word first); it is kept if the word is at least p 2^32,
- * rounded to whole.  x / (1 - p) + residual is rounded once in fp32, with 1 / (1 - p) as an fp32 number.
+ * Dropout whose mask is never stored: out = (residual +) x / (1 - p) where a value is kept, residual (or 0) where it is not, whatever x is
+ * there.  The same call on the gradient of out, without residual, is the gradient of x.
+ * Value j of row i has word j mod 4 of block number (offset + i ceil(cols / 4) + j / 4) mod 2^64 of Philox4x32-10 (Salmon et al., "Parallel
+ * random numbers: as easy as 1, 2, 3", 2011) with the counter (low word of the number, high word, 0, 0) and the seed as key (low word first);
+ * it is kept if the word is at least p 2^32, rounded to whole.  x / (1 - p) + residual is rounded once in fp32, with 1 / (1 - p) as an fp32
+ * number.
  *   x         DEVICE dtype[rows][ld_x]
  *   residual  DEVICE dtype[rows][ld_residual], or NULL
  *   p         0 .. 1

@@ -126,6 +126,8 @@ LINEAR_SIZES = [               # rows, vocab, dim, leading dimension and offset 
     (150, 400, 135, 2, 1, 1.0),
     (128, 128, 128, 0, 0, 1.0),
     (191, 129, 191, 0, 0, 1.25),
+    (200, 300, 136, 1, 1, 1.0),
+    (200, 300, 200, 8, 4, 1.0),
     (4100, 5000, 136, 0, 0, 1.0),
     (300, 9000, 2100, 0, 0, 1.0),
     (4100, 300, 4200, 0, 0, 1.0),
@@ -250,6 +252,23 @@ def test_linear_logprobs_single_outputs_and_no_rows():
         assert (d_w == (3.0 if accumulate else 0.0)).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [5, 20])
+def test_rows_far_apart(dtype, rows):
+    """Offsets within a tile, and of 32 rows, beyond 32 bits of bytes."""
+    dtype = TYPES[dtype]
+    vocab, dim, ld = 24, 40, 2 ** 25 + 8
+    x, w = matrix(rows, dim, dtype, 1).t, matrix(vocab, dim, dtype, 2, 0.3, ld).t
+    t = some_targets(rows, vocab, 3)
+    stats = check_linear(x, w, t)
+    check_linear_backward(x, w, t, stats)
+    far = matrix(rows, dim, dtype, 1, 1.0, ld).t
+    assert torch.equal(far, x)
+    for a, b in zip(run_linear(far, w, t), run_linear(x, w, t)):
+        assert torch.equal(a, b)
+    check_linear_backward(far, w, t, stats)
+
+
 def test_linear_logprobs_gradient_against_differences():
     """The loss sum(d log p) along a direction in x and W: differences of the forward pass in fp32."""
     rows, vocab, dim = 12, 50, 24
@@ -305,6 +324,8 @@ GATED_SIZES = [                # rows, dim, hidden, more, offset
     (150, 135, 400, 1, 1),
     (128, 128, 128, 0, 0),
     (191, 191, 129, 0, 0),
+    (200, 136, 300, 1, 1),
+    (200, 200, 304, 8, 4),
     (4100, 136, 2600, 0, 0),
     (300, 2100, 4500, 0, 0),
 ]
@@ -588,8 +609,9 @@ def test_a_training_step_with_all_of_them(dtype):
 
 
 def test_gradients_of_the_example_that_makes_everything_again():
-    """Relative bounds in the Frobenius norm: a bf16 value is off by u = 2^-9 of itself at most, and on the way to a gradient lie at most ten of
-    them (a, y, h1, d_z, d_h1, its dropout, d_a, d_g or d_u, the result), two of which (h1 and a) enter twice."""
+    """Relative bounds in the Frobenius norm: a bf16 value is off by u = 2^-8 of itself at most and half of that in the root of the mean square
+    (u / sqrt 3 of a power of two, less above it), and on the way to a gradient lie at most ten of them (a, y, h1, d_z, d_h1, its dropout,
+    d_a, d_g or d_u, the result), two of which (h1 and a) enter twice: 6 u if all of them pointed the same way."""
     from paper_2502_11034_amd.example_training import Chain, Model
     p = 0.25
     model, chain = Model(300, 96, 160, 777, seed=3, again=True, dropout=p), Chain(300)
@@ -605,11 +627,11 @@ def test_gradients_of_the_example_that_makes_everything_again():
     logp = torch.log_softmax((h0 + torch.where(kept, a @ w[3].t() / (1 - p), 0.0)) @ w[4].t(), 1)
     lp = torch.where(target >= 0, logp.gather(1, target.clamp(min=0)[:, None])[:, 0], 0.0)
     (-lp.mean()).backward()
-    u = 2.0 ** -9
-    assert (logprob - lp).abs().max() < 60 * u           # four roundings of values of size up to 5, summed over a row of weights
+    u = 2.0 ** -8
+    assert (logprob - lp).abs().max() < 30 * u           # four roundings of values of size up to 5, summed over a row of weights
     for got, want in zip(model.grads, w):
         got, want = got.cpu().double(), want.grad
-        assert (got - want).norm() <= 12 * u * want.norm()
+        assert (got - want).norm() <= 6 * u * want.norm()
 
 
 def test_the_example_runs_with_everything_made_again():
