@@ -107,7 +107,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void stats_kernel(const StatsArgs a
     });
 }
 
-// Few rows: a thread for each value.
+// Few rows: a thread for each value; a workgroup leaves one part of each row, of all its columns.
 template <class T, int TM>
 __global__ __launch_bounds__(kThinThreads, 4) void thin_stats_kernel(const StatsArgs a)
 {
@@ -115,6 +115,7 @@ __global__ __launch_bounds__(kThinThreads, 4) void thin_stats_kernel(const Stats
     const int own_row = threadIdx.x / kThinColumns;
     const int64_t target = a.targets && own_row < a.p.m ? a.targets[own_row] : -1;
     const float c = a.scale * kLog2e;
+    float most_yet = -__builtin_inff(), sum_yet = 0.f;
     thin_tiles<T, TM, false>(a.p, lds, [](int64_t) {}, [&](int64_t n0, int row, int at, float z, float) __attribute__((always_inline)) {
         if (row >= a.p.m) return;                          // (whole halves of waves)
         const int64_t col = n0 + at;
@@ -125,9 +126,12 @@ __global__ __launch_bounds__(kThinThreads, 4) void thin_stats_kernel(const Stats
         float sum = __builtin_amdgcn_exp2f((z - (most == -__builtin_inff() ? 0.f : most)) * c);
 #pragma unroll
         for (int d = 1; d < kThinColumns; d *= 2) sum += __shfl_xor(sum, d);
-        if (at == 0) a.parts[row * a.pitch + n0 / kThinColumns] = float2{most, sum};
+        const float both = maximum(most_yet, most);
+        sum_yet = rescaled(most_yet, sum_yet, both, c) + rescaled(most, sum, both, c);
+        most_yet = both;
         if (target == col && col < a.p.n) a.target_logit[row] = z;
     });
+    if (own_row < a.p.m && threadIdx.x % kThinColumns == 0) a.parts[own_row * a.pitch + blockIdx.x] = float2{most_yet, sum_yet};
 }
 
 struct JoinArgs {
@@ -389,10 +393,8 @@ int stats_of(StatsArgs a, int64_t* tiles, hipStream_t s)
 {
     constexpr int32_t dtype = sizeof(T) == 4 ? ADAGC_F32 : ADAGC_BF16;
     if (thin(a.p, dtype)) {
-        *tiles = (a.p.n + kThinColumns - 1) / kThinColumns;
-        for_rows(a.p.m, [&](auto TM) {
-            thin_stats_kernel<T, decltype(TM)::value><<<dim3((uint32_t)std::min<int64_t>(*tiles, kThinGrid)), dim3(kThinThreads), 0, s>>>(a);
-        });
+        *tiles = std::min<int64_t>((a.p.n + kThinColumns - 1) / kThinColumns, kThinGrid);
+        for_rows(a.p.m, [&](auto TM) { thin_stats_kernel<T, decltype(TM)::value><<<dim3((uint32_t)*tiles), dim3(kThinThreads), 0, s>>>(a); });
         return launched();
     }
     const AlongPlan p = plan_of(&a.p, dtype);
