@@ -1251,19 +1251,23 @@ __global__ __launch_bounds__(S::kThreads, 2) void plain_kernel(const PlainArgs a
     const bool uneven = a.k % kTogether;
     const int64_t m_readable = ACROSS_Y ? a.m_readable : a.m;
     struct Place {
-        int     item, product;
+        int     item, product, slot;           // slot: of a split tile's part in the workspace
         int64_t m0, n0, m_least, n_least;
     };
     int step0, step1;
     bool rest;
     auto place_of = [&](int item) __attribute__((always_inline)) {
-        int tile = item, part = 0;
+        int tile = item, slot = 0;
         step0 = 0;
         step1 = full;
         rest = uneven;
         if (item >= a.whole) {
-            tile = __builtin_amdgcn_readfirstlane(a.whole + (item - a.whole) / a.split);
-            part = __builtin_amdgcn_readfirstlane((item - a.whole) % a.split);
+            // an XCD has neighbours here too: tiles of the same part of k
+            const int split_items = items - a.whole, tiles = split_items / a.split, i = item - a.whole, xcd = i % 8;
+            const int at = xcd * (split_items / 8) + min(xcd, split_items % 8) + i / 8;
+            const int part = __builtin_amdgcn_readfirstlane(at / tiles);
+            tile = __builtin_amdgcn_readfirstlane(a.whole + at % tiles);
+            slot = (tile - a.whole) * a.split + part;
             step0 = __builtin_amdgcn_readfirstlane((int)((int64_t)full * part / a.split));
             step1 = __builtin_amdgcn_readfirstlane((int)((int64_t)full * (part + 1) / a.split));
             rest = uneven && part == a.split - 1;
@@ -1271,6 +1275,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void plain_kernel(const PlainArgs a
         const int per_product = a.tiles_m * a.tiles_n;
         Place p;
         p.item = item;
+        p.slot = slot;
         p.product = a.products > 1 && tile >= per_product;
         int tm, tn;
         place_of_tile(tile - p.product * per_product, a.tiles_m, a.tiles_n, &tm, &tn);
@@ -1323,8 +1328,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void plain_kernel(const PlainArgs a
         }
     };
     auto finish = [&](const Place& p) __attribute__((always_inline)) {
-        // (a tile at the matrix's end looks where it ends; within it the time of an address and a check for every four results showed: 14 of 460 us
-        // of a weight gradient of 16128 x 4096 from 4096 tokens)
+        // (a tile at the matrix's end looks where it ends; within it an address and a check for every four results showed: 5 of 459 us of a weight
+        // gradient of 16128 x 4096 from 4096 tokens)
         const bool inside = p.m0 == p.m_least && p.m0 + S::BM <= a.m && p.n0 == p.n_least && p.n0 + S::BN <= a.n && a.out_bf16 == a.add_bf16;
         if (p.item < a.whole && inside) {
             void* out = p.product ? a.out[1] : a.out[0];
@@ -1336,7 +1341,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void plain_kernel(const PlainArgs a
                 store_plain(a, p.product, p.m0 + r, p.m_least, p.n0 + c, p.n_least, v);
             });
         } else {
-            f32x4_p* to = reinterpret_cast<f32x4_p*>(a.workspace) + (size_t)(p.item - a.whole) * (S::BM * S::BN / 4) + thread_anew();
+            f32x4_p* to = reinterpret_cast<f32x4_p*>(a.workspace) + (size_t)p.slot * (S::BM * S::BN / 4) + thread_anew();
             each_piece<S>(acc, [&](int m, int n, int, int, const f32x4_p& v) __attribute__((always_inline)) { to[(m * S::kTN + n) * S::kThreads] = v; });
         }
     };
@@ -1418,7 +1423,6 @@ struct PlainPlan {
     bool    checked, direct;
     int64_t tiles_m, tiles_n, whole, rest, split;
     int64_t workspace() const { return split > 1 ? rest * split * size * size * 4 : 0; }
-    bool    launchable() const { return (whole + rest * split) * (direct ? 512 : 256) <= UINT32_MAX; }      // lanes
 };
 // m (with Y across k) and n: of the readable columns; pairs: of operands that are summed; products: side by side; aligned: the rows of both
 // operands are.  A workspace is sized for both.
@@ -1430,12 +1434,16 @@ inline PlainPlan plain_plan(int64_t m, int64_t n, int64_t k, int32_t dtype, bool
     const bool far = ld_x >= (int64_t)1 << 24 || (across_y && ld_y >= (int64_t)1 << 24);
     p.direct = aligned && !far && dtype == ADAGC_BF16 && (across_y || ld_y < (int64_t)1 << 23) && n >= 128 && n % 8 == 0 &&
                (!across_y || (m >= 128 && m % 8 == 0));
+    const int64_t steps = k / (kStepBytes / dtype_size(dtype)) / (p.direct ? 2 : 1) * (p.direct ? 2 : 1);
     p.size = tile_size(p.direct, dtype, tiles);
+    // Few large tiles, if along k there are 64 steps for each compute unit, by which the partial sums are paid for: 4096 x 768 from 16384, 48 tiles in
+    // five parts 120 us and 17 for joining, 192 small tiles 175; 333 x 765 in parts from 8191, 36 steps each, 18 small tiles in 14 parts 33 and 4.
+    if (p.direct && p.size < 256 && steps * pairs * tiles(256) >= 64 * kUnits) p.size = 256;
     if (p.size == 256 && (m < 256 || n < 256)) p.size = 128;
     p.checked = far || n < p.size || (across_y && m < p.size);
     p.tiles_m = (m + p.size - 1) / p.size;
     p.tiles_n = (n + p.size - 1) / p.size;
-    const int64_t all = tiles(p.size), steps = k / (kStepBytes / dtype_size(dtype)) / (p.direct ? 2 : 1) * (p.direct ? 2 : 1);
+    const int64_t all = tiles(p.size);
     const int64_t round = p.direct ? kUnits : 2 * kUnits;   // a ring fills a compute unit's LDS; the others' workgroups share a unit in pairs
     p.rest = all % round;
     // a part has eight steps at least (of each pair)

@@ -165,6 +165,17 @@ def test_linear_logprobs_in_pieces_of_the_vocabulary(dtype, rows, vocab, dim):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows, vocab, dim", [(513, 22116, 64), (513, 22116, 130), (1000, 33000, 1032)])
+def test_linear_logprobs_of_rounds_that_are_not_full(dtype, rows, vocab, dim):
+    """A last round of smaller tiles; few tiles that share a long sum out."""
+    dtype = TYPES[dtype]
+    x, w, t = matrix(rows, dim, dtype, 4).t, matrix(vocab, dim, dtype, 5, dim ** -0.5).t, some_targets(rows, vocab, 6)
+    t[0], t[2], t[3] = vocab - 1, vocab - 200, vocab - 360          # on both sides of where the smaller tiles begin
+    stats = check_linear(x, w, t)
+    check_linear_backward(x, w, t, stats)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows, vocab, dim", [(19, 70, 40), (140, 900, 264), (4096, 2048, 64)])
 def test_products_of_whole_numbers_are_exact(dtype, rows, vocab, dim):
     """Small whole numbers: every sum is exact, whatever its order, and a place that is missed or counted twice shows."""
