@@ -50,11 +50,11 @@ __device__ __forceinline__ void store_parts(uint16_t* to, int64_t part, const f3
 
 // T: of the operands; O: of what else is read and written.  PARTS: of d_g and d_u, 1 or kParts, the latter with zeros in rows past the last one
 // and columns past the last one.
-template <class S, class T, class O, bool BACKWARD, int PARTS>
+template <class S, class T, class O, bool BACKWARD, int PARTS, Sum SUM>
 __global__ __launch_bounds__(S::kThreads, 2) void gated_kernel(const GatedArgs a)
 {
     __shared__ __attribute__((aligned(512))) uint8_t lds[S::kLds];
-    along_tiles<S, T, true>(a.p, lds, [](int64_t, int64_t) {}, [&](Sums<S>& acc, int64_t m0, int64_t n0, uint8_t*) __attribute__((always_inline)) {
+    along_tiles<S, T, true, SUM>(a.p, lds, [](int64_t, int64_t) {}, [&](Sums<S>& acc, int64_t m0, int64_t n0, uint8_t*) __attribute__((always_inline)) {
         const int t = thread_anew(), lane = t & 63, wave = t >> 6;
         const int first_row = wave / S::kWN * S::kTM * 16 + lane % 16, first_col = wave % S::kWN * (S::kTN / 2) * 16 + lane / 16 * 4;
         const int64_t row0 = m0 + first_row, col0 = n0 + first_col;
@@ -248,8 +248,9 @@ int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 struct Work {
     Layout  layout;
     int64_t x, weight;                             // weight: of each
-    int64_t ld, rows, gradients, partial;
-    int64_t forward() const { return x + 2 * weight; }
+    int64_t along;                                 // partial sums of the projections
+    int64_t ld, rows, gradients, partial;          // partial: of them and of the products
+    int64_t forward() const { return x + 2 * weight + along; }
     int64_t backward() const { return 2 * gradients + partial + x + 2 * weight; }
 };
 Work work_of(int64_t rows, int64_t dim, int64_t hidden, int32_t dtype)
@@ -266,6 +267,10 @@ Work work_of(int64_t rows, int64_t dim, int64_t hidden, int32_t dtype)
     w.gradients = up16(w.rows * w.ld * (parts ? 2 * kParts : dtype_size(dtype)));
     const int32_t type = w.layout.anew ? ADAGC_BF16 : dtype;
     const int64_t columns = w.layout.anew ? (dim + 7) / 8 * 8 : dim;
+    const int64_t k = w.layout.anew ? w.layout.ld : dim;
+    for (const bool aligned : {false, true})
+        if (rows > kThinRows) w.along = std::max(w.along, along_plan(rows, 2 * hidden, k, w.layout.segments, type, aligned, k, k).workspace());
+    w.partial = w.along;
     for (const bool aligned : {false, true})
         w.partial = std::max({w.partial, plain_plan((hidden + 7) / 8 * 8, columns, w.rows, type, true, w.ld, columns, w.layout.segments, 2, aligned).workspace(),
                               plain_plan(rows, columns, parts ? w.ld : hidden, type, false, w.ld, columns, 2 * w.layout.segments, 1, aligned).workspace()});
@@ -304,18 +309,29 @@ int projections(GatedArgs a, hipStream_t s)
         }
     }
     const bool aligned = rows_aligned(a.p.y, a.p.ld_y, dtype) && rows_aligned(a.p.x[0], a.p.ld_x[0], dtype) && rows_aligned(a.p.x[1], a.p.ld_x[1], dtype);
-    const AlongPlan p = along_plan(a.p.m, 2 * a.p.n, dtype, aligned, a.p.ld_y, std::max(a.p.ld_x[0], a.p.ld_x[1]));
+    const AlongPlan p = along_plan(a.p.m, 2 * a.p.n, a.p.k, a.p.segments, dtype, aligned, a.p.ld_y, std::max(a.p.ld_x[0], a.p.ld_x[1]));
     a.p.tiles_m = (int32_t)p.tiles_m;
     a.p.tiles_n = (int32_t)p.tiles_n;
+    a.p.split = (int32_t)p.split;
     const dim3 grid((uint32_t)(p.tiles_m * p.tiles_n));
     if constexpr (sizeof(T) == 2) {
-        const dim3 small(grid_of<Small>(p.tiles_m * p.tiles_n));
         constexpr int kOf = BACKWARD && sizeof(O) == 4 ? kParts : 1;       // (fp32 data is laid out in parts)
-        if (p.size == 256) gated_kernel<Large, T, O, BACKWARD, kOf><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
-        else if (p.direct) gated_kernel<Small, T, O, BACKWARD, kOf><<<small, dim3(Small::kThreads), 0, s>>>(a);
+        if (p.size == 256) {
+            gated_kernel<Large, T, O, BACKWARD, kOf, Sum::kWhole><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
+        } else if (p.direct && p.split > 1) {
+            launch_parts<Small, T, true>(a.p, s);
+            gated_kernel<Small, T, O, BACKWARD, kOf, Sum::kJoined><<<grid, dim3(Small::kThreads), 0, s>>>(a);
+        } else if (p.direct) {
+            gated_kernel<Small, T, O, BACKWARD, kOf, Sum::kWhole><<<dim3(grid_of<Small>(p.tiles_m * p.tiles_n)), dim3(Small::kThreads), 0, s>>>(a);
+        }
     }
     if constexpr (sizeof(T) == sizeof(O)) {
-        if (!p.direct) gated_kernel<Staged<T>, T, O, BACKWARD, 1><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+        if (!p.direct && p.split > 1) {
+            launch_parts<Staged<T>, T, true>(a.p, s);
+            gated_kernel<Staged<T>, T, O, BACKWARD, 1, Sum::kJoined><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+        } else if (!p.direct) {
+            gated_kernel<Staged<T>, T, O, BACKWARD, 1, Sum::kWhole><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+        }
     }
     return launched();
 }
@@ -324,6 +340,7 @@ template <class T>
 int forward(const Work& w, GatedArgs a, uint8_t* workspace, hipStream_t s)
 {
     if (const int rc = lay_operands<T>(w, &a.p, workspace, s)) return rc;
+    a.p.partial = reinterpret_cast<float*>(workspace + w.x + 2 * w.weight);
     return w.layout.anew ? projections<uint16_t, T, false>(a, s) : projections<T, T, false>(a, s);
 }
 
@@ -378,6 +395,7 @@ int backward(const Work& w, Backward b, uint8_t* workspace, hipStream_t s)
         b.g.ld_gate = b.g.ld_up = w.ld;
         b.g.part = part;
         b.g.rows = w.rows;
+        b.g.p.partial = reinterpret_cast<float*>(workspace + 2 * w.gradients);
         if (const int rc = anew ? projections<uint16_t, T, true>(b.g, s) : projections<T, T, true>(b.g, s)) return rc;
     }
     PlainArgs both{};
@@ -458,7 +476,7 @@ extern "C" int adagc_gated_linear(const void* x, int64_t ld_x, const void* w_gat
     const int64_t need = w.forward();
     if (need > 0 && (!workspace || workspace_bytes < need || misaligned(workspace, 16))) return ADAGC_ERR_INVALID_ARG;
     GatedArgs a{};
-    a.p = {x, {w_gate, w_up}, ld_x, {ld_w_gate, ld_w_up}, rows, hidden, dim, 0, 0, 1, 0, 0};
+    a.p = {x, {w_gate, w_up}, ld_x, {ld_w_gate, ld_w_up}, rows, hidden, dim, 0, 0, 1, 0, 0, nullptr, 1};
     a.out = out;
     a.ld_out = ld_out;
     a.gate = gate;
@@ -503,7 +521,7 @@ extern "C" int adagc_gated_linear_backward(const void* d_out, int64_t ld_d_out, 
     const int64_t need = w.backward();
     if (need > 0 && (!workspace || workspace_bytes < need || misaligned(workspace, 16))) return ADAGC_ERR_INVALID_ARG;
     Backward b{};
-    b.g.p = {x, {w_gate, w_up}, ld_x, {ld_w_gate, ld_w_up}, rows, hidden, dim, 0, 0, 1, 0, 0};
+    b.g.p = {x, {w_gate, w_up}, ld_x, {ld_w_gate, ld_w_up}, rows, hidden, dim, 0, 0, 1, 0, 0, nullptr, 1};
     b.g.out = out;
     b.g.ld_out = ld_out;
     b.g.d_out = d_out;

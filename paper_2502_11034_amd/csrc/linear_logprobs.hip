@@ -28,12 +28,12 @@ struct StatsArgs {
 // sum of exp(scale (m_i - m) ) s_i for the joint maximum m; a part of -inf has sum 0
 __device__ __forceinline__ float rescaled(float mi, float si, float m, float c) { return mi == -__builtin_inff() ? 0.f : si * __builtin_amdgcn_exp2f((mi - m) * c); }
 
-template <class S, class T>
+template <class S, class T, Sum SUM>
 __global__ __launch_bounds__(S::kThreads, 2) void stats_kernel(const StatsArgs a)
 {
     __shared__ __attribute__((aligned(512))) uint8_t lds[S::kLds];
     const float c = a.scale * kLog2e;
-    along_tiles<S, T, false>(a.p, lds, [](int64_t, int64_t) {}, [&](Sums<S>& acc, int64_t m0, int64_t n0, uint8_t* scratch) __attribute__((always_inline)) {
+    along_tiles<S, T, false, SUM>(a.p, lds, [](int64_t, int64_t) {}, [&](Sums<S>& acc, int64_t m0, int64_t n0, uint8_t* scratch) __attribute__((always_inline)) {
         const LanePlace<S> at;
         const int tid = thread_anew(), lane = tid & 63, wave = tid >> 6;
         if (n0 + S::BN > a.p.n) {
@@ -198,7 +198,7 @@ struct GradArgs {
 };
 
 // PARTS: 1, or kParts, with zeros in rows past the last one and columns past the piece's end.
-template <class S, class T, int PARTS>
+template <class S, class T, int PARTS, Sum SUM>
 __global__ __launch_bounds__(S::kThreads, 2) void grad_kernel(const GradArgs a)
 {
     __shared__ __attribute__((aligned(512))) uint8_t lds[S::kLds];
@@ -223,7 +223,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void grad_kernel(const GradArgs a)
         settle_now(log2_sum);
         settle_now(d);
     };
-    along_tiles<S, T, false>(a.p, lds, before, [&](Sums<S>& acc, int64_t m0, int64_t n0, uint8_t*) __attribute__((always_inline)) {
+    along_tiles<S, T, false, SUM>(a.p, lds, before, [&](Sums<S>& acc, int64_t m0, int64_t n0, uint8_t*) __attribute__((always_inline)) {
         const LanePlace<S> at;
 #pragma unroll
         for (int m = 0; m < S::kTM; ++m) {
@@ -290,9 +290,9 @@ struct Work {
     Layout  layout;
     int64_t size, number;                          // of a piece, of pieces
     int64_t pitch, parts, targets;                 // forward: tiles of a row at most; their parts, the targets' logits
-    int64_t ld, d_logits, sums, partial;           // backward: the gradients of a piece's logits; sums of dx in fp32; partial sums of a product
+    int64_t ld, d_logits, sums, partial;           // backward: the gradients of a piece's logits; sums of dx in fp32; partial: sums of a product
     int64_t x, weight;                             // operands laid out
-    int64_t forward() const { return parts + targets + x + weight; }
+    int64_t forward() const { return parts + targets + x + weight + partial; }
     int64_t backward() const { return d_logits + sums + partial + x + weight; }
 };
 // Columns of a piece, so many at most: the weight's gradient takes 256-tiles in whole rounds of the compute units where that many fill some.
@@ -303,6 +303,14 @@ int64_t piece_of(int64_t vocab, int64_t dim, int64_t most)
     int64_t rounds = most / 256 * wide / kUnits;
     if (rounds == 0) rounds = 2 * most / 256 * wide / kUnits;
     return rounds ? std::min(vocab, rounds * kUnits / wide * 256) : most;
+}
+// Columns of W whose tiles fill whole rounds; 0: those after them are no smaller tiles.  They are, if those are a round at most: 1024 x 50257 from
+// 768, 788 tiles, 95 us, and 78 and 12 with the last five columns of tiles small.
+int64_t columns_of_whole_rounds(const AlongPlan& p, int64_t m, int64_t n)
+{
+    if (p.size < 256) return 0;
+    const int64_t columns = p.tiles_m * p.tiles_n / kUnits * kUnits / p.tiles_m * 256;
+    return columns < n && (m + 127) / 128 * ((n - columns + 127) / 128) <= kUnits ? columns : 0;
 }
 Work work_of(int64_t rows, int64_t vocab, int64_t dim, int32_t dtype, bool backward)
 {
@@ -325,8 +333,17 @@ Work work_of(int64_t rows, int64_t vocab, int64_t dim, int32_t dtype, bool backw
         w.x = w.layout.bytes(rows);
         w.weight = w.layout.bytes(w.size);
     }
-    if (!backward) return w;
     const int32_t type = w.layout.anew ? ADAGC_BF16 : dtype;
+    const int64_t k_along = w.layout.anew ? w.layout.ld : dim;
+    for (const int64_t n : {w.size, vocab - (w.number - 1) * w.size})
+        for (const bool aligned : {false, true}) {
+            if (rows <= kThinRows) continue;
+            const AlongPlan p = along_plan(rows, n, k_along, w.layout.segments, type, aligned, k_along, k_along);
+            w.partial = std::max(w.partial, p.workspace());
+            if (const int64_t columns = columns_of_whole_rounds(p, rows, n))
+                w.partial = std::max(w.partial, along_plan(rows, n - columns, k_along, w.layout.segments, type, aligned, k_along, k_along).workspace());
+        }
+    if (!backward) return w;
     const int64_t columns = w.layout.anew ? (dim + 7) / 8 * 8 : dim;
     for (const int64_t n : {w.size, vocab - (w.number - 1) * w.size})
         for (const bool aligned : {false, true}) {
@@ -380,9 +397,10 @@ AlongArgs along_args(const Operands& o, const Work& w, int64_t rows, int64_t n, 
 }
 AlongPlan plan_of(AlongArgs* p, int32_t dtype)
 {
-    const AlongPlan plan = along_plan(p->m, p->n, dtype, rows_aligned(p->y, p->ld_y, dtype) && rows_aligned(p->x[0], p->ld_x[0], dtype), p->ld_y, p->ld_x[0]);
+    const AlongPlan plan = along_plan(p->m, p->n, p->k, p->segments, dtype, rows_aligned(p->y, p->ld_y, dtype) && rows_aligned(p->x[0], p->ld_x[0], dtype), p->ld_y, p->ld_x[0]);
     p->tiles_m = (int32_t)plan.tiles_m;
     p->tiles_n = (int32_t)plan.tiles_n;
+    p->split = (int32_t)plan.split;
     return plan;
 }
 int launched() { return hipGetLastError() == hipSuccess ? ADAGC_OK : ADAGC_ERR_HIP; }
@@ -401,15 +419,12 @@ int stats_of(StatsArgs a, int64_t* tiles, hipStream_t s)
     *tiles = p.tiles_n;
     const dim3 grid((uint32_t)(p.tiles_m * p.tiles_n));
     if constexpr (sizeof(T) == 2) {
-        // The tiles after the last whole round are small ones if those are a round at most: 1024 x 50257 from 768, 788 tiles, 95 us, and 78 and 12 with
-        // the last five columns of tiles small.
-        const int64_t whole = p.size == 256 ? p.tiles_m * p.tiles_n / kUnits * kUnits / p.tiles_m : 0, columns = whole * 256;      // columns of tiles, of W
-        if (whole && columns < a.p.n && (a.p.m + 127) / 128 * ((a.p.n - columns + 127) / 128) <= kUnits) {
+        if (const int64_t columns = columns_of_whole_rounds(p, a.p.m, a.p.n)) {
             StatsArgs last = a;
             last.p.x[0] = last.p.x[1] = static_cast<const T*>(a.p.x[0]) + columns * a.p.ld_x[0];
             last.p.n -= columns;
             last.first += columns;
-            last.parts += whole;
+            last.parts += columns / 256;
             a.p.n = columns;
             int64_t more = 0;
             if (const int rc = stats_of<T>(a, tiles, s)) return rc;
@@ -418,10 +433,21 @@ int stats_of(StatsArgs a, int64_t* tiles, hipStream_t s)
             return rc;
         }
         const dim3 small(grid_of<Small>(p.tiles_m * p.tiles_n));
-        if (p.size == 256) stats_kernel<Large, T><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
-        else if (p.direct) stats_kernel<Small, T><<<small, dim3(Small::kThreads), 0, s>>>(a);
+        if (p.size == 256) {
+            stats_kernel<Large, T, Sum::kWhole><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
+        } else if (p.direct && p.split > 1) {
+            launch_parts<Small, T, false>(a.p, s);
+            stats_kernel<Small, T, Sum::kJoined><<<grid, dim3(Small::kThreads), 0, s>>>(a);
+        } else if (p.direct) {
+            stats_kernel<Small, T, Sum::kWhole><<<small, dim3(Small::kThreads), 0, s>>>(a);
+        }
     }
-    if (!p.direct) stats_kernel<Staged<T>, T><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+    if (!p.direct && p.split > 1) {
+        launch_parts<Staged<T>, T, false>(a.p, s);
+        stats_kernel<Staged<T>, T, Sum::kJoined><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+    } else if (!p.direct) {
+        stats_kernel<Staged<T>, T, Sum::kWhole><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+    }
     return launched();
 }
 
@@ -429,12 +455,14 @@ template <class T>
 int forward(const Work& w, Operands o, int64_t rows, int64_t vocab, int64_t dim, StatsArgs a, JoinArgs join, uint8_t* workspace, hipStream_t s)
 {
     uint8_t* laid = workspace + w.parts + w.targets;
+    float* partial = reinterpret_cast<float*>(laid + w.x + w.weight);
     for (int64_t first = 0; first < vocab; first += w.size) {
         const int64_t n = std::min(w.size, vocab - first);
         Operands piece;
         if (const int rc = lay_piece<T>(w, rows, first, n, dim, &o, &piece, laid, s)) return rc;
         StatsArgs b = a;
         b.p = along_args(piece, w, rows, n, dim);
+        b.p.partial = partial;
         b.first = first;
         b.parts += join.tiles;
         int64_t tiles = 0;
@@ -458,12 +486,26 @@ int gradient(GradArgs a, int parts, hipStream_t s)
     const dim3 grid((uint32_t)(p.tiles_m * p.tiles_n));
     if constexpr (sizeof(T) == 2) {
         const dim3 large(grid_of<Large>(p.tiles_m * p.tiles_n)), small(grid_of<Small>(p.tiles_m * p.tiles_n));
-        if (p.size == 256 && parts > 1) grad_kernel<Large, T, kParts><<<large, dim3(Large::kThreads), 0, s>>>(a);
-        else if (p.size == 256) grad_kernel<Large, T, 1><<<large, dim3(Large::kThreads), 0, s>>>(a);
-        else if (p.direct && parts > 1) grad_kernel<Small, T, kParts><<<small, dim3(Small::kThreads), 0, s>>>(a);
-        else if (p.direct) grad_kernel<Small, T, 1><<<small, dim3(Small::kThreads), 0, s>>>(a);
+        auto direct_ones = [&](auto PARTS) {
+            constexpr int kOf = decltype(PARTS)::value;
+            if (p.size == 256) {
+                grad_kernel<Large, T, kOf, Sum::kWhole><<<large, dim3(Large::kThreads), 0, s>>>(a);
+            } else if (p.direct && p.split > 1) {
+                launch_parts<Small, T, false>(a.p, s);
+                grad_kernel<Small, T, kOf, Sum::kJoined><<<grid, dim3(Small::kThreads), 0, s>>>(a);
+            } else if (p.direct) {
+                grad_kernel<Small, T, kOf, Sum::kWhole><<<small, dim3(Small::kThreads), 0, s>>>(a);
+            }
+        };
+        if (parts > 1) direct_ones(std::integral_constant<int, kParts>{});
+        else direct_ones(std::integral_constant<int, 1>{});
     }
-    if (!p.direct) grad_kernel<Staged<T>, T, 1><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+    if (!p.direct && p.split > 1) {
+        launch_parts<Staged<T>, T, false>(a.p, s);
+        grad_kernel<Staged<T>, T, 1, Sum::kJoined><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+    } else if (!p.direct) {
+        grad_kernel<Staged<T>, T, 1, Sum::kWhole><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
+    }
     return launched();
 }
 
@@ -505,6 +547,7 @@ int backward(const Work& w, Operands o, int64_t rows, int64_t vocab, int64_t dim
             if (const int rc = lay_piece<T>(w, rows, first, n, dim, &o, &piece, laid, s)) return rc;
             GradArgs a = all;
             a.p = along_args(piece, w, rows, n, dim);
+            a.p.partial = partial;
             a.first = first;
             a.d_logits = workspace;
             a.ld = w.ld;

@@ -886,7 +886,8 @@ inline bool rows_aligned(const void* p, int64_t ld, int32_t dtype) { return !mis
 struct AlongPlan {
     int     size;                 // 256, 128 or 64
     bool    direct;
-    int64_t tiles_m, tiles_n;
+    int64_t tiles_m, tiles_n, split;       // split: workgroups that share a tile's k
+    int64_t workspace() const { return split > 1 ? tiles_m * tiles_n * split * size * size * 4 : 0; }
 };
 // fp32 as it is: the matrix cores' rate is a sixteenth, which staging and a small tile keep up with.
 template <class F>
@@ -894,7 +895,7 @@ inline int tile_size(bool direct, int32_t dtype, F&& tiles)
 {
     return direct && tiles(256) >= kUnits / 2 ? 256 : dtype == ADAGC_F32 ? 64 : 128;
 }
-inline AlongPlan along_plan(int64_t m, int64_t n, int32_t dtype, bool aligned, int64_t ld_y, int64_t ld_x)
+inline AlongPlan along_plan(int64_t m, int64_t n, int64_t k, int segments, int32_t dtype, bool aligned, int64_t ld_y, int64_t ld_x)
 {
     AlongPlan p{};
     auto tiles = [&](int64_t size) { return ((m + size - 1) / size) * ((n + size - 1) / size); };
@@ -902,6 +903,9 @@ inline AlongPlan along_plan(int64_t m, int64_t n, int32_t dtype, bool aligned, i
     p.size = tile_size(p.direct, dtype, tiles);
     p.tiles_m = (m + p.size - 1) / p.size;
     p.tiles_n = (n + p.size - 1) / p.size;
+    // Tiles that leave half of the chip without work or more, along a long k: parts of 16 steps at least, whose sums a second launch joins.
+    const int64_t round = p.direct ? kUnits : 2 * kUnits, all = p.tiles_m * p.tiles_n, steps = k / (kStepBytes / dtype_size(dtype)) * segments;
+    p.split = steps >= 64 ? std::max<int64_t>(1, std::min(round / all, steps / 16)) : 1;
     return p;
 }
 
@@ -938,12 +942,17 @@ struct AlongArgs {
     int64_t     part_y, part_x;   // operands in parts: elements from part to part
     int32_t     segments;         // products that are summed: 1, or kSegments of operands in three parts
     int32_t     tiles_m, tiles_n;
+    float*      partial;          // sums of the parts of split tiles
+    int32_t     split;
 };
+
+// Whole tiles; one part of a tile's k, whose sums go to `partial`; a tile's parts, added in order.
+enum class Sum { kWhole, kPart, kJoined };
 
 // The workgroup's tiles.  before(m0, n0): loads for finish, which come before the next tile's in the order that loads are waited for in;
 // finish(acc, m0, n0, scratch): the sums of the tile whose first row is m0 and whose first row of X (or of each) is n0, and an LDS place
 // free to use.
-template <class S, class T, bool PAIR, class Before, class Finish>
+template <class S, class T, bool PAIR, Sum SUM, class Before, class Finish>
 __device__ __forceinline__ void along_tiles(const AlongArgs& a, uint8_t* lds, Before&& before, Finish&& finish)
 {
     constexpr int kColumns = PAIR ? S::BN / 2 : S::BN;
@@ -971,7 +980,53 @@ __device__ __forceinline__ void along_tiles(const AlongArgs& a, uint8_t* lds, Be
         m0 = (int64_t)tm * S::BM;
         n0 = (int64_t)tn * kColumns;
     };
-    if constexpr (!S::kDirect) {
+    auto aim = [&](int first, int number) __attribute__((always_inline)) {
+        // a load of a wave is 8 rows, and a lane's are a multiple of 32 apart: with two matrices, all of one
+        static_assert(!S::kDirect || S::kThreads / 8 % 32 == 0);
+        const int tid = thread_anew();
+        const bool second = PAIR && (wave >> 1 & 1);
+        const int64_t ld_x = second ? a.ld_x[1] : a.ld_x[0];
+        sy.set_rows_direct(tid, y + m0 * a.ld_y, a.ld_y, [&](int r) { return min(m0 + r, a.m - 1) - m0; });
+        sy.set_pairs(first, number, a.segments, a.part_y, kPartsOfY);
+        sx.set_rows_direct(tid, static_cast<const T*>(second ? a.x[1] : a.x[0]) + n0 * ld_x, ld_x, [&](int r) { return row_of_x(r) - n0; });
+        sx.set_pairs(first, number, a.segments, a.part_x, kPartsOfX);
+    };
+    if constexpr (SUM == Sum::kJoined) {
+        to_tile((int)blockIdx.x);
+        before(m0, n0);
+        const f32x4_p* from = reinterpret_cast<const f32x4_p*>(a.partial) + (size_t)blockIdx.x * a.split * (S::BM * S::BN / 4) + tid;
+        clear<S>(acc);
+        for (int p = 0; p < a.split; ++p)
+#pragma unroll
+            for (int m = 0; m < S::kTM; ++m)
+#pragma unroll
+                for (int n = 0; n < S::kTN; ++n) acc[m][n] += from[((size_t)p * S::kTM * S::kTN + m * S::kTN + n) * S::kThreads];
+        finish(acc, m0, n0, lds);
+    } else if constexpr (SUM == Sum::kPart) {
+        // an XCD has neighbours: tiles of the same part
+        const int items = (int)gridDim.x, xcd = (int)blockIdx.x % 8, at = xcd * (items / 8) + min(xcd, items % 8) + (int)blockIdx.x / 8;
+        const int tiles = a.tiles_m * a.tiles_n, part = __builtin_amdgcn_readfirstlane(at / tiles), tile = __builtin_amdgcn_readfirstlane(at % tiles);
+        constexpr int kTogether = (S::kDirect ? 2 : 1) * S::kDeep;
+        const int full = (int)(a.k / kTogether), first = __builtin_amdgcn_readfirstlane((int)((int64_t)full * part / a.split));
+        const int number = __builtin_amdgcn_readfirstlane((int)((int64_t)full * (part + 1) / a.split)) - first;
+        const bool rest = a.k % kTogether && part == a.split - 1;
+        to_tile(tile);
+        clear<S>(acc);
+        if constexpr (S::kDirect) {
+            if (rest) {
+                aim_staged();
+                accumulate_rest<S, T>(acc, sy, sx, 2 * (int64_t)full, a.k, 0, 0);
+            }
+            aim(first, number);
+            start_products<S>(sy, sx, lds0, number, a.segments);
+            accumulate_products<S, T>(acc, sy, sx, lds0, number, a.segments);
+        } else {
+            aim_staged();
+            accumulate<S, T, false>(acc, sy, sx, first, first + number, rest, full, a.k, 0, 0);
+        }
+        f32x4_p* to = reinterpret_cast<f32x4_p*>(a.partial) + ((size_t)tile * a.split + part) * (S::BM * S::BN / 4) + thread_anew();
+        each_piece<S>(acc, [&](int m, int n, int, int, const f32x4_p& v) __attribute__((always_inline)) { to[(m * S::kTN + n) * S::kThreads] = v; });
+    } else if constexpr (!S::kDirect) {
         to_tile((int)blockIdx.x);
         aim_staged();
         clear<S>(acc);
@@ -982,21 +1037,10 @@ __device__ __forceinline__ void along_tiles(const AlongArgs& a, uint8_t* lds, Be
     } else {
         const int pairs = (int)(a.k / (2 * S::kDeep)), tiles = a.tiles_m * a.tiles_n;
         const bool rest = a.k % (2 * S::kDeep);        // (not with several segments)
-        auto aim = [&]() __attribute__((always_inline)) {
-            // a load of a wave is 8 rows, and a lane's are a multiple of 32 apart: with two matrices, all of one
-            static_assert(S::kThreads / 8 % 32 == 0);
-            const int tid = thread_anew();
-            const bool second = PAIR && (wave >> 1 & 1);
-            const int64_t ld_x = second ? a.ld_x[1] : a.ld_x[0];
-            sy.set_rows_direct(tid, y + m0 * a.ld_y, a.ld_y, [&](int r) { return min(m0 + r, a.m - 1) - m0; });
-            sy.set_pairs(0, pairs, a.segments, a.part_y, kPartsOfY);
-            sx.set_rows_direct(tid, static_cast<const T*>(second ? a.x[1] : a.x[0]) + n0 * ld_x, ld_x, [&](int r) { return row_of_x(r) - n0; });
-            sx.set_pairs(0, pairs, a.segments, a.part_x, kPartsOfX);
-        };
         int n = (int)blockIdx.x;
         to_tile(n);
         if (!rest) {
-            aim();
+            aim(0, pairs);
             start_products<S>(sy, sx, lds0, pairs, a.segments);
         }
         while (true) {
@@ -1004,7 +1048,7 @@ __device__ __forceinline__ void along_tiles(const AlongArgs& a, uint8_t* lds, Be
             if (rest) {
                 aim_staged();
                 accumulate_rest<S, T>(acc, sy, sx, 2 * pairs, a.k, 0, 0);
-                aim();
+                aim(0, pairs);
                 start_products<S>(sy, sx, lds0, pairs, a.segments);
             }
             accumulate_products<S, T>(acc, sy, sx, lds0, pairs, a.segments);
@@ -1014,7 +1058,7 @@ __device__ __forceinline__ void along_tiles(const AlongArgs& a, uint8_t* lds, Be
             if (n < tiles) {
                 to_tile(n);
                 if (!rest) {
-                    aim();
+                    aim(0, pairs);
                     start_products<S>(sy, sx, lds0, pairs, a.segments);
                 }
             }
@@ -1029,6 +1073,19 @@ template <class S>
 inline uint32_t grid_of(int64_t tiles)
 {
     return (uint32_t)(S::kDirect ? std::min<int64_t>(tiles, kUnits) : tiles);
+}
+
+template <class S, class T, bool PAIR>
+__global__ __launch_bounds__(S::kThreads, 2) void part_kernel(const AlongArgs a)
+{
+    __shared__ __attribute__((aligned(512))) uint8_t lds[S::kLds];
+    along_tiles<S, T, PAIR, Sum::kPart>(a, lds, [](int64_t, int64_t) {}, [](Sums<S>&, int64_t, int64_t, uint8_t*) {});
+}
+// The parts of split tiles; Sum::kJoined is to follow.
+template <class S, class T, bool PAIR>
+void launch_parts(const AlongArgs& a, hipStream_t s)
+{
+    part_kernel<S, T, PAIR><<<dim3((uint32_t)(a.tiles_m * a.tiles_n * a.split)), dim3(S::kThreads), 0, s>>>(a);
 }
 
 // Waves meet, their LDS accesses done; loads into LDS may be on their way (which __syncthreads would not leave).
@@ -1580,6 +1637,12 @@ extern template int run_plain<uint16_t, false>(PlainArgs, hipStream_t);
 extern template int run_plain<uint16_t, true>(PlainArgs, hipStream_t);
 extern template int lay<float>(const LaySource*, int, int64_t, const Layout&, hipStream_t);
 extern template int lay<uint16_t>(const LaySource*, int, int64_t, const Layout&, hipStream_t);
+extern template void launch_parts<Small, uint16_t, false>(const AlongArgs&, hipStream_t);
+extern template void launch_parts<Small, uint16_t, true>(const AlongArgs&, hipStream_t);
+extern template void launch_parts<Staged<uint16_t>, uint16_t, false>(const AlongArgs&, hipStream_t);
+extern template void launch_parts<Staged<uint16_t>, uint16_t, true>(const AlongArgs&, hipStream_t);
+extern template void launch_parts<Staged<float>, float, false>(const AlongArgs&, hipStream_t);
+extern template void launch_parts<Staged<float>, float, true>(const AlongArgs&, hipStream_t);
 
 }  // namespace product
 }  // namespace adagc
