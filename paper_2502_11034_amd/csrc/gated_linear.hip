@@ -253,10 +253,10 @@ struct Work {
     int64_t forward() const { return x + 2 * weight + along; }
     int64_t backward() const { return 2 * gradients + partial + x + 2 * weight; }
 };
-Work work_of(int64_t rows, int64_t dim, int64_t hidden, int32_t dtype)
+Work work_of(int64_t rows, int64_t dim, int64_t hidden, int32_t dtype, bool backward)
 {
     Work w{};
-    w.layout = layout_of(rows, hidden, dim, dtype);
+    w.layout = layout_of(rows, hidden, dim, dtype, backward);
     if (w.layout.anew) {
         w.x = w.layout.bytes(rows);
         w.weight = w.layout.bytes(hidden);
@@ -456,7 +456,7 @@ using namespace adagc;
 extern "C" int64_t adagc_gated_linear_workspace_bytes(int64_t rows, int64_t dim, int64_t hidden, int32_t dtype)
 {
     if (const int rc = check(rows, dim, hidden, dtype)) return rc;
-    return work_of(rows, dim, hidden, dtype).forward();
+    return work_of(rows, dim, hidden, dtype, false).forward();
 }
 
 extern "C" int adagc_gated_linear(const void* x, int64_t ld_x, const void* w_gate, int64_t ld_w_gate, const void* w_up, int64_t ld_w_up, int32_t dtype,
@@ -472,7 +472,7 @@ extern "C" int adagc_gated_linear(const void* x, int64_t ld_x, const void* w_gat
         return ADAGC_ERR_INVALID_ARG;
     if (gate && (ld_gate < hidden || ld_up < hidden || misaligned(gate, size) || misaligned(up, size))) return ADAGC_ERR_INVALID_ARG;
     if (std::max({ld_x, ld_w_gate, ld_w_up, ld_out}) > kMaxLd || (gate && std::max(ld_gate, ld_up) > kMaxLd)) return ADAGC_ERR_TOO_LARGE;
-    const Work w = work_of(rows, dim, hidden, dtype);
+    const Work w = work_of(rows, dim, hidden, dtype, false);
     const int64_t need = w.forward();
     if (need > 0 && (!workspace || workspace_bytes < need || misaligned(workspace, 16))) return ADAGC_ERR_INVALID_ARG;
     GatedArgs a{};
@@ -491,7 +491,7 @@ extern "C" int adagc_gated_linear(const void* x, int64_t ld_x, const void* w_gat
 extern "C" int64_t adagc_gated_linear_backward_workspace_bytes(int64_t rows, int64_t dim, int64_t hidden, int32_t dtype)
 {
     if (const int rc = check(rows, dim, hidden, dtype)) return rc;
-    return work_of(rows, dim, hidden, dtype).backward();
+    return work_of(rows, dim, hidden, dtype, true).backward();
 }
 
 extern "C" int adagc_gated_linear_backward(const void* d_out, int64_t ld_d_out, const void* x, int64_t ld_x, const void* w_gate, int64_t ld_w_gate,
@@ -517,7 +517,7 @@ extern "C" int adagc_gated_linear_backward(const void* d_out, int64_t ld_d_out, 
             return ADAGC_ERR_TOO_LARGE;
     }
     if (d_w_gate && std::max(ld_d_w_gate, ld_d_w_up) > kMaxLd) return ADAGC_ERR_TOO_LARGE;
-    const Work w = work_of(rows, dim, hidden, dtype);
+    const Work w = work_of(rows, dim, hidden, dtype, true);
     const int64_t need = w.backward();
     if (need > 0 && (!workspace || workspace_bytes < need || misaligned(workspace, 16))) return ADAGC_ERR_INVALID_ARG;
     Backward b{};

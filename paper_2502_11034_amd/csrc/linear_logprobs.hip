@@ -315,7 +315,7 @@ int64_t columns_of_whole_rounds(const AlongPlan& p, int64_t m, int64_t n)
 Work work_of(int64_t rows, int64_t vocab, int64_t dim, int32_t dtype, bool backward)
 {
     Work w{};
-    w.layout = layout_of(rows, vocab, dim, dtype);
+    w.layout = layout_of(rows, vocab, dim, dtype, backward);
     const int64_t cap = (int64_t)1 << (w.layout.parts > 1 ? 25 : 26);
     int64_t most = std::max<int64_t>(2048, cap / std::max<int64_t>(rows, 1) / 256 * 256);
     if (w.layout.anew) most = std::max<int64_t>(2048, std::min(backward ? most : INT64_MAX, cap / w.layout.ld / 256 * 256));

@@ -3,7 +3,13 @@
 //
 // A block tile's sums  acc[row][col] += sum_k Y[row][k] X[col][k]  on the matrix cores, fp32 accumulation.  Each operand lies in memory
 // either with k consecutive ("along": rows of k) or with k as the slow index ("across": k rows of consecutive rows or columns of the
-// result).  bf16 products are exact in fp32, fp32 ones are rounded by the matrix cores' fp32 instruction.
+// result).  bf16 products are exact in fp32; fp32 operands go through the matrix cores' fp32 instruction, or, for more rows, are three bf16
+// numbers each (kSegments below).
+//
+// What bounds it, bf16: of large products the power limit (a step of 32 k on a 256-tile 0.72 - 0.75 us at some 1.8 GHz, 0.55 if the matrix cores never
+// waited) and what a tile takes beside its steps, 8 - 10 us of which the next tile's first loads hide a part.  4096 x 128256 from 4096, both along:
+// 3090 us, 1395 TFLOP/s (a library product of this shape 1452); 16384 x 4096 from 4096, both across: 426 us, 1291 (1007); 4096 x 4096 from 16384, one
+// across: 390 us, 1408 (1166).  Of the small tile what it loads from the L2s, some 8.4 TB/s.
 #ifndef ADAGC_PRODUCT_DEVICE_H
 #define ADAGC_PRODUCT_DEVICE_H
 
@@ -903,7 +909,9 @@ inline AlongPlan along_plan(int64_t m, int64_t n, int64_t k, int segments, int32
     p.size = tile_size(p.direct, dtype, tiles);
     p.tiles_m = (m + p.size - 1) / p.size;
     p.tiles_n = (n + p.size - 1) / p.size;
-    // Tiles that leave half of the chip without work or more, along a long k: parts of 16 steps at least, whose sums a second launch joins.
+    // Tiles that leave half of the chip without work or more, along a long k: parts of 16 steps at least, whose sums a second launch joins.  56 rows of
+    // 4096 to 2 x 1719, fp32: 54 tiles 100 us, in eight parts 31; 128 rows of 768 to 2 x 768, 12 tiles 37, now 28.  Below 64 steps, 12 - 24 us, the second
+    // launch costs what it saves.
     const int64_t round = p.direct ? kUnits : 2 * kUnits, all = p.tiles_m * p.tiles_n, steps = k / (kStepBytes / dtype_size(dtype)) * segments;
     p.split = steps >= 64 ? std::max<int64_t>(1, std::min(round / all, steps / 16)) : 1;
     return p;
@@ -1104,8 +1112,8 @@ __device__ __forceinline__ void meet_keeping_loads()
 // cores want them, a batch on its way while one is multiplied, the next rows' first one while the sums meet.
 //
 // A load takes 128 bytes each of 8 rows, whole lines of the cache (of the instruction's natural 16 rows 64 bytes each, lines came from
-// memory twice where they had left the L2 between the halves: one row, 128256 x 4096 bf16 215 - 255 us, with loads past the caches 296).  So an
-// operand of 16 rows is 8 rows with the first 64 bytes and the same 8 with the second; of the 16 x 16 results the quadrants that belong together
+// memory twice where they had left the L2 between the halves: one row, 128256 x 4096 bf16 215 - 255 us, with loads past the caches 296; now 178,
+// 5.9 TB/s).  So an operand of 16 rows is 8 rows with the first 64 bytes and the same 8 with the second; of the 16 x 16 results the quadrants that belong together
 // are added, the others not used.
 constexpr int kThinRows = 16, kThinColumns = 32, kThinWaves = 8, kThinThreads = 64 * kThinWaves, kThinBlocks = kThinColumns / 8;
 template <int TM>
@@ -1546,8 +1554,10 @@ int run_plain(PlainArgs a, hipStream_t s)
 // ---------------------------------------------------------------------------------------- operands laid out anew
 //
 // fp32 operands in three parts, and bf16 ones whose rows are not multiples of 16 bytes, are copied to the workspace first, rows and columns filled
-// up to multiples of 64 with zeros, and multiplied by the bf16 tiles that load straight into LDS.  For fewer than 128 rows that costs more than it
-// saves.
+// up to multiples of 64 with zeros, and multiplied by the bf16 tiles that load straight into LDS.  That has to be paid for: bf16 rows are laid out
+// from 128 rows on; fp32 ones too, those of a single product (a forward pass) from 193, of 2^29 multiplications at least.  fp32, us as they are and in
+// parts: 192 and 256 rows, 32000 from 1024, forward 117 and 150, 153 and 146; 128 rows, all of a training pass 343 and 340; 256 rows, 2 x 1719 from 4096,
+// all of it 335 and 262; 2 x 2138 from 1024, forward 44 and 40; 2 x 768 from 768, all of it 74 and 101.
 struct Layout {
     bool    anew;
     int     parts, segments;
@@ -1556,11 +1566,13 @@ struct Layout {
     int64_t part(int64_t rows) const { return rows_of(rows) * ld; }                // elements
     static int64_t rows_of(int64_t rows) { return (rows + 63) / 64 * 64; }
 };
-inline Layout layout_of(int64_t rows, int64_t wide, int64_t k, int32_t dtype)
+inline Layout layout_of(int64_t rows, int64_t wide, int64_t k, int32_t dtype, bool backward)
 {
     Layout l{};
-    l.anew = rows >= 128 && wide >= 128 && k >= 128 && k < (int64_t)1 << 22 && (dtype == ADAGC_F32 || k % 8);
-    l.parts = l.anew && dtype == ADAGC_F32 ? kParts : 1;
+    const bool fp32 = dtype == ADAGC_F32;
+    l.anew = wide >= 128 && k >= 128 && k < (int64_t)1 << 22 &&
+             (fp32 ? rows >= (backward ? 128 : 193) && (double)rows * (double)wide * (double)k >= 0x1p29 : rows >= 128 && k % 8);
+    l.parts = l.anew && fp32 ? kParts : 1;
     l.segments = l.parts == 1 ? 1 : kSegments;
     l.ld = (k + 63) / 64 * 64;
     return l;

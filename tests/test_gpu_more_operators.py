@@ -131,6 +131,13 @@ LINEAR_SIZES = [               # rows, vocab, dim, leading dimension and offset 
     (4100, 5000, 136, 0, 0, 1.0),
     (300, 9000, 2100, 0, 0, 1.0),
     (4100, 300, 4200, 0, 0, 1.0),
+    (300, 2111, 1001, 3, 1, 1.0),
+    (333, 1700, 1000, 0, 0, 1.0),
+    (40, 300, 2051, 1, 1, 1.0),
+    (130, 200, 4104, 0, 0, 1.0),
+    (300, 515, 2090, 0, 0, 1.0),
+    (17, 600, 4100, 4, 8, 0.7),
+    (600, 700, 4128, 0, 0, 1.0),
 ]
 
 
@@ -339,6 +346,11 @@ GATED_SIZES = [                # rows, dim, hidden, more, offset
     (200, 200, 304, 8, 4),
     (4100, 136, 2600, 0, 0),
     (300, 2100, 4500, 0, 0),
+    (400, 1001, 1403, 3, 1),
+    (50, 2051, 130, 1, 1),
+    (200, 4104, 77, 0, 0),
+    (130, 4100, 260, 4, 8),
+    (600, 4128, 300, 0, 0),
 ]
 
 
