@@ -269,7 +269,7 @@ Work work_of(int64_t rows, int64_t dim, int64_t hidden, int32_t dtype, bool back
     const int64_t columns = w.layout.anew ? (dim + 7) / 8 * 8 : dim;
     const int64_t k = w.layout.anew ? w.layout.ld : dim;
     for (const bool aligned : {false, true})
-        if (rows > kThinRows) w.along = std::max(w.along, along_plan(rows, 2 * hidden, k, w.layout.segments, type, aligned, k, k).workspace());
+        if (rows > 8) w.along = std::max(w.along, along_plan(rows, 2 * hidden, k, w.layout.segments, type, aligned, k, k).workspace());
     w.partial = w.along;
     for (const bool aligned : {false, true})
         w.partial = std::max({w.partial, plain_plan((hidden + 7) / 8 * 8, columns, w.rows, type, true, w.ld, columns, w.layout.segments, 2, aligned).workspace(),
@@ -326,12 +326,16 @@ int projections(GatedArgs a, hipStream_t s)
         }
     }
     if constexpr (sizeof(T) == sizeof(O)) {
-        if (!p.direct && p.split > 1) {
-            launch_parts<Staged<T>, T, true>(a.p, s);
-            gated_kernel<Staged<T>, T, O, BACKWARD, 1, Sum::kJoined><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
-        } else if (!p.direct) {
-            gated_kernel<Staged<T>, T, O, BACKWARD, 1, Sum::kWhole><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
-        }
+        if (!p.direct)
+            staged_tile<T>(p, [&](auto tile) {
+                using S = decltype(tile);
+                if (p.split > 1) {
+                    launch_parts<S, T, true>(a.p, s);
+                    gated_kernel<S, T, O, BACKWARD, 1, Sum::kJoined><<<grid, dim3(S::kThreads), 0, s>>>(a);
+                } else {
+                    gated_kernel<S, T, O, BACKWARD, 1, Sum::kWhole><<<grid, dim3(S::kThreads), 0, s>>>(a);
+                }
+            });
     }
     return launched();
 }

@@ -337,7 +337,7 @@ Work work_of(int64_t rows, int64_t vocab, int64_t dim, int32_t dtype, bool backw
     const int64_t k_along = w.layout.anew ? w.layout.ld : dim;
     for (const int64_t n : {w.size, vocab - (w.number - 1) * w.size})
         for (const bool aligned : {false, true}) {
-            if (rows <= kThinRows) continue;
+            if (rows <= 8) continue;
             const AlongPlan p = along_plan(rows, n, k_along, w.layout.segments, type, aligned, k_along, k_along);
             w.partial = std::max(w.partial, p.workspace());
             if (const int64_t columns = columns_of_whole_rounds(p, rows, n))
@@ -442,12 +442,16 @@ int stats_of(StatsArgs a, int64_t* tiles, hipStream_t s)
             stats_kernel<Small, T, Sum::kWhole><<<small, dim3(Small::kThreads), 0, s>>>(a);
         }
     }
-    if (!p.direct && p.split > 1) {
-        launch_parts<Staged<T>, T, false>(a.p, s);
-        stats_kernel<Staged<T>, T, Sum::kJoined><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
-    } else if (!p.direct) {
-        stats_kernel<Staged<T>, T, Sum::kWhole><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
-    }
+    if (!p.direct)
+        staged_tile<T>(p, [&](auto tile) {
+            using S = decltype(tile);
+            if (p.split > 1) {
+                launch_parts<S, T, false>(a.p, s);
+                stats_kernel<S, T, Sum::kJoined><<<grid, dim3(S::kThreads), 0, s>>>(a);
+            } else {
+                stats_kernel<S, T, Sum::kWhole><<<grid, dim3(S::kThreads), 0, s>>>(a);
+            }
+        });
     return launched();
 }
 
@@ -500,12 +504,16 @@ int gradient(GradArgs a, int parts, hipStream_t s)
         if (parts > 1) direct_ones(std::integral_constant<int, kParts>{});
         else direct_ones(std::integral_constant<int, 1>{});
     }
-    if (!p.direct && p.split > 1) {
-        launch_parts<Staged<T>, T, false>(a.p, s);
-        grad_kernel<Staged<T>, T, 1, Sum::kJoined><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
-    } else if (!p.direct) {
-        grad_kernel<Staged<T>, T, 1, Sum::kWhole><<<grid, dim3(Staged<T>::kThreads), 0, s>>>(a);
-    }
+    if (!p.direct)
+        staged_tile<T>(p, [&](auto tile) {
+            using S = decltype(tile);
+            if (p.split > 1) {
+                launch_parts<S, T, false>(a.p, s);
+                grad_kernel<S, T, 1, Sum::kJoined><<<grid, dim3(S::kThreads), 0, s>>>(a);
+            } else {
+                grad_kernel<S, T, 1, Sum::kWhole><<<grid, dim3(S::kThreads), 0, s>>>(a);
+            }
+        });
     return launched();
 }
 

@@ -13,6 +13,8 @@ template void launch_parts<Small, uint16_t, false>(const AlongArgs&, hipStream_t
 template void launch_parts<Small, uint16_t, true>(const AlongArgs&, hipStream_t);
 template void launch_parts<Staged<uint16_t>, uint16_t, false>(const AlongArgs&, hipStream_t);
 template void launch_parts<Staged<uint16_t>, uint16_t, true>(const AlongArgs&, hipStream_t);
+template void launch_parts<Slim, float, false>(const AlongArgs&, hipStream_t);
+template void launch_parts<Slim, float, true>(const AlongArgs&, hipStream_t);
 template void launch_parts<Staged<float>, float, false>(const AlongArgs&, hipStream_t);
 template void launch_parts<Staged<float>, float, true>(const AlongArgs&, hipStream_t);
 }  // namespace product

@@ -850,6 +850,27 @@ __device__ __forceinline__ f32x4_p load4(const uint16_t* p)
     return f32x4_p{__uint_as_float(two[0] << 16), __uint_as_float(two[0] & 0xFFFF0000u), __uint_as_float(two[1] << 16), __uint_as_float(two[1] & 0xFFFF0000u)};
 }
 
+// Two blocks' four consecutive results each, of blocks next to each other, `to`: of the lane's first column of the first.  bf16: lanes 16 apart exchange
+// halves, so that a lane stores eight consecutive ones.
+__device__ __forceinline__ void store_blocks(float* to, const f32x4_p& a, const f32x4_p& b)
+{
+    store4(to, a);
+    store4(to + 16, b);
+}
+__device__ __forceinline__ void store_blocks(uint16_t* to, const f32x4_p& a, const f32x4_p& b)
+{
+    uint32_t w[2][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const f32x2_t two = {a[2 * h], a[2 * h + 1]}, other = {b[2 * h], b[2 * h + 1]};
+        const auto swapped = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, __builtin_convertvector(two, bf16x2_t)),
+                                                              __builtin_bit_cast(uint32_t, __builtin_convertvector(other, bf16x2_t)), false, false);
+        w[0][h] = swapped[0];
+        w[1][h] = swapped[1];
+    }
+    store_whole(to + (threadIdx.x / 16 % 2 ? 12 : 0), {u32x4{w[0][0], w[0][1], w[1][0], w[1][1]}});
+}
+
 // Four consecutive results from column `col` of a row that ends at `end` on; those before `least` are left as they are.
 template <class T>
 __device__ __forceinline__ void store4(T* row, int64_t col, int64_t least, int64_t end, const f32x4_p& v)
@@ -883,6 +904,7 @@ __device__ __forceinline__ f32x4_p load4(const T* row, int64_t col, int64_t leas
 using Large = Tile<uint16_t, 256, 256, 2, 4, 5>;
 using Small = Tile<uint16_t, 128, 128, 2, 4, 10>;
 template <class T> using Staged = Tile<T, sizeof(T) == 4 ? 64 : 128, sizeof(T) == 4 ? 64 : 128, 2, 2, 0>;
+using Slim = Tile<float, 32, 64, 1, 2, 0>;         // up to 32 rows
 
 // Rows of an operand start at multiples of 16 bytes.
 inline bool rows_aligned(const void* p, int64_t ld, int32_t dtype) { return !misaligned(p, 16) && ld * dtype_size(dtype) % 16 == 0; }
@@ -890,10 +912,10 @@ inline bool rows_aligned(const void* p, int64_t ld, int32_t dtype) { return !mis
 
 // Tiles for a product of rows along k; n: of both matrices where there are two.
 struct AlongPlan {
-    int     size;                 // 256, 128 or 64
+    int     size, rows;           // columns: 256, 128 or 64; rows: as many, or 32
     bool    direct;
     int64_t tiles_m, tiles_n, split;       // split: workgroups that share a tile's k
-    int64_t workspace() const { return split > 1 ? tiles_m * tiles_n * split * size * size * 4 : 0; }
+    int64_t workspace() const { return split > 1 ? tiles_m * tiles_n * split * rows * size * 4 : 0; }
 };
 // fp32 as it is: the matrix cores' rate is a sixteenth, which staging and a small tile keep up with.
 template <class F>
@@ -907,12 +929,13 @@ inline AlongPlan along_plan(int64_t m, int64_t n, int64_t k, int segments, int32
     auto tiles = [&](int64_t size) { return ((m + size - 1) / size) * ((n + size - 1) / size); };
     p.direct = aligned && dtype == ADAGC_BF16 && ld_y < (int64_t)1 << 23 && ld_x < (int64_t)1 << 23;          // 256 rows are within 32 bits
     p.size = tile_size(p.direct, dtype, tiles);
-    p.tiles_m = (m + p.size - 1) / p.size;
+    p.rows = p.size == 64 && m <= Slim::BM ? Slim::BM : p.size;
+    p.tiles_m = (m + p.rows - 1) / p.rows;
     p.tiles_n = (n + p.size - 1) / p.size;
     // Tiles that leave half of the chip without work or more, along a long k: parts of 16 steps at least, whose sums a second launch joins.  56 rows of
     // 4096 to 2 x 1719, fp32: 54 tiles 100 us, in eight parts 31; 128 rows of 768 to 2 x 768, 12 tiles 37, now 28.  Below 64 steps, 12 - 24 us, the second
     // launch costs what it saves.
-    const int64_t round = p.direct ? kUnits : 2 * kUnits, all = p.tiles_m * p.tiles_n, steps = k / (kStepBytes / dtype_size(dtype)) * segments;
+    const int64_t round = p.direct ? kUnits : p.rows == 32 ? 6 * kUnits : 2 * kUnits, all = p.tiles_m * p.tiles_n, steps = k / (kStepBytes / dtype_size(dtype)) * segments;
     p.split = steps >= 64 ? std::max<int64_t>(1, std::min(round / all, steps / 16)) : 1;
     return p;
 }
@@ -1237,7 +1260,12 @@ __device__ __forceinline__ void thin_tiles(const AlongArgs& a, uint8_t* lds, Bef
     }
 }
 
-inline bool thin(const AlongArgs& a, int32_t dtype) { return a.m <= kThinRows && a.k >= 16 / dtype_size(dtype); }
+inline bool thin(const AlongArgs& a, int32_t dtype)
+{
+    // fp32, more than 8 rows: 128256 x 4096 from 10 rows 545 us, 32 x 64-tiles 433; 32000 x 1024 from 12 rows 44 and 52
+    if (dtype == ADAGC_F32 && a.m > 8 && a.n * a.k >= (int64_t)1 << 28) return false;
+    return a.m <= kThinRows && a.k >= 16 / dtype_size(dtype);
+}
 
 // f(integral_constant blocks of 8 rows) for up to kThinRows rows
 template <class F>
@@ -1383,13 +1411,14 @@ __global__ __launch_bounds__(S::kThreads, 2) void plain_kernel(const PlainArgs a
 #pragma unroll
                 for (int n = 0; n < S::kTN; ++n) old[n] = load4(from + m * 16 * ld_add + n * 16);
 #pragma unroll
-                for (int n = 0; n < S::kTN; ++n) store4(to + m * 16 * ld + n * 16, acc[m][n] * a.factor + old[n]);
+                for (int n = 0; n < S::kTN; n += 2)
+                    store_blocks(to + m * 16 * ld + n * 16, acc[m][n] * a.factor + old[n], acc[m][n + 1] * a.factor + old[n + 1]);
             }
         } else {
 #pragma unroll
             for (int m = 0; m < S::kTM; ++m)
 #pragma unroll
-                for (int n = 0; n < S::kTN; ++n) store4(to + m * 16 * ld + n * 16, acc[m][n] * a.factor);
+                for (int n = 0; n < S::kTN; n += 2) store_blocks(to + m * 16 * ld + n * 16, acc[m][n] * a.factor, acc[m][n + 1] * a.factor);
         }
     };
     auto finish = [&](const Place& p) __attribute__((always_inline)) {
@@ -1642,6 +1671,16 @@ int lay(const LaySource* sources, int number, int64_t cols, const Layout& l, hip
     return hipGetLastError() == hipSuccess ? ADAGC_OK : ADAGC_ERR_HIP;
 }
 
+// f(the tile of operands staged through registers)
+template <class T, class F>
+inline void staged_tile(const AlongPlan& p, F&& f)
+{
+    if constexpr (sizeof(T) == 4) {
+        if (p.rows == Slim::BM) return f(Slim{});
+    }
+    f(Staged<T>{});
+}
+
 // instantiated in product.hip
 extern template int run_plain<float, false>(PlainArgs, hipStream_t);
 extern template int run_plain<float, true>(PlainArgs, hipStream_t);
@@ -1653,6 +1692,8 @@ extern template void launch_parts<Small, uint16_t, false>(const AlongArgs&, hipS
 extern template void launch_parts<Small, uint16_t, true>(const AlongArgs&, hipStream_t);
 extern template void launch_parts<Staged<uint16_t>, uint16_t, false>(const AlongArgs&, hipStream_t);
 extern template void launch_parts<Staged<uint16_t>, uint16_t, true>(const AlongArgs&, hipStream_t);
+extern template void launch_parts<Slim, float, false>(const AlongArgs&, hipStream_t);
+extern template void launch_parts<Slim, float, true>(const AlongArgs&, hipStream_t);
 extern template void launch_parts<Staged<float>, float, false>(const AlongArgs&, hipStream_t);
 extern template void launch_parts<Staged<float>, float, true>(const AlongArgs&, hipStream_t);
 
