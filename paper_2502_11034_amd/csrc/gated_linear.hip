@@ -106,24 +106,32 @@ __global__ __launch_bounds__(S::kThreads, 2) void gated_kernel(const GatedArgs a
             O* out = static_cast<O*>(a.out) + row0 * a.ld_out + col0;
             O *gate = static_cast<O*>(a.gate) + row0 * a.ld_gate + col0, *up = static_cast<O*>(a.up) + row0 * a.ld_up + col0;
             const O* d_out = static_cast<const O*>(a.d_out) + row0 * a.ld_d_out + col0;
+            // blocks of the same array at a time: two where a wave has two, stored together
+            constexpr int kOf = S::kTN % 4 == 0 ? 2 : 1;
+            auto store = [](O* to, const f32x4_p (&v)[kOf]) __attribute__((always_inline)) {
+                if constexpr (kOf == 2) store_blocks(to, v[0], v[1]);
+                else store4(to, v[0]);
+            };
 #pragma unroll
             for (int m = 0; m < S::kTM; ++m)
 #pragma unroll
-                for (int n = 0; n < S::kTN; n += 2) {
-                    f32x4_p o;
-                    if constexpr (BACKWARD) {
-                        f32x4_p dg, du;
-                        gradients(m, n, load4(d_out + m * 16 * a.ld_d_out + n * 8), o, dg, du);
-                        store4(gate + m * 16 * a.ld_gate + n * 8, dg);
-                        store4(up + m * 16 * a.ld_up + n * 8, du);
-                    } else {
-                        results(m, n, o);
-                        if (a.gate) {
-                            store4(gate + m * 16 * a.ld_gate + n * 8, acc[m][n]);
-                            store4(up + m * 16 * a.ld_up + n * 8, acc[m][n + 1]);
+                for (int n = 0; n < S::kTN; n += 2 * kOf) {
+                    f32x4_p o[kOf], first[kOf], second[kOf];
+#pragma unroll
+                    for (int i = 0; i < kOf; ++i) {
+                        if constexpr (BACKWARD) {
+                            gradients(m, n + 2 * i, load4(d_out + m * 16 * a.ld_d_out + (n + 2 * i) * 8), o[i], first[i], second[i]);
+                        } else {
+                            results(m, n + 2 * i, o[i]);
+                            first[i] = acc[m][n + 2 * i];
+                            second[i] = acc[m][n + 2 * i + 1];
                         }
                     }
-                    if (!BACKWARD || a.out) store4(out + m * 16 * a.ld_out + n * 8, o);
+                    if (BACKWARD || a.gate) {
+                        store(gate + m * 16 * a.ld_gate + n * 8, first);
+                        store(up + m * 16 * a.ld_up + n * 8, second);
+                    }
+                    if (!BACKWARD || a.out) store(out + m * 16 * a.ld_out + n * 8, o);
                 }
             return;
         }

@@ -230,18 +230,24 @@ __global__ __launch_bounds__(S::kThreads, 2) void grad_kernel(const GradArgs a)
             const int64_t row = m0 + at.row + m * 16;
             if (row >= (PARTS == 1 ? a.p.m : a.rows)) continue;
             T* to = static_cast<T*>(a.d_logits) + row * a.ld + n0 + at.col;
-#pragma unroll
-            for (int n = 0; n < S::kTN; ++n) {
-                if (PARTS > 1 && n0 + at.col + n * 16 >= a.ld) continue;
+            auto gradients = [&](int n) __attribute__((always_inline)) {
                 f32x4_p v;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float p = __builtin_amdgcn_exp2f((acc[m][n][r] - most[m]) * c - log2_sum[m]);
                     v[r] = d[m] == 0.f ? 0.f : ((target[m] == n * 16 + r ? 1.f : 0.f) - p) * d[m];
                 }
-                if constexpr (PARTS == 1) {
-                    store4(to + n * 16, v);        // (columns past the piece's end are within ld, and not read)
-                } else {
+                return v;
+            };
+            if constexpr (PARTS == 1) {
+                // (columns past the piece's end are within ld, and not read)
+#pragma unroll
+                for (int n = 0; n < S::kTN; n += 2) store_blocks(to + n * 16, gradients(n), gradients(n + 1));
+            } else {
+#pragma unroll
+                for (int n = 0; n < S::kTN; ++n) {
+                    if (n0 + at.col + n * 16 >= a.ld) continue;
+                    f32x4_p v = gradients(n);
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
                         if (row >= a.p.m || n0 + at.col + n * 16 + r >= a.p.n) v[r] = 0.f;
