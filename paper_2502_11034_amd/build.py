@@ -1,6 +1,8 @@
 """Build libadagc.so for gfx950 with hipcc, in-tree (next to this file)."""
+import concurrent.futures
 import os
 import subprocess
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -12,6 +14,9 @@ SOURCES = ["api.cpp", "segment_table.cpp", "kernels.hip", "static_step.hip", "mu
 HEADERS = [os.path.join(ROOT, "include", "adagc.h"), os.path.join(CSRC, "adagc_internal.h"), os.path.join(CSRC, "adagc_device.h"), os.path.join(CSRC, "muon_internal.h"),
            os.path.join(CSRC, "muon_plan.h"), os.path.join(CSRC, "walk_lines.h"), os.path.join(CSRC, "operators_internal.h"),
            os.path.join(CSRC, "act8_device.h"), os.path.join(CSRC, "product_device.h")]
+
+
+JOBS = 8                       # compilers at a time
 
 
 def hipcc():
@@ -36,23 +41,30 @@ def build(force=True, verbose=False, extra_flags=(), out=None):
     if out == LIB and not force and not is_stale():
         return LIB
     tmp = out + ".tmp.%d" % os.getpid()
-    cmd = [hipcc(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
-           # packed-fp32 code generation is switched off on purpose (known-bad forms on this part)
-           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-           "-Wall", "-Wextra", "-Wno-unused-parameter",
-           # an access that claims more alignment than its address has: tensors may start anywhere
-           "-Werror=align-mismatch",
-           "-I" + os.path.join(ROOT, "include"), "-I" + CSRC, "-x", "hip"]
-    cmd += list(extra_flags)
-    cmd += [os.path.join(CSRC, s) for s in SOURCES]
-    cmd += ["-o", tmp]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    noise = "is not a recognized feature for this target"
-    err = "\n".join(l for l in res.stderr.splitlines() if noise not in l)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + err)
-    if verbose and err.strip():
-        print(err)
+    flags = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
+             # packed-fp32 code generation is switched off on purpose (known-bad forms on this part)
+             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+             "-Wall", "-Wextra", "-Wno-unused-parameter",
+             # an access that claims more alignment than its address has: tensors may start anywhere
+             "-Werror=align-mismatch",
+             "-I" + os.path.join(ROOT, "include"), "-I" + CSRC] + list(extra_flags)
+
+    def run(cmd):
+        res = subprocess.run(cmd, capture_output=True, text=True)
+        noise = "is not a recognized feature for this target"
+        err = "\n".join(l for l in res.stderr.splitlines() if noise not in l)
+        if res.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + err)
+        if verbose and err.strip():
+            print(err)
+
+    with tempfile.TemporaryDirectory() as objects, concurrent.futures.ThreadPoolExecutor(min(JOBS, os.cpu_count() or 1)) as pool:
+        names = [os.path.join(objects, s + ".o") for s in SOURCES]
+        # the longest ones first
+        jobs = [pool.submit(run, [hipcc(), *flags, "-x", "hip", "-c", os.path.join(CSRC, s), "-o", o]) for s, o in reversed(list(zip(SOURCES, names)))]
+        for job in jobs:
+            job.result()
+        run([hipcc(), "--offload-arch=gfx950", "-fPIC", "-shared", *names, "-o", tmp])
     os.replace(tmp, out)
     return out
 

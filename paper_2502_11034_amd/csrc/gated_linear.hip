@@ -5,6 +5,10 @@
 // Blocks of 16 columns of the two weights' rows take turns in a tile, so that a lane holds g and u of the same places.  Backward: d_g and
 // d_u go to the workspace (bf16 with bf16 operands: they go into the matrix cores as they are), from g and u that the forward pass kept,
 // or from both products made again; from there dx, one product over both, and the two weight gradients, in one launch.
+//
+// What bounds it: the matrix cores.  8192 rows, 14336 from 4096, bf16: forward with g and u kept 1470 - 1540 us (1.25 - 1.31 PFLOP/s), d_g and d_u from
+// them 199 (5.9 TB/s), the weights' gradients 1465 - 1600, dx 1350 - 1480.  24 rows: the weights' way to the compute units, 39 us from the memory-side
+// cache, 47 from memory (5 TB/s).
 #include "product_device.h"
 
 namespace adagc {
@@ -277,7 +281,7 @@ Work work_of(int64_t rows, int64_t dim, int64_t hidden, int32_t dtype, bool back
     const int64_t columns = w.layout.anew ? (dim + 7) / 8 * 8 : dim;
     const int64_t k = w.layout.anew ? w.layout.ld : dim;
     for (const bool aligned : {false, true})
-        if (rows > 8) w.along = std::max(w.along, along_plan(rows, 2 * hidden, k, w.layout.segments, type, aligned, k, k).workspace());
+        if (!always_thin(rows, dtype)) w.along = std::max(w.along, along_plan(rows, 2 * hidden, k, w.layout.segments, type, aligned, k, k).workspace());
     w.partial = w.along;
     for (const bool aligned : {false, true})
         w.partial = std::max({w.partial, plain_plan((hidden + 7) / 8 * 8, columns, w.rows, type, true, w.ld, columns, w.layout.segments, 2, aligned).workspace(),

@@ -904,7 +904,8 @@ __device__ __forceinline__ f32x4_p load4(const T* row, int64_t col, int64_t leas
 using Large = Tile<uint16_t, 256, 256, 2, 4, 5>;
 using Small = Tile<uint16_t, 128, 128, 2, 4, 10>;
 template <class T> using Staged = Tile<T, sizeof(T) == 4 ? 64 : 128, sizeof(T) == 4 ? 64 : 128, 2, 2, 0>;
-using Slim = Tile<float, 32, 64, 1, 2, 0>;         // up to 32 rows
+// Up to 32 fp32 rows, whose matrix instructions take the time: 128256 from 29 rows of 4096 698 us in 64-tiles, 451.
+using Slim = Tile<float, 32, 64, 1, 2, 0>;
 
 // Rows of an operand start at multiples of 16 bytes.
 inline bool rows_aligned(const void* p, int64_t ld, int32_t dtype) { return !misaligned(p, 16) && ld * dtype_size(dtype) % 16 == 0; }
@@ -933,8 +934,9 @@ inline AlongPlan along_plan(int64_t m, int64_t n, int64_t k, int segments, int32
     p.tiles_m = (m + p.rows - 1) / p.rows;
     p.tiles_n = (n + p.size - 1) / p.size;
     // Tiles that leave half of the chip without work or more, along a long k: parts of 16 steps at least, whose sums a second launch joins.  56 rows of
-    // 4096 to 2 x 1719, fp32: 54 tiles 100 us, in eight parts 31; 128 rows of 768 to 2 x 768, 12 tiles 37, now 28.  Below 64 steps, 12 - 24 us, the second
-    // launch costs what it saves.
+    // 4096 to 2 x 1719, fp32: 54 tiles 100 us, in nine parts 31; 128 rows of 768 to 2 x 768, three bf16 parts, 12 tiles 37, in nine 28.  Below 64 steps, 12 - 24 us, the second
+    // launch costs what it saves.  Workgroups of 32 rows are small: six on a compute unit, 12382 x 2 from 17 rows of 4096 162 us in 387 whole tiles, 92 and
+    // 5 in three parts each.
     const int64_t round = p.direct ? kUnits : p.rows == 32 ? 6 * kUnits : 2 * kUnits, all = p.tiles_m * p.tiles_n, steps = k / (kStepBytes / dtype_size(dtype)) * segments;
     p.split = steps >= 64 ? std::max<int64_t>(1, std::min(round / all, steps / 16)) : 1;
     return p;
@@ -1260,11 +1262,12 @@ __device__ __forceinline__ void thin_tiles(const AlongArgs& a, uint8_t* lds, Bef
     }
 }
 
+// whatever the matrices (those with less than a vector along k have no parts either)
+inline bool always_thin(int64_t rows, int32_t dtype) { return rows <= (dtype == ADAGC_F32 ? 8 : kThinRows); }
+// fp32, more than 8 rows: 128256 x 4096 from 10 rows 545 us, 32 x 64-tiles 433 - 488; 32000 x 1024 from 12 rows 44 and 52
 inline bool thin(const AlongArgs& a, int32_t dtype)
 {
-    // fp32, more than 8 rows: 128256 x 4096 from 10 rows 545 us, 32 x 64-tiles 433; 32000 x 1024 from 12 rows 44 and 52
-    if (dtype == ADAGC_F32 && a.m > 8 && a.n * a.k >= (int64_t)1 << 28) return false;
-    return a.m <= kThinRows && a.k >= 16 / dtype_size(dtype);
+    return a.k >= 16 / dtype_size(dtype) && (always_thin(a.m, dtype) || (a.m <= kThinRows && a.n * a.k < (int64_t)1 << 28));
 }
 
 // f(integral_constant blocks of 8 rows) for up to kThinRows rows
