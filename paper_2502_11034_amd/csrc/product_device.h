@@ -697,22 +697,19 @@ __device__ __forceinline__ void accumulate_direct(Sums<S>& acc, SideY& sy, SideX
     __syncthreads();
 }
 
-// Operands in three parts, with a ring of ten places: all six products of a pair of steps one after the other, in an order in which each takes
-// over an operand of the one before: seven tiles loaded instead of twelve.  (The small tile's loop is bound by what it loads: with the
-// products one after the other over all of k, 192 tiles of 765 numbers 55 us, now 39.)
+// Operands in three parts, with a ring of ten places: of a pair of steps' six tiles, loaded once, all six products of the first step, then all of the
+// second, in an order in which each takes over an operand of the one before, in registers: 18 fragments read for six products instead of 36.
+// (The products one after the other over all of k, 192 tiles of 765 numbers, were bound by the loads, 55 us; a pair's products two steps each, by
+// the reads from LDS, 39, and 40 with both operands across k; now 38 and 35.)
 //
-// Of pair c the tiles come in the order y lo, x hi, y mid, x mid, y hi, x lo, x hi, tile u into place 7 c + u (mod 10), and the products are
-// tiles (0, 1), (2, 1), (2, 3), (4, 3), (4, 5), (4, 6).  Each is two steps, and the waves meet after the first one, by which what its second
-// one needs has been read: then a tile that no later product takes gives its place to the tile ten later.  What is loaded past the last pair is the
-// last pair again: every wait counts the same loads.
+// Tile u of pair c, in the order y lo, x hi, y mid, x mid, y hi, x lo, is in place 6 c + u (mod 10), and gives it to the tile ten later.  Step k of six
+// multiplies (y lo, x hi), (y mid, x hi), (y mid, x mid), (y hi, x mid), (y hi, x lo), (y hi, x hi); what the next one needs is read meanwhile.  Waves
+// meet three times in a pair's twelve steps: after step 5, when y lo and x hi have been read for the last time, their places are loaded, with y hi and x lo of
+// the next pair; after step 9 the other four, with the first four tiles of the pair after it; the first time after step 1, when this pair's y hi and x lo
+// have to be there, six steps after their loads.  What is loaded past the last pair is the last pair again: every wait counts the same loads.
 struct PartsOrder {
-    static constexpr int y[kSegments] = {0, 2, 2, 4, 4, 4}, x[kSegments] = {1, 1, 3, 3, 5, 6};        // tiles of a product
-    static constexpr int part[7] = {2, 0, 1, 1, 0, 2, 0};                                             // of a tile
-    static constexpr bool is_y[7] = {true, false, true, false, true, false, false};
-    // in step 2 s + second of a pair's twelve: the tile (of the next pair, the first one of the one after it) to load, or -1
-    static constexpr int load[2 * kSegments] = {1, 2, 3, 4, -1, 5, -1, 6, -1, -1, -1, 7};
-    // tiles loaded since the one that the product after s needs, when the waves meet in s
-    static constexpr int since[kSegments] = {6, 7, 7, 7, 7, 5};
+    static constexpr int part[6] = {2, 0, 1, 1, 0, 2};                     // of a tile
+    static constexpr bool is_y[6] = {true, false, true, false, true, false};
 };
 template <class S, int TILE, class SideY, class SideX>
 __device__ __forceinline__ void load_tile(const SideY& sy, const SideX& sx, int d, uint32_t lds_at)
@@ -727,13 +724,16 @@ __device__ __forceinline__ void load_tile(const SideY& sy, const SideX& sx, int 
         for (int u = 0; u < S::kXLoads; ++u) sx.load_part(from, u, lds_at);
     }
 }
+// (the last place of the ring is left free)
 template <class S, class SideY, class SideX>
 __device__ __forceinline__ void start_parts(const SideY& sy, const SideX& sx, uint32_t lds0, int pairs)
 {
     if (pairs <= 0) return;
     const uint32_t lds_wave = lds0 + (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * 1024u;
-    each<7>([&](auto TILE) __attribute__((always_inline)) { load_tile<S, decltype(TILE)::value>(sy, sx, 0, lds_wave + decltype(TILE)::value * S::kPlace); });
-    load_tile<S, 0>(sy, sx, min(1, pairs - 1), lds_wave + 7 * S::kPlace);
+    each<9>([&](auto I) __attribute__((always_inline)) {
+        constexpr int i = decltype(I)::value;
+        load_tile<S, i % 6>(sy, sx, min(i / 6, pairs - 1), lds_wave + i * S::kPlace);
+    });
 }
 template <class S, class T, class SideY, class SideX>
 __device__ __forceinline__ void accumulate_parts(Sums<S>& acc, const SideY& sy, const SideX& sx, uint32_t lds0, int pairs)
@@ -743,50 +743,62 @@ __device__ __forceinline__ void accumulate_parts(Sums<S>& acc, const SideY& sy, 
     if (pairs <= 0) return;
     const uint32_t lds_wave = lds0 + (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * 1024u;
     auto meet = []() __attribute__((always_inline)) {
+        ADAGC_P_WAIT_LDS(0);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         ADAGC_P_FENCE();
     };
     int base = 0;                                  // the place of the pair's first tile
-    auto place = [&](int u) __attribute__((always_inline)) { return (uint32_t)((base + u >= 20 ? base + u - 20 : base + u >= 10 ? base + u - 10 : base + u) * S::kPlace); };
-    u32x4 y[2][kTM], x[2][kTN];
-    ADAGC_P_WAIT_VMEM(6 * kLoads);                 // all but six of eight tiles
+    auto place = [&](int u) __attribute__((always_inline)) { return (uint32_t)((base + u >= 10 ? base + u - 10 : base + u) * S::kPlace); };
+    u32x4 y[2][kTM], x_hi[2][kTN], x[2][kTN];      // x: mid, lo
+    ADAGC_P_WAIT_VMEM(5 * kLoads);                 // four of nine tiles
     meet();
+    load_tile<S, 3>(sy, sx, min(1, pairs - 1), lds_wave + 9 * S::kPlace);
 #pragma unroll
-    for (int n = 0; n < kTN; ++n) x[0][n] = sx.read(n, S::kPlace);
+    for (int n = 0; n < kTN; ++n) x_hi[0][n] = sx.read(n, S::kPlace);
 #pragma unroll
     for (int m = 0; m < kTM; ++m) y[0][m] = sy.read(m, 0);
     for (int d = 0; d < pairs; ++d) {
-        each<2 * kSegments>([&](auto STEP) __attribute__((always_inline)) {
-            constexpr int step = decltype(STEP)::value, s = step / 2, second = step % 2, kSlots = kTM * kTN, kReads = kTM + kTN;
-            // of the step that is read: this product's second one, or the next product's first
-            constexpr int next = second ? (s + 1) % kSegments : s, later = second && s + 1 == kSegments ? 7 : 0;
-            const uint32_t from_y = place(PartsOrder::y[next] + later), from_x = place(PartsOrder::x[next] + later);
-            constexpr int tile = PartsOrder::load[step];
+        each<12>([&](auto STEP) __attribute__((always_inline)) {
+            constexpr int step = decltype(STEP)::value, second = step / 6, k = step % 6, kSlots = kTM * kTN;
+            constexpr int of_y = (k == 0 ? 0 : k < 3 ? 1 : 0) ^ second;                         // the set of y that is multiplied; the other one is read to
+            constexpr bool reads_y = k % 2 == 0 ? k < 4 : k == 5, reads_x = k % 2 == 1;
+            constexpr int next_second = k == 5 ? second ^ 1 : second;
+            const uint32_t from_y = place(k == 0 ? 2 : k == 2 ? 4 : second ? 6 : 0), from_x = place(k == 1 ? 3 : k == 3 ? 5 : second ? 7 : 1);
             each<kSlots>([&](auto SLOT) __attribute__((always_inline)) {
                 constexpr int slot = decltype(SLOT)::value, m = slot / kTN, n = slot % kTN;
-                multiply<T>(x[second][n], y[second][m], acc[m][n]);
+                multiply<T>(k == 2 || k == 3 ? x[0][n] : k == 4 ? x[1][n] : x_hi[second][n], y[of_y][m], acc[m][n]);
                 ADAGC_P_FENCE();
+                constexpr int kReads = (reads_x ? kTN : 0) + (reads_y ? kTM : 0);
                 each<kReads>([&](auto R) __attribute__((always_inline)) {
                     constexpr int r = decltype(R)::value;
                     if constexpr (r * (kSlots / 2) / kReads == slot) {
-                        if constexpr (r < kTN) x[second ^ 1][r] = sx.read(r, from_x, !second);
-                        else y[second ^ 1][r - kTN] = sy.read(r - kTN, from_y, !second);
+                        if constexpr (reads_x && r < kTN) {
+                            if constexpr (k == 5) x_hi[second ^ 1][r] = sx.read(r, from_x, next_second);
+                            else x[k / 2][r] = sx.read(r, from_x, next_second);
+                        } else {
+                            constexpr int block = reads_x ? r - kTN : r;
+                            y[of_y ^ 1][block] = sy.read(block, from_y, next_second);
+                        }
                     }
                 });
-                if constexpr (tile >= 0 && slot == kSlots / 2) {
-                    // tile `tile` of the next pair, or the first one of the pair after it, ten after the one whose place it takes
-                    load_tile<S, tile % 7>(sy, sx, min(d + 1 + tile / 7, pairs - 1), lds_wave + place(tile + 7));
+                if constexpr (slot == kSlots / 2) {
+                    if constexpr (step == 6) load_tile<S, 4>(sy, sx, min(d + 1, pairs - 1), lds_wave + place(0));
+                    if constexpr (step == 7) load_tile<S, 5>(sy, sx, min(d + 1, pairs - 1), lds_wave + place(1));
+                    if constexpr (step == 10) load_tile<S, 0>(sy, sx, min(d + 2, pairs - 1), lds_wave + place(2));
+                    if constexpr (step == 11) load_tile<S, 2>(sy, sx, min(d + 2, pairs - 1), lds_wave + place(4));
+                }
+                if constexpr (slot == kSlots - 1) {
+                    if constexpr (step == 10) load_tile<S, 1>(sy, sx, min(d + 2, pairs - 1), lds_wave + place(3));
+                    if constexpr (step == 11) load_tile<S, 3>(sy, sx, min(d + 2, pairs - 1), lds_wave + place(5));
                 }
                 ADAGC_P_FENCE();
             });
-            if constexpr (!second) {
-                ADAGC_P_WAIT_VMEM(PartsOrder::since[s] * kLoads);
-                ADAGC_P_WAIT_LDS(0);
-                meet();
-            }
+            if constexpr (step == 1) ADAGC_P_WAIT_VMEM(4 * kLoads);        // y hi and x lo of this pair
+            if constexpr (step == 9) ADAGC_P_WAIT_VMEM(2 * kLoads);        // the first four tiles of the next one
+            if constexpr (step == 1 || step == 5 || step == 9) meet();
         });
-        base = base + 7 >= 10 ? base - 3 : base + 7;
+        base = base + 6 >= 10 ? base - 4 : base + 6;
     }
     ADAGC_P_WAIT_VMEM(0);
     __syncthreads();
