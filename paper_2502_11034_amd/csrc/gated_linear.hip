@@ -329,7 +329,8 @@ int projections(GatedArgs a, hipStream_t s)
     if constexpr (sizeof(T) == 2) {
         constexpr int kOf = BACKWARD && sizeof(O) == 4 ? kParts : 1;       // (fp32 data is laid out in parts)
         if (p.size == 256) {
-            gated_kernel<Large, T, O, BACKWARD, kOf, Sum::kWhole><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
+            if constexpr (sizeof(O) == 2)
+                gated_kernel<Large, T, O, BACKWARD, 1, Sum::kWhole><<<dim3(grid_of<Large>(p.tiles_m * p.tiles_n)), dim3(Large::kThreads), 0, s>>>(a);
         } else if (p.direct && p.split > 1) {
             launch_parts<Small, T, true>(a.p, s);
             gated_kernel<Small, T, O, BACKWARD, kOf, Sum::kJoined><<<grid, dim3(Small::kThreads), 0, s>>>(a);

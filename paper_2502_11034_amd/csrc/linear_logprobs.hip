@@ -500,19 +500,18 @@ int gradient(GradArgs a, int parts, hipStream_t s)
     const dim3 grid((uint32_t)(p.tiles_m * p.tiles_n));
     if constexpr (sizeof(T) == 2) {
         const dim3 large(grid_of<Large>(p.tiles_m * p.tiles_n)), small(grid_of<Small>(p.tiles_m * p.tiles_n));
-        auto direct_ones = [&](auto PARTS) {
+        auto small_ones = [&](auto PARTS) {
             constexpr int kOf = decltype(PARTS)::value;
-            if (p.size == 256) {
-                grad_kernel<Large, T, kOf, Sum::kWhole><<<large, dim3(Large::kThreads), 0, s>>>(a);
-            } else if (p.direct && p.split > 1) {
+            if (p.split > 1) {
                 launch_parts<Small, T, false>(a.p, s);
                 grad_kernel<Small, T, kOf, Sum::kJoined><<<grid, dim3(Small::kThreads), 0, s>>>(a);
-            } else if (p.direct) {
+            } else {
                 grad_kernel<Small, T, kOf, Sum::kWhole><<<small, dim3(Small::kThreads), 0, s>>>(a);
             }
         };
-        if (parts > 1) direct_ones(std::integral_constant<int, kParts>{});
-        else direct_ones(std::integral_constant<int, 1>{});
+        if (p.size == 256) grad_kernel<Large, T, 1, Sum::kWhole><<<large, dim3(Large::kThreads), 0, s>>>(a);
+        else if (p.direct && parts > 1) small_ones(std::integral_constant<int, kParts>{});
+        else if (p.direct) small_ones(std::integral_constant<int, 1>{});
     }
     if (!p.direct)
         staged_tile<T>(p, [&](auto tile) {

@@ -132,9 +132,8 @@ __device__ __forceinline__ void place_of_tile(int n, int tiles_m, int tiles_n, i
 
 // fp32 operands in three bf16 parts, hi + mid + lo, each the nearest to what the ones before it leave (8 + 8 + 8 significant bits, exact but
 // next to the type's ends): of the nine products of parts the six that count, smallest first; the others are some 2^-26 of the whole.  The
-// matrix cores' bf16 rate is 16 times the fp32 one.  Segment s takes the parts that digit s of these says; a single segment takes the last one's.
+// matrix cores' bf16 rate is 16 times the fp32 one.  Segments: products that are summed, one of operands as they are, or these.
 constexpr int kSegments = 6, kParts = 3;
-constexpr uint32_t kPartsOfY = 0x001102, kPartsOfX = 0x010120;
 
 // How one operand's tile (B rows or columns of the result) is loaded, staged in LDS and read: kUnits units of 16 bytes a step for a lane.
 //
@@ -232,11 +231,10 @@ struct Side {
     static constexpr int kLoads = 2 * kUnits, kAlong = ACROSS ? kVectors : 8;
     uint32_t off[ACROSS ? 1 : kLoads];     // bytes from the first step's address, which is the same in all lanes
     const T* base;
-    // the next pair of steps to load, of a segment's the pairs from `first` on; segments follow each other
+    // the next pair of steps to load, and the first one
     const T* at;
-    int      first, pairs, left, segment;
+    int      first;
     int64_t  part;
-    uint32_t parts_table;
 
     // Position i of row r gets vector unplaced(r, i), so that vector v is where place(r, v) says (its own inverse).
     static __device__ __forceinline__ int unplaced(int r, int i) { return (int)(place(r, i) % (uint32_t)kPitch) / 16; }
@@ -258,19 +256,12 @@ struct Side {
         const int r = tid / kAlong;
         off[0] = ((uint32_t)r * (uint32_t)ld_ + (uint32_t)unplaced(r, tid % kAlong) * kE) * (uint32_t)sizeof(T);
     }
-    __device__ __forceinline__ void to_segment()
-    {
-        at = base + (parts_table >> (4 * segment) & 15) * part + (ACROSS ? (int64_t)(first * 2 * kDeep) * ld : (int64_t)first * 2 * kDeep);
-        left = pairs;
-    }
-    __device__ __forceinline__ void set_pairs(int first_, int pairs_, int segments, int64_t part_, uint32_t table)
+    // first_: of the pairs of steps; part_: operands in parts: elements from part to part
+    __device__ __forceinline__ void set_first(int first_, int64_t part_)
     {
         first = first_;
-        pairs = pairs_;
-        segment = kSegments - segments;
         part = part_;
-        parts_table = table;
-        to_segment();
+        at = part_at(0, 0);
     }
     __device__ __forceinline__ void load_direct(int u, uint32_t lds_at) const
     {
@@ -279,14 +270,7 @@ struct Side {
         if constexpr (ACROSS) load_to_lds(at + (int64_t)(u * kRows) * ld, off[0], lds_at + (uint32_t)(u * kThreads * 16));
         else load_to_lds(at, off[u], lds_at + (uint32_t)(u * kThreads * 16));
     }
-    __device__ __forceinline__ void advance()
-    {
-        at += ACROSS ? 2 * kDeep * ld : (int64_t)(2 * kDeep);
-        if (--left == 0) {
-            ++segment;
-            to_segment();
-        }
-    }
+    __device__ __forceinline__ void advance() { at += ACROSS ? 2 * kDeep * ld : (int64_t)(2 * kDeep); }
 
     // the same for part p of operands in parts, pair of steps d from the first one on
     __device__ __forceinline__ const T* part_at(int p, int d) const
@@ -543,7 +527,7 @@ __device__ __forceinline__ void start_direct(SideY& sy, SideX& sx, uint32_t lds0
         }
 }
 
-// total: pairs of steps of all segments
+// total: pairs of steps
 template <class S, class T, class SideY, class SideX>
 __device__ __forceinline__ void accumulate_direct(Sums<S>& acc, SideY& sy, SideX& sx, uint32_t lds0, int total)
 {
@@ -701,6 +685,8 @@ __device__ __forceinline__ void accumulate_direct(Sums<S>& acc, SideY& sy, SideX
 // second, in an order in which each takes over an operand of the one before, in registers: 18 fragments read for six products instead of 36.
 // (The products one after the other over all of k, 192 tiles of 765 numbers, were bound by the loads, 55 us; a pair's products two steps each, by
 // the reads from LDS, 39, and 40 with both operands across k; now 38 and 35.)
+// The large tile's ring does not hold six tiles: with twelve loaded for six products, 597 rows, 2 x 11373 from 4096 and back took 3440 us, now 2810;
+// 300 x 128256 from 1024 906, now 756; 512 x 32000 from 1024 205, now 213.
 //
 // Tile u of pair c, in the order y lo, x hi, y mid, x mid, y hi, x lo, is in place 6 c + u (mod 10), and gives it to the tile ten later.  Step k of six
 // multiplies (y lo, x hi), (y mid, x hi), (y mid, x mid), (y hi, x mid), (y hi, x lo), (y hi, x hi); what the next one needs is read meanwhile.  Waves
@@ -804,14 +790,14 @@ __device__ __forceinline__ void accumulate_parts(Sums<S>& acc, const SideY& sy, 
     __syncthreads();
 }
 
-// The one or the other: `pairs` of steps of each segment, from the sides' first one on.
+// The one or the other: `pairs` of steps, from the sides' first one on.
 template <class S, class SideY, class SideX>
 __device__ __forceinline__ void start_products(SideY& sy, SideX& sx, uint32_t lds0, int pairs, int segments)
 {
     if constexpr (S::kRing == 10) {
         if (segments == kSegments) return start_parts<S>(sy, sx, lds0, pairs);
     }
-    start_direct<S>(sy, sx, lds0, pairs * segments);
+    start_direct<S>(sy, sx, lds0, pairs);
 }
 template <class S, class T, class SideY, class SideX>
 __device__ __forceinline__ void accumulate_products(Sums<S>& acc, SideY& sy, SideX& sx, uint32_t lds0, int pairs, int segments)
@@ -819,7 +805,7 @@ __device__ __forceinline__ void accumulate_products(Sums<S>& acc, SideY& sy, Sid
     if constexpr (S::kRing == 10) {
         if (segments == kSegments) return accumulate_parts<S, T>(acc, sy, sx, lds0, pairs);
     }
-    accumulate_direct<S, T>(acc, sy, sx, lds0, pairs * segments);
+    accumulate_direct<S, T>(acc, sy, sx, lds0, pairs);
 }
 
 // The lane's first row and column of a tile.
@@ -942,6 +928,7 @@ inline AlongPlan along_plan(int64_t m, int64_t n, int64_t k, int segments, int32
     auto tiles = [&](int64_t size) { return ((m + size - 1) / size) * ((n + size - 1) / size); };
     p.direct = aligned && dtype == ADAGC_BF16 && ld_y < (int64_t)1 << 23 && ld_x < (int64_t)1 << 23;          // 256 rows are within 32 bits
     p.size = tile_size(p.direct, dtype, tiles);
+    if (p.size == 256 && segments > 1) p.size = 128;        // parts stay in the small tile's ring; see accumulate_parts
     p.rows = p.size == 64 && m <= Slim::BM ? Slim::BM : p.size;
     p.tiles_m = (m + p.rows - 1) / p.rows;
     p.tiles_n = (n + p.size - 1) / p.size;
@@ -1025,16 +1012,16 @@ __device__ __forceinline__ void along_tiles(const AlongArgs& a, uint8_t* lds, Be
         m0 = (int64_t)tm * S::BM;
         n0 = (int64_t)tn * kColumns;
     };
-    auto aim = [&](int first, int number) __attribute__((always_inline)) {
+    auto aim = [&](int first) __attribute__((always_inline)) {
         // a load of a wave is 8 rows, and a lane's are a multiple of 32 apart: with two matrices, all of one
         static_assert(!S::kDirect || S::kThreads / 8 % 32 == 0);
         const int tid = thread_anew();
         const bool second = PAIR && (wave >> 1 & 1);
         const int64_t ld_x = second ? a.ld_x[1] : a.ld_x[0];
         sy.set_rows_direct(tid, y + m0 * a.ld_y, a.ld_y, [&](int r) { return min(m0 + r, a.m - 1) - m0; });
-        sy.set_pairs(first, number, a.segments, a.part_y, kPartsOfY);
+        sy.set_first(first, a.part_y);
         sx.set_rows_direct(tid, static_cast<const T*>(second ? a.x[1] : a.x[0]) + n0 * ld_x, ld_x, [&](int r) { return row_of_x(r) - n0; });
-        sx.set_pairs(first, number, a.segments, a.part_x, kPartsOfX);
+        sx.set_first(first, a.part_x);
     };
     if constexpr (SUM == Sum::kJoined) {
         to_tile((int)blockIdx.x);
@@ -1062,7 +1049,7 @@ __device__ __forceinline__ void along_tiles(const AlongArgs& a, uint8_t* lds, Be
                 aim_staged();
                 accumulate_rest<S, T>(acc, sy, sx, 2 * (int64_t)full, a.k, 0, 0);
             }
-            aim(first, number);
+            aim(first);
             start_products<S>(sy, sx, lds0, number, a.segments);
             accumulate_products<S, T>(acc, sy, sx, lds0, number, a.segments);
         } else {
@@ -1085,7 +1072,7 @@ __device__ __forceinline__ void along_tiles(const AlongArgs& a, uint8_t* lds, Be
         int n = (int)blockIdx.x;
         to_tile(n);
         if (!rest) {
-            aim(0, pairs);
+            aim(0);
             start_products<S>(sy, sx, lds0, pairs, a.segments);
         }
         while (true) {
@@ -1093,7 +1080,7 @@ __device__ __forceinline__ void along_tiles(const AlongArgs& a, uint8_t* lds, Be
             if (rest) {
                 aim_staged();
                 accumulate_rest<S, T>(acc, sy, sx, 2 * pairs, a.k, 0, 0);
-                aim(0, pairs);
+                aim(0);
                 start_products<S>(sy, sx, lds0, pairs, a.segments);
             }
             accumulate_products<S, T>(acc, sy, sx, lds0, pairs, a.segments);
@@ -1103,7 +1090,7 @@ __device__ __forceinline__ void along_tiles(const AlongArgs& a, uint8_t* lds, Be
             if (n < tiles) {
                 to_tile(n);
                 if (!rest) {
-                    aim(0, pairs);
+                    aim(0);
                     start_products<S>(sy, sx, lds0, pairs, a.segments);
                 }
             }
@@ -1410,8 +1397,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void plain_kernel(const PlainArgs a
         if constexpr (ACROSS_Y) sy.set_columns_direct(tid, y + p.m0, a.ld_y);
         else sy.set_rows_direct(tid, y + p.m0 * a.ld_y, a.ld_y, [&](int r) { return min(p.m0 + r, a.m - 1) - p.m0; });
         sx.set_columns_direct(tid, x_of(second) + p.n0, second ? a.ld_x[1] : a.ld_x[0]);
-        sy.set_pairs(step0, step1 - step0, a.segments, a.part_y, kPartsOfY);
-        sx.set_pairs(step0, step1 - step0, a.segments, a.part_x, kPartsOfX);
+        sy.set_first(step0, a.part_y);
+        sx.set_first(step0, a.part_x);
     };
     Sums<S> acc;
     auto finish_inside = [&](const Place& p, auto* out, const auto* add) __attribute__((always_inline)) {
@@ -1533,7 +1520,7 @@ struct PlainPlan {
     int64_t tiles_m, tiles_n, whole, rest, split;
     int64_t workspace() const { return split > 1 ? rest * split * size * size * 4 : 0; }
 };
-// m (with Y across k) and n: of the readable columns; pairs: of operands that are summed; products: side by side; aligned: the rows of both
+// m (with Y across k) and n: of the readable columns; pairs: of operands that are summed, times segments; products: side by side; aligned: the rows of both
 // operands are.  A workspace is sized for both.
 inline PlainPlan plain_plan(int64_t m, int64_t n, int64_t k, int32_t dtype, bool across_y, int64_t ld_y, int64_t ld_x, int pairs, int products, bool aligned)
 {
@@ -1546,9 +1533,9 @@ inline PlainPlan plain_plan(int64_t m, int64_t n, int64_t k, int32_t dtype, bool
     const int64_t steps = k / (kStepBytes / dtype_size(dtype)) / (p.direct ? 2 : 1) * (p.direct ? 2 : 1);
     p.size = tile_size(p.direct, dtype, tiles);
     // Few large tiles, if along k there are 64 steps for each compute unit, by which the partial sums are paid for: 4096 x 768 from 16384, 48 tiles in
-    // five parts 120 us and 17 for joining, 192 small tiles 175; 333 x 765 in parts from 8191, 36 steps each, 18 small tiles in 14 parts 33 and 4.
+    // five parts 110 - 128 us and 14 - 18 for joining, 192 small tiles 175.
     if (p.direct && p.size < 256 && steps * pairs * tiles(256) >= 64 * kUnits) p.size = 256;
-    if (p.size == 256 && (m < 256 || n < 256)) p.size = 128;
+    if (p.size == 256 && (m < 256 || n < 256 || pairs >= kSegments)) p.size = 128;
     p.checked = far || n < p.size || (across_y && m < p.size);
     p.tiles_m = (m + p.size - 1) / p.size;
     p.tiles_n = (n + p.size - 1) / p.size;
