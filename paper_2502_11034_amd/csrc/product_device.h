@@ -902,7 +902,8 @@ __device__ __forceinline__ f32x4_p load4(const T* row, int64_t col, int64_t leas
 using Large = Tile<uint16_t, 256, 256, 2, 4, 5>;
 using Small = Tile<uint16_t, 128, 128, 2, 4, 10>;
 template <class T> using Staged = Tile<T, sizeof(T) == 4 ? 64 : 128, sizeof(T) == 4 ? 64 : 128, 2, 2, 0>;
-// Up to 32 fp32 rows, whose matrix instructions take the time: 128256 from 29 rows of 4096 698 us in 64-tiles, 451.
+// Up to 32 fp32 rows, whose matrix instructions take the time: 128256 from 29 rows of 4096 698 us in 64-tiles, 451; the gradient of 17 rows of 4096 from
+// 2 x 12382 155, 124.
 using Slim = Tile<float, 32, 64, 1, 2, 0>;
 
 // Rows of an operand start at multiples of 16 bytes.
@@ -1515,10 +1516,10 @@ __global__ __launch_bounds__(S::kThreads) void plain_join_kernel(const PlainArgs
 
 // How a product is cut: tiles, and those of the last, partial round of workgroups also along k, so that they fill the chip too.
 struct PlainPlan {
-    int     size;                 // 256, 128 or 64
+    int     size, rows;           // columns: 256, 128 or 64; rows: as many, or 32
     bool    checked, direct;
     int64_t tiles_m, tiles_n, whole, rest, split;
-    int64_t workspace() const { return split > 1 ? rest * split * size * size * 4 : 0; }
+    int64_t workspace() const { return split > 1 ? rest * split * rows * size * 4 : 0; }
 };
 // m (with Y across k) and n: of the readable columns; pairs: of operands that are summed, times segments; products: side by side; aligned: the rows of both
 // operands are.  A workspace is sized for both.
@@ -1537,10 +1538,12 @@ inline PlainPlan plain_plan(int64_t m, int64_t n, int64_t k, int32_t dtype, bool
     if (p.direct && p.size < 256 && steps * pairs * tiles(256) >= 64 * kUnits) p.size = 256;
     if (p.size == 256 && (m < 256 || n < 256 || pairs >= kSegments)) p.size = 128;
     p.checked = far || n < p.size || (across_y && m < p.size);
-    p.tiles_m = (m + p.size - 1) / p.size;
+    p.rows = p.size == 64 && !across_y && m <= Slim::BM ? Slim::BM : p.size;
+    p.tiles_m = (m + p.rows - 1) / p.rows;
     p.tiles_n = (n + p.size - 1) / p.size;
-    const int64_t all = tiles(p.size);
-    const int64_t round = p.direct ? kUnits : 2 * kUnits;   // a ring fills a compute unit's LDS; the others' workgroups share a unit in pairs
+    const int64_t all = products * p.tiles_m * p.tiles_n;
+    // a ring fills a compute unit's LDS; the others' workgroups share a unit in pairs, small ones six at a time
+    const int64_t round = p.direct ? kUnits : p.rows == 32 ? 6 * kUnits : 2 * kUnits;
     p.rest = all % round;
     // a part has eight steps at least (of each pair)
     p.split = p.rest ? std::max<int64_t>(1, std::min(round / p.rest, steps * pairs / 8)) : 1;
@@ -1578,6 +1581,9 @@ int run_plain(PlainArgs a, hipStream_t s)
     if constexpr (sizeof(T) == 2) {
         if (p.size == 256) return launch_plain<Large, T, ACROSS_Y, false>(a, p, s);
         if (p.direct) return launch_plain<Small, T, ACROSS_Y, false>(a, p, s);
+    }
+    if constexpr (sizeof(T) == 4 && !ACROSS_Y) {
+        if (p.rows == Slim::BM) return p.checked ? launch_plain<Slim, T, false, true>(a, p, s) : launch_plain<Slim, T, false, false>(a, p, s);
     }
     return p.checked ? launch_plain<Staged<T>, T, ACROSS_Y, true>(a, p, s) : launch_plain<Staged<T>, T, ACROSS_Y, false>(a, p, s);
 }
