@@ -6,8 +6,8 @@
 // d_u go to the workspace (bf16 with bf16 operands: they go into the matrix cores as they are), from g and u that the forward pass kept,
 // or from both products made again; from there dx, one product over both, and the two weight gradients, in one launch.
 //
-// What bounds it: the matrix cores.  8192 rows, 14336 from 4096, bf16: forward with g and u kept 1470 - 1540 us (1.25 - 1.31 PFLOP/s), d_g and d_u from
-// them 199 (5.9 TB/s), the weights' gradients 1465 - 1600, dx 1350 - 1480.  24 rows: the weights' way to the compute units, 39 us from the memory-side
+// What bounds it: the matrix cores.  8192 rows, 14336 from 4096, bf16: forward with g and u kept 1410 - 1620 us (1.19 - 1.37 PFLOP/s), d_g and d_u from
+// them 199 (5.9 TB/s), the weights' gradients 1465 - 1660, dx 1350 - 1500.  24 rows: the weights' way to the compute units, 38 us from the memory-side
 // cache, 47 from memory (5 TB/s).
 #include "product_device.h"
 

@@ -8,8 +8,8 @@
 // summed over the pieces in fp32.
 //
 // What bounds it: the matrix cores, and of short sums what a tile takes beside them, 3 - 4 us of a 256-tile's exponentials among it.  4096 rows,
-// 128256 from 4096, bf16: forward 3090 - 3190 us and 10 for joining; a piece of 16384 columns 412 for its gradients, 426 for the weight's, 390 - 400 for
-// x's.  1024 rows, 50257 from 768, forward: 78 + 12 + 5.  One row, 128256 from 4096: 179 + 5, memory (5.9 TB/s).
+// 128256 from 4096, bf16: forward 3050 - 3240 us and 10 for joining; a piece of 16384 columns 399 - 429 for its gradients, 404 - 432 for the weight's,
+// 382 - 406 for x's.  1024 rows, 50257 from 768, forward: 77 + 11 + 5.  One row, 128256 from 4096: 179 + 5, memory (5.9 TB/s).
 #include "product_device.h"
 
 namespace adagc {

@@ -8,8 +8,8 @@
 //
 // What bounds it, bf16: of large products the power limit (a step of 32 k on a 256-tile 0.72 - 0.75 us at some 1.8 GHz, 0.55 if the matrix cores never
 // waited) and what a tile takes beside its steps, 8 - 10 us of which the next tile's first loads hide a part.  4096 x 128256 from 4096, both along:
-// 3090 us, 1395 TFLOP/s (a library product of this shape 1452); 16384 x 4096 from 4096, both across: 426 us, 1291 (1007); 4096 x 4096 from 16384, one
-// across: 390 us, 1408 (1166).  Of the small tile what it loads from the L2s, some 8.4 TB/s.
+// 3050 - 3240 us, 1330 - 1410 TFLOP/s (a library product of this shape 1452); 16384 x 4096 from 4096, both across: 404 - 432 us, 1270 - 1360 (1007);
+// 4096 x 4096 from 16384, one across: 382 - 406 us, 1350 - 1440 (1166).  Of the small tile what it loads from the L2s, some 8.4 TB/s.
 #ifndef ADAGC_PRODUCT_DEVICE_H
 #define ADAGC_PRODUCT_DEVICE_H
 
