@@ -183,6 +183,29 @@ def test_linear_logprobs_of_rounds_that_are_not_full(dtype, rows, vocab, dim):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows, wide, dim", [(40, 300, 2051), (17, 600, 4100), (300, 2111, 1001), (513, 22116, 64), (70, 300, 136), (9, 70, 33)])
+def test_nothing_is_written_beyond_a_workspace(dtype, rows, wide, dim, monkeypatch):
+    guard, spaces = 1 << 16, []
+
+    def guarded(n):
+        space = torch.full((n + guard,), 0xFF, dtype=torch.uint8, device=DEV)
+        space[n:] = 0x5A
+        spaces.append(space[n:])
+        return space[:n]
+
+    monkeypatch.setitem(globals(), "workspace", guarded)
+    dtype = TYPES[dtype]
+    x, w, t = matrix(rows, dim, dtype, 4).t, matrix(wide, dim, dtype, 5, dim ** -0.5).t, some_targets(rows, wide, 6)
+    stats = check_linear(x, w, t)
+    check_linear_backward(x, w, t, stats)
+    d_x, d_w = torch.empty_like(x.contiguous()), [torch.empty(wide, dim, device=DEV) for _ in range(2)]
+    out, gate, up = run_gated(x, w, w, kept=True)
+    run_gated_backward(out, x, w, w, d_x, *d_w)
+    run_gated_backward(out, x, w, w, d_x, *d_w, gate=gate, up=up)
+    assert all(bool((space == 0x5A).all()) for space in spaces) and len(spaces) >= 4
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows, vocab, dim", [(19, 70, 40), (140, 900, 264), (4096, 2048, 64)])
 def test_products_of_whole_numbers_are_exact(dtype, rows, vocab, dim):
     """Small whole numbers: every sum is exact, whatever its order, and a place that is missed or counted twice shows."""
