@@ -322,6 +322,13 @@ int64_t columns_of_whole_rounds(const AlongPlan& p, int64_t m, int64_t n)
     const int64_t columns = p.tiles_m * p.tiles_n / kUnits * kUnits / p.tiles_m * 256;
     return columns < n && (m + 127) / 128 * ((n - columns + 127) / 128) <= kUnits ? columns : 0;
 }
+// Columns of a piece's gradients that the weight's product may read, n or more.  Parts are multiplied by the small tile's ring alone, which wants a whole
+// tile of them: those past a shorter piece's end are 0, to the end of the tile that made them (ld is two tiles at least).
+int64_t readable_of(const Layout& l, int64_t n)
+{
+    const int64_t up = (n + 7) / 8 * 8;
+    return l.parts > 1 ? std::max<int64_t>(up, Small::BM) : up;
+}
 Work work_of(int64_t rows, int64_t vocab, int64_t dim, int32_t dtype, bool backward)
 {
     Work w{};
@@ -357,7 +364,7 @@ Work work_of(int64_t rows, int64_t vocab, int64_t dim, int32_t dtype, bool backw
     const int64_t columns = w.layout.anew ? (dim + 7) / 8 * 8 : dim;
     for (const int64_t n : {w.size, vocab - (w.number - 1) * w.size})
         for (const bool aligned : {false, true}) {
-            const int64_t readable = (n + 7) / 8 * 8, k = w.layout.parts > 1 ? Layout::rows_of(rows) : rows;
+            const int64_t readable = readable_of(w.layout, n), k = w.layout.parts > 1 ? Layout::rows_of(rows) : rows;
             w.partial = std::max({w.partial, plain_plan(readable, columns, k, type, true, w.ld, columns, w.layout.segments, 1, aligned).workspace(),
                                   plain_plan(rows, columns, w.layout.parts > 1 ? Layout::rows_of(n) : n, type, false, w.ld, columns, w.layout.segments, 1, aligned).workspace()});
         }
@@ -582,7 +589,7 @@ int backward(const Work& w, Operands o, int64_t rows, int64_t vocab, int64_t dim
             a.add[0] = out.accumulate ? a.out[0] : nullptr;
             a.ld_add[0] = out.ld_d_weight;
             a.m = n;
-            a.m_readable = (n + 7) / 8 * 8;
+            a.m_readable = readable_of(w.layout, n);
             a.k = rows_dz;
             a.out_bf16 = a.add_bf16 = out.weight_dtype == ADAGC_BF16;
             if (const int rc = product_across(a)) return rc;

@@ -1574,6 +1574,7 @@ int run_plain(PlainArgs a, hipStream_t s)
         ld_x = std::max(ld_x, a.ld_x[i]);
     }
     const PlainPlan p = plain_plan(m, a.n_readable, a.k, dtype, ACROSS_Y, a.ld_y, ld_x, a.pairs * a.segments, a.products, aligned);
+    if (a.segments > 1 && !p.direct) return ADAGC_ERR_TOO_LARGE;           // the staged tiles take operands as they are, and would multiply the first parts alone
     a.tiles_m = (int32_t)p.tiles_m;
     a.tiles_n = (int32_t)p.tiles_n;
     a.whole = (int32_t)p.whole;
