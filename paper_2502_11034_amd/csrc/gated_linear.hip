@@ -269,12 +269,14 @@ Work work_of(int64_t rows, int64_t dim, int64_t hidden, int32_t dtype, bool back
 {
     Work w{};
     w.layout = layout_of(rows, hidden, dim, dtype, backward);
+    w.ld = (hidden + 63) / 64 * 64;
+    // d_g and d_u in parts are for the rings alone, which their rows are too far apart for
+    if (backward && w.layout.parts > 1 && w.ld >= kFarAlong) w.layout = Layout{false, 1, 1, w.layout.ld};
     if (w.layout.anew) {
         w.x = w.layout.bytes(rows);
         w.weight = w.layout.bytes(hidden);
     }
     const bool parts = w.layout.parts > 1;
-    w.ld = (hidden + 63) / 64 * 64;
     w.rows = parts ? Layout::rows_of(rows) : rows;
     w.gradients = up16(w.rows * w.ld * (parts ? 2 * kParts : dtype_size(dtype)));
     const int32_t type = w.layout.anew ? ADAGC_BF16 : dtype;

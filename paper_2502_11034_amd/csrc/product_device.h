@@ -910,6 +910,9 @@ using Slim = Tile<float, 32, 64, 1, 2, 0>;
 inline bool rows_aligned(const void* p, int64_t ld, int32_t dtype) { return !misaligned(p, 16) && ld * dtype_size(dtype) % 16 == 0; }
 
 
+// Elements from row to row from which on 256 rows along k are not within 32 bits of bytes: no operand of the rings.
+constexpr int64_t kFarAlong = (int64_t)1 << 23;
+
 // Tiles for a product of rows along k; n: of both matrices where there are two.
 struct AlongPlan {
     int     size, rows;           // columns: 256, 128 or 64; rows: as many, or 32
@@ -927,7 +930,7 @@ inline AlongPlan along_plan(int64_t m, int64_t n, int64_t k, int segments, int32
 {
     AlongPlan p{};
     auto tiles = [&](int64_t size) { return ((m + size - 1) / size) * ((n + size - 1) / size); };
-    p.direct = aligned && dtype == ADAGC_BF16 && ld_y < (int64_t)1 << 23 && ld_x < (int64_t)1 << 23;          // 256 rows are within 32 bits
+    p.direct = aligned && dtype == ADAGC_BF16 && ld_y < kFarAlong && ld_x < kFarAlong;
     p.size = tile_size(p.direct, dtype, tiles);
     if (p.size == 256 && segments > 1) p.size = 128;        // parts stay in the small tile's ring; see accumulate_parts
     p.rows = p.size == 64 && m <= Slim::BM ? Slim::BM : p.size;
@@ -1527,9 +1530,9 @@ inline PlainPlan plain_plan(int64_t m, int64_t n, int64_t k, int32_t dtype, bool
 {
     PlainPlan p{};
     auto tiles = [&](int64_t size) { return products * ((m + size - 1) / size) * ((n + size - 1) / size); };
-    // 32 rows across, 256 along k are not within 32 bits
+    // 32 rows across k are not within 32 bits
     const bool far = ld_x >= (int64_t)1 << 24 || (across_y && ld_y >= (int64_t)1 << 24);
-    p.direct = aligned && !far && dtype == ADAGC_BF16 && (across_y || ld_y < (int64_t)1 << 23) && n >= 128 && n % 8 == 0 &&
+    p.direct = aligned && !far && dtype == ADAGC_BF16 && (across_y || ld_y < kFarAlong) && n >= 128 && n % 8 == 0 &&
                (!across_y || (m >= 128 && m % 8 == 0));
     const int64_t steps = k / (kStepBytes / dtype_size(dtype)) / (p.direct ? 2 : 1) * (p.direct ? 2 : 1);
     p.size = tile_size(p.direct, dtype, tiles);

@@ -99,3 +99,22 @@ def check_certain(rows, vocab, dim, name, seed=1):
 def test_gradients_of_a_short_last_piece_of_the_vocabulary(rows, vocab, dim):
     """fp32 operands in parts, the last piece of 1 to 121 tokens: fewer than a tile has, and a few more than its products have to have."""
     check_certain(rows, vocab, dim, "f32")
+
+
+def test_input_gradient_from_very_many_gated_columns():
+    """fp32, rows of d_g and d_u 2^23 numbers apart and more, beyond the 32-bit offsets of the tiles that take parts.  Gates of 64, whose sigmoid is 1:
+    d_u = 64 d_out; ups of 0: d_g = 0."""
+    rows, dim, hidden = 128, 128, 2 ** 23 + 5
+    g = gen(3)
+    x = torch.randn(rows, dim, generator=g, device=DEV)
+    w_gate, w_up = (torch.randn(hidden, dim, generator=g, device=DEV) for _ in range(2))
+    own = torch.randint(0, hidden, (rows,), generator=g, device=DEV)
+    own[:2] = torch.tensor([0, hidden - 1], device=DEV)
+    w_up[own] = numbers(rows, dim, 24, g)
+    d, d_out = numbers(1, rows, 1, g)[0], torch.zeros(rows, hidden, device=DEV)
+    d_out[torch.arange(rows, device=DEV), own] = d
+    gate, up = torch.full((rows, hidden), 64.0, device=DEV), torch.zeros(rows, hidden, device=DEV)
+    d_x = torch.empty_like(x)
+    B.adagc_gated_linear_backward(d_out, x, w_gate, w_up, d_x, gate=gate, up=up,
+                                  workspace=torch.empty(B.adagc_gated_linear_backward_workspace_bytes(rows, dim, hidden, B.ADAGC_F32), dtype=torch.uint8, device=DEV))
+    assert torch.equal(d_x.double(), 64 * d.double()[:, None] * w_up[own].double())
