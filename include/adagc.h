@@ -595,7 +595,8 @@ int adagc_linear_logprobs_backward(const void* x, int64_t ld_x, const void* weig
  *   gate, up      DEVICE dtype[rows][ld_...]: g and u for the backward pass, rounded to the type, or both NULL
  *   workspace     DEVICE, adagc_gated_linear_workspace_bytes of it (0: may be NULL), 16-byte aligned, contents without meaning: room for operands
  *                 that are laid out anew (fp32 data; dim no multiple of 8) and, where the product's tiles are few, partial sums, 33 MB at most
- * Gates below -88 count as silu(g) = 0.
+ * Beside what g and u are off by as sums, and before it is rounded to its type, a result is off by at most 12 * 2^-24 of itself with fp32 data, whatever
+ * the gate (bf16: (13 + 2 |g|) * 2^-24), also where silu(g) is next to fp32's least numbers; gates below -167 count as silu(g) = 0.
  * Errors: INVALID_ARG, TOO_LARGE (also 2^24 rows or more, 2^34 values of out, 2^33 of a weight, 2^34 of x, and half of that where rows
  * and columns fill their tiles badly), HIP.
  */
