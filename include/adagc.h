@@ -555,7 +555,7 @@ int adagc_act8_wgrad(const void* d_out, int32_t dtype, int64_t ld_d_out, const v
  *   stats      DEVICE fp32[rows][2]: M and L, which the backward pass takes; or NULL
  *   workspace  DEVICE, adagc_linear_logprobs_workspace_bytes of it, 16-byte aligned, contents before and after without meaning: 8 bytes
  *              for each row and 32 to 128 tokens, where operands are laid out anew (fp32 data; dim no multiple of 8) x and a piece of
- *              the weight, and where the product's tiles are few partial sums, 33 MB at most
+ *              the weight, and where the product's tiles are few partial sums, 34 MB at most
  * At least one output is wanted.  A row whose logits are all -inf has log-probability -inf, M = -inf, L = 0; a row with a NaN or +inf among its
  * logits has a NaN log-probability.
  * Errors: INVALID_ARG, TOO_LARGE (also 2^24 rows or more, 2^35 logits or values of the weight, 2^34 of x, and half of that where rows and
@@ -594,7 +594,7 @@ int adagc_linear_logprobs_backward(const void* x, int64_t ld_x, const void* weig
  *   out           DEVICE dtype[rows][ld_out], hidden values a row
  *   gate, up      DEVICE dtype[rows][ld_...]: g and u for the backward pass, rounded to the type, or both NULL
  *   workspace     DEVICE, adagc_gated_linear_workspace_bytes of it (0: may be NULL), 16-byte aligned, contents without meaning: room for operands
- *                 that are laid out anew (fp32 data; dim no multiple of 8) and, where the product's tiles are few, partial sums, 33 MB at most
+ *                 that are laid out anew (fp32 data; dim no multiple of 8) and, where the product's tiles are few, partial sums, 34 MB at most
  * Beside what g and u are off by as sums, and before it is rounded to its type, a result is off by at most 12 * 2^-24 of itself with fp32 data, whatever
  * the gate (bf16: (13 + 2 |g|) * 2^-24), also where silu(g) is next to fp32's least numbers; gates below -167 count as silu(g) = 0.
  * Errors: INVALID_ARG, TOO_LARGE (also 2^24 rows or more, 2^34 values of out, 2^33 of a weight, 2^34 of x, and half of that where rows

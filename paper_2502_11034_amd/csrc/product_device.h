@@ -941,7 +941,8 @@ inline AlongPlan along_plan(int64_t m, int64_t n, int64_t k, int segments, int32
     // launch costs what it saves.  Workgroups of 32 rows are small: six on a compute unit, 12382 x 2 from 17 rows of 4096 162 us in 387 whole tiles, 92 and
     // 5 in three parts each.
     const int64_t round = p.direct ? kUnits : p.rows == 32 ? 6 * kUnits : 2 * kUnits, all = p.tiles_m * p.tiles_n, steps = k / (kStepBytes / dtype_size(dtype)) * segments;
-    p.split = steps >= 64 ? std::max<int64_t>(1, std::min(round / all, steps / 16)) : 1;
+    // (Large tiles are half as many as compute units at least, and whole.)
+    p.split = p.size < 256 && steps >= 64 ? std::max<int64_t>(1, std::min(round / all, steps / 16)) : 1;
     return p;
 }
 
