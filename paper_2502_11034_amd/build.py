@@ -37,7 +37,7 @@ def is_stale():
 def build(force=True, verbose=False, extra_flags=(), out=None):
     """Compile every source for gfx950 and link the shared library.  Cross-compiles without a GPU.
     extra_flags/out build a variant (e.g. another chunk size) somewhere else, for measurements."""
-    out = out or LIB
+    out, extra_flags = out or LIB, list(extra_flags)
     if out == LIB and not force and not is_stale():
         return LIB
     tmp = out + ".tmp.%d" % os.getpid()
@@ -47,7 +47,7 @@ def build(force=True, verbose=False, extra_flags=(), out=None):
              "-Wall", "-Wextra", "-Wno-unused-parameter",
              # an access that claims more alignment than its address has: tensors may start anywhere
              "-Werror=align-mismatch",
-             "-I" + os.path.join(ROOT, "include"), "-I" + CSRC] + list(extra_flags)
+             "-I" + os.path.join(ROOT, "include"), "-I" + CSRC] + extra_flags
 
     def run(cmd):
         res = subprocess.run(cmd, capture_output=True, text=True)
@@ -64,7 +64,7 @@ def build(force=True, verbose=False, extra_flags=(), out=None):
         jobs = [pool.submit(run, [hipcc(), *flags, "-x", "hip", "-c", os.path.join(CSRC, s), "-o", o]) for s, o in reversed(list(zip(SOURCES, names)))]
         for job in jobs:
             job.result()
-        run([hipcc(), "--offload-arch=gfx950", "-fPIC", "-shared", *names, "-o", tmp])
+        run([hipcc(), "--offload-arch=gfx950", "-fPIC", "-shared", *extra_flags, *names, "-o", tmp])
     os.replace(tmp, out)
     return out
 
