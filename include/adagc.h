@@ -597,8 +597,8 @@ int adagc_linear_logprobs_backward(const void* x, int64_t ld_x, const void* weig
  *                 that are laid out anew (fp32 data; dim no multiple of 8) and, where the product's tiles are few, partial sums, 34 MB at most
  * Beside what g and u are off by as sums, and before it is rounded to its type, a result is off by at most 12 * 2^-24 of itself with fp32 data, whatever
  * the gate (bf16: (13 + 2 |g|) * 2^-24), also where silu(g) is next to fp32's least numbers; gates below -167 count as silu(g) = 0.
- * Errors: INVALID_ARG, TOO_LARGE (also 2^24 rows or more, 2^34 values of out, 2^33 of a weight, 2^34 of x, and half of that where rows
- * and columns fill their tiles badly), HIP.
+ * Errors: INVALID_ARG, TOO_LARGE (also 2^24 rows or more, 2^34 values of out, 2^33 of a weight, 2^34 of x, some 2^35 of x and both weights where they
+ * are laid out anew, and half of that where rows and columns fill their tiles badly), HIP.
  */
 int64_t adagc_gated_linear_workspace_bytes(int64_t rows, int64_t dim, int64_t hidden, int32_t dtype);
 int adagc_gated_linear(const void* x, int64_t ld_x, const void* w_gate, int64_t ld_w_gate, const void* w_up, int64_t ld_w_up, int32_t dtype,

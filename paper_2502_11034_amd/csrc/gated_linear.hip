@@ -265,6 +265,9 @@ int check(int64_t rows, int64_t dim, int64_t hidden, int32_t dtype)
     const int64_t m = (rows + 63) / 64, k = (dim + 63) / 64, n = (hidden + 31) / 32;
     // lanes of a launch are within 32 bits
     if (m * n >= 1 << 23 || std::max(n * k, m * k) >= 1 << 22 || m * 64 * (n * 32 / 4) > (int64_t)UINT32_MAX - kKept) return ADAGC_ERR_TOO_LARGE;
+    // x and both weights are laid out in one launch
+    const Layout l = layout_of(rows, hidden, dim, dtype, true);
+    if (l.anew && (l.part(rows) + 2 * l.part(hidden)) / 8 > (int64_t)UINT32_MAX - 3 * kLay) return ADAGC_ERR_TOO_LARGE;
     return ADAGC_OK;
 }
 int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }

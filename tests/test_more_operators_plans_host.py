@@ -22,3 +22,12 @@ def test_projections_have_no_more_partial_sums_than_their_documentation_says():
                 assert B.adagc_linear_logprobs_workspace_bytes(rows, wide, dim, B.ADAGC_BF16) <= 2 ** 25 + parts, (rows, dim, wide)
     assert B.adagc_gated_linear_workspace_bytes(1024, 4096, 4096, B.ADAGC_BF16) == 0                       # 128 tiles of 256 x 256
     assert B.adagc_linear_logprobs_workspace_bytes(2048, 4096, 4096, B.ADAGC_BF16) < 2 ** 20
+
+
+def test_operands_that_one_launch_cannot_lay_out_are_too_large():
+    """bf16 rows of no whole vectors, laid out anew in one launch of 2^32 lanes, 8 numbers each, at most: x of 5824 rows and both weights of 2912, each within its own
+    limit, are more."""
+    for f in (B.lib().adagc_gated_linear_workspace_bytes, B.lib().adagc_gated_linear_backward_workspace_bytes):
+        assert f(5824, 46000 * 64 - 3, 2912, B.ADAGC_BF16) == B.ADAGC_ERR_TOO_LARGE
+        assert f(5824, 45500 * 64 - 3, 2912, B.ADAGC_BF16) > 0
+        assert f(5824, 46000 * 64, 2912, B.ADAGC_BF16) >= 0              # as they are
