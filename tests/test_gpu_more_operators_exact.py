@@ -1,14 +1,18 @@
 """Products of the operators that keep nothing between the passes, bit for bit: operands whose sums are exact in fp32 in any order, with numbers
-of so many bits that every part of a product counts that is taken as three bf16 numbers."""
+of so many bits that every part of a product counts that is taken as three bf16 numbers (test_exact_products_host.py shows that they tell)."""
+import math
+
 import pytest
 import torch
 
+from exact_products import BITS, numbers, one_place
 from paper_2502_11034_amd import binding as B
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 CODES = {torch.float32: B.ADAGC_F32, torch.bfloat16: B.ADAGC_BF16}
+U32 = 2.0 ** -24
 
 
 def gen(seed):
@@ -17,21 +21,6 @@ def gen(seed):
 
 def workspace(n):
     return torch.full((n,), 0xFF, dtype=torch.uint8, device=DEV)
-
-
-def numbers(rows, cols, bits, g):
-    """Whole numbers of exactly so many bits, of both signs; of one bit: powers of two from 1 to 8."""
-    shape = (rows, cols)
-    if bits == 1:
-        n = 2 ** torch.randint(0, 4, shape, generator=g, device=DEV)
-    else:
-        n = torch.randint(2 ** (bits - 1), 2 ** bits, shape, generator=g, device=DEV) | 1
-    return (n * (2 * torch.randint(0, 2, shape, generator=g, device=DEV) - 1)).float()
-
-
-# Bits of the operand and of the gradient that it is multiplied with: 24 bits are all three parts of a number, one bit the first alone, 12 bits the first
-# two; and 24 are what a product may have, for fp32 to hold it.
-BITS = {"f32": [(24, 1), (1, 24), (12, 12)], "bf16": [(8, 1), (1, 8), (4, 4)]}
 
 
 class Certain:
@@ -99,6 +88,136 @@ def check_certain(rows, vocab, dim, name, seed=1):
 def test_gradients_of_a_short_last_piece_of_the_vocabulary(rows, vocab, dim):
     """fp32 operands in parts, the last piece of 1 to 121 tokens: fewer than a tile has, and a few more than its products have to have."""
     check_certain(rows, vocab, dim, "f32")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows, vocab, dim", [(1, 3, 65), (8, 700, 768), (9, 700, 93), (16, 17000, 200), (17, 600, 4100), (33, 129, 100), (40, 300, 2051), (127, 259, 765),
+                                              (130, 127, 72), (300, 1024, 1000), (300, 515, 2090), (300, 9000, 2100), (600, 700, 4128), (513, 22116, 130), (4100, 300, 4200),
+                                              (4100, 5000, 136), (2100, 4100, 264), (16500, 3900, 130)])
+def test_gradients_of_certain_tokens(dtype, rows, vocab, dim):
+    check_certain(rows, vocab, dim, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows, vocab, dim", [(2, 257, 8), (5, 20011, 136), (16, 17000, 200), (20, 5003, 40), (64, 50257, 33), (300, 1024, 1000), (300, 9000, 2100), (513, 22116, 64),
+                                              (2100, 4100, 264)])
+def test_every_logit_is_counted_once(dtype, rows, vocab, dim):
+    """All logits of a row are equal, in the odd rows 0: L = ln vocab, and one logit more or less would change it by 1 / vocab."""
+    g = gen(5)
+    x, w = torch.randint(-3, 4, (rows, dim), generator=g, device=DEV).to(TYPES[dtype]), torch.randint(-3, 4, (1, dim), generator=g, device=DEV).to(TYPES[dtype])
+    x[1::2] = 0
+    z = (x.double() * w.double()).sum(1)
+    w = w.expand(vocab, dim).contiguous()
+    t = torch.arange(rows, device=DEV) * 7 % vocab
+    logprob, stats = torch.empty(rows, device=DEV), torch.empty(rows, 2, device=DEV)
+    B.adagc_linear_logprobs(x, w, t, logprob, stats, workspace=workspace(B.adagc_linear_logprobs_workspace_bytes(rows, vocab, dim, CODES[x.dtype])))
+    assert torch.equal(stats[:, 0].double(), z)
+    want = math.log(vocab)
+    # zeros: sums of ones, which are exact, and a logarithm of two steps; others: exponentials of two half steps and what puts them right, four more, and
+    # sums of equal numbers: vocab / 256 + 24 additions one after another
+    off = torch.full((rows,), 4 * U32 * want, device=DEV, dtype=torch.float64)
+    off[0::2] += (vocab / 256 + 24 + 6) * U32
+    assert (off < 0.9 / vocab).all()
+    assert ((stats[:, 1].double() - want).abs() <= off).all() and ((logprob.double() + want).abs() <= off).all()
+
+
+# rows, dim, hidden; fp32: from 193 rows (backward 128) and 2^29 multiplications on in parts
+GATED = [(8, 768, 512), (16, 61, 700), (24, 264, 96), (33, 40, 130), (129, 765, 333), (300, 72, 64), (300, 1000, 264), (200, 1001, 2700), (193, 130, 22000), (200, 4128, 700),
+         (600, 4104, 300), (1100, 1000, 600), (4097, 72, 1031), (4100, 136, 2600), (2060, 264, 2056), (1030, 4096, 4096)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows, dim, hidden", GATED)
+def test_gated_projections(dtype, rows, dim, hidden):
+    """Rows of x, or of the weights, have one number: both products, which are left in gate and up, are single products."""
+    code, kind, g = CODES[TYPES[dtype]], TYPES[dtype], gen(6)
+    for one in ("x", "w"):
+        for bits, other in BITS[dtype]:
+            if one == "x":
+                at, x = one_place(rows, dim, bits, g)
+                weights = [numbers(hidden, dim, other, g) for _ in range(2)]
+                want = [x.double().gather(1, at[:, None]) * w.double()[:, at].t() for w in weights]
+            else:
+                x = numbers(rows, dim, bits, g)
+                placed = [one_place(hidden, dim, other, g) for _ in range(2)]
+                placed[1] = ((placed[1][0] + 1) % dim, placed[1][1].roll(1, 1))            # other places than the gate's
+                weights = [w for _, w in placed]
+                want = [x.double()[:, at] * w.double().gather(1, at[:, None])[:, 0] for at, w in placed]
+            out, gate, up = (torch.full((rows, hidden), 77.0, dtype=kind, device=DEV) for _ in range(3))
+            B.adagc_gated_linear(x.to(kind), weights[0].to(kind), weights[1].to(kind), out, gate, up,
+                                 workspace=workspace(B.adagc_gated_linear_workspace_bytes(rows, dim, hidden, code)))
+            assert torch.equal(gate.double(), want[0]) and torch.equal(up.double(), want[1]), (one, bits, other)
+
+
+def gated_backward(d_out, x, w_gate, w_up, d_x, d_w_gate, d_w_up, up):
+    """Gates of 64, whose sigmoid is 1 and slope 1, kept: d_u = 64 d_out, and d_g = up d_out."""
+    rows, hidden = d_out.shape
+    gate, up = torch.full_like(d_out, 64.0), torch.full_like(d_out, up)
+    B.adagc_gated_linear_backward(d_out, x, w_gate, w_up, d_x, d_w_gate, d_w_up, gate=gate, up=up,
+                                  workspace=workspace(B.adagc_gated_linear_backward_workspace_bytes(rows, x.shape[1], hidden, CODES[x.dtype])))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows, dim, hidden", GATED)
+def test_gated_gradients(dtype, rows, dim, hidden):
+    kind, g = TYPES[dtype], gen(7)
+    for bits, other in BITS[dtype]:
+        w_gate, w_up = (numbers(hidden, dim, bits, g) for _ in range(2))
+        # d_x: a row has a gradient in one column ...
+        at, d = one_place(rows, hidden, other, g)
+        own = d.double().gather(1, at[:, None])
+        for up, a, b, want in ((0.0, w_gate, w_up, 64 * own * w_up.double()[at]), (1.0, w_gate, torch.zeros_like(w_up), own * w_gate.double()[at])):
+            d_x = torch.full((rows, dim), 77.0, dtype=kind, device=DEV)
+            gated_backward(d.to(kind), torch.zeros_like(d_x), a.to(kind), b.to(kind), d_x, None, None, up)
+            assert torch.equal(d_x.double(), want), (bits, other, up)
+        # ... or in all, and a column of a weight one number
+        at, of_column = one_place(dim, hidden, bits, g)
+        w = of_column.t().contiguous()
+        d = numbers(rows, hidden, other, g)
+        d_x = torch.full((rows, dim), 77.0, dtype=kind, device=DEV)
+        gated_backward(d.to(kind), torch.zeros_like(d_x), w_gate.to(kind), w.to(kind), d_x, None, None, 0.0)
+        assert torch.equal(d_x.double(), 64 * d.double()[:, at] * of_column.double().gather(1, at[:, None])[:, 0]), (bits, other)
+        # the weights' gradients: a column's gradient is in one row ...
+        x, w = numbers(rows, dim, bits, g), torch.zeros(hidden, dim, dtype=kind, device=DEV)
+        at, of_column = one_place(hidden, rows, other, g)
+        d_gate, d_up = (torch.full((hidden, dim), 77.0, dtype=kind, device=DEV) for _ in range(2))
+        gated_backward(of_column.t().contiguous().to(kind), x.to(kind), w, w, None, d_gate, d_up, 1.0)
+        want = of_column.double().gather(1, at[:, None]) * x.double()[at]
+        assert torch.equal(d_gate.double(), want) and torch.equal(d_up.double(), 64 * want), (bits, other)
+        # ... or in all, and a column of x one number
+        at, of_column = one_place(dim, rows, bits, g)
+        d = numbers(rows, hidden, other, g)
+        gated_backward(d.to(kind), of_column.t().contiguous().to(kind), w, w, None, d_gate, d_up, 1.0)
+        want = d.double()[at].t() * of_column.double().gather(1, at[:, None])[:, 0]
+        assert torch.equal(d_gate.double(), want) and torch.equal(d_up.double(), 64 * want), (bits, other)
+
+
+def root_mean_square(got, want, k):
+    """fp32 sums of k products in six parts: 6 k additions at most, each off by up to half a step of what has been summed so far, all directions alike: sqrt(1 / 3) of
+    half a step in the root of the mean square, of a sum whose square grows evenly: sqrt(6 k / 3 / 2) half steps of the whole.  The products of parts that
+    are left out are 2^-26 of it, and the result is rounded: 4 half steps more than cover both."""
+    assert (got.double() - want).norm() <= (math.sqrt(k) + 4) * U32 * want.norm()
+
+
+def test_random_products_in_parts():
+    """Dense random operands, where parts of one tile with another's would show everywhere: less than a product of parts left out."""
+    g = gen(8)
+    rows, dim, hidden = 300, 256, 7100
+    x, w_gate, w_up = (torch.randn(*s, generator=g, device=DEV) for s in ((rows, dim), (hidden, dim), (hidden, dim)))
+    out, gate, up = (torch.empty(rows, hidden, device=DEV) for _ in range(3))
+    B.adagc_gated_linear(x, w_gate, w_up, out, gate, up, workspace=workspace(B.adagc_gated_linear_workspace_bytes(rows, dim, hidden, B.ADAGC_F32)))
+    for got, w in ((gate, w_gate), (up, w_up)):
+        root_mean_square(got, x.double() @ w.double().t(), dim)
+    d, d_w_gate, d_w_up = torch.randn(rows, hidden, generator=g, device=DEV), torch.empty_like(w_gate), torch.empty_like(w_up)
+    gated_backward(d, x, w_gate, w_up, None, d_w_gate, d_w_up, 1.0)
+    want = d.double().t() @ x.double()
+    root_mean_square(d_w_gate, want, rows)
+    root_mean_square(d_w_up, 64 * want, rows)
+    rows, dim, hidden = 2100, 2100, 129
+    x, w = torch.zeros(rows, dim, device=DEV), torch.randn(hidden, dim, generator=g, device=DEV)
+    d, d_x = torch.randn(rows, hidden, generator=g, device=DEV), torch.empty(rows, dim, device=DEV)
+    gated_backward(d, x, w, w, d_x, None, None, 0.0)
+    root_mean_square(d_x, 64 * (d.double() @ w.double()), hidden)
 
 
 def test_input_gradient_from_very_many_gated_columns():
