@@ -540,7 +540,7 @@ int adagc_act8_wgrad(const void* d_out, int32_t dtype, int64_t ld_d_out, const v
 /*
  * Operators that keep nothing between the passes but their inputs.  As above; products are sums in fp32 of bf16 products, which are exact, or of
  * fp32 ones: those of 128 rows and 2^29 multiplications or more may be taken as three bf16 numbers each and are off by some 2^-26 of themselves then
- * (an infinity among their operands may give NaN), the others are rounded to fp32.  The workspace sizes are negative error codes for sizes that are
+ * (an infinity among their operands, or a product beyond fp32's range, may make their sum NaN), the others are rounded to fp32.  The workspace sizes are negative error codes for sizes that are
  * refused.  Results do not depend on what else runs: sums are taken in a fixed order.
  *
  * Log-probabilities of given tokens straight from the head's input and weights: what adagc_token_logprobs gives for the logits z = x W^T,
@@ -556,8 +556,8 @@ int adagc_act8_wgrad(const void* d_out, int32_t dtype, int64_t ld_d_out, const v
  *   workspace  DEVICE, adagc_linear_logprobs_workspace_bytes of it, 16-byte aligned, contents before and after without meaning: 8 bytes
  *              for each row and 32 to 128 tokens, where operands are laid out anew (fp32 data; dim no multiple of 8) x and a piece of
  *              the weight, and where the product's tiles are few partial sums, 34 MB at most
- * At least one output is wanted.  A row whose logits are all -inf has log-probability -inf, M = -inf, L = 0; a row with a NaN or +inf among its
- * logits has a NaN log-probability.
+ * At least one output is wanted.  A row whose logits are all -inf (as sums, see above) has log-probability -inf, M = -inf, L = 0; a row with a NaN or +inf
+ * among its logits has a NaN log-probability.
  * Errors: INVALID_ARG, TOO_LARGE (also 2^24 rows or more, 2^35 logits or values of the weight, 2^34 of x, and half of that where rows and
  * columns fill their tiles badly), HIP.
  */

@@ -60,8 +60,8 @@ def build(force=True, verbose=False, extra_flags=(), out=None):
 
     with tempfile.TemporaryDirectory() as objects, concurrent.futures.ThreadPoolExecutor(min(JOBS, os.cpu_count() or 1)) as pool:
         names = [os.path.join(objects, s + ".o") for s in SOURCES]
-        # the longest ones first
-        jobs = [pool.submit(run, [hipcc(), *flags, "-x", "hip", "-c", os.path.join(CSRC, s), "-o", o]) for s, o in reversed(list(zip(SOURCES, names)))]
+        # in the list's order: those that take the longest, muon_gemm.hip and kernels.hip, are among the first
+        jobs = [pool.submit(run, [hipcc(), *flags, "-x", "hip", "-c", os.path.join(CSRC, s), "-o", o]) for s, o in zip(SOURCES, names)]
         for job in jobs:
             job.result()
         run([hipcc(), "--offload-arch=gfx950", "-fPIC", "-shared", *extra_flags, *names, "-o", tmp])

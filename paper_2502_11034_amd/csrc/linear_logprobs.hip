@@ -295,7 +295,8 @@ int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 // What a call needs, in bytes, and how it goes through the vocabulary.
 //
 // The backward pass and operands that are laid out anew go in pieces: 2^26 gradients of logits, which the memory-side cache holds as bf16 (as three
-// parts half as many), and as many weights, laid out, at most; 2048 columns at least.
+// parts half as many), and as many weights, laid out, at most, or 2048 columns where that is more; up to twice that where fewer would not fill a round
+// of the weight's gradient (piece_of).
 struct Work {
     Layout  layout;
     int64_t size, number;                          // of a piece, of pieces
@@ -305,7 +306,8 @@ struct Work {
     int64_t forward() const { return parts + targets + x + weight + partial; }
     int64_t backward() const { return d_logits + sums + partial + x + weight; }
 };
-// Columns of a piece, so many at most: the weight's gradient takes 256-tiles in whole rounds of the compute units where that many fill some.
+// Columns of a piece, so many at most: the weight's gradient takes 256-tiles in whole rounds of the compute units where that many fill some, or one
+// round where twice as many do.
 int64_t piece_of(int64_t vocab, int64_t dim, int64_t most)
 {
     if (vocab <= most) return vocab;

@@ -1,5 +1,6 @@
 // Shared by the kernels of the operators around the step: token log-probabilities (logprobs.hip), 8-bit checkpoints and the gated
-// activation (act8.hip), the weight gradient from a checkpoint (act8_wgrad.hip).
+// activation (act8.hip), the weight gradient from a checkpoint (act8_wgrad.hip), log-probabilities from the head's input (linear_logprobs.hip),
+// gated projections (gated_linear.hip), their products (product_device.h, product.hip), dropout (dropout.hip).
 #ifndef ADAGC_OPERATORS_INTERNAL_H
 #define ADAGC_OPERATORS_INTERNAL_H
 

@@ -1430,7 +1430,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void plain_kernel(const PlainArgs a
     };
     auto finish = [&](const Place& p) __attribute__((always_inline)) {
         // (a tile at the matrix's end looks where it ends; within it an address and a check for every four results showed: 5 of 459 us of a weight
-        // gradient of 16128 x 4096 from 4096 tokens)
+        // gradient of 16128 x 4096 from 4096 tokens.  bf16 results with nothing added, d_x but the fp32 sums of its pieces, have add_bf16 = 0 and take the
+        // way of the ends too.)
         const bool inside = p.m0 == p.m_least && p.m0 + S::BM <= a.m && p.n0 == p.n_least && p.n0 + S::BN <= a.n && a.out_bf16 == a.add_bf16;
         if (p.item < a.whole && inside) {
             void* out = p.product ? a.out[1] : a.out[0];
@@ -1595,9 +1596,11 @@ int run_plain(PlainArgs a, hipStream_t s)
 
 // ---------------------------------------------------------------------------------------- operands laid out anew
 //
-// fp32 operands in three parts, and bf16 ones whose rows are not multiples of 16 bytes, are copied to the workspace first, rows and columns filled
-// up to multiples of 64 with zeros, and multiplied by the bf16 tiles that load straight into LDS.  That has to be paid for: bf16 rows are laid out
-// from 128 rows on; fp32 ones too, those of a single product (a forward pass) from 193, of 2^29 multiplications at least.  fp32, us as they are and in
+// fp32 operands in three parts, and bf16 ones whose rows have no whole number of 16-byte vectors (k no multiple of 8), are copied to the workspace first,
+// rows and columns filled up to multiples of 64 with zeros, and multiplied by the bf16 tiles that load straight into LDS.  The workspace's size knows no
+// addresses: bf16 rows of whole vectors that start elsewhere than at multiples of 16 bytes are taken as they are, through registers (1024 x 50257 from
+// 768 forward 93 us, from rows 769 apart 166; 4096 x 14336 from 4096 364 and 760).  Laying out has to be paid for: bf16 rows are laid out from 128 rows on
+// (1024 x 50257 from 767 113 us); fp32 ones too, those of a single product (a forward pass) from 193, of 2^29 multiplications at least.  fp32, us as they are and in
 // parts: 192 and 256 rows, 32000 from 1024, forward 117 and 150, 153 and 146; 128 rows, all of a training pass 343 and 340; 256 rows, 2 x 1719 from 4096,
 // all of it 335 and 262; 2 x 2138 from 1024, forward 44 and 40; 2 x 768 from 768, all of it 74 and 101.
 struct Layout {

@@ -237,3 +237,42 @@ def test_input_gradient_from_very_many_gated_columns():
     B.adagc_gated_linear_backward(d_out, x, w_gate, w_up, d_x, gate=gate, up=up,
                                   workspace=torch.empty(B.adagc_gated_linear_backward_workspace_bytes(rows, dim, hidden, B.ADAGC_F32), dtype=torch.uint8, device=DEV))
     assert torch.equal(d_x.double(), 64 * d.double()[:, None] * w_up[own].double())
+
+
+def test_rows_that_are_no_numbers_stay_by_themselves_in_parts():
+    """fp32 operands in parts: a row of x with an infinity, a NaN, or products beyond the range changes no other row."""
+    rows, vocab, dim = 200, 2700, 1001
+    g = gen(9)
+    x, w = torch.randn(rows, dim, generator=g, device=DEV), torch.randn(vocab, dim, generator=g, device=DEV) * 0.03
+    t = torch.randint(0, vocab, (rows,), generator=g, device=DEV)
+    odd = x.clone()
+    odd[3, 7], odd[4, 1000], odd[70, 0], odd[199] = math.inf, -math.inf, math.nan, 3e38
+    bad = torch.zeros(rows, dtype=torch.bool, device=DEV)
+    bad[[3, 4, 70, 199]] = True
+    d = torch.where(bad, 0.0, 1.0)
+    results = []
+    for a in (x, odd):
+        logprob, stats, d_x, d_w = torch.empty(rows, device=DEV), torch.empty(rows, 2, device=DEV), torch.empty_like(x), torch.empty_like(w)
+        B.adagc_linear_logprobs(a, w, t, logprob, stats, workspace=workspace(B.adagc_linear_logprobs_workspace_bytes(rows, vocab, dim, B.ADAGC_F32)))
+        B.adagc_linear_logprobs_backward(a, w, t, stats, d, d_x, None, workspace=workspace(B.adagc_linear_logprobs_backward_workspace_bytes(rows, vocab, dim, B.ADAGC_F32)))
+        results.append((logprob, stats, d_x))
+    for plain, now in zip(*results):
+        assert torch.equal(plain[~bad], now[~bad])
+    assert torch.isnan(results[1][0][bad][:3]).all() and (results[1][2][bad] == 0).all()
+
+
+def test_statistics_that_start_at_any_number():
+    """Pairs of fp32 numbers 4 bytes from a multiple of 8."""
+    rows, vocab, dim = 21, 300, 40
+    g = gen(10)
+    x, w, t = torch.randn(rows, dim, generator=g, device=DEV), torch.randn(vocab, dim, generator=g, device=DEV), torch.arange(rows, device=DEV)
+    space = workspace(max(B.adagc_linear_logprobs_workspace_bytes(rows, vocab, dim, B.ADAGC_F32), B.adagc_linear_logprobs_backward_workspace_bytes(rows, vocab, dim, B.ADAGC_F32)))
+    results = []
+    for offset in (0, 1):
+        buffer = torch.full((2 * rows + 2,), 77.0, device=DEV)
+        stats, d_w = buffer[offset:offset + 2 * rows].view(rows, 2), torch.empty_like(w)
+        B.adagc_linear_logprobs(x, w, t, None, stats, workspace=space)
+        B.adagc_linear_logprobs_backward(x, w, t, stats, torch.ones(rows, device=DEV), None, d_w, workspace=space)
+        assert (buffer[:offset] == 77).all() and (buffer[offset + 2 * rows:] == 77).all()
+        results.append((stats.clone(), d_w))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
