@@ -570,7 +570,8 @@ int adagc_linear_logprobs(const void* x, int64_t ld_x, const void* weight, int64
  * Its gradients for the gradient d of the log-probabilities, the logits made again in pieces of the vocabulary: with p_j = exp(logp_j),
  *     d_z_j = d (1[j = target] - p_j),   d_x = scale d_z W,   d_weight = scale d_z^T x   (+ d_weight with accumulate = 1),
  * d_z being 0 for rows without a target, rows of nothing but -inf and rows whose d is 0 (x has to be finite there too: 0 times it is part of
- * d_weight).  With bf16 data d_z is rounded to bf16 before the products (off by 2^-8 of itself at most, to nearest even); sums are fp32.
+ * d_weight).  With bf16 data d_z is rounded to bf16 before the products (off by 2^-8 of itself at most, to nearest even); sums are fp32.  x and weight in
+ * fp32 keep it in fp32.
  *   x, weight, targets, scale   as the forward call had them
  *   stats      DEVICE, the forward call's
  *   d_logprob  DEVICE fp32[rows]
@@ -609,7 +610,7 @@ int adagc_gated_linear(const void* x, int64_t ld_x, const void* w_gate, int64_t 
  * Its gradients, from g and u as the forward call left them, or (gate and up NULL) with both products made again: with t = 1 / (1 + exp(-g)),
  *     d_g = d_out u t (1 + g (1 - t)),  d_u = d_out g t,  d_x = d_g Wg + d_u Wu,  d_w_gate = d_g^T x,  d_w_up = d_u^T x
  * (the last two added to what is there with accumulate = 1), and, for the next layer's weight gradient, out again.  With bf16 data d_g and
- * d_u are rounded to bf16 before the products (off by 2^-8 of themselves at most); sums are fp32.  Kept products save a third of the
+ * d_u are rounded to bf16 before the products (off by 2^-8 of themselves at most); sums are fp32.  Data in fp32 keeps them in fp32.  Kept products save a third of the
  * multiplications of a training pass's backward half and cost their own rounding, which the gradients inherit.
  *   d_out             DEVICE dtype[rows][ld_d_out]
  *   d_x               DEVICE dtype[rows][ld_d_x]; or NULL

@@ -3,8 +3,8 @@
 //     d_g = d u t (1 + g (1 - t)),  d_u = d g t,  dx = d_g Wg + d_u Wu,  dWg = d_g^T x,  dWu = d_u^T x.
 //
 // Blocks of 16 columns of the two weights' rows take turns in a tile, so that a lane holds g and u of the same places.  Backward: d_g and
-// d_u go to the workspace (bf16 with bf16 operands: they go into the matrix cores as they are), from g and u that the forward pass kept,
-// or from both products made again; from there dx, one product over both, and the two weight gradients, in one launch.
+// d_u go to the workspace (bf16 with bf16 operands: they go into the matrix cores as they are, and a second part of them would double the time of the
+// products), from g and u that the forward pass kept, or from both products made again; from there dx, one product over both, and the two weight gradients, in one launch.
 //
 // What bounds it: the matrix cores.  8192 rows, 14336 from 4096, bf16: forward with g and u kept 1410 - 1620 us (1.19 - 1.37 PFLOP/s), d_g and d_u from
 // them 199 (5.9 TB/s), the weights' gradients 1465 - 1660, dx 1350 - 1500.  24 rows: the weights' way to the compute units, 38 us from the memory-side

@@ -4,8 +4,8 @@
 //
 // Forward: the product's tiles stay in registers; of every row a tile leaves its maximum and its sum of exponentials relative to that,
 // and the target's logit, and a second kernel joins a row's tiles in order.  Backward: the logits of a piece of the vocabulary again, their
-// gradients (bf16 with bf16 operands: they go into the matrix cores as they are) to the workspace, and from there the two products; dx is
-// summed over the pieces in fp32.
+// gradients (bf16 with bf16 operands: they go into the matrix cores as they are, and a second part of them would double the time of both products)
+// to the workspace, and from there the two products; dx is summed over the pieces in fp32.
 //
 // What bounds it: the matrix cores, and of short sums what a tile takes beside them, 3 - 4 us of a 256-tile's exponentials among it.  4096 rows,
 // 128256 from 4096, bf16: forward 3050 - 3240 us and 10 for joining; a piece of 16384 columns 399 - 429 for its gradients, 404 - 432 for the weight's,
