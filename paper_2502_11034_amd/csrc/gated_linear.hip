@@ -53,8 +53,10 @@ template <bool FINE>
 __device__ __forceinline__ void gradients_of(float g, float u, float d, float& out, float& d_g, float& d_u)
 {
     const Gate t = gate_of<FINE>(g);
+    // of a gradient above 1 w is taken first: d u would leave the range, which w brings it back into, and d w does not
+    const bool above = __builtin_fabsf(d) > 1.f;
     out = t.silu * u * t.w;
-    d_g = d * (u * t.slope) * t.w;
+    d_g = d * (above ? t.w : 1.f) * (u * t.slope) * (above ? 1.f : t.w);
     d_u = d * t.silu * t.w;
 }
 

@@ -122,3 +122,25 @@ def test_gates_without_a_number():
             assert (d_x[:2, 0] == 0).all()
             if w_up is zero:
                 assert d_x[3, 0] == 6.0 and torch.isnan(d_x[4, 0])               # the sigmoid's slope is 0: d u, three times
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kept", [False, True])
+@pytest.mark.parametrize("rows, dim, hidden", [FEW, TILES, LARGE])
+def test_factors_whose_product_leaves_the_range_before_a_far_gate_brings_it_back(dtype, kept, rows, dim, hidden):
+    """d_g of gates below -87: d u is 2^190 and the like, d u t a normal number."""
+    dtype = TYPES[dtype]
+    for up, d in ((2.0 ** 90, 2.0 ** 100), (-2.0 ** 100, 2.0 ** 90), (2.0 ** 120, 1.0), (2.0 ** -20, 2.0 ** 120), (2.0 ** 120, 2.0 ** -20)):
+        g, x, w_gate, w_up = inputs(rows, dim, hidden, dtype, up, 3)
+        g = g.clamp(max=-87.5).to(dtype).double()
+        x[:, 0] = g.to(dtype)
+        d_out, d_x = torch.zeros(rows, hidden, dtype=dtype, device=DEV), torch.empty_like(x)
+        d_out[:, hidden // 2] = d
+        held = {"gate": x[:, :1].expand(rows, hidden).contiguous(), "up": x[:, 1:2].expand(rows, hidden).contiguous()} if kept else {}
+        B.adagc_gated_linear_backward(d_out, x, w_gate, w_up, d_x, **held,
+                                      workspace=space(B.adagc_gated_linear_backward_workspace_bytes(rows, dim, hidden, CODES[dtype])))
+        want = d * up * torch.sigmoid(g) * (1 + g)
+        assert (want.abs() < 2.0 ** 100).all()
+        bf16 = 2.0 ** -8 if dtype == torch.bfloat16 else 0.0
+        # the sigmoid, 1 + g and three products
+        within(d_x[:, 0], want, sigmoid_off(g, dtype) + 6, 2.0 ** -125 + torch.where(g < FAR, 1.0, 0.0) * want.abs() + bf16 * want.abs(), dtype)
