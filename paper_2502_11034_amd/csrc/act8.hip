@@ -143,7 +143,7 @@ __device__ __forceinline__ void unpack_vector(const Packed& p, float (&x)[N])
 
 // t = 1 / (1 + exp(-g)) as p w, w a power of two, and 1 - t.
 // FAR, for gates below kFar, where t is exp(g) in all its bits and next to the least normal number or below it (large factors make normal
-// results of those too): p is exp(g) 2^116 (0 below -167).  Products are taken with p first and with w last.  Other gates' results are
+// results of those too): p is exp(g) 2^116 (0 below -167).  Products are taken with p first and with w last, but for d_gate.  Other gates' results are
 // the same either way.
 // FINE, for fp32 values: what the exponential's argument g log2 e loses by its rounding is multiplied in after, so that t is off by
 // 8 * 2^-24 of itself at most.  Without, that is 2 |g| more, 2^-16 of t at the least: nothing beside the 2^-8 of bf16 results.  The
@@ -305,7 +305,9 @@ __global__ __launch_bounds__(kThreads) void swiglu_backward_kernel(const Args a)
                 for (int i = 0; i < N; ++i) {
                     const Gate t = sigmoid<sizeof(T) == 4, decltype(FAR)::value>(g[i]);
                     const float silu = g[i] * t.p;
-                    dg[i] = d[i] * (u[i] * (t.p * fmaf(g[i], t.rest, 1.f))) * t.w;
+                    // of a gradient above 1 w is taken first: d u would leave the range, which w brings it back into, and d w does not
+                    const bool above = decltype(FAR)::value && __builtin_fabsf(d[i]) > 1.f;
+                    dg[i] = d[i] * (above ? t.w : 1.f) * (u[i] * (t.p * fmaf(g[i], t.rest, 1.f))) * (above ? 1.f : t.w);
                     h[i] = silu * u[i] * t.w;
                     d[i] = d[i] * silu * t.w;
                 }
