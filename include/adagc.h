@@ -540,8 +540,8 @@ int adagc_act8_wgrad(const void* d_out, int32_t dtype, int64_t ld_d_out, const v
 /*
  * Operators that keep nothing between the passes but their inputs.  As above; products are sums in fp32 of bf16 products, which are exact, or of
  * fp32 ones: those of 128 rows and 2^29 multiplications or more may be taken as three bf16 numbers each and are off by some 2^-26 of themselves then
- * (an infinity among their operands, or a product beyond fp32's range, may make their sum NaN), the others are rounded to fp32.  The workspace sizes are negative error codes for sizes that are
- * refused.  Results do not depend on what else runs: sums are taken in a fixed order.
+ * (an infinity among their operands, or a product beyond fp32's range, may make their sum NaN), the others are rounded to fp32.  The workspace sizes
+ * are negative error codes for sizes that are refused.  Results do not depend on what else runs: sums are taken in a fixed order.
  *
  * Log-probabilities of given tokens straight from the head's input and weights: what adagc_token_logprobs gives for the logits z = x W^T,
  * without the logits.  With M = max_j z_j and L = ln sum_j exp(scale (z_j - M)),
@@ -610,8 +610,8 @@ int adagc_gated_linear(const void* x, int64_t ld_x, const void* w_gate, int64_t 
  * Its gradients, from g and u as the forward call left them, or (gate and up NULL) with both products made again: with t = 1 / (1 + exp(-g)),
  *     d_g = d_out u t (1 + g (1 - t)),  d_u = d_out g t,  d_x = d_g Wg + d_u Wu,  d_w_gate = d_g^T x,  d_w_up = d_u^T x
  * (the last two added to what is there with accumulate = 1), and, for the next layer's weight gradient, out again.  With bf16 data d_g and
- * d_u are rounded to bf16 before the products (off by 2^-8 of themselves at most); sums are fp32.  Data in fp32 keeps them in fp32.  Kept products save a third of the
- * multiplications of a training pass's backward half and cost their own rounding, which the gradients inherit.
+ * d_u are rounded to bf16 before the products (off by 2^-8 of themselves at most); sums are fp32.  Data in fp32 keeps them in fp32.  Kept products save
+ * a third of the multiplications of a training pass's backward half and cost their own rounding, which the gradients inherit.
  *   d_out             DEVICE dtype[rows][ld_d_out]
  *   d_x               DEVICE dtype[rows][ld_d_x]; or NULL
  *   d_w_gate, d_w_up  DEVICE weight_dtype[hidden][ld_...], zero rows make them 0 (or leave them); or both NULL

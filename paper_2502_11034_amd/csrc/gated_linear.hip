@@ -4,7 +4,8 @@
 //
 // Blocks of 16 columns of the two weights' rows take turns in a tile, so that a lane holds g and u of the same places.  Backward: d_g and
 // d_u go to the workspace (bf16 with bf16 operands: they go into the matrix cores as they are, and a second part of them would double the time of the
-// products), from g and u that the forward pass kept, or from both products made again; from there dx, one product over both, and the two weight gradients, in one launch.
+// products), from g and u that the forward pass kept, or from both products made again; from there dx, one product over both, and the two
+// weight gradients, in one launch.
 //
 // What bounds it: the matrix cores.  8192 rows, 14336 from 4096, bf16: forward with g and u kept 1410 - 1620 us (1.19 - 1.37 PFLOP/s), d_g and d_u from
 // them 199 (5.9 TB/s), the weights' gradients 1465 - 1660, dx 1350 - 1500.  24 rows: the weights' way to the compute units, 38 us from the memory-side
@@ -18,10 +19,10 @@ using namespace product;
 
 // silu(g) = g t and its slope t (1 + g (1 - t)), t = 1 / (1 + exp(-g)): both times 1 / w, w a power of two.  For gates below kFar, where t is exp(g) in all its
 // bits and next to the least normal number or below it (large factors make normal results of those too), w is 2^-116 (and t 0 below
-// -167); for others it is 1.  Products are taken with silu or slope first and with w last.
+// -167); for others it is 1.  Products are taken with silu or slope first and with w last, but for d_g.
 // FINE, for fp32 data: what the exponential's argument g log2 e loses by its rounding is multiplied in after, so that t is off by 8 * 2^-24 of
 // itself at most.  Without, that is 2 |g| more, 2^-16 of t at the least: nothing beside the 2^-8 of bf16 results.  No branch: 17 fp32 rows, 2 x 12382 from
-// 4096 and back, 463 us; with e^-g as it is and a division 457, and every larger case the same either way.
+// 4096 and back, 462 us; with e^-g as it is and a division 457, and every larger case the same either way.
 struct Gate {
     float silu, slope, w;
 };
